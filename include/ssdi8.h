@@ -349,6 +349,46 @@ ssdi8_status_t ssdi8_ssd_step(const ssdi8_dims_t* dims, const int8_t* xq, const 
 ssdi8_status_t ssdi8_softplus_dt(const float* dt_raw, const float* dt_bias, int64_t rows, int32_t H, float* dt,
                                  void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * The operators around the layer in a Mamba-2 block (Figure 1(a): in-proj, convolution, SSD, norm, out-proj).  The paper runs
+ * them beside its SSD kernels without describing them (Section 5, "Quantization Setup"; the projections W8A8, the convolution
+ * unmodified); the int8 codes they write follow Eq. 1.  The quotient of a code that one of them writes is defined in exact
+ * arithmetic on the given inputs, weights and step sizes: code = rne(value / step) saturated, whatever the kernels carry
+ * between; NaN has the code +127.  Element types: dtype 0 = fp32, 1 = fp16, 2 = bf16.  Strides count elements. */
+
+/* Slots.  A serving program keeps one slot per sequence (ring rows of the convolution, state cache).  slots[b] names the slot of
+ * the call's sequence b; a negative one marks a sequence of padding, whose slot data and outputs are left alone (or cleared,
+ * where an entry says so).  A slot or position that no call may have (slots[b] >= nslots, pos[b] < 0) and a slot that an earlier
+ * sequence of the same call names already are taken for padding, and *status (if given) becomes SSDI8_ERR_SHAPE; it is not
+ * written otherwise. */
+
+/* Causal convolution of a prompt: depthwise, `width` taps (2, 3 or 4), bias, SiLU, and the entry quantiser (Section 4.2,
+ * "Quantization of B,C") in one pass over xBC.
+ *   v[t,ch] = bias[ch] + sum_k weight[ch][k] xBC[t - width + 1 + k, ch];  u = v / (1 + exp(-v))
+ *   codes: xq = rne(u / s_x[ch]), Bq = rne(u / s_B[g]), Cq = rne(u / s_C[g]);  or out = u in xBC's type (xq = NULL)
+ *   dt (if given): float(dt_raw), with SSDI8_FLAG_DT_SOFTPLUS softplus(dt_raw + dt_bias) as ssdi8_softplus_dt forms it
+ * Sequence b has lens[b] tokens (clamped to [0, seqlen]; NULL: all), the first at position pos[b] (NULL: 0) of the sequence.
+ * Tokens ahead of the call come from the ring, row t mod width of its slot for token t; those of negative positions are zeros, so
+ * a slot needs no clearing for a new sequence.  The last `width` tokens are left there.  ring = NULL: zeros ahead, nothing is
+ * kept, slots ignored.  slots = NULL: slot b.  Rows from lens[b] on get codes, out and dt of 0, which pass through the chunk scan without
+ * a trace (pad seqlen to a multiple of the chunk); a padding sequence has no tokens at all.
+ * dims.chunk is ignored; seqlen may be 0.  weight [Ch][width], bias [Ch] or NULL, Ch = H*P + 2*G*N; dt_raw has xBC's type.
+ * weight, s_x, xq, Bq, Cq, out and ring 16-byte aligned, xBC and dt_raw at an element's alignment, any strides of tokens and sequences. */
+typedef struct {
+  const void* xBC; int64_t stride_b, stride_t;               /* [B][L][Ch]                       */
+  const float* weight; const float* bias;                    /* [Ch][width], [Ch]                */
+  const int32_t* lens; const int32_t* slots; const int32_t* pos;   /* [B] each                   */
+  void* ring; int32_t nslots;                                /* [nslots][width][Ch], xBC's type  */
+  const float* s_x; const float* s_B; const float* s_C;      /* [H*P], [G], [G]                  */
+  int8_t* xq; int8_t* Bq; int8_t* Cq;                        /* [B,L,H,P], [B,L,G,N] x2          */
+  void* out;                                                 /* [B,L,Ch]                         */
+  const void* dt_raw; int64_t dt_stride_b, dt_stride_t;      /* [B][L][H]                        */
+  const float* dt_bias; float* dt;                           /* [H], [B,L,H]                     */
+  int32_t* status;                                           /* 1 word, or NULL                  */
+} ssdi8_conv_args_t;
+ssdi8_status_t ssdi8_conv_fwd(const ssdi8_dims_t* dims, const ssdi8_conv_args_t* args, int32_t dtype, int32_t width,
+                              uint32_t flags, void* stream);
+
 /* Measurement aid (the paper has no counterpart): what tcgen05.mma.kind::i8 sustains on the current
  * device, for the "fraction of the int8 tensor-pipe peak" a benchmark reports.  One CTA per SM issues
  * `mma_per_sm` (rounded down to a multiple of 128, at least 128) dense MMAs of M 128 x N 256 x K 32

@@ -47,7 +47,8 @@ EXPORTS = ("ssdi8_status_string", "ssdi8_workspace_bytes", "ssdi8_quantize_act",
            "ssdi8_mean_correction_workspace_bytes", "ssdi8_quantize_entry",
            "ssdi8_layer_fwd", "ssdi8_layer_fwd_workspace_bytes",
            "ssdi8_layer_fwd_host", "ssdi8_layer_fwd_host_scratch_bytes",
-           "ssdi8_int8_mma_peak", "ssdi8_selftest_bounded_wait", "ssdi8_softplus_dt")
+           "ssdi8_int8_mma_peak", "ssdi8_selftest_bounded_wait", "ssdi8_softplus_dt",
+           "ssdi8_conv_fwd")
 STATIC_WORKSPACE_BYTES = 16 << 20
 
 
@@ -281,6 +282,18 @@ def ssdi8_softplus_dt(dt_raw, dt_bias, rows: int, H: int, dt, stream=None) -> No
     code = _m.softplus_dt(dt_raw, dt_bias, rows, H, dt, stream)
     if code:
         _check(code, "ssdi8_softplus_dt")
+
+
+# ---- the operators around the layer: sizes, strides and element types come from the tensors
+def ssdi8_conv_fwd(dims: Dims, xBC, weight, bias=None, *, s_x=None, s_B=None, s_C=None, xq=None, Bq=None, Cq=None, out=None,
+                   dt_raw=None, dt_bias=None, dt=None, lens=None, ring=None, slots=None, pos=None, status=None, flags: int = 0,
+                   stream=None) -> None:
+    """Causal convolution with SiLU of a prompt: xBC [B, L, Ch] (any strides of B and L) to the int8 codes xq, Bq, Cq, or to
+    `out` in xBC's type; dt_raw [B, L, H] to dt.  ring [nslots, width, Ch] keeps the last tokens of each slot."""
+    code = _m.conv_fwd(dims, xBC, weight, bias, s_x, s_B, s_C, xq, Bq, Cq, out, dt_raw, dt_bias, dt, lens, ring, slots, pos,
+                       status, flags, stream)
+    if code:
+        _check(code, "ssdi8_conv_fwd")
 
 
 def ssdi8_int8_mma_peak(mma_per_sm: int, status=None, stream=None) -> float:

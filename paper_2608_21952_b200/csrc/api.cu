@@ -27,25 +27,6 @@ bool dims_supported(const ssdi8_dims_t* d, bool need_chunks) {
   return true;
 }
 
-// The kernels are built for sm_100a only (tensor-memory MMA does not exist elsewhere).
-// (First use on a device fills the cache under a lock: two threads may make their first call at once.)
-ssdi8_status_t check_arch() {
-  static int ok_device[64];  // 0 unknown, 1 ok, -1 wrong
-  static std::mutex mu;
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return SSDI8_ERR_CUDA;
-  if (dev < 0 || dev >= 64) return SSDI8_ERR_CUDA;
-  std::lock_guard<std::mutex> lock(mu);
-  if (ok_device[dev] == 0) {
-    int major = 0, minor = 0;
-    if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
-        cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev) != cudaSuccess)
-      return SSDI8_ERR_CUDA;
-    ok_device[dev] = (major == 10 && minor == 0) ? 1 : -1;
-  }
-  return ok_device[dev] == 1 ? SSDI8_OK : SSDI8_ERR_ARCH;
-}
-
 struct Workspace {
   size_t pack, gamma, cbq, loc, hq, total;
 };
@@ -64,6 +45,27 @@ Workspace layout(const Dims& d) {
 }
 
 }  // namespace
+
+namespace ssdi8 {
+// The kernels are built for sm_100a only (tensor-memory MMA does not exist elsewhere).
+// (First use on a device fills the cache under a lock: two threads may make their first call at once.)
+ssdi8_status_t check_arch() {
+  static int ok_device[64];  // 0 unknown, 1 ok, -1 wrong
+  static std::mutex mu;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return SSDI8_ERR_CUDA;
+  if (dev < 0 || dev >= 64) return SSDI8_ERR_CUDA;
+  std::lock_guard<std::mutex> lock(mu);
+  if (ok_device[dev] == 0) {
+    int major = 0, minor = 0;
+    if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev) != cudaSuccess)
+      return SSDI8_ERR_CUDA;
+    ok_device[dev] = (major == 10 && minor == 0) ? 1 : -1;
+  }
+  return ok_device[dev] == 1 ? SSDI8_OK : SSDI8_ERR_ARCH;
+}
+}  // namespace ssdi8
 
 extern "C" {
 

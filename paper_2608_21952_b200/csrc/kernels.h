@@ -66,6 +66,7 @@ inline ssdi8_status_t launch_configured(void (*kernel)(KArgs...), dim3 grid, dim
   return launch_sized(kernel, grid, block, smem, smem, carveout, check_static, st, std::forward<Args>(args)...);
 }
 int sm_count();   // of the current device (0 on failure)
+ssdi8_status_t check_arch();   // of the current device: SSDI8_OK or SSDI8_ERR_ARCH, _CUDA
 
 // L1 / shared memory split of the streaming kernels that lead a layer (ChunkCumsum, the quantisers), in percent
 // of shared memory: 64 KB of 228.  Launched through programmatic dependent launch right behind ChunkScan they
@@ -171,6 +172,9 @@ constexpr int kMeanCorrMaxSlabs = 256;
 int mean_correction_slabs(i64 R);
 ssdi8_status_t launch_mean_correction(const float* y, const float* yq, i64 R, i64 Ch, float eta, float* corr,
                                       double* partial, cudaStream_t st);
+
+// the operators around the layer (conv.cu)
+ssdi8_status_t launch_conv(const Dims& d, const ssdi8_conv_args_t& a, int dtype, int width, bool softplus, cudaStream_t st);
 
 // measurement aid and self-test (selftest.cu): `nbatch` batches of int8_mma_peak_batch() MMAs of
 // M 128 x N 256 x K 32 on every SM (ctas = number of CTAs launched); a bounded wait that runs out

@@ -105,6 +105,55 @@ void* stream(PyObject* o) {
   return p;
 }
 
+// Tensors of the operators around the layer.  These take their sizes and strides from the tensors, so the shapes are checked here:
+// a wrong one is SSDI8_ERR_SHAPE, as from the library; a wrong element type a TypeError, a tensor of another device than the
+// current one (the stream's) a ValueError.
+constexpr int kInt8 = -1, kInt32 = -2;   // beside the library's 0 = fp32, 1 = fp16, 2 = bf16
+constexpr int kAnyFloat = -3;
+struct BadShape {};
+struct Tensor {
+  const at::Tensor* t = nullptr;
+  int dtype = 0;
+  explicit operator bool() const { return t != nullptr; }
+  void* data() const { return t ? t->data_ptr() : nullptr; }
+  template <typename E>
+  E* as() const { return static_cast<E*>(data()); }
+  int64_t size(int i) const { return t->size(i); }
+  int64_t stride(int i) const { return t->stride(i); }
+};
+// strided: the last axis contiguous, the others free (as the caller reads the strides)
+Tensor tensor(PyObject* o, const char* name, int dtype, std::initializer_list<int64_t> shape, bool optional = false, bool strided = false) {
+  Tensor r;
+  if (o == Py_None && optional) return r;
+  if (!THPVariable_Check(o)) {
+    PyErr_Format(PyExc_TypeError, "%s: a tensor is expected", name);
+    throw BadArgument{};
+  }
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!t.is_cuda() || !(strided ? t.dim() > 0 && (t.size(-1) <= 1 || t.stride(-1) == 1) : t.is_contiguous())) {
+    PyErr_Format(PyExc_AssertionError, "%s must be a CUDA tensor with %s", name, strided ? "a contiguous last axis" : "contiguous elements");
+    throw BadArgument{};
+  }
+  if (t.device().index() != c10::cuda::current_device()) {
+    PyErr_Format(PyExc_ValueError, "%s lives on another device than the current one", name);
+    throw BadArgument{};
+  }
+  const auto st = t.scalar_type();
+  r.dtype = st == at::kFloat ? 0 : st == at::kHalf ? 1 : st == at::kBFloat16 ? 2 : st == at::kChar ? kInt8 : st == at::kInt ? kInt32 : -4;
+  if (dtype == kAnyFloat ? r.dtype < 0 : r.dtype != dtype) {
+    PyErr_Format(PyExc_TypeError, "%s has the wrong element type", name);
+    throw BadArgument{};
+  }
+  if ((size_t)t.dim() != shape.size()) throw BadShape{};
+  int i = 0;
+  for (int64_t n : shape) {
+    if (n >= 0 && t.size(i) != n) throw BadShape{};   // (-1: any)
+    ++i;
+  }
+  r.t = &t;
+  return r;
+}
+
 // the library call with the interpreter lock released; the status code as a Python integer
 template <typename F>
 PyObject* call(F f) {
@@ -126,6 +175,8 @@ PyObject* entry(Py_ssize_t n, F f) {
     return f();
   } catch (const BadArgument&) {
     return nullptr;
+  } catch (const BadShape&) {
+    return PyLong_FromLong(SSDI8_ERR_SHAPE);
   } catch (const std::exception& e) {
     PyErr_SetString(PyExc_RuntimeError, e.what());
     return nullptr;
@@ -261,13 +312,47 @@ ENTRY(softplus_dt, 6) {   // dt_raw, dt_bias, rows, H, dt, stream
   return call([=] { return ssdi8_softplus_dt(raw, bias, rows, H, dt, st); });
 } END
 
+// dims, xBC, weight, bias, s_x, s_B, s_C, xq, Bq, Cq, out, dt_raw, dt_bias, dt, lens, ring, slots, pos, status, flags, stream
+ENTRY(conv_fwd, 21) {
+  DimsArg d(a[0]);
+  const int64_t B = d.get()->batch, L = d.get()->seqlen, H = d.get()->nheads, HP = H * d.get()->headdim,
+                GN = (int64_t)d.get()->ngroups * d.get()->dstate, Ch = HP + 2 * GN;
+  ssdi8_conv_args_t c = {};
+  const Tensor x = tensor(a[1], "xBC", kAnyFloat, {B, L, Ch}, false, true);
+  const Tensor w = tensor(a[2], "weight", 0, {Ch, -1});
+  const int width = (int)w.size(1);
+  c.xBC = x.data(); c.stride_b = x.stride(0); c.stride_t = x.stride(1);
+  c.weight = w.as<float>();
+  c.bias = tensor(a[3], "bias", 0, {Ch}, true).as<float>();
+  c.s_x = tensor(a[4], "s_x", 0, {HP}, true).as<float>();
+  c.s_B = tensor(a[5], "s_B", 0, {d.get()->ngroups}, true).as<float>();
+  c.s_C = tensor(a[6], "s_C", 0, {d.get()->ngroups}, true).as<float>();
+  c.xq = tensor(a[7], "xq", kInt8, {B, L, HP}, true).as<int8_t>();
+  c.Bq = tensor(a[8], "Bq", kInt8, {B, L, GN}, true).as<int8_t>();
+  c.Cq = tensor(a[9], "Cq", kInt8, {B, L, GN}, true).as<int8_t>();
+  c.out = tensor(a[10], "out", x.dtype, {B, L, Ch}, true).data();
+  const Tensor raw = tensor(a[11], "dt_raw", x.dtype, {B, L, H}, true, true);
+  if (raw) { c.dt_raw = raw.data(); c.dt_stride_b = raw.stride(0); c.dt_stride_t = raw.stride(1); }
+  c.dt_bias = tensor(a[12], "dt_bias", 0, {H}, true).as<float>();
+  c.dt = tensor(a[13], "dt", 0, {B, L, H}, true).as<float>();
+  c.lens = tensor(a[14], "lens", kInt32, {B}, true).as<int32_t>();
+  const Tensor ring = tensor(a[15], "ring", x.dtype, {-1, width, Ch}, true);
+  if (ring) { c.ring = ring.data(); c.nslots = (int32_t)ring.size(0); }
+  c.slots = tensor(a[16], "slots", kInt32, {B}, true).as<int32_t>();
+  c.pos = tensor(a[17], "pos", kInt32, {B}, true).as<int32_t>();
+  c.status = tensor(a[18], "status", kInt32, {1}, true).as<int32_t>();
+  const uint32_t flags = (uint32_t)integer(a[19]);
+  void* st = stream(a[20]);
+  return call([&] { return ssdi8_conv_fwd(d.get(), &c, x.dtype, width, flags, st); });
+} END
+
 #undef ENTRY
 #undef END
 
 #define METHOD(NAME) {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(NAME)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {METHOD(init), METHOD(quantize_act), METHOD(quantize_entry), METHOD(chunk_scan_fwd), METHOD(chunk_scan_fwd_static),
                           METHOD(layer_fwd), METHOD(layer_fwd_host), METHOD(calibrate), METHOD(mean_correction),
-                          METHOD(state_passing), METHOD(ssd_step), METHOD(softplus_dt), {nullptr, nullptr, 0, nullptr}};
+                          METHOD(state_passing), METHOD(ssd_step), METHOD(softplus_dt), METHOD(conv_fwd), {nullptr, nullptr, 0, nullptr}};
 #undef METHOD
 
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
