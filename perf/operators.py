@@ -391,6 +391,8 @@ def _own(st):
         st["dims"] = bd.Dims(c["batch"], c.get("seqlen", 1), c["nheads"], P, c["dstate"], c["ngroups"], 0)
         if op != "conv":
             st["handle"] = bd.cache_of(st["dims"], **st["cache"])
+        if op == "cache":   # (a full window is read as it stands, with its 16 tokens beside the codes)
+            st["first"] = torch.maximum(st["cache"]["start"][st["slots"].long()], (st["pos"] - 1) // WINDOW * WINDOW)
     if op == "conv":
         bd.ssdi8_conv_fwd(st["dims"], st["xBC"], st["weight"], st["bias"], s_x=st["s_x"], s_B=st["s_B"], s_C=st["s_C"],
                           xq=st["xq"], Bq=st["Bq"], Cq=st["Cq"], out=st["out"], dt_raw=st["dt_raw"], dt_bias=st["dt_bias"],
@@ -402,7 +404,8 @@ def _own(st):
         bd.ssdi8_cache_write(st["dims"], st["handle"], st["slots"], st["pos"], st["state"])
         return {k: cache[k] for k in ("codes", "scales", "start")}
     if op == "cache":
-        bd.ssdi8_cache_read(st["dims"], st["handle"], st["slots"], st["pos"], st["A"], st["s_x"], st["s_B"], st["state"])
+        bd.ssdi8_cache_read(st["dims"], st["handle"], st["slots"], st["pos"], st["A"], st["s_x"], st["s_B"], st["state"],
+                            first=st["first"])
         return {"state": st["state"]}
     bd.ssdi8_token_step(st["dims"], st["handle"], st["xBC"], st["weight"], st["bias"], st["dt_raw"], st["dt_bias"], st["A"],
                         st["D"], st["corr"], st["s_x"], st["s_B"], st["s_C"], st["slots"], st["pos"], st["y"],
