@@ -389,6 +389,64 @@ typedef struct {
 ssdi8_status_t ssdi8_conv_fwd(const ssdi8_dims_t* dims, const ssdi8_conv_args_t* args, int32_t dtype, int32_t width,
                               uint32_t flags, void* stream);
 
+/* A cache of SSM states in 8 bits, one slot per sequence.  (The paper keeps its inter-chunk states in INT8 within a call, Section 4.2,
+ * Eq. 4 and 7; between calls it says nothing.)  A slot holds the state as int8 codes with a step size per row of N, and beside it
+ * the int8 x and B and the time steps of the up to 16 tokens that are not in the codes yet: token t in row t mod 16 of the window.
+ * Re-quantising the state at every token would keep small updates from ever moving a code; with the window the step reads the codes
+ * and writes one window row, and the codes are formed anew once in 16 tokens.
+ * A slot at position pos (tokens of the sequence so far) has the tokens from max(start, pos - pos mod 16) on in its window and all
+ * earlier ones in its codes.
+ * codes, scales, xwin, Bwin, dtwin, ring: 16-byte aligned. */
+#define SSDI8_CACHE_WINDOW 16
+typedef struct {
+  int32_t nslots;
+  int32_t width, dtype;   /* of the convolution's ring (ssdi8_conv_fwd) */
+  int8_t* codes;          /* [nslots][H][P][N]                          */
+  float* scales;          /* [nslots][H][P]                             */
+  int8_t* xwin;           /* [nslots][H][16][P]  codes, step s_x        */
+  int8_t* Bwin;           /* [nslots][G][16][N]  codes, step s_B        */
+  float* dtwin;           /* [nslots][H][16]                            */
+  int32_t* start;         /* [nslots] position that the slot was written at */
+  void* ring;             /* [nslots][width][Ch], or NULL where only states are written and read */
+} ssdi8_cache_t;
+
+/* Writes fp32 states [B,H,P,N] (NULL: zeros) into their slots, as they stand at position pos[b] (NULL: 0), with empty windows:
+ *   step = fdiv(absmax over n, 127) (1 if that is 0), code = rne(fdiv(S, step)) saturated;  start = pos
+ * (a NaN counts for nothing in the absmax and has the code +127).  The ring is ssdi8_conv_fwd's to write.  state 16-byte aligned;
+ * dims.seqlen and dims.chunk are ignored, here and below.  slots, padding and status: as above. */
+ssdi8_status_t ssdi8_cache_write(const ssdi8_dims_t* dims, const ssdi8_cache_t* cache, const int32_t* slots, const int32_t* pos,
+                                 const float* state, int32_t* status, void* stream);
+
+/* Reads the states of slots at position pos[b] (what ssdi8_chunk_scan_fwd takes as init_state):
+ *   S = E step code + sum_j (w_j s_x s_B x_j) B_j,  E = exp(A sum dt),  w_j = dt_j exp(A sum of the dt behind j)
+ * over the waiting tokens j.  first[b] (NULL: as a slot is left by ssdi8_cache_write and ssdi8_token_step, above): position of the first
+ * token that the codes do not hold; a window of more than 16 tokens or less than none is taken for padding.  A, s_x, s_B as for the step.
+ * Padding leaves its rows of state alone. */
+ssdi8_status_t ssdi8_cache_read(const ssdi8_dims_t* dims, const ssdi8_cache_t* cache, const int32_t* slots, const int32_t* first,
+                                const int32_t* pos, const float* A, const float* s_x, const float* s_B, float* state, int32_t* status,
+                                void* stream);
+
+/* One token for every sequence of the batch: the convolution of ssdi8_conv_fwd on the ring, its codes and time step, and the
+ * recurrence of ssdi8_ssd_step on the cache, in one launch.  pos[b] tokens of the sequence came before.
+ *   x, B, C: codes as in ssdi8_conv_fwd; the token goes into row pos mod width of the ring and row pos mod 16 of the window
+ *   y = s_C (E scale sum_n C[n] code[p,n] + s_x s_B sum_j w_j (C . B_j) x_j[p]) + D s_x x + corr,  the token itself among the j
+ *   if pos mod 16 = 15, behind that: S as in ssdi8_cache_read with all 16 tokens, in binary64; scale = (float)(absmax / 127)
+ *   (1 if that is 0), code = rne(S / scale) saturated
+ * E and w_j as in ssdi8_cache_read; the integer sums are exact.  y [B][H*P] is fp32, or 16-bit with SSDI8_FLAG_Y_FP16 / _BF16;
+ * SSDI8_FLAG_DT_SOFTPLUS as in ssdi8_conv_fwd.  Padding leaves its row of y alone.  A slot whose start lies behind pos is
+ * taken for padding, with the status.  weight 16-byte aligned; bias, dt_bias, D, corr may be NULL. */
+typedef struct {
+  const void* xBC; int64_t stride_b;          /* [B][Ch], the ring's type */
+  const float* weight; const float* bias;     /* [Ch][width], [Ch]        */
+  const void* dt_raw; int64_t dt_stride_b;    /* [B][H], the ring's type  */
+  const float* dt_bias; const float* A; const float* D; const float* corr;   /* [H], [H], [H], [H*P] */
+  const float* s_x; const float* s_B; const float* s_C;                      /* [H*P], [G], [G]      */
+  const int32_t* slots; const int32_t* pos;   /* [B]                      */
+  void* y; int32_t* status;
+} ssdi8_token_args_t;
+ssdi8_status_t ssdi8_token_step(const ssdi8_dims_t* dims, const ssdi8_cache_t* cache, const ssdi8_token_args_t* args, uint32_t flags,
+                                void* stream);
+
 /* Measurement aid (the paper has no counterpart): what tcgen05.mma.kind::i8 sustains on the current
  * device, for the "fraction of the int8 tensor-pipe peak" a benchmark reports.  One CTA per SM issues
  * `mma_per_sm` (rounded down to a multiple of 128, at least 128) dense MMAs of M 128 x N 256 x K 32

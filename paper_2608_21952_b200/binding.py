@@ -48,8 +48,9 @@ EXPORTS = ("ssdi8_status_string", "ssdi8_workspace_bytes", "ssdi8_quantize_act",
            "ssdi8_layer_fwd", "ssdi8_layer_fwd_workspace_bytes",
            "ssdi8_layer_fwd_host", "ssdi8_layer_fwd_host_scratch_bytes",
            "ssdi8_int8_mma_peak", "ssdi8_selftest_bounded_wait", "ssdi8_softplus_dt",
-           "ssdi8_conv_fwd")
+           "ssdi8_conv_fwd", "ssdi8_cache_write", "ssdi8_cache_read", "ssdi8_token_step")
 STATIC_WORKSPACE_BYTES = 16 << 20
+CACHE_WINDOW = 16
 
 
 class Dims(C.Structure):
@@ -78,7 +79,13 @@ class LayerArgs(C.Structure):
     _fields_ = [(k, C.c_void_p) for k in _LAYER_FIELDS]
 
 
-_m.init(Dims, FwdArgs, LayerArgs, C.Structure.__base__, C.ArgumentError)
+class Cache(C.Structure):
+    """Slots of the 8-bit state cache (ssdi8_cache_t); made by cache_of or make_cache, which keep the tensors with it."""
+    _fields_ = [(k, C.c_int32) for k in ("nslots", "width", "dtype")] + \
+        [(k, C.c_void_p) for k in ("codes", "scales", "xwin", "Bwin", "dtwin", "start", "ring")]
+
+
+_m.init(Dims, FwdArgs, LayerArgs, Cache, C.Structure.__base__, C.ArgumentError)
 
 
 _lib.ssdi8_status_string.restype = C.c_char_p
@@ -294,6 +301,64 @@ def ssdi8_conv_fwd(dims: Dims, xBC, weight, bias=None, *, s_x=None, s_B=None, s_
                        status, flags, stream)
     if code:
         _check(code, "ssdi8_conv_fwd")
+
+
+def cache_of(dims: Dims, codes, scales, xwin, Bwin, dtwin, start, ring=None) -> Cache:
+    """The cache whose slots are these tensors (shapes as in ssdi8_cache_t; ring None where only states are written and read)."""
+    n, H, P, N, G = codes.shape[0], dims.nheads, dims.headdim, dims.dstate, dims.ngroups
+    want = {"codes": (codes, (n, H, P, N), torch.int8), "scales": (scales, (n, H, P), torch.float32),
+            "xwin": (xwin, (n, H, CACHE_WINDOW, P), torch.int8), "Bwin": (Bwin, (n, G, CACHE_WINDOW, N), torch.int8),
+            "dtwin": (dtwin, (n, H, CACHE_WINDOW), torch.float32), "start": (start, (n,), torch.int32)}
+    if ring is not None:
+        want["ring"] = (ring, (n, ring.shape[1], H * P + 2 * G * N), ring.dtype)
+        if ring.dtype not in _ENTRY_DTYPES:
+            raise TypeError("ring has the wrong element type")
+    c = Cache(nslots=n)
+    for name, (t, shape, dtype) in want.items():
+        if tuple(t.shape) != shape:
+            raise SSDi8Error(ERR_SHAPE, f"cache_of: {name} is {tuple(t.shape)}, not {shape}")
+        if t.dtype != dtype:
+            raise TypeError(f"{name} has the wrong element type")
+        if t.device != codes.device:
+            raise ValueError(f"{name} lives on another device than codes")
+        setattr(c, name, _ptr(t))
+    if ring is not None:
+        c.width, c.dtype = ring.shape[1], _ENTRY_DTYPES[ring.dtype]
+    c.tensors = {name: t for name, (t, _, _) in want.items()}   # (the struct holds raw pointers: they stay alive with it)
+    return c
+
+
+def make_cache(dims: Dims, nslots: int, dtype=torch.bfloat16, width: int = 4, device="cuda") -> Cache:
+    """A cache of `nslots` slots, each as a new sequence needs it (state 0 at position 0).  Its tensors are in `.tensors`."""
+    H, P, N, G = dims.nheads, dims.headdim, dims.dstate, dims.ngroups
+    z = lambda *shape, dtype: torch.zeros(shape, dtype=dtype, device=device)  # noqa: E731
+    return cache_of(dims, codes=z(nslots, H, P, N, dtype=torch.int8), scales=z(nslots, H, P, dtype=torch.float32).fill_(1.0),
+                    xwin=z(nslots, H, CACHE_WINDOW, P, dtype=torch.int8), Bwin=z(nslots, G, CACHE_WINDOW, N, dtype=torch.int8),
+                    dtwin=z(nslots, H, CACHE_WINDOW, dtype=torch.float32), start=z(nslots, dtype=torch.int32),
+                    ring=z(nslots, width, H * P + 2 * G * N, dtype=dtype))
+
+
+def ssdi8_cache_write(dims: Dims, cache: Cache, slots, pos, state, status=None, stream=None) -> None:
+    """fp32 states [B, H, P, N] (None: zeros) into slots, at position pos[b]."""
+    code = _m.cache_write(dims, cache, slots, pos, state, status, stream)
+    if code:
+        _check(code, "ssdi8_cache_write")
+
+
+def ssdi8_cache_read(dims: Dims, cache: Cache, slots, pos, A, s_x, s_B, state, first=None, status=None, stream=None) -> None:
+    """States of slots at position pos[b], with the tokens that wait in their windows, into fp32 `state` [B, H, P, N]."""
+    code = _m.cache_read(dims, cache, slots, first, pos, A, s_x, s_B, state, status, stream)
+    if code:
+        _check(code, "ssdi8_cache_read")
+
+
+def ssdi8_token_step(dims: Dims, cache: Cache, xBC, weight, bias, dt_raw, dt_bias, A, D, corr, s_x, s_B, s_C, slots, pos, y,
+                     status=None, flags: int = 0, stream=None) -> None:
+    """One token of every sequence: xBC [B, Ch] and dt_raw [B, H] (rows of any stride) to y [B, H * P] (fp32, fp16 or bf16)."""
+    code = _m.token_step(dims, cache, xBC, weight, bias, dt_raw, dt_bias, A, D, corr, s_x, s_B, s_C, slots, pos, y, status, flags,
+                         stream)
+    if code:
+        _check(code, "ssdi8_token_step")
 
 
 def ssdi8_int8_mma_peak(mma_per_sm: int, status=None, stream=None) -> float:

@@ -17,6 +17,18 @@ bool heads_supported(const ssdi8_dims_t* d) {
   return d->nheads % d->ngroups == 0 && (i64)d->nheads * 64 + 2 * (i64)d->ngroups * d->dstate < (1 << 28);
 }
 
+// the slots of a cache; ring: with the convolution's
+ssdi8_status_t cache_supported(const ssdi8_dims_t* d, const ssdi8_cache_t* c, const int32_t* slots, bool ring) {
+  if (!heads_supported(d) || c->nslots <= 0 || (!slots && c->nslots < d->batch) || (i64)d->batch * d->nheads > 0x7fffffff) return SSDI8_ERR_SHAPE;
+  if (ring && (c->dtype < 0 || c->dtype > 2)) return SSDI8_ERR_UNSUPPORTED;
+  if (ring && (c->width < 2 || c->width > 4)) return SSDI8_ERR_SHAPE;
+  if (!c->codes || !c->scales || !c->xwin || !c->Bwin || !c->dtwin || !c->start || (ring && !c->ring)) return SSDI8_ERR_NULL;
+  const void* ptrs[] = {c->codes, c->scales, c->xwin, c->Bwin, c->dtwin, c->ring};
+  for (const void* p : ptrs)
+    if (!aligned16(p)) return SSDI8_ERR_ALIGN;
+  return SSDI8_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -39,6 +51,44 @@ ssdi8_status_t ssdi8_conv_fwd(const ssdi8_dims_t* dims, const ssdi8_conv_args_t*
   const ssdi8_status_t s = check_arch();
   if (s != SSDI8_OK) return s;
   return launch_conv(make_dims(dims), *a, dtype, width, (flags & SSDI8_FLAG_DT_SOFTPLUS) != 0, static_cast<cudaStream_t>(stream));
+}
+
+ssdi8_status_t ssdi8_cache_write(const ssdi8_dims_t* dims, const ssdi8_cache_t* cache, const int32_t* slots, const int32_t* pos,
+                                 const float* state, int32_t* status, void* stream) {
+  if (!dims || !cache) return SSDI8_ERR_NULL;
+  ssdi8_status_t s = cache_supported(dims, cache, slots, false);
+  if (s != SSDI8_OK) return s;
+  if (!aligned16(state)) return SSDI8_ERR_ALIGN;
+  if ((s = check_arch()) != SSDI8_OK) return s;
+  return launch_cache_write(make_dims(dims), *cache, slots, pos, state, status, static_cast<cudaStream_t>(stream));
+}
+
+ssdi8_status_t ssdi8_cache_read(const ssdi8_dims_t* dims, const ssdi8_cache_t* cache, const int32_t* slots, const int32_t* first,
+                                const int32_t* pos, const float* A, const float* s_x, const float* s_B, float* state, int32_t* status,
+                                void* stream) {
+  if (!dims || !cache) return SSDI8_ERR_NULL;
+  ssdi8_status_t s = cache_supported(dims, cache, slots, false);
+  if (s != SSDI8_OK) return s;
+  if (!pos || !A || !s_x || !s_B || !state) return SSDI8_ERR_NULL;
+  if (!aligned16(state)) return SSDI8_ERR_ALIGN;
+  if ((s = check_arch()) != SSDI8_OK) return s;
+  return launch_cache_read(make_dims(dims), *cache, slots, first, pos, A, s_x, s_B, state, status, static_cast<cudaStream_t>(stream));
+}
+
+ssdi8_status_t ssdi8_token_step(const ssdi8_dims_t* dims, const ssdi8_cache_t* cache, const ssdi8_token_args_t* a, uint32_t flags,
+                                void* stream) {
+  if (!dims || !cache || !a) return SSDI8_ERR_NULL;
+  constexpr uint32_t y16 = SSDI8_FLAG_Y_FP16 | SSDI8_FLAG_Y_BF16;
+  if ((flags & ~(y16 | (uint32_t)SSDI8_FLAG_DT_SOFTPLUS)) != 0 || (flags & y16) == y16) return SSDI8_ERR_UNSUPPORTED;
+  ssdi8_status_t s = cache_supported(dims, cache, a->slots, true);
+  if (s != SSDI8_OK) return s;
+  if (!a->xBC || !a->weight || !a->dt_raw || !a->A || !a->s_x || !a->s_B || !a->s_C || !a->pos || !a->y) return SSDI8_ERR_NULL;
+  const size_t e = elem_size(cache->dtype);
+  if (!aligned16(a->weight) || !aligned_to(a->xBC, e) || !aligned_to(a->dt_raw, e) || !aligned_to(a->y, (flags & y16) ? 2 : 4))
+    return SSDI8_ERR_ALIGN;
+  if ((s = check_arch()) != SSDI8_OK) return s;
+  return launch_token_step(make_dims(dims), *cache, *a, (flags & SSDI8_FLAG_DT_SOFTPLUS) != 0,
+                           (flags & SSDI8_FLAG_Y_FP16) ? 1 : (flags & SSDI8_FLAG_Y_BF16) ? 2 : 0, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

@@ -55,7 +55,7 @@ float real(PyObject* o) {
 // The binding's ctypes types, given once at its import (init): a structure of another type, or any other object with a
 // buffer, would be read as pointers and sizes that it does not hold.  The errors are those of ctypes' byref and argtypes.
 struct Types {
-  PyObject *dims = nullptr, *fwd = nullptr, *layer = nullptr, *ctypes_base = nullptr, *argument_error = nullptr;
+  PyObject *dims = nullptr, *fwd = nullptr, *layer = nullptr, *cache = nullptr, *ctypes_base = nullptr, *argument_error = nullptr;
 } g_types;
 
 // the memory of a ctypes structure
@@ -92,6 +92,11 @@ struct FwdArg : Struct {
 struct LayerArg : Struct {
   explicit LayerArg(PyObject* o) : Struct(o, g_types.layer, sizeof(ssdi8_layer_args_t)) {}
   const ssdi8_layer_args_t* get() const { return static_cast<const ssdi8_layer_args_t*>(b.buf); }
+};
+
+struct CacheArg : Struct {
+  explicit CacheArg(PyObject* o) : Struct(o, g_types.cache, sizeof(ssdi8_cache_t)) {}
+  const ssdi8_cache_t* get() const { return static_cast<const ssdi8_cache_t*>(b.buf); }
 };
 
 // the stream of a call: the current one of the current device for None, else a torch stream object's
@@ -186,15 +191,15 @@ PyObject* entry(Py_ssize_t n, F f) {
 #define ENTRY(NAME, N) PyObject* NAME(PyObject*, PyObject* const* a, Py_ssize_t n) { return entry<N>(n, [&]() -> PyObject*
 #define END ); }
 
-ENTRY(init, 5) {   // Dims, FwdArgs, LayerArgs, the base type of ctypes objects, ctypes.ArgumentError
-  for (int i = 0; i < 5; ++i) {
+ENTRY(init, 6) {   // Dims, FwdArgs, LayerArgs, Cache, the base type of ctypes objects, ctypes.ArgumentError
+  for (int i = 0; i < 6; ++i) {
     if (!PyType_Check(a[i])) {
       PyErr_SetString(PyExc_TypeError, "a type is expected");
       throw BadArgument{};
     }
     Py_INCREF(a[i]);   // (kept for the life of the process, like the module)
   }
-  g_types = {a[0], a[1], a[2], a[3], a[4]};
+  g_types = {a[0], a[1], a[2], a[3], a[4], a[5]};
   Py_RETURN_NONE;
 } END
 
@@ -346,13 +351,73 @@ ENTRY(conv_fwd, 21) {
   return call([&] { return ssdi8_conv_fwd(d.get(), &c, x.dtype, width, flags, st); });
 } END
 
+ENTRY(cache_write, 7) {   // dims, cache, slots, pos, state, status, stream
+  DimsArg d(a[0]);
+  CacheArg c(a[1]);
+  const int64_t B = d.get()->batch;
+  const int32_t* slots = tensor(a[2], "slots", kInt32, {B}, true).as<int32_t>();
+  const int32_t* pos = tensor(a[3], "pos", kInt32, {B}, true).as<int32_t>();
+  const float* state = tensor(a[4], "state", 0, {B, d.get()->nheads, d.get()->headdim, d.get()->dstate}, true).as<float>();
+  int32_t* status = tensor(a[5], "status", kInt32, {1}, true).as<int32_t>();
+  void* st = stream(a[6]);
+  return call([&] { return ssdi8_cache_write(d.get(), c.get(), slots, pos, state, status, st); });
+} END
+
+ENTRY(cache_read, 11) {   // dims, cache, slots, first, pos, A, s_x, s_B, state, status, stream
+  DimsArg d(a[0]);
+  CacheArg c(a[1]);
+  const int64_t B = d.get()->batch, H = d.get()->nheads, P = d.get()->headdim;
+  const int32_t* slots = tensor(a[2], "slots", kInt32, {B}, true).as<int32_t>();
+  const int32_t* first = tensor(a[3], "first", kInt32, {B}, true).as<int32_t>();
+  const int32_t* pos = tensor(a[4], "pos", kInt32, {B}).as<int32_t>();
+  const float* A = tensor(a[5], "A", 0, {H}).as<float>();
+  const float* s_x = tensor(a[6], "s_x", 0, {H * P}).as<float>();
+  const float* s_B = tensor(a[7], "s_B", 0, {d.get()->ngroups}).as<float>();
+  float* state = tensor(a[8], "state", 0, {B, H, P, d.get()->dstate}).as<float>();
+  int32_t* status = tensor(a[9], "status", kInt32, {1}, true).as<int32_t>();
+  void* st = stream(a[10]);
+  return call([&] { return ssdi8_cache_read(d.get(), c.get(), slots, first, pos, A, s_x, s_B, state, status, st); });
+} END
+
+// dims, cache, xBC, weight, bias, dt_raw, dt_bias, A, D, corr, s_x, s_B, s_C, slots, pos, y, status, flags, stream
+ENTRY(token_step, 19) {
+  DimsArg d(a[0]);
+  CacheArg c(a[1]);
+  const int64_t B = d.get()->batch, H = d.get()->nheads, G = d.get()->ngroups, HP = H * d.get()->headdim,
+                Ch = HP + 2 * G * d.get()->dstate;
+  const int dtype = c.get()->dtype;
+  const uint32_t flags = (uint32_t)integer(a[17]);
+  ssdi8_token_args_t t = {};
+  const Tensor x = tensor(a[2], "xBC", dtype, {B, Ch}, false, true), raw = tensor(a[5], "dt_raw", dtype, {B, H}, false, true);
+  t.xBC = x.data(); t.stride_b = x.stride(0);
+  t.weight = tensor(a[3], "weight", 0, {Ch, c.get()->width}).as<float>();
+  t.bias = tensor(a[4], "bias", 0, {Ch}, true).as<float>();
+  t.dt_raw = raw.data(); t.dt_stride_b = raw.stride(0);
+  t.dt_bias = tensor(a[6], "dt_bias", 0, {H}, true).as<float>();
+  t.A = tensor(a[7], "A", 0, {H}).as<float>();
+  t.D = tensor(a[8], "D", 0, {H}, true).as<float>();
+  t.corr = tensor(a[9], "corr", 0, {HP}, true).as<float>();
+  t.s_x = tensor(a[10], "s_x", 0, {HP}).as<float>();
+  t.s_B = tensor(a[11], "s_B", 0, {G}).as<float>();
+  t.s_C = tensor(a[12], "s_C", 0, {G}).as<float>();
+  t.slots = tensor(a[13], "slots", kInt32, {B}, true).as<int32_t>();
+  t.pos = tensor(a[14], "pos", kInt32, {B}).as<int32_t>();
+  const Tensor y = tensor(a[15], "y", kAnyFloat, {B, HP});
+  t.y = y.data();
+  t.status = tensor(a[16], "status", kInt32, {1}, true).as<int32_t>();
+  const uint32_t fl = flags | (y.dtype == 1 ? SSDI8_FLAG_Y_FP16 : y.dtype == 2 ? SSDI8_FLAG_Y_BF16 : 0);
+  void* st = stream(a[18]);
+  return call([&] { return ssdi8_token_step(d.get(), c.get(), &t, fl, st); });
+} END
+
 #undef ENTRY
 #undef END
 
 #define METHOD(NAME) {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(NAME)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {METHOD(init), METHOD(quantize_act), METHOD(quantize_entry), METHOD(chunk_scan_fwd), METHOD(chunk_scan_fwd_static),
                           METHOD(layer_fwd), METHOD(layer_fwd_host), METHOD(calibrate), METHOD(mean_correction),
-                          METHOD(state_passing), METHOD(ssd_step), METHOD(softplus_dt), METHOD(conv_fwd), {nullptr, nullptr, 0, nullptr}};
+                          METHOD(state_passing), METHOD(ssd_step), METHOD(softplus_dt), METHOD(conv_fwd), METHOD(cache_write),
+                          METHOD(cache_read), METHOD(token_step), {nullptr, nullptr, 0, nullptr}};
 #undef METHOD
 
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};

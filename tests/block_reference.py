@@ -43,3 +43,96 @@ def conv(x, weight, bias, lens, ring, slots, pos):
             for t in range(max(0, n - W), n):
                 ring[s, (p + t) % W] = x[b, t]
     return u
+
+
+class Slots:
+    """The 8-bit state cache and the token step from their definitions, in 64 bits.  `t`: the cache's arrays by name."""
+
+    def __init__(self, t, A, s_x, s_B, s_C=None, D=None, corr=None):
+        f = lambda v: None if v is None else np.asarray(v, np.float64)  # noqa: E731
+        self.t, self.A, self.s_x, self.s_B, self.s_C, self.D, self.corr = t, f(A), f(s_x), f(s_B), f(s_C), f(D), f(corr)
+        self.n, self.H, self.P, self.N = t["codes"].shape
+        self.G = t["Bwin"].shape[1]
+        self.group = np.arange(self.H) // (self.H // self.G)
+
+    def valid(self, slots, pos, b):
+        s = b if slots is None else int(slots[b])
+        return 0 <= s < self.n and pos[b] >= 0 and not (slots is not None and s in slots[:b])
+
+    def terms(self, slot, tokens):
+        """decay of the codes and the weight of each waiting token, per head; and the exponents' magnitudes"""
+        dt = np.array([self.t["dtwin"][slot, :, j % WINDOW].astype(np.float64) for j in tokens]).reshape(len(tokens), self.H)
+        behind = dt.sum(0) - np.cumsum(dt, 0)
+        return np.exp(self.A * dt.sum(0)), dt * np.exp(self.A * behind), np.abs(self.A) * dt.sum(0)
+
+    def state(self, slot, tokens):
+        """[H, P, N] with the waiting tokens, and the sum of the magnitudes of its terms"""
+        E, w, _ = self.terms(slot, tokens)
+        base = E[:, None, None] * self.t["scales"][slot].astype(np.float64)[..., None] * self.t["codes"][slot]
+        S, size = base, np.abs(base)
+        for i, j in enumerate(tokens):
+            x = self.s_x.reshape(self.H, self.P) * self.t["xwin"][slot, :, j % WINDOW]
+            B = (self.s_B[:, None] * self.t["Bwin"][slot, :, j % WINDOW])[self.group]
+            add = w[i][:, None, None] * x[..., None] * B[:, None]
+            S, size = S + add, size + np.abs(add)
+        return S, size
+
+    def write(self, slots, pos, state):
+        for b in range(state.shape[0]):
+            p = np.zeros(state.shape[0], int) if pos is None else pos
+            if not self.valid(slots, p, b):
+                continue
+            s = b if slots is None else int(slots[b])
+            with np.errstate(all="ignore"):
+                top = np.fmax.reduce(np.abs(state[b]), -1)
+                top = np.where(np.isnan(top), np.float32(0), top)
+                step = (top / np.float32(127)).astype(np.float32)
+                step[step == 0] = 1
+                q = (state[b] / step[..., None]).astype(np.float32)
+            self.t["codes"][s], self.t["scales"][s], self.t["start"][s] = code(q), step, p[b]
+
+    def step(self, u, dt, slots, pos, xBC, y):
+        """u [B, Ch]: SiLU of the convolution (64 bits); dt [B, H] fp32; xBC raw rows.  y [B, H * P] (64 bits) is changed; returns
+        the bound of binary32's error of y: the sum over the terms of (32 + |exponent|) 2^-24 of each (the exponential 4, its
+        argument |exponent|, the products and sums below 16, the epilogue 4)."""
+        bound = np.zeros_like(y)
+        HP, GN = self.H * self.P, self.G * self.N
+        sx = self.s_x.reshape(self.H, self.P)
+        for b in range(u.shape[0]):
+            s, p = (b if slots is None else int(slots[b])), int(pos[b])
+            if not self.valid(slots, pos, b):
+                continue
+            first = max(int(self.t["start"][s]), p - p % WINDOW)
+            if first > p:
+                continue
+            x = code(u[b, :HP] / self.s_x).reshape(self.H, self.P)
+            B = code(u[b, HP:HP + GN].reshape(self.G, self.N) / self.s_B[:, None])
+            Cq = code(u[b, HP + GN:].reshape(self.G, self.N) / self.s_C[:, None])
+            self.t["ring"][s, p % self.t["ring"].shape[1]] = xBC[b]
+            self.t["xwin"][s, :, p % WINDOW], self.t["Bwin"][s, :, p % WINDOW] = x, B
+            self.t["dtwin"][s, :, p % WINDOW] = dt[b]
+            tokens = list(range(first, p + 1))
+            E, w, exponent = self.terms(s, tokens)
+            Ch = Cq.astype(np.float64)[self.group]
+            part = E[:, None] * self.t["scales"][s] * (self.t["codes"][s] * Ch[:, None]).sum(-1)
+            v, size = part, np.abs(part)
+            # (a row's integer sum is exact, but eight lanes add their parts of it in binary32, each with its factor)
+            size = np.maximum(size, E[:, None] * self.t["scales"][s] * np.abs(self.t["codes"][s] * Ch[:, None]).sum(-1))
+            for i, j in enumerate(tokens):
+                cb = (Cq.astype(np.float64) * self.t["Bwin"][s, :, j % WINDOW]).sum(-1)[self.group]
+                part = sx * self.s_B[self.group][:, None] * (w[i] * cb)[:, None] * self.t["xwin"][s, :, j % WINDOW]
+                v, size = v + part, size + np.abs(part)
+            sC = self.s_C[self.group][:, None]
+            v, size = sC * v, sC * size
+            if self.D is not None:
+                v, size = v + self.D[:, None] * sx * x, size + np.abs(self.D[:, None] * sx * x)
+            if self.corr is not None:
+                v, size = v + self.corr.reshape(self.H, self.P), size + np.abs(self.corr.reshape(self.H, self.P))
+            y[b] = v.reshape(-1)
+            bound[b] = (2.0 ** -24 * (32 + exponent)[:, None] * size).reshape(-1)
+            if p % WINDOW == WINDOW - 1:
+                S, _ = self.state(s, tokens)
+                step = (np.abs(S).max(-1) / 127.0).astype(np.float32)
+                step[step == 0] = 1
+                self.t["codes"][s], self.t["scales"][s] = code(S / step[..., None].astype(np.float64)), step
+        return bound

@@ -253,3 +253,268 @@ def test_conv_on_a_side_stream_and_in_a_graph():
     again = {**c, "x": x}
     torch.cuda.synchronize()
     _conv_check(again, o, True, ring=ring, ring_before=before, pos=np.array([40, 40], np.int32))
+
+
+# ------------------------------------------------------------------------------------------------ 8-bit state cache
+class TokenArgs(C.Structure):
+    _fields_ = [("xBC", C.c_void_p), ("stride_b", C.c_int64), ("weight", C.c_void_p), ("bias", C.c_void_p), ("dt_raw", C.c_void_p),
+                ("dt_stride_b", C.c_int64)] + [(k, C.c_void_p) for k in ("dt_bias", "A", "D", "corr", "s_x", "s_B", "s_C", "slots",
+                                                                         "pos", "y", "status")]
+
+
+def _cache_struct(bd, **kw):
+    c = bd.Cache(nslots=4, width=4, dtype=2)
+    for k in ("codes", "scales", "xwin", "Bwin", "dtwin", "start", "ring"):
+        setattr(c, k, ADDR)
+    for k, v in kw.items():
+        setattr(c, k, v)
+    return c
+
+
+CACHE_REFUSALS = [
+    ("ERR_SHAPE", {"headdim": 128}, {}), ("ERR_SHAPE", {"dstate": 32}, {}), ("ERR_SHAPE", {"nheads": 5}, {}), ("ERR_SHAPE", {"batch": 0}, {}),
+    ("ERR_SHAPE", {}, {"nslots": 0}), ("ERR_SHAPE", {"batch": 5}, {}), ("ERR_NULL", {}, {"codes": None}), ("ERR_NULL", {}, {"scales": None}),
+    ("ERR_NULL", {}, {"xwin": None}), ("ERR_NULL", {}, {"Bwin": None}), ("ERR_NULL", {}, {"dtwin": None}), ("ERR_NULL", {}, {"start": None}),
+    ("ERR_ALIGN", {}, {"codes": ADDR + 8}), ("ERR_ALIGN", {}, {"xwin": ADDR + 4}),
+]
+
+
+@pytest.mark.parametrize("want,dims,cache", CACHE_REFUSALS)
+def test_cache_refuses(want, dims, cache):
+    bd, lib = _lib()
+    d, c, want = _dims(bd, **dims), _cache_struct(bd, **cache), getattr(bd, want)
+    a = TokenArgs(**{k: ADDR for k in ("xBC", "weight", "dt_raw", "A", "s_x", "s_B", "s_C", "pos", "y")})
+    p = C.c_void_p(ADDR)
+    assert lib.ssdi8_cache_write(C.byref(d), C.byref(c), None, p, p, None, None) == want
+    assert lib.ssdi8_cache_read(C.byref(d), C.byref(c), None, None, p, p, p, p, p, None, None) == want
+    assert lib.ssdi8_token_step(C.byref(d), C.byref(c), C.byref(a), 0, None) == want
+
+
+def test_cache_refuses_what_one_entry_needs():
+    bd, lib = _lib()
+    d, c, p = _dims(bd), _cache_struct(bd), C.c_void_p(ADDR)
+    assert lib.ssdi8_cache_write(C.byref(d), None, None, p, p, None, None) == bd.ERR_NULL
+    assert lib.ssdi8_cache_write(C.byref(d), C.byref(c), None, p, C.c_void_p(ADDR + 4), None, None) == bd.ERR_ALIGN
+    for k in range(4, 9):
+        args = [C.byref(d), C.byref(c), None, None] + [p] * 5
+        args[k] = None
+        assert lib.ssdi8_cache_read(*args, None, None) == bd.ERR_NULL
+    good = {k: ADDR for k in ("xBC", "weight", "dt_raw", "A", "s_x", "s_B", "s_C", "pos", "y")}
+    call = lambda cc, flags=0, **kw: lib.ssdi8_token_step(C.byref(d), C.byref(cc), C.byref(TokenArgs(**{**good, **kw})), flags, None)  # noqa: E731
+    for k in good:
+        assert call(c, **{k: None}) == bd.ERR_NULL, k
+    assert call(c, flags=bd.FLAG_Y_FP16 | bd.FLAG_Y_BF16) == bd.ERR_UNSUPPORTED
+    assert call(c, flags=bd.FLAG_INT8_STATE) == bd.ERR_UNSUPPORTED
+    assert call(c, y=ADDR + 2) == bd.ERR_ALIGN and call(c, xBC=ADDR + 1) == bd.ERR_ALIGN and call(c, weight=ADDR + 4) == bd.ERR_ALIGN
+    assert call(_cache_struct(bd, ring=None)) == bd.ERR_NULL
+    assert call(_cache_struct(bd, width=5)) == bd.ERR_SHAPE and call(_cache_struct(bd, width=1)) == bd.ERR_SHAPE
+    assert call(_cache_struct(bd, dtype=3)) == bd.ERR_UNSUPPORTED
+
+
+def _cache(rng, n, H, N, G, dtype="bfloat16", width=4, start=None):
+    """a cache with random contents, and the same as arrays"""
+    from paper_2608_21952_b200 import binding as bd
+    import torch
+    code = lambda *s: np.clip(np.rint(rng.standard_normal(s) * 40), -127, 127).astype(np.int8)  # noqa: E731
+    a = {"codes": code(n, H, 64, N), "scales": rng.uniform(0.001, 0.05, (n, H, 64)).astype(np.float32), "xwin": code(n, H, 16, 64),
+         "Bwin": code(n, G, 16, N), "dtwin": ref.softplus(rng.standard_normal((n, H, 16)) - 2).astype(np.float32),
+         "start": np.zeros(n, np.int32) if start is None else np.asarray(start, np.int32)}
+    ring = _t(rng.standard_normal((n, width, 64 * H + 2 * G * N)).astype(np.float32), dtype)
+    c = bd.cache_of(_dims(bd, 1, 1, H, 64, N, G), ring=ring, **{k: _t(v) for k, v in a.items()})
+    a["ring"] = _np(ring).copy()
+    return c, a, torch
+
+
+def _same(c, a, names=("codes", "scales", "xwin", "Bwin", "dtwin", "start", "ring")):
+    for k in names:
+        np.testing.assert_array_equal(_np(c.tensors[k]), a[k], err_msg=k)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("B,H,N,G", [(1, 1, 64, 1), (3, 5, 128, 1), (6, 4, 64, 2), (2, 24, 128, 1), (9, 16, 128, 8)])
+def test_cache_write(B, H, N, G):
+    from paper_2608_21952_b200 import binding as bd
+    rng = np.random.default_rng(B * H)
+    c, a, torch = _cache(rng, B + 3, H, N, G)
+    d = _dims(bd, B, 1, H, 64, N, G)
+    S = (rng.standard_normal((B, H, 64, N)) * 10.0 ** rng.uniform(-3, 3, (B, H, 64, 1))).astype(np.float32)
+    S[0, 0, 0], S[0, 0, 1], S[0, 0, 2, 3], S[0, 0, 3, 5] = 0, 1e-44, np.nan, np.inf
+    S[0, 0, 4] *= 1e-34
+    S[0, 0, 5], S[0, 0, 6] = 0, np.nan
+    S[0, 0, 5, 0] = 2.0 ** -149
+    slots, pos = rng.permutation(B + 3)[:B].astype(np.int32), rng.integers(0, 99, B).astype(np.int32)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    if B > 3:
+        slots[-1], slots[-2], slots[-3], pos[1] = -1, slots[0], B + 3, -1
+    s = ref.Slots(a, np.ones(H), np.ones(H * 64), np.ones(G))
+    s.write(slots, pos, S)
+    bd.ssdi8_cache_write(d, c, _t(slots), _t(pos), _t(S), status)
+    _same(c, a)
+    assert int(status.item()) == (-2 if B > 3 else 0)
+    s.write(None, None, np.zeros_like(S))   # (no state: zeros, slot b, position 0)
+    bd.ssdi8_cache_write(d, c, None, None, None)
+    _same(c, a)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("B,H,N,G", [(1, 1, 64, 1), (3, 5, 128, 1), (20, 4, 64, 2), (18, 16, 128, 8)])
+def test_cache_read(B, H, N, G):
+    from paper_2608_21952_b200 import binding as bd
+    rng = np.random.default_rng(B + H)
+    n = B + 2
+    pos = rng.integers(0, 64, B).astype(np.int32)
+    pos[:min(B, 3)] = [48, 31, 17][:min(B, 3)]
+    slots = rng.permutation(n)[:B].astype(np.int32)
+    start = np.zeros(n, np.int32)
+    start[slots] = np.maximum(0, pos - rng.integers(0, 12, B))
+    if B > 3:
+        slots[4], slots[5], pos[6] = -3, slots[0], -2
+        start[slots[7]] = pos[7] + 1   # (written behind where it is read)
+    c, a, torch = _cache(rng, n, H, N, G, start=start)
+    A = -np.exp(rng.uniform(0, np.log(16), H)).astype(np.float32)
+    A[0] = 0.05   # (a growing head)
+    s_x, s_B = rng.uniform(0.01, 0.05, H * 64).astype(np.float32), rng.uniform(0.01, 0.02, G).astype(np.float32)
+    s = ref.Slots(a, A, s_x, s_B)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    for first in (None, np.maximum(0, pos - rng.integers(0, 17, B)).astype(np.int32)):
+        if first is not None and B > 8:
+            first[8], first[9] = pos[8] - 17, pos[9] + 1
+        out = torch.full((B, H, 64, N), 7.0, device="cuda")
+        bd.ssdi8_cache_read(_dims(bd, B, 1, H, 64, N, G), c, _t(slots), _t(pos), _t(A), _t(s_x), _t(s_B), out,
+                            first=None if first is None else _t(first), status=status)
+        got = _np(out)
+        for b in range(B):
+            ok = s.valid(slots, pos, b)
+            f = 0 if not ok else max(int(start[slots[b]]), pos[b] - pos[b] % 16) if first is None else int(first[b])
+            if not ok or f < 0 or not 0 <= pos[b] - f <= 16:
+                assert np.all(got[b] == 7.0)
+                continue
+            S, size = s.state(int(slots[b]), list(range(f, pos[b])))
+            # binary32: the exponential's and the factors' roundings, a product and up to 16 fused additions
+            assert np.all(np.abs(got[b] - S) <= 24 * 2.0 ** -24 * size + 1e-38), b
+        assert int(status.item()) == (-2 if B > 3 else 0)
+    _same(c, a)   # (nothing is written)
+
+
+# ------------------------------------------------------------------------------------------------ token step
+def _token_params(rng, H, N, G, W):
+    HP, Ch = 64 * H, 64 * H + 2 * G * N
+    w = rng.uniform(-0.5, 0.5, (Ch, W)).astype(np.float32)
+    w[rng.permutation(HP)[:2]] *= 50
+    A = -np.exp(rng.uniform(0, np.log(16), H)).astype(np.float32)
+    return {"w": w, "bias": (0.1 * rng.standard_normal(Ch)).astype(np.float32), "dt_bias": (-3 + rng.standard_normal(H)).astype(np.float32),
+            "A": A, "D": rng.standard_normal(H).astype(np.float32), "corr": (0.1 * rng.standard_normal(HP)).astype(np.float32),
+            "s_x": (3.0 / 127 * np.sqrt((w[:HP] ** 2).sum(1) + 0.01)).astype(np.float32),
+            "s_B": rng.uniform(0.01, 0.02, G).astype(np.float32), "s_C": rng.uniform(0.01, 0.02, G).astype(np.float32)}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("B,H,N,G,W,dtype,ydt,steps", [
+    (1, 1, 64, 1, 4, "bfloat16", "float32", 34), (1, 3, 128, 1, 3, "float16", "float16", 18), (5, 4, 64, 2, 2, "float32", "float32", 18),
+    (3, 24, 128, 1, 4, "bfloat16", "bfloat16", 17), (4, 9, 128, 3, 4, "bfloat16", "float32", 17), (2, 16, 64, 8, 4, "bfloat16", "bfloat16", 17),
+])
+def test_token_steps(B, H, N, G, W, dtype, ydt, steps):
+    """sequences at different positions (0 among them, and one whose slot was written in the middle of a window), step after step:
+    every tensor of the cache equal, y within binary32's error; a padding row and its slot stay as they are"""
+    from paper_2608_21952_b200 import binding as bd
+    rng = np.random.default_rng(10 * B + H)
+    n = B + 3
+    slots = rng.permutation(n)[:B].astype(np.int32)
+    pos = rng.integers(0, 40, B).astype(np.int32)
+    pos[0] = 0
+    start = rng.integers(0, 1, n)
+    start[slots] = np.maximum(0, pos - rng.integers(0, 9, B))
+    if B > 2:
+        slots[B - 1] = -1
+    c, a, torch = _cache(rng, n, H, N, G, dtype, W, start)
+    p = _token_params(rng, H, N, G, W)
+    p["bias"] = None if W == 3 else p["bias"]
+    p["corr"] = None if W == 2 else p["corr"]
+    p["D"] = None if W == 2 else p["D"]
+    s = ref.Slots(a, p["A"], p["s_x"], p["s_B"], p["s_C"], p["D"], p["corr"])
+    dev = {k: None if v is None else _t(v) for k, v in p.items()}
+    Ch, d = 64 * H + 2 * G * N, _dims(bd, B, 1, H, 64, N, G)
+    y = torch.full((B, 64 * H), 5.0, device="cuda").to(getattr(torch, ydt))
+    want = np.full((B, 64 * H), 5.0)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    half = {"float32": 0.0, "float16": 2.0 ** -11, "bfloat16": 2.0 ** -8}[ydt]
+    live = slots >= 0
+    for step in range(steps):
+        rows = _t(rng.standard_normal((B, 3 + Ch + H)).astype(np.float32), dtype)
+        x, raw = rows[:, 3:3 + Ch], rows[:, 3 + Ch:]
+        u = ref.conv(_np(x)[:, None], p["w"], p["bias"], None, a["ring"].copy(), slots, pos)[:, 0]
+        bd.ssdi8_token_step(d, c, x, dev["w"], dev["bias"], raw, dev["dt_bias"], dev["A"], dev["D"], dev["corr"], dev["s_x"], dev["s_B"],
+                            dev["s_C"], _t(slots), _t(pos), y, status=status, flags=bd.FLAG_DT_SOFTPLUS)
+        dt = ref.softplus((_np(raw) + p["dt_bias"]).astype(np.float64))
+        got = np.stack([_np(c.tensors["dtwin"])[max(slots[b], 0), :, pos[b] % 16] for b in range(B)])
+        np.testing.assert_allclose(got[live], dt[live], rtol=2.0 ** -23)
+        bound = s.step(u, got, slots, pos, _np(x), want)
+        _same(c, a)
+        off = np.abs(_np(y) - want)
+        assert np.all(off <= bound + half * (np.abs(want) + bound) + (2.0 ** -25 if ydt == "float16" else 0)), (step, off.max())
+        pos = pos + 1
+    assert int(status.item()) == 0
+
+
+@pytest.mark.gpu
+def test_token_step_takes_bad_rows_for_padding():
+    """a slot out of range, one named twice, a negative position, a slot written behind the position: status set, the rows' y and
+    slots as they were, the other rows right; without the softplus, without slots"""
+    from paper_2608_21952_b200 import binding as bd
+    rng = np.random.default_rng(3)
+    B, H, N, G = 6, 2, 64, 1
+    slots, pos = np.array([2, 7, 2, 0, 1, 3], np.int32), np.array([4, 4, 4, -1, 9, 20], np.int32)
+    c, a, torch = _cache(rng, 6, H, N, G, start=[0, 10, 0, 0, 0, 0])
+    p = _token_params(rng, H, N, G, 4)
+    s = ref.Slots(a, p["A"], p["s_x"], p["s_B"], p["s_C"], p["D"], p["corr"])
+    dev = {k: _t(v) for k, v in p.items()}
+    x = _t(rng.standard_normal((B, 64 * H + 2 * N)).astype(np.float32), "bfloat16")
+    raw = _t(rng.uniform(0.01, 0.1, (B, H)).astype(np.float32), "bfloat16")
+    for sl in (slots, None):
+        y = torch.full((B, 64 * H), 5.0, device="cuda")
+        want, status = np.full((B, 64 * H), 5.0), torch.zeros(1, dtype=torch.int32, device="cuda")
+        u = ref.conv(_np(x)[:, None], p["w"], p["bias"], None, a["ring"].copy(), sl, pos)[:, 0]
+        bd.ssdi8_token_step(_dims(bd, B, 1, H, 64, N, G), c, x, dev["w"], dev["bias"], raw, dev["dt_bias"], dev["A"], dev["D"], dev["corr"],
+                            dev["s_x"], dev["s_B"], dev["s_C"], None if sl is None else _t(sl), _t(pos), y, status=status)
+        bound = s.step(u, _np(raw), sl, pos, _np(x), want)
+        _same(c, a)
+        assert np.all(np.abs(_np(y) - want) <= bound)
+        assert int(status.item()) == -2
+    assert np.all(want[3] == 5.0)
+
+
+@pytest.mark.gpu
+def test_token_steps_in_a_graph_equal_eager_ones():
+    """one captured step, replayed 20 times with the position counted on the device, on two caches that share nothing"""
+    from paper_2608_21952_b200 import binding as bd
+    rng = np.random.default_rng(4)
+    B, H, N, G = 3, 4, 128, 1
+    c, a, torch = _cache(rng, B, H, N, G)
+    other = bd.cache_of(_dims(bd, B, 1, H, 64, N, G), **{k: t.clone() for k, t in c.tensors.items()})
+    dev = {k: _t(v) for k, v in _token_params(rng, H, N, G, 4).items()}
+    tokens = _t(rng.standard_normal((20, B, 64 * H + 2 * N)).astype(np.float32), "bfloat16")
+    raws = _t(rng.standard_normal((20, B, H)).astype(np.float32), "bfloat16")
+    x, raw, pos, y = tokens[0].clone(), raws[0].clone(), torch.tensor([0, 5, 11], dtype=torch.int32, device="cuda"), torch.empty(B, 64 * H, device="cuda")
+
+    def step(cache, out):
+        bd.ssdi8_token_step(_dims(bd, B, 1, H, 64, N, G), cache, x, dev["w"], dev["bias"], raw, dev["dt_bias"], dev["A"], dev["D"], dev["corr"],
+                            dev["s_x"], dev["s_B"], dev["s_C"], None, pos, out, flags=bd.FLAG_DT_SOFTPLUS)
+    y2 = torch.empty_like(y)
+    keep = {k: t.clone() for k, t in c.tensors.items()}
+    step(c, y)   # (first use outside the capture)
+    for k, t in keep.items():
+        c.tensors[k].copy_(t)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(c, y)
+        pos += 1
+    pos.copy_(torch.tensor([0, 5, 11]))
+    for i in range(20):
+        x.copy_(tokens[i])
+        raw.copy_(raws[i])
+        step(other, y2)   # (before the replay counts the position on)
+        graph.replay()
+        assert torch.equal(y, y2), i
+        for k in c.tensors:
+            assert torch.equal(c.tensors[k], other.tensors[k]), (i, k)
