@@ -30,7 +30,7 @@ __global__ void __launch_bounds__(SC_T) cache_write_kernel(CacheView c, const in
   const i64 row0 = ((i64)slot * H + h) * 64 + p0;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    float m = fmaxf(fmaxf(fabsf(v[r].x), fabsf(v[r].y)), fmaxf(fabsf(v[r].z), fabsf(v[r].w)));
+    float m = fmaxf(fmaxf(fmaxf(fabsf(v[r].x), fabsf(v[r].y)), fmaxf(fabsf(v[r].z), fabsf(v[r].w))), 0.f);   // (not NaN)
 #pragma unroll
     for (int o = N4 / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
     float s = step_of_max(__float_as_uint(m));
