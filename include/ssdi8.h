@@ -447,6 +447,39 @@ typedef struct {
 ssdi8_status_t ssdi8_token_step(const ssdi8_dims_t* dims, const ssdi8_cache_t* cache, const ssdi8_token_args_t* args, uint32_t flags,
                                 void* stream);
 
+/* RMS norm of rows with the block's gate, ending in the int8 codes of a projection's input (Eq. 1, one step size per token or one in all):
+ *   u = x z / (1 + exp(-z)) (z = NULL: u = x);  o = u w / sqrt(mean over the channel's group of u^2 + eps) (w = NULL: 1)
+ *   static_scale = NULL: step = absmax of the row's o / 127 (1 if that is 0), code = rne(127 o / absmax), scale[row] = (float)step
+ *   else:                code = rne(o / *static_scale) saturated; scale is not written
+ * A NaN counts for nothing in the absmax and has the code +127.  A row of width channels is `groups` groups of consecutive ones: groups = 1
+ * and width % 16 = 0, or groups of a multiple of 128; width <= 16384.  x has type dtype, z zdtype (ignored without z), any strides of rows;
+ * xq [rows][width]; weight and xq 16-byte aligned, x and z at an element's alignment.  rows may be 0. */
+typedef struct {
+  const void* x; int64_t stride_x; const void* z; int64_t stride_z;
+  const float* weight;                              /* [width] or NULL                */
+  int8_t* xq; float* scale;                         /* [rows][width], [rows] or NULL  */
+  const float* static_scale;                        /* 1 word on the DEVICE, or NULL  */
+  int64_t rows; int32_t width, groups; float eps;
+} ssdi8_norm_args_t;
+ssdi8_status_t ssdi8_norm_quantize(const ssdi8_norm_args_t* args, int32_t dtype, int32_t zdtype, void* stream);
+
+/* Int8 projection (the in-proj and out-proj of the block, W8A8) with everything behind the product in its epilogue:
+ *   acc[t,o] = sum_k xq[t,k] wq[o,k], INT32, exact;  out = act(s_row[t] s_w[o] acc + bias[o]) + residual[t,o]
+ * in binary32, rounded once to out's type.  act: SSDI8_ACT_NONE, v / (1 + exp(-v)) (_SILU), max(v, 0)^2 (_RELU2).  xq [rows][inner],
+ * wq [outs][inner] (step sizes s_w per output), dense and 16-byte aligned; inner % 16 = 0, 16 <= inner <= 131072 (the sums stay in
+ * 32 bits).  s_row, bias, residual may be NULL (1, 0, 0): the paper adds its mean correction at the out-proj (Section 4.3), which is `bias`
+ * here.  out, residual: type dtype, any strides of rows (overlapping rows aside); residual may be out itself.  rows may be 0. */
+enum { SSDI8_ACT_NONE = 0, SSDI8_ACT_SILU = 1, SSDI8_ACT_RELU2 = 2 };
+typedef struct {
+  const int8_t* xq; const int8_t* wq;
+  const float* s_row; const float* s_w; const float* bias;   /* [rows], [outs], [outs] */
+  const void* residual; int64_t stride_residual;
+  void* out; int64_t stride_out;
+  int32_t rows, outs, inner, act;
+  int32_t* status;                                           /* 1 word, or NULL: SSDI8_ERR_DEVICE_TIMEOUT if a wait ran out */
+} ssdi8_linear_args_t;
+ssdi8_status_t ssdi8_linear(const ssdi8_linear_args_t* args, int32_t dtype, void* stream);
+
 /* Measurement aid (the paper has no counterpart): what tcgen05.mma.kind::i8 sustains on the current
  * device, for the "fraction of the int8 tensor-pipe peak" a benchmark reports.  One CTA per SM issues
  * `mma_per_sm` (rounded down to a multiple of 128, at least 128) dense MMAs of M 128 x N 256 x K 32

@@ -48,9 +48,11 @@ EXPORTS = ("ssdi8_status_string", "ssdi8_workspace_bytes", "ssdi8_quantize_act",
            "ssdi8_layer_fwd", "ssdi8_layer_fwd_workspace_bytes",
            "ssdi8_layer_fwd_host", "ssdi8_layer_fwd_host_scratch_bytes",
            "ssdi8_int8_mma_peak", "ssdi8_selftest_bounded_wait", "ssdi8_softplus_dt",
-           "ssdi8_conv_fwd", "ssdi8_cache_write", "ssdi8_cache_read", "ssdi8_token_step")
+           "ssdi8_conv_fwd", "ssdi8_cache_write", "ssdi8_cache_read", "ssdi8_token_step",
+           "ssdi8_norm_quantize", "ssdi8_linear")
 STATIC_WORKSPACE_BYTES = 16 << 20
 CACHE_WINDOW = 16
+ACT_NONE, ACT_SILU, ACT_RELU2 = 0, 1, 2
 
 
 class Dims(C.Structure):
@@ -359,6 +361,21 @@ def ssdi8_token_step(dims: Dims, cache: Cache, xBC, weight, bias, dt_raw, dt_bia
                          stream)
     if code:
         _check(code, "ssdi8_token_step")
+
+
+def ssdi8_norm_quantize(x, xq, weight=None, z=None, groups: int = 1, eps: float = 1e-5, scale=None, static_scale=None,
+                        stream=None) -> None:
+    """RMS norm of x [T, D], with the gate z [T, D] if given (rows of any stride), to int8 codes xq and a step size per row."""
+    code = _m.norm_quantize(x, xq, weight, z, groups, eps, scale, static_scale, stream)
+    if code:
+        _check(code, "ssdi8_norm_quantize")
+
+
+def ssdi8_linear(xq, wq, s_w, out, s_row=None, bias=None, residual=None, act: int = ACT_NONE, status=None, stream=None) -> None:
+    """out [T, O] = act(s_row s_w (xq [T, K] wq [O, K]^T) + bias) + residual (rows of out and residual of any stride)."""
+    code = _m.linear(xq, wq, s_w, out, s_row, bias, residual, act, status, stream)
+    if code:
+        _check(code, "ssdi8_linear")
 
 
 def ssdi8_int8_mma_peak(mma_per_sm: int, status=None, stream=None) -> float:

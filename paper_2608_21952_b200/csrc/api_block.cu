@@ -91,4 +91,32 @@ ssdi8_status_t ssdi8_token_step(const ssdi8_dims_t* dims, const ssdi8_cache_t* c
                            (flags & SSDI8_FLAG_Y_FP16) ? 1 : (flags & SSDI8_FLAG_Y_BF16) ? 2 : 0, static_cast<cudaStream_t>(stream));
 }
 
+ssdi8_status_t ssdi8_norm_quantize(const ssdi8_norm_args_t* a, int32_t dtype, int32_t zdtype, void* stream) {
+  if (!a) return SSDI8_ERR_NULL;
+  if (dtype < 0 || dtype > 2 || (a->z && (zdtype < 0 || zdtype > 2))) return SSDI8_ERR_UNSUPPORTED;
+  if (a->rows < 0 || a->rows > 0x7fffffff || a->width <= 0 || a->width > kMaxNormWidth || a->width % 16 != 0 || a->groups <= 0) return SSDI8_ERR_SHAPE;
+  if (a->groups > 1 && (a->width % a->groups != 0 || (a->width / a->groups) % 128 != 0)) return SSDI8_ERR_SHAPE;
+  if (!(a->eps >= 0.f)) return SSDI8_ERR_SHAPE;
+  if (a->rows == 0) return SSDI8_OK;
+  if (!a->x || !a->xq) return SSDI8_ERR_NULL;
+  if (!aligned16(a->weight) || !aligned16(a->xq) || !aligned_to(a->x, elem_size(dtype)) || !aligned_to(a->z, elem_size(zdtype)))
+    return SSDI8_ERR_ALIGN;
+  const ssdi8_status_t s = check_arch();
+  if (s != SSDI8_OK) return s;
+  return launch_norm_quantize(*a, dtype, zdtype, static_cast<cudaStream_t>(stream));
+}
+
+ssdi8_status_t ssdi8_linear(const ssdi8_linear_args_t* a, int32_t dtype, void* stream) {
+  if (!a) return SSDI8_ERR_NULL;
+  if (dtype < 0 || dtype > 2 || a->act < SSDI8_ACT_NONE || a->act > SSDI8_ACT_RELU2) return SSDI8_ERR_UNSUPPORTED;
+  if (a->rows < 0 || a->outs <= 0 || a->inner < 16 || a->inner > 131072 || a->inner % 16 != 0) return SSDI8_ERR_SHAPE;
+  if (a->rows == 0) return SSDI8_OK;
+  if (!a->xq || !a->wq || !a->s_w || !a->out) return SSDI8_ERR_NULL;
+  if (!aligned16(a->xq) || !aligned16(a->wq) || !aligned_to(a->out, elem_size(dtype)) || !aligned_to(a->residual, elem_size(dtype)))
+    return SSDI8_ERR_ALIGN;
+  const ssdi8_status_t s = check_arch();
+  if (s != SSDI8_OK) return s;
+  return launch_linear(*a, dtype, static_cast<cudaStream_t>(stream));
+}
+
 }  // extern "C"

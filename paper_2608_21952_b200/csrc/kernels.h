@@ -173,13 +173,16 @@ int mean_correction_slabs(i64 R);
 ssdi8_status_t launch_mean_correction(const float* y, const float* yq, i64 R, i64 Ch, float eta, float* corr,
                                       double* partial, cudaStream_t st);
 
-// the operators around the layer (conv.cu, state_cache.cu, token_step.cu)
+// the operators around the layer (conv.cu, state_cache.cu, token_step.cu, norm_quantize.cu, linear.cu)
 ssdi8_status_t launch_conv(const Dims& d, const ssdi8_conv_args_t& a, int dtype, int width, bool softplus, cudaStream_t st);
 ssdi8_status_t launch_cache_write(const Dims& d, const ssdi8_cache_t& c, const int32_t* slots, const int32_t* pos, const float* state,
                                   int32_t* status, cudaStream_t st);
 ssdi8_status_t launch_cache_read(const Dims& d, const ssdi8_cache_t& c, const int32_t* slots, const int32_t* first, const int32_t* pos,
                                  const float* A, const float* s_x, const float* s_B, float* state, int32_t* status, cudaStream_t st);
 ssdi8_status_t launch_token_step(const Dims& d, const ssdi8_cache_t& c, const ssdi8_token_args_t& a, bool softplus, int ydt, cudaStream_t st);
+constexpr int kMaxNormWidth = 16384;
+ssdi8_status_t launch_norm_quantize(const ssdi8_norm_args_t& a, int dtype, int zdtype, cudaStream_t st);
+ssdi8_status_t launch_linear(const ssdi8_linear_args_t& a, int dtype, cudaStream_t st);
 
 // measurement aid and self-test (selftest.cu): `nbatch` batches of int8_mma_peak_batch() MMAs of
 // M 128 x N 256 x K 32 on every SM (ctas = number of CTAs launched); a bounded wait that runs out

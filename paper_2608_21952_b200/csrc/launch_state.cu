@@ -12,11 +12,11 @@ struct Slot {
   std::atomic<const void*> kernel{nullptr};
   std::atomic<uint64_t> devices{0};
 };
-constexpr int kSlots = 256;   // the library has about two hundred kernels, most of them with attributes
+constexpr int kSlots = 512;   // the library has some 250 kernels, most of them with attributes
 Slot g_slots[kSlots];
 
 Slot* find_slot(const void* kernel) {
-  size_t i = (reinterpret_cast<uintptr_t>(kernel) >> 4) * 0x9E3779B97F4A7C15ull >> 56;
+  size_t i = (reinterpret_cast<uintptr_t>(kernel) >> 4) * 0x9E3779B97F4A7C15ull >> 55;
   for (int probe = 0; probe < kSlots; ++probe, i = (i + 1) & (kSlots - 1)) {
     const void* seen = g_slots[i].kernel.load(std::memory_order_acquire);
     if (seen == kernel) return &g_slots[i];

@@ -410,6 +410,47 @@ ENTRY(token_step, 19) {
   return call([&] { return ssdi8_token_step(d.get(), c.get(), &t, fl, st); });
 } END
 
+ENTRY(norm_quantize, 9) {   // x, xq, weight, z, groups, eps, scale, static_scale, stream
+  const Tensor x = tensor(a[0], "x", kAnyFloat, {-1, -1}, false, true);
+  const int64_t T = x.size(0), D = x.size(1);
+  if (D > 0x7fffffff) throw BadShape{};
+  ssdi8_norm_args_t n = {};
+  n.x = x.data(); n.stride_x = x.stride(0);
+  n.xq = tensor(a[1], "xq", kInt8, {T, D}).as<int8_t>();
+  n.weight = tensor(a[2], "weight", 0, {D}, true).as<float>();
+  const Tensor z = tensor(a[3], "z", kAnyFloat, {T, D}, true, true);
+  if (z) { n.z = z.data(); n.stride_z = z.stride(0); }
+  n.groups = (int32_t)integer(a[4]);
+  n.eps = real(a[5]);
+  n.scale = tensor(a[6], "scale", 0, {T}, true).as<float>();
+  n.static_scale = tensor(a[7], "static_scale", 0, {1}, true).as<float>();
+  n.rows = T; n.width = (int32_t)D;
+  void* st = stream(a[8]);
+  return call([&] { return ssdi8_norm_quantize(&n, x.dtype, z.dtype, st); });
+} END
+
+ENTRY(linear, 10) {   // xq, wq, s_w, out, s_row, bias, residual, act, status, stream
+  const Tensor x = tensor(a[0], "xq", kInt8, {-1, -1});
+  const int64_t T = x.size(0), K = x.size(1);
+  const Tensor w = tensor(a[1], "wq", kInt8, {-1, K});
+  const int64_t O = w.size(0);
+  if (T > 0x7fffffff || O > 0x7fffffff || K > 0x7fffffff) throw BadShape{};
+  ssdi8_linear_args_t l = {};
+  l.xq = x.as<int8_t>(); l.wq = w.as<int8_t>();
+  l.s_w = tensor(a[2], "s_w", 0, {O}).as<float>();
+  const Tensor out = tensor(a[3], "out", kAnyFloat, {T, O}, false, true);
+  l.out = out.data(); l.stride_out = out.stride(0);
+  l.s_row = tensor(a[4], "s_row", 0, {T}, true).as<float>();
+  l.bias = tensor(a[5], "bias", 0, {O}, true).as<float>();
+  const Tensor r = tensor(a[6], "residual", out.dtype, {T, O}, true, true);
+  if (r) { l.residual = r.data(); l.stride_residual = r.stride(0); }
+  l.rows = (int32_t)T; l.outs = (int32_t)O; l.inner = (int32_t)K;
+  l.act = (int32_t)integer(a[7]);
+  l.status = tensor(a[8], "status", kInt32, {1}, true).as<int32_t>();
+  void* st = stream(a[9]);
+  return call([&] { return ssdi8_linear(&l, out.dtype, st); });
+} END
+
 #undef ENTRY
 #undef END
 
@@ -417,7 +458,7 @@ ENTRY(token_step, 19) {
 PyMethodDef kMethods[] = {METHOD(init), METHOD(quantize_act), METHOD(quantize_entry), METHOD(chunk_scan_fwd), METHOD(chunk_scan_fwd_static),
                           METHOD(layer_fwd), METHOD(layer_fwd_host), METHOD(calibrate), METHOD(mean_correction),
                           METHOD(state_passing), METHOD(ssd_step), METHOD(softplus_dt), METHOD(conv_fwd), METHOD(cache_write),
-                          METHOD(cache_read), METHOD(token_step), {nullptr, nullptr, 0, nullptr}};
+                          METHOD(cache_read), METHOD(token_step), METHOD(norm_quantize), METHOD(linear), {nullptr, nullptr, 0, nullptr}};
 #undef METHOD
 
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};

@@ -136,3 +136,26 @@ class Slots:
                 step[step == 0] = 1
                 self.t["codes"][s], self.t["scales"][s] = code(S / step[..., None].astype(np.float64)), step
         return bound
+
+
+def norm(x, z, weight, groups, eps):
+    """o of the gated RMS norm, and the same without the norm where the row is one group (it cancels out of 127 o / absmax)"""
+    T, D = x.shape
+    with np.errstate(all="ignore"):
+        u = x.astype(np.float64) if z is None else x.astype(np.float64) * silu(z.astype(np.float64))
+        g = u.reshape(T, groups, D // groups)
+        w = np.ones(D) if weight is None else weight.astype(np.float64)
+        o = (g / np.sqrt((g * g).mean(-1, keepdims=True) + eps)).reshape(T, D) * w
+        return o, (u * w if groups == 1 else o)
+
+
+def norm_codes(x, z, weight, groups, eps, static=None):
+    o, v = norm(x, z, weight, groups, eps)
+    with np.errstate(all="ignore"):
+        if static is not None:
+            return code(o / np.float64(static)), None
+        if groups == 1:   # (an overflow of the squares alone must not reach the codes)
+            v = np.where(np.isnan(o), np.nan, v)
+        top, of = np.nan_to_num(np.fmax.reduce(np.abs(v), -1), nan=0.0, posinf=np.inf), np.nan_to_num(np.fmax.reduce(np.abs(o), -1), nan=0.0, posinf=np.inf)
+        q = np.where(top[:, None] > 0, 127.0 * v / np.where(top > 0, top, 1)[:, None], v)
+        return code(q), np.where(of > 0, of / 127.0, 1.0)

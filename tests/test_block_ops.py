@@ -518,3 +518,209 @@ def test_token_steps_in_a_graph_equal_eager_ones():
         assert torch.equal(y, y2), i
         for k in c.tensors:
             assert torch.equal(c.tensors[k], other.tensors[k]), (i, k)
+
+
+# ------------------------------------------------------------------------------------------------ norm
+class NormArgs(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("stride_x", C.c_int64), ("z", C.c_void_p), ("stride_z", C.c_int64), ("weight", C.c_void_p),
+                ("xq", C.c_void_p), ("scale", C.c_void_p), ("static_scale", C.c_void_p), ("rows", C.c_int64), ("width", C.c_int32),
+                ("groups", C.c_int32), ("eps", C.c_float)]
+
+
+@pytest.mark.parametrize("want,args,dtype,zdtype", [
+    ("ERR_UNSUPPORTED", {}, 3, 0), ("ERR_UNSUPPORTED", {"z": ADDR}, 0, 3), ("ERR_UNSUPPORTED", {}, -1, 0),
+    ("ERR_SHAPE", {"rows": -1}, 0, 0), ("ERR_SHAPE", {"rows": 1 << 31}, 0, 0), ("ERR_SHAPE", {"width": 0}, 0, 0), ("ERR_SHAPE", {"width": 72}, 0, 0),
+    ("ERR_SHAPE", {"width": 16400}, 0, 0), ("ERR_SHAPE", {"groups": 0}, 0, 0), ("ERR_SHAPE", {"groups": 3}, 0, 0),
+    ("ERR_SHAPE", {"width": 128, "groups": 2}, 0, 0), ("ERR_SHAPE", {"eps": -1.0}, 0, 0), ("ERR_SHAPE", {"eps": float("nan")}, 0, 0),
+    ("ERR_NULL", {"x": None}, 0, 0), ("ERR_NULL", {"xq": None}, 0, 0), ("ERR_ALIGN", {"xq": ADDR + 4}, 0, 0),
+    ("ERR_ALIGN", {"weight": ADDR + 4}, 0, 0), ("ERR_ALIGN", {"x": ADDR + 2}, 0, 0), ("ERR_ALIGN", {"z": ADDR + 1}, 0, 1), ("OK", {"rows": 0, "x": None}, 0, 0),
+])
+def test_norm_refuses(want, args, dtype, zdtype):
+    bd, lib = _lib()
+    a = NormArgs(**{**dict(x=ADDR, stride_x=512, xq=ADDR, scale=ADDR, rows=4, width=512, groups=1, eps=1e-5), **args})
+    assert lib.ssdi8_norm_quantize(C.byref(a), dtype, zdtype, None) == getattr(bd, want)
+    assert lib.ssdi8_norm_quantize(None, 0, 0, None) == bd.ERR_NULL
+
+
+def _norm_check(x, z, weight, groups, eps, static=None, scale=True):
+    from paper_2608_21952_b200 import binding as bd
+    import torch
+    T, D = x.shape
+    xq = torch.full((T, D), 99, dtype=torch.int8, device="cuda")
+    sc = torch.full((T,), 7.0, device="cuda") if scale else None
+    bd.ssdi8_norm_quantize(x, xq, weight=None if weight is None else _t(weight), z=z, groups=groups, eps=eps, scale=sc,
+                           static_scale=None if static is None else _t(np.array([static], np.float32)))
+    want, step = ref.norm_codes(_np(x), None if z is None else _np(z), weight, groups, eps, static)
+    np.testing.assert_array_equal(_np(xq), want)
+    if scale and static is None:
+        # binary32: 12 eps of u w, 24 of the norm, and the quotient
+        np.testing.assert_allclose(_np(sc), step, rtol=40 * 2.0 ** -24, atol=1e-38)
+
+
+NORM = [  # T, D, groups, dtype, gate, offset
+    (1, 16, 1, "float32", None, 0), (3, 48, 1, "bfloat16", "bfloat16", 1), (5, 144, 1, "float16", "float32", 0), (130, 768, 1, "bfloat16", None, 2),
+    (7, 1536, 2, "float32", "bfloat16", 0), (300, 2560, 1, "float32", "float16", 4), (33, 5120, 1, "bfloat16", "bfloat16", 3),
+    (9, 8192, 8, "bfloat16", "bfloat16", 0), (2, 16384, 1, "float16", "float16", 0), (2, 16384, 4, "float32", None, 1), (40, 5120, 1, "float32", "bfloat16", 0),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,D,groups,dtype,gate,offset", NORM)
+def test_norm(T, D, groups, dtype, gate, offset):
+    rng = np.random.default_rng(T + D)
+    x = rng.standard_normal((T, D + 2 * offset)).astype(np.float32)
+    x[:, rng.permutation(D)[:max(1, D // 100)]] *= 20
+    x = _t(x, dtype)[:, offset:offset + D]
+    z = None if gate is None else _t((2 * rng.standard_normal((T, D + 7))).astype(np.float32), gate)[:, offset:offset + D]
+    weight = rng.uniform(0.5, 1.5, D).astype(np.float32)
+    _norm_check(x, z, weight, groups, 1e-5)
+    _norm_check(x, z, weight, groups, 1e-5, static=0.04, scale=False)
+    if gate:
+        _norm_check(x, z, None if groups == 1 else weight, groups, 0.1)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("groups", [1, 2])
+@pytest.mark.parametrize("gate", [None, "float32"])
+def test_norm_of_extreme_rows(groups, gate):
+    """rows of zeros, of one value, beyond binary32's squares on either side, with infinities and NaN, with gates that close"""
+    rng = np.random.default_rng(8)
+    D = 512
+    x, z = rng.standard_normal((14, D)).astype(np.float32), rng.standard_normal((14, D)).astype(np.float32)
+    weight = rng.uniform(0.5, 1.5, D).astype(np.float32)
+    x[0], x[1, 1:], x[2], x[3] = 0, 0, x[2] * 1e25, x[3] * 1e-30
+    x[4, 7], x[5, 9], x[6] = np.nan, np.inf, np.nan
+    z[7], z[8, ::2], z[9, 3] = -95, -200, np.inf
+    x[10, :256], x[11, 256:], x[12, 5] = 0, 1e-42, -np.inf
+    z[13] = -60
+    x[13] *= 1e3
+    t = _t(x)
+    zt = None if gate is None else _t(z)
+    _norm_check(t, zt, weight, groups, 1e-5)
+    _norm_check(t, zt, weight, groups, 1e-5, static=0.03)
+    _norm_check(t[:1], None if zt is None else zt[:1], weight, groups, 0.0 if groups == 3 else 1e-12)
+
+
+@pytest.mark.gpu
+def test_norm_ties_go_to_the_even_code():
+    """bf16 rows without gate or weight whose absmax is 127: every x of the form k + 1/2 is a tie of 127 x / absmax"""
+    torch = pytest.importorskip("torch")
+    x = np.zeros((2, 256), np.float32)
+    x[:, :127] = np.arange(127) + 0.5
+    x[:, 127], x[1] = 127, -x[1]
+    x[1, 200] = -127
+    _norm_check(torch.from_numpy(x).cuda(), None, None, 1, 1e-5)
+
+
+# ------------------------------------------------------------------------------------------------ int8 projection
+class LinearArgs(C.Structure):
+    _fields_ = [("xq", C.c_void_p), ("wq", C.c_void_p), ("s_row", C.c_void_p), ("s_w", C.c_void_p), ("bias", C.c_void_p),
+                ("residual", C.c_void_p), ("stride_residual", C.c_int64), ("out", C.c_void_p), ("stride_out", C.c_int64),
+                ("rows", C.c_int32), ("outs", C.c_int32), ("inner", C.c_int32), ("act", C.c_int32), ("status", C.c_void_p)]
+
+
+@pytest.mark.parametrize("want,args,dtype", [
+    ("ERR_UNSUPPORTED", {}, 3), ("ERR_UNSUPPORTED", {"act": 3}, 0), ("ERR_UNSUPPORTED", {"act": -1}, 0), ("ERR_SHAPE", {"rows": -1}, 0),
+    ("ERR_SHAPE", {"outs": 0}, 0), ("ERR_SHAPE", {"inner": 0}, 0), ("ERR_SHAPE", {"inner": 24}, 0), ("ERR_SHAPE", {"inner": 131088}, 0),
+    ("ERR_NULL", {"xq": None}, 0), ("ERR_NULL", {"wq": None}, 0), ("ERR_NULL", {"s_w": None}, 0), ("ERR_NULL", {"out": None}, 0),
+    ("ERR_ALIGN", {"xq": ADDR + 8}, 0), ("ERR_ALIGN", {"wq": ADDR + 1}, 0), ("ERR_ALIGN", {"out": ADDR + 2}, 0), ("ERR_ALIGN", {"residual": ADDR + 1}, 1),
+    ("OK", {"rows": 0, "out": None}, 0),
+])
+def test_linear_refuses(want, args, dtype):
+    bd, lib = _lib()
+    a = LinearArgs(**{**dict(xq=ADDR, wq=ADDR, s_w=ADDR, out=ADDR, stride_out=64, rows=4, outs=64, inner=64), **args})
+    assert lib.ssdi8_linear(C.byref(a), dtype, None) == getattr(bd, want)
+    assert lib.ssdi8_linear(None, 0, None) == bd.ERR_NULL
+
+
+def _linear_check(seed, T, O, K, dtype, act="none", bias=True, residual="own", s_row=True, pad=0, offset=0, extremes=False):
+    from paper_2608_21952_b200 import binding as bd
+    import torch
+    rng = np.random.default_rng(seed)
+    code = lambda *s: np.clip(np.rint(rng.standard_normal(s) * 40), -127, 127).astype(np.int8)  # noqa: E731
+    x, w = code(T, K), code(O, K)
+    if extremes:   # (the largest sums there are, of both signs)
+        x[0], w[0], w[-1] = 127, 127, -127
+    sr = rng.uniform(0.01, 0.05, T).astype(np.float32) if s_row else None
+    sw = (rng.uniform(0.5, 1.5, O) / (40 * np.sqrt(K))).astype(np.float32)
+    b = rng.standard_normal(O).astype(np.float32) if bias else None
+    whole = torch.full((T, O + pad + offset), 3.0, device="cuda").to(getattr(torch, dtype))
+    out = whole[:, offset:offset + O]
+    res = None
+    if residual == "own":
+        res = _t(rng.standard_normal((T, O + 5)).astype(np.float32), dtype)[:, 2:2 + O]
+    if residual == "out":
+        out.copy_(_t(rng.standard_normal((T, O)).astype(np.float32), dtype))
+        res = out
+    before = None if res is None else _np(res).astype(np.float64).copy()
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    bd.ssdi8_linear(_t(x), _t(w), _t(sw), out, s_row=None if sr is None else _t(sr), bias=None if b is None else _t(b), residual=res,
+                    act={"none": bd.ACT_NONE, "silu": bd.ACT_SILU, "relu2": bd.ACT_RELU2}[act], status=status)
+    acc = x.astype(np.float64) @ w.astype(np.float64).T   # (whole numbers below 2^53: exact)
+    eps = 2.0 ** -24
+    part = acc * (1.0 if sr is None else sr.astype(np.float64)[:, None]) * sw
+    v = part + (0 if b is None else b.astype(np.float64))
+    err = eps * (3 * np.abs(part) + np.abs(v) + 2 * 2 * eps)   # the sum as a float, the two products, the fused addition
+    if act == "silu":
+        u = ref.silu(v)
+        err = 1.1 * err + eps * (10 + 1.5 * np.abs(v)) * np.abs(u)
+    elif act == "relu2":
+        u = np.maximum(v, 0) ** 2
+        err = 2 * np.abs(v) * err + err * err + 2 * eps * u
+    else:
+        u = v
+    if before is not None:
+        u = u + before
+        err = err + eps * np.abs(u)
+    half = {"float32": 0.0, "float16": 2.0 ** -11, "bfloat16": 2.0 ** -8}[dtype]
+    got = _np(out)
+    assert np.all(np.abs(got - u) <= err * 1.001 + half * (np.abs(u) + err) + (2.0 ** -25 if dtype == "float16" else 0)), np.abs(got - u).max()
+    edge = _np(whole)
+    assert np.all(edge[:, :offset] == 3.0) and np.all(edge[:, offset + O:] == 3.0)
+    assert int(status.item()) == 0
+
+
+LINEAR = [  # T, O, K, dtype, act, bias, residual, s_row, pad, offset
+    (1, 1, 16, "float32", "none", False, None, False, 0, 0), (1, 8, 48, "bfloat16", "none", True, "own", True, 0, 0),
+    (7, 100, 128, "float16", "silu", True, None, True, 4, 0), (64, 3352, 768, "bfloat16", "none", False, None, True, 0, 0),
+    (129, 129, 640, "float32", "relu2", True, "own", True, 3, 1), (128, 256, 4096, "bfloat16", "none", True, "out", True, 0, 0),
+    (300, 300, 144, "bfloat16", "silu", False, "out", False, 4, 4), (513, 2560, 272, "bfloat16", "none", True, "own", True, 0, 0),
+    (2000, 1999, 96, "float16", "relu2", True, None, True, 1, 0), (257, 7000, 64, "float32", "none", True, "own", True, 8, 8),
+    (2, 24, 8192, "float32", "none", True, None, True, 0, 0), (33, 515, 1040, "bfloat16", "none", True, "own", True, 0, 0),
+    (200, 10576, 256, "bfloat16", "none", False, None, True, 0, 0),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,O,K,dtype,act,bias,residual,s_row,pad,offset", LINEAR)
+def test_linear(T, O, K, dtype, act, bias, residual, s_row, pad, offset):
+    _linear_check(T + O + K, T, O, K, dtype, act, bias, residual, s_row, pad, offset)
+
+
+@pytest.mark.gpu
+def test_linear_of_the_longest_rows():
+    """sums of 131072 products at the ends of the codes: 2.1e9 of either sign, in 32 bits"""
+    _linear_check(1, 5, 40, 131072, "float32", residual=None, extremes=True)
+
+
+@pytest.mark.gpu
+def test_linear_on_two_streams_and_in_a_graph():
+    torch = pytest.importorskip("torch")
+    from paper_2608_21952_b200 import binding as bd
+    rng = np.random.default_rng(2)
+    x, w = (_t(rng.integers(-127, 128, s).astype(np.int8)) for s in ((150, 320), (700, 320)))
+    sw = _t(rng.uniform(0.5, 1.5, 700).astype(np.float32))
+    want, a, b, c = (torch.empty(150, 700, device="cuda") for _ in range(4))
+    bd.ssdi8_linear(x, w, sw, want)
+    torch.cuda.synchronize()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(5):
+        bd.ssdi8_linear(x, w, sw, a, stream=s1)
+        bd.ssdi8_linear(x, w, sw, b, stream=s2)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        bd.ssdi8_linear(x, w, sw, c)
+        bd.ssdi8_linear(x, w, sw, c, residual=c)
+    graph.replay()
+    assert torch.equal(a, want) and torch.equal(b, want) and torch.equal(c, 2 * want)
