@@ -145,8 +145,10 @@ def norm(x, z, weight, groups, eps):
         u = x.astype(np.float64) if z is None else x.astype(np.float64) * silu(z.astype(np.float64))
         g = u.reshape(T, groups, D // groups)
         w = np.ones(D) if weight is None else weight.astype(np.float64)
-        o = (g / np.sqrt((g * g).mean(-1, keepdims=True) + eps)).reshape(T, D) * w
-        return o, (u * w if groups == 1 else o)
+        root = np.sqrt((g * g).mean(-1, keepdims=True) + eps)
+        o = (g / root).reshape(T, D) * w
+        # (an infinite or missing norm does not cancel: o is then 0 or NaN)
+        return o, np.where(np.isfinite(root[:, 0]), u * w, o) if groups == 1 else o
 
 
 def norm_codes(x, z, weight, groups, eps, static=None):
@@ -154,8 +156,6 @@ def norm_codes(x, z, weight, groups, eps, static=None):
     with np.errstate(all="ignore"):
         if static is not None:
             return code(o / np.float64(static)), None
-        if groups == 1:   # (an overflow of the squares alone must not reach the codes)
-            v = np.where(np.isnan(o), np.nan, v)
         top, of = np.nan_to_num(np.fmax.reduce(np.abs(v), -1), nan=0.0, posinf=np.inf), np.nan_to_num(np.fmax.reduce(np.abs(o), -1), nan=0.0, posinf=np.inf)
         q = np.where(top[:, None] > 0, 127.0 * v / np.where(top > 0, top, 1)[:, None], v)
         return code(q), np.where(of > 0, of / 127.0, 1.0)
