@@ -434,7 +434,7 @@ ssdi8_status_t ssdi8_cache_read(const ssdi8_dims_t* dims, const ssdi8_cache_t* c
  *   (1 if that is 0), code = rne(S / scale) saturated
  * E and w_j as in ssdi8_cache_read; the integer sums are exact.  y [B][H*P] is fp32, or 16-bit with SSDI8_FLAG_Y_FP16 / _BF16;
  * SSDI8_FLAG_DT_SOFTPLUS as in ssdi8_conv_fwd.  Padding leaves its row of y alone.  A slot whose start lies behind pos is
- * taken for padding, with the status.  weight 16-byte aligned; bias, dt_bias, D, corr may be NULL. */
+ * taken for padding, with the status.  weight and s_x 16-byte aligned; bias, dt_bias, D, corr may be NULL. */
 typedef struct {
   const void* xBC; int64_t stride_b;          /* [B][Ch], the ring's type */
   const float* weight; const float* bias;     /* [Ch][width], [Ch]        */

@@ -84,7 +84,7 @@ ssdi8_status_t ssdi8_token_step(const ssdi8_dims_t* dims, const ssdi8_cache_t* c
   if (s != SSDI8_OK) return s;
   if (!a->xBC || !a->weight || !a->dt_raw || !a->A || !a->s_x || !a->s_B || !a->s_C || !a->pos || !a->y) return SSDI8_ERR_NULL;
   const size_t e = elem_size(cache->dtype);
-  if (!aligned16(a->weight) || !aligned_to(a->xBC, e) || !aligned_to(a->dt_raw, e) || !aligned_to(a->y, (flags & y16) ? 2 : 4))
+  if (!aligned16(a->weight) || !aligned16(a->s_x) || !aligned_to(a->xBC, e) || !aligned_to(a->dt_raw, e) || !aligned_to(a->y, (flags & y16) ? 2 : 4))
     return SSDI8_ERR_ALIGN;
   if ((s = check_arch()) != SSDI8_OK) return s;
   return launch_token_step(make_dims(dims), *cache, *a, (flags & SSDI8_FLAG_DT_SOFTPLUS) != 0,
