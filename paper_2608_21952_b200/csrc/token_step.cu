@@ -13,6 +13,9 @@ namespace {
 #ifndef TOKEN_HPC
 #define TOKEN_HPC 4
 #endif
+#ifndef TOKEN_MINB
+#define TOKEN_MINB 4
+#endif
 constexpr int TS_T = 256;            // threads that convolve and have rows of y
 constexpr int TS_ALL = TS_T + 32;    // and a warp for the time steps
 
@@ -33,60 +36,72 @@ struct TokenParams {
   const float *dt_bias, *A, *D, *corr, *s_x, *s_B, *s_C;
   const int32_t *slots, *pos;
   void* y; int32_t* status;
-  int H, G, softplus, ydt, hblocks;   // hblocks: blocks per group of heads
+  int H, G, hpg, softplus, ydt, b0;   // hpg: heads per group; b0: the launch's first sequence
 };
 
-// codes of channels ch and ch + 1 (ch even) of the token, as two bytes: taps from the ring and the token itself, which goes into the ring
+// Two channels of the token, ch and ch + 1 (ch even): what does not depend on the slot, loaded while the slot is on its way
 template <typename T>
-__device__ __forceinline__ uint32_t channel_pair(const TokenParams<T>& p, const T* x, T* ring, int Ch, int ch, int pos, float2 step, bool keep) {
-  struct alignas(2 * sizeof(T)) T2 { T a, b; };
-  const int W = p.width;
-  float2 xs[4], w[4];
-  T2 own;
-  own.a = x[ch];
-  own.b = x[ch + 1];
+struct alignas(2 * sizeof(T)) Pair { T a, b; };
+template <typename T>
+struct ChannelPair {
+  float2 w[4], bias, step, xs[3];
+  Pair<T> own;
+  __device__ __forceinline__ void load(const TokenParams<T>& p, const T* x, int ch, const float* steps, bool each) {
+    const int W = p.width;
+    own.a = x[ch];
+    own.b = x[ch + 1];
+    if (W == 4) {
+      const float4 u = *reinterpret_cast<const float4*>(p.weight + (i64)ch * 4), v = *reinterpret_cast<const float4*>(p.weight + (i64)ch * 4 + 4);
+      w[0] = make_float2(u.x, v.x); w[1] = make_float2(u.y, v.y); w[2] = make_float2(u.z, v.z); w[3] = make_float2(u.w, v.w);
+    } else {
 #pragma unroll
-  for (int k = 0; k < 3; ++k) {   // taps 4 - W .. 3 are the convolution's
-    const int t = pos - 3 + k;
-    xs[k] = w[k] = make_float2(0.f, 0.f);
-    if (k >= 4 - W && t >= 0) {
-      const T2 v = *reinterpret_cast<const T2*>(ring + (i64)((uint32_t)t % (uint32_t)W) * Ch + ch);
-      xs[k] = make_float2(Elem<T>::get(v.a), Elem<T>::get(v.b));
+      for (int k = 0; k < 4; ++k)   // taps 4 - W .. 3 are the convolution's
+        w[k] = k >= 4 - W ? make_float2(p.weight[(i64)ch * W + k - 4 + W], p.weight[(i64)(ch + 1) * W + k - 4 + W]) : make_float2(0.f, 0.f);
+    }
+    bias = p.bias ? make_float2(p.bias[ch], p.bias[ch + 1]) : make_float2(0.f, 0.f);
+    step = each ? *reinterpret_cast<const float2*>(steps) : make_float2(*steps, *steps);
+  }
+  // the tokens ahead, from the ring; those of negative positions are zeros
+  __device__ __forceinline__ void past(const TokenParams<T>& p, const T* ring, int Ch, int pos) {
+    const int W = p.width;
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      const int t = pos - 3 + k;
+      xs[k] = make_float2(0.f, 0.f);
+      if (k >= 4 - W && t >= 0) {
+        const Pair<T> v = *reinterpret_cast<const Pair<T>*>(ring + (i64)(W == 4 ? t & 3 : t % W) * Ch);
+        xs[k] = make_float2(Elem<T>::get(v.a), Elem<T>::get(v.b));
+      }
     }
   }
-  xs[3] = make_float2(Elem<T>::get(own.a), Elem<T>::get(own.b));
-  if (W == 4) {
-    const float4 u = *reinterpret_cast<const float4*>(p.weight + (i64)ch * 4), v = *reinterpret_cast<const float4*>(p.weight + (i64)ch * 4 + 4);
-    w[0] = make_float2(u.x, v.x); w[1] = make_float2(u.y, v.y); w[2] = make_float2(u.z, v.z); w[3] = make_float2(u.w, v.w);
-  } else {
+  // their codes as two bytes
+  __device__ __forceinline__ uint32_t codes() const {
+    const float2 x3 = make_float2(Elem<T>::get(own.a), Elem<T>::get(own.b));
+    float2 v = bias, m = make_float2(fabsf(bias.x), fabsf(bias.y));
 #pragma unroll
-    for (int k = 1; k < 4; ++k)
-      if (k >= 4 - W) w[k] = make_float2(p.weight[(i64)ch * W + k - 4 + W], p.weight[(i64)(ch + 1) * W + k - 4 + W]);
+    for (int k = 0; k < 4; ++k) {
+      const float2 x = k < 3 ? xs[k] : x3;
+      v = __ffma2_rn(w[k], x, v);
+      m = make_float2(fmaf(fabsf(w[k].x), fabsf(x.x), m.x), fmaf(fabsf(w[k].y), fabsf(x.y), m.y));
+    }
+    // true: near the middle of two integers (see block.cuh; M is the token's own here, and the step size's reciprocal is off by 2 eps)
+    auto one = [&](float v, float m, float step, float* r) -> bool {
+      const float inv = rcp_approx(step);
+      const float q = v * rcp_approx(1.0f + ex2_approx(v * -1.44269504f)) * inv;
+      float cl;
+      asm("min.xorsign.abs.f32 %0, %1, %2;" : "=f"(cl) : "f"(q), "f"(127.0f));
+      *r = __fadd_rn(cl, kMagicOut);
+      const float off = fabsf(cl - __fadd_rn(*r, -kMagicOut));
+      return !(fmaf(fmaf(2.0f * kEps, fabsf(v), 14.0f * kEps), fabsf(cl), fmaf(5.0f * kEps * m, inv, off)) <= 0.5f) || !(step >= 1e-30f && step <= 1e30f);
+    };
+    float r0, r1;
+    if (one(v.x, m.x, step.x, &r0))
+      r0 = __uint_as_float(rne_clamp_bits(silu_quotient_exact<4>(xs[0].x, xs[1].x, xs[2].x, x3.x, w[0].x, w[1].x, w[2].x, w[3].x, bias.x, step.x)));
+    if (one(v.y, m.y, step.y, &r1))
+      r1 = __uint_as_float(rne_clamp_bits(silu_quotient_exact<4>(xs[0].y, xs[1].y, xs[2].y, x3.y, w[0].y, w[1].y, w[2].y, w[3].y, bias.y, step.y)));
+    return __byte_perm(__float_as_uint(r0), __float_as_uint(r1), 0x0040u) & 0xffffu;
   }
-  const float2 bias = p.bias ? make_float2(p.bias[ch], p.bias[ch + 1]) : make_float2(0.f, 0.f);
-  if (keep) *reinterpret_cast<T2*>(ring + (i64)((uint32_t)pos % (uint32_t)W) * Ch + ch) = own;
-  float2 v = bias, m = make_float2(fabsf(bias.x), fabsf(bias.y));
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    v = __ffma2_rn(w[k], xs[k], v);
-    m = make_float2(fmaf(fabsf(w[k].x), fabsf(xs[k].x), m.x), fmaf(fabsf(w[k].y), fabsf(xs[k].y), m.y));
-  }
-  auto one = [&](float v, float m, float step, float* r) -> bool {   // true: near the middle of two integers (see block.cuh; M is the token's own here)
-    const float inv = __frcp_rn(step);
-    const float q = v * rcp_approx(1.0f + ex2_approx(v * -1.44269504f)) * inv;
-    float cl;
-    asm("min.xorsign.abs.f32 %0, %1, %2;" : "=f"(cl) : "f"(q), "f"(127.0f));
-    *r = __fadd_rn(cl, kMagicOut);
-    const float off = fabsf(cl - __fadd_rn(*r, -kMagicOut));
-    return !(fmaf(fmaf(2.0f * kEps, fabsf(v), 12.0f * kEps), fabsf(cl), fmaf(5.0f * kEps * m, inv, off)) <= 0.5f) || !(step >= 1e-30f && step <= 1e30f);
-  };
-  float r0, r1;
-  if (one(v.x, m.x, step.x, &r0))
-    r0 = __uint_as_float(rne_clamp_bits(silu_quotient_exact<4>(xs[0].x, xs[1].x, xs[2].x, xs[3].x, w[0].x, w[1].x, w[2].x, w[3].x, bias.x, step.x)));
-  if (one(v.y, m.y, step.y, &r1))
-    r1 = __uint_as_float(rne_clamp_bits(silu_quotient_exact<4>(xs[0].y, xs[1].y, xs[2].y, xs[3].y, w[0].y, w[1].y, w[2].y, w[3].y, bias.y, step.y)));
-  return __byte_perm(__float_as_uint(r0), __float_as_uint(r1), 0x0040u) & 0xffffu;
-}
+};
 
 __device__ __forceinline__ int dot16(const uint4& a, const uint4& b, int s) {
   s = __dp4a((int)a.x, (int)b.x, s);
@@ -102,7 +117,7 @@ struct TokenSmem {
   __align__(16) int8_t xnow[HPC][64];        // x of the token
   __align__(16) int8_t C[N];
   __align__(16) int8_t B[N];
-  __align__(16) int CB[kWin];                // C . B_j
+  __align__(16) float g[HPC][kWin];          // w_j C . B_j
   __align__(16) float w[HPC][kWin];          // w_j
   float E[HPC];
   uint64_t bar[HPC];
@@ -113,94 +128,119 @@ struct TokenSmem {
 // product as 4 N / 16 dp4a in turned order (no two lanes on one bank) and nothing to exchange.  Eight warps convolve, one more forms the time
 // steps and decays beside them.
 template <typename T, int N, int HPC>
-__global__ void __launch_bounds__(TS_ALL, 4) token_kernel(const __grid_constant__ TokenParams<T> p) {
+__global__ void __launch_bounds__(TS_ALL, TOKEN_MINB) token_kernel(const __grid_constant__ TokenParams<T> p) {
+  constexpr int QH = (HPC + 3) / 4;   // heads that a thread has a row of
   extern __shared__ uint8_t smem_raw[];
   TokenSmem<N, HPC>& s = *reinterpret_cast<TokenSmem<N, HPC>*>((reinterpret_cast<uintptr_t>(smem_raw) + 127) & ~(uintptr_t)127);
   const int tid = threadIdx.x, lane = tid & 31;
-  if (tid == 0) {
-    for (int i = 0; i < HPC; ++i) sm100::mbar_init(&s.bar[i], 1);
-    sm100::fence_mbar_init();
-  }
+  if (tid < HPC) sm100::mbar_init(&s.bar[tid], 1);
+  if (tid < 32) sm100::fence_mbar_init();
   pdl_wait();
-  const int hb = blockIdx.x % p.hblocks, bg = blockIdx.x / p.hblocks, g = bg % p.G, b = bg / p.G;
-  const int hpg = p.H / p.G, h0 = g * hpg + hb * HPC, nh = min(HPC, hpg - hb * HPC);
+  const int hb = blockIdx.x, g = blockIdx.y, b = blockIdx.z + p.b0;
+  const int h0 = g * p.hpg + hb * HPC, nh = min(HPC, p.hpg - hb * HPC);
+  const int HP = p.H * 64, GN = p.G * N, Ch = HP + 2 * GN;
+  const T* const x = p.xBC + b * p.sb;
+  // channels of this thread: x of the heads, then B and C
+  const int nch = 64 * nh + 2 * N;
+  auto channel_of = [&](int k) { return k < 64 * nh ? h0 * 64 + k : k < 64 * nh + N ? HP + g * N + k - 64 * nh : HP + GN + g * N + k - 64 * nh - N; };
+  auto steps_of = [&](int k) { return k < 64 * nh ? p.s_x + h0 * 64 + k : (k < 64 * nh + N ? p.s_B : p.s_C) + g; };
+  ChannelPair<T> cp;
+  float dtn = 0.f;   // the warp of the time steps: those of the token
+  if (tid < TS_T) {
+    if (2 * tid < nch) cp.load(p, x, channel_of(2 * tid), steps_of(2 * tid), 2 * tid < 64 * nh);
+  } else if (lane < nh) {
+    dtn = Elem<T>::get(p.dt_raw[b * p.dt_sb + h0 + lane]);
+    if (p.softplus) dtn = softplus_dt(dtn, p.dt_bias ? p.dt_bias[h0 + lane] : 0.f);
+  }
   bool bad;
   const int slot = slot_of(p.slots, p.pos, p.c.nslots, b, &bad);
-  int pos = 0, f = 0;
-  if (slot >= 0) {
-    pos = p.pos[b];
-    f = max(p.c.start[slot], pos - pos % kWin);
-    bad = f > pos;
-  }
+  const int pos = slot >= 0 ? p.pos[b] : 0;
   if (bad && hb == 0 && g == 0 && tid == 0 && p.status) atomicExch(p.status, (int32_t)SSDI8_ERR_SHAPE);
-  if (slot < 0 || bad) return;
-  const int now = pos % kWin, first = f % kWin, n = pos - f;   // rows of the token and of the first waiting one, and how many wait
+  if (slot < 0) return;
+  const int start = p.c.start[slot], now = pos % kWin, f = max(start, pos - now);
   const i64 sh0 = (i64)slot * p.H + h0;
-  if (tid == 0)
-    for (int i = 0; i < nh; ++i) {
-      sm100::mbar_expect_tx(&s.bar[i], 64 * N + kWin * 64);
-      sm100::bulk_load(&s.codes[i][0][0], p.c.codes + (sh0 + i) * 64 * N, 64 * N, &s.bar[i]);
-      sm100::bulk_load(&s.x[i][0][0], p.c.xwin + (sh0 + i) * kWin * 64, kWin * 64, &s.bar[i]);
-    }
-  const int HP = p.H * 64, GN = p.G * N, Ch = HP + 2 * GN;
-  const int j = tid >> 4, piece = tid & 15;   // row j of the window, N / 16 bytes of it
-  const int head = tid >> 6, row = tid & 63;  // of y
+  const int j = (tid >> 4) % kWin, piece = tid & 15;   // row j of the window, N / 16 bytes of it
+  const int head = tid >> 6, row = tid & 63;           // of y
+  int8_t* const Bw = p.c.Bwin + ((i64)slot * p.G + g) * kWin * N;
+  T* const ring = p.ring + (i64)slot * p.width * Ch;
   uint32_t Bv[N / 64];
-  float scale[(HPC + 3) / 4], sx[(HPC + 3) / 4];
   if (tid < TS_T) {
-    int8_t* const Bw = p.c.Bwin + ((i64)slot * p.G + g) * kWin * N;
-    const bool waits = (j - first + kWin) % kWin < n;   // (the token's own row does not)
+    if (2 * tid < nch) cp.past(p, ring + channel_of(2 * tid), Ch, pos);
 #pragma unroll
-    for (int k = 0; k < N / 64; ++k) Bv[k] = waits ? reinterpret_cast<const uint32_t*>(Bw + j * N)[piece * (N / 64) + k] : 0u;
+    for (int k = 0; k < N / 64; ++k) Bv[k] = reinterpret_cast<const uint32_t*>(Bw + j * N)[piece * (N / 64) + k];
+  }
+  if (start > pos) {   // the slot was written behind this position
+    if (hb == 0 && g == 0 && tid == 0 && p.status) atomicExch(p.status, (int32_t)SSDI8_ERR_SHAPE);
+    return;
+  }
+  if (tid >= TS_T && lane < nh) {
+    sm100::mbar_expect_tx(&s.bar[lane], 64 * N + kWin * 64);
+    sm100::bulk_load(&s.codes[lane][0][0], p.c.codes + (sh0 + lane) * 64 * N, 64 * N, &s.bar[lane]);
+    sm100::bulk_load(&s.x[lane][0][0], p.c.xwin + (sh0 + lane) * kWin * 64, kWin * 64, &s.bar[lane]);
+  }
+  const int first = f % kWin, n = pos - f;   // row of the first waiting token, and how many wait
+  float scale[QH], sx[QH], corr[QH], D[QH];
+  if (tid < TS_T) {
 #pragma unroll
-    for (int q = 0; q < (HPC + 3) / 4; ++q) {
+    for (int q = 0; q < QH; ++q) {
       const bool in = 4 * q + head < nh;
+      const int ch = (h0 + 4 * q + head) * 64 + row;
       scale[q] = in ? p.c.scales[(sh0 + 4 * q + head) * 64 + row] : 0.f;
-      sx[q] = in ? p.s_x[(h0 + 4 * q + head) * 64 + row] : 0.f;
+      sx[q] = in ? p.s_x[ch] : 0.f;
+      corr[q] = in && p.corr ? p.corr[ch] : 0.f;
+      D[q] = in && p.D ? p.D[h0 + 4 * q + head] : 0.f;
     }
-    // codes of x of the heads, then of B and C
-    const T* const x = p.xBC + b * p.sb;
-    T* const ring = p.ring + (i64)slot * p.width * Ch;
-    for (int k = 2 * tid; k < 64 * nh + 2 * N; k += 2 * TS_T) {
-      if (k < 64 * nh) {
-        const int ch = h0 * 64 + k;
-        const uint32_t c = channel_pair(p, x, ring, Ch, ch, pos, *reinterpret_cast<const float2*>(p.s_x + ch), true);
+    if (((j - first) & (kWin - 1)) >= n) {   // (nor does the token's own row wait)
+#pragma unroll
+      for (int k = 0; k < N / 64; ++k) Bv[k] = 0u;
+    }
+#pragma unroll
+    for (int k0 = 0; k0 < 64 * HPC + 2 * N; k0 += 2 * TS_T) {
+      const int k = k0 + 2 * tid;
+      if (k >= nch) break;
+      const int ch = channel_of(k);
+      const bool isx = k < 64 * nh;
+      if (k0 > 0) {
+        cp.load(p, x, ch, steps_of(k), isx);
+        cp.past(p, ring + ch, Ch, pos);
+      }
+      if (isx || hb == 0) *reinterpret_cast<Pair<T>*>(ring + (i64)(p.width == 4 ? pos & 3 : pos % p.width) * Ch + ch) = cp.own;
+      const uint32_t c = cp.codes();
+      if (isx) {
         *reinterpret_cast<uint16_t*>(&s.xnow[0][0] + k) = (uint16_t)c;
         *reinterpret_cast<uint16_t*>(p.c.xwin + ((sh0 + (k >> 6)) * kWin + now) * 64 + (k & 63)) = (uint16_t)c;
       } else {
-        const int at = (k - 64 * nh) % N;
+        const int at = (k - 64 * nh) & (N - 1);
         const bool isC = k - 64 * nh >= N;
-        const float st = (isC ? p.s_C : p.s_B)[g];
-        const uint32_t c = channel_pair(p, x, ring, Ch, HP + (isC ? GN : 0) + g * N + at, pos, make_float2(st, st), hb == 0);
         *reinterpret_cast<uint16_t*>((isC ? s.C : s.B) + at) = (uint16_t)c;
         if (!isC && hb == 0) *reinterpret_cast<uint16_t*>(Bw + now * N + at) = (uint16_t)c;
       }
     }
   } else {
-    // time steps and decays, two heads at a time, lane j of a half-warp for row j of the window; the new time steps of all first
-    float dtn = 0.f;
-    if (lane < nh) {
-      dtn = Elem<T>::get(p.dt_raw[b * p.dt_sb + h0 + lane]);
-      if (p.softplus) dtn = softplus_dt(dtn, p.dt_bias ? p.dt_bias[h0 + lane] : 0.f);
-      p.c.dtwin[(sh0 + lane) * kWin + now] = dtn;
-    }
-    const int rw = lane & 15, order = (rw - first + kWin) % kWin;
+    // decays, two heads at a time, lane j of a half-warp for row j of the window
+    if (lane < nh) p.c.dtwin[(sh0 + lane) * kWin + now] = dtn;
+    const int rw = lane & 15, order = (rw - first) & (kWin - 1);
+    float old[(HPC + 1) / 2], A[(HPC + 1) / 2];
 #pragma unroll
     for (int i0 = 0; i0 < HPC; i0 += 2) {
       const int i = i0 + (lane >> 4);
-      float dt = __shfl_sync(0xffffffffu, dtn, i & 31);
-      if (rw != now) dt = i < nh && order < n ? p.c.dtwin[(sh0 + i) * kWin + rw] : 0.f;
+      old[i0 / 2] = i < nh && order < n ? p.c.dtwin[(sh0 + i) * kWin + rw] : 0.f;
+      A[i0 / 2] = i < nh ? p.A[h0 + i] : 0.f;
+    }
+#pragma unroll
+    for (int i0 = 0; i0 < HPC; i0 += 2) {
+      const int i = i0 + (lane >> 4);
+      const float fresh = __shfl_sync(0xffffffffu, dtn, i & 31), dt = rw == now ? fresh : old[i0 / 2];
       const Waiting w = waiting_of(dt, order);
       if (i < nh) {
-        const double A = (double)p.A[h0 + i];
-        s.w[i][rw] = dt * expf((float)(A * w.behind));
-        if (rw == 0) s.E[i] = expf((float)(A * w.all));
+        s.w[i][rw] = dt * expf((float)((double)A[i0 / 2] * w.behind));
+        if (rw == 0) s.E[i] = expf((float)((double)A[i0 / 2] * w.all));
       }
     }
   }
   __syncthreads();
   if (tid >= TS_T) return;
-  // C . B_j
+  // C . B_j, with the weights of the heads (0 for a row without a waiting token)
   {
     int d = 0;
 #pragma unroll
@@ -211,35 +251,47 @@ __global__ void __launch_bounds__(TS_ALL, 4) token_kernel(const __grid_constant_
     }
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
-    if (piece == 0) s.CB[j] = d;
+    if (piece < nh) s.g[piece][j] = s.w[piece][j] * (float)d;
   }
   const float sB = p.s_B[g], sC = p.s_C[g];
   named_bar(1, TS_T);
+  // a thread's rows side by side: what they read of C is read once
+  if (head >= nh) return;
+  float win[QH];
+  int d[QH];
 #pragma unroll
-  for (int q = 0; q < (HPC + 3) / 4; ++q) {
+  for (int q = 0; q < QH; ++q) {
+    const int i = 4 * q + head;
+    win[q] = 0.f;
+    d[q] = 0;
+    if (i < nh) {
+      win[q] = s.g[i][now] * (float)s.xnow[i][row];   // the token itself; its row of s.x is stale
+      if (!sm100::mbar_wait_inline<0>(&s.bar[i], 0, p.status)) drain();
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < kWin; k += 4)
+#pragma unroll
+    for (int q = 0; q < QH; ++q) {
+      const int i = min(4 * q + head, HPC - 1);
+      const float4 w = *reinterpret_cast<const float4*>(&s.g[i][k]);
+      const float gj[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) win[q] = fmaf(k + e == now ? 0.f : gj[e], (float)s.x[i][k + e][row], win[q]);
+    }
+#pragma unroll
+  for (int k = 0; k < N / 16; ++k) {
+    const int c = N == 128 ? (k + row) & 7 : (k + (row >> 1)) & 3;
+    const uint4 C16 = reinterpret_cast<const uint4*>(s.C)[c];
+#pragma unroll
+    for (int q = 0; q < QH; ++q) d[q] = dot16(reinterpret_cast<const uint4*>(&s.codes[min(4 * q + head, HPC - 1)][row][0])[c], C16, d[q]);
+  }
+#pragma unroll
+  for (int q = 0; q < QH; ++q) {
     const int i = 4 * q + head;
     if (i < nh) {
-      // the waiting tokens and the token itself
-      const float xn = (float)s.xnow[i][row];
-      float win = s.w[i][now] * (float)s.CB[now] * xn;
-      if (!sm100::mbar_wait_inline<0>(&s.bar[i], 0, p.status)) drain();
-#pragma unroll 4
-      for (int o = 0; o < n; ++o) {
-        const int jj = (first + o) % kWin;
-        win = fmaf(s.w[i][jj] * (float)s.CB[jj], (float)s.x[i][jj][row], win);
-      }
-      int d = 0;
-      const uint4* const cr = reinterpret_cast<const uint4*>(&s.codes[i][row][0]);
-#pragma unroll
-      for (int k = 0; k < N / 16; ++k) {
-        const int c = N == 128 ? (k + row) & 7 : (k + (row >> 1)) & 3;
-        d = dot16(cr[c], reinterpret_cast<const uint4*>(s.C)[c], d);
-      }
-      const int ch = (h0 + i) * 64 + row;
-      float v = sC * fmaf(s.E[i] * scale[q], (float)d, sx[q] * sB * win);
-      if (p.D) v = fmaf(p.D[h0 + i] * sx[q], xn, v);
-      if (p.corr) v += p.corr[ch];
-      const i64 at = (i64)b * HP + ch;
+      const float v = sC * fmaf(s.E[i] * scale[q], (float)d[q], sx[q] * sB * win[q]) + fmaf(D[q] * sx[q], (float)s.xnow[i][row], corr[q]);
+      const i64 at = (i64)b * HP + (h0 + i) * 64 + row;
       if (p.ydt == 0) static_cast<float*>(p.y)[at] = v;
       else if (p.ydt == 1) static_cast<__half*>(p.y)[at] = __float2half_rn(v);
       else static_cast<__nv_bfloat16*>(p.y)[at] = __float2bfloat16_rn(v);
@@ -493,16 +545,21 @@ ssdi8_status_t launch(const Dims& d, const ssdi8_cache_t& c, const ssdi8_token_a
   p.dt_raw = static_cast<const T*>(a.dt_raw); p.dt_sb = a.dt_stride_b; p.dt_bias = a.dt_bias;
   p.A = a.A; p.D = a.D; p.corr = a.corr; p.s_x = a.s_x; p.s_B = a.s_B; p.s_C = a.s_C;
   p.slots = a.slots; p.pos = a.pos; p.y = a.y; p.status = a.status;
-  p.H = d.H; p.G = d.G; p.softplus = softplus; p.ydt = ydt;
-  auto go = [&](auto kernel, size_t smem) -> ssdi8_status_t {
-    const i64 blocks = (i64)d.b * d.G * p.hblocks;
-    if (blocks > 0x7fffffff) return SSDI8_ERR_SHAPE;
-    return launch_configured(kernel, dim3((unsigned)blocks), dim3(TS_ALL), smem, -1, false, st, p);
+  p.H = d.H; p.G = d.G; p.hpg = d.H / d.G; p.softplus = softplus; p.ydt = ydt;
+  auto go = [&](auto kernel, int hpc, size_t smem) -> ssdi8_status_t {
+    const int hblocks = (p.hpg + hpc - 1) / hpc;
+    if (d.G > 65535) return SSDI8_ERR_SHAPE;
+    // (the grid's third axis holds 65535 sequences)
+    for (p.b0 = 0; p.b0 < d.b; p.b0 += 65535) {
+      const ssdi8_status_t s = launch_configured(kernel, dim3(hblocks, d.G, d.b - p.b0 < 65535 ? d.b - p.b0 : 65535), dim3(TS_ALL), smem, -1, false, st, p);
+      if (s != SSDI8_OK) return s;
+    }
+    return SSDI8_OK;
   };
   auto pick = [&](auto hpc) -> ssdi8_status_t {
     constexpr int HPC = decltype(hpc)::value;
-    p.hblocks = (d.H / d.G + HPC - 1) / HPC;
-    return d.N == 128 ? go(token_kernel<T, 128, HPC>, sizeof(TokenSmem<128, HPC>) + 128) : go(token_kernel<T, 64, HPC>, sizeof(TokenSmem<64, HPC>) + 128);
+    return d.N == 128 ? go(token_kernel<T, 128, HPC>, HPC, sizeof(TokenSmem<128, HPC>) + 128)
+                      : go(token_kernel<T, 64, HPC>, HPC, sizeof(TokenSmem<64, HPC>) + 128);
   };
   const ssdi8_status_t s = pick(std::integral_constant<int, TOKEN_HPC>{});
   if (s != SSDI8_OK) return s;
