@@ -10,12 +10,6 @@
 namespace ssdi8 {
 namespace {
 
-#ifndef TOKEN_HPC
-#define TOKEN_HPC 4
-#endif
-#ifndef TOKEN_MINB
-#define TOKEN_MINB 4
-#endif
 constexpr int TS_T = 256;            // threads that convolve and have rows of y
 constexpr int TS_ALL = TS_T + 32;    // and a warp for the time steps
 
@@ -124,12 +118,12 @@ struct TokenSmem {
 };
 
 // A block has up to HPC heads of one group: the convolution of B and C is theirs together.  The codes and windows of its heads are
-// requested as bulk copies into shared memory as soon as the slot is known; a thread then has a whole row of one head, its dot
-// product as 4 N / 16 dp4a in turned order (no two lanes on one bank) and nothing to exchange.  Eight warps convolve, one more forms the time
+// requested as bulk copies into shared memory as soon as the slot is known.  Eight warps convolve, one more forms the time
 // steps and decays beside them.
 template <typename T, int N, int HPC>
-__global__ void __launch_bounds__(TS_ALL, TOKEN_MINB) token_kernel(const __grid_constant__ TokenParams<T> p) {
+__global__ void __launch_bounds__(TS_ALL, HPC == 8 ? 3 : 4) token_kernel(const __grid_constant__ TokenParams<T> p) {
   constexpr int QH = (HPC + 3) / 4;   // heads that a thread has a row of
+  constexpr int LPR = N / 16;
   extern __shared__ uint8_t smem_raw[];
   TokenSmem<N, HPC>& s = *reinterpret_cast<TokenSmem<N, HPC>*>((reinterpret_cast<uintptr_t>(smem_raw) + 127) & ~(uintptr_t)127);
   const int tid = threadIdx.x, lane = tid & 31;
@@ -160,7 +154,8 @@ __global__ void __launch_bounds__(TS_ALL, TOKEN_MINB) token_kernel(const __grid_
   const int start = p.c.start[slot], now = pos % kWin, f = max(start, pos - now);
   const i64 sh0 = (i64)slot * p.H + h0;
   const int j = (tid >> 4) % kWin, piece = tid & 15;   // row j of the window, N / 16 bytes of it
-  const int head = tid >> 6, row = tid & 63;           // of y
+  // y: a warp has 32 rows of a head, LPR lanes with 16 codes each per row, and a lane in the end the row whose sum it keeps
+  const int head = tid >> 6, half = tid & 32, row = half + lane % LPR * (32 / LPR) + lane / LPR;
   int8_t* const Bw = p.c.Bwin + ((i64)slot * p.G + g) * kWin * N;
   T* const ring = p.ring + (i64)slot * p.width * Ch;
   uint32_t Bv[N / 64];
@@ -279,12 +274,21 @@ __global__ void __launch_bounds__(TS_ALL, TOKEN_MINB) token_kernel(const __grid_
 #pragma unroll
       for (int e = 0; e < 4; ++e) win[q] = fmaf(k + e == now ? 0.f : gj[e], (float)s.x[i][k + e][row], win[q]);
     }
+  const uint4 C16 = reinterpret_cast<const uint4*>(s.C)[lane % LPR];
 #pragma unroll
-  for (int k = 0; k < N / 16; ++k) {
-    const int c = N == 128 ? (k + row) & 7 : (k + (row >> 1)) & 3;
-    const uint4 C16 = reinterpret_cast<const uint4*>(s.C)[c];
+  for (int q = 0; q < QH; ++q) {
+    int part[LPR];   // of rows lane / LPR + t 32 / LPR
+    const uint4* const codes = reinterpret_cast<const uint4*>(&s.codes[min(4 * q + head, HPC - 1)][half][0]) + lane;
 #pragma unroll
-    for (int q = 0; q < QH; ++q) d[q] = dot16(reinterpret_cast<const uint4*>(&s.codes[min(4 * q + head, HPC - 1)][row][0])[c], C16, d[q]);
+    for (int t = 0; t < LPR; ++t) part[t] = dot16(codes[32 * t], C16, 0);
+    // each exchange halves the rows that a lane still has
+#pragma unroll
+    for (int k = LPR / 2; k >= 1; k >>= 1) {
+      const bool up = lane & k;
+#pragma unroll
+      for (int t = 0; t < k; ++t) part[t] = (up ? part[t + k] : part[t]) + __shfl_xor_sync(0xffffffffu, up ? part[t] : part[t + k], k);
+    }
+    d[q] = part[0];
   }
 #pragma unroll
   for (int q = 0; q < QH; ++q) {
@@ -561,10 +565,13 @@ ssdi8_status_t launch(const Dims& d, const ssdi8_cache_t& c, const ssdi8_token_a
     return d.N == 128 ? go(token_kernel<T, 128, HPC>, HPC, sizeof(TokenSmem<128, HPC>) + 128)
                       : go(token_kernel<T, 64, HPC>, HPC, sizeof(TokenSmem<64, HPC>) + 128);
   };
-  const ssdi8_status_t s = pick(std::integral_constant<int, TOKEN_HPC>{});
-  if (s != SSDI8_OK) return s;
   const int sms = sm_count();
   if (sms <= 0) return SSDI8_ERR_CUDA;
+  // Eight heads to a block (three of them per SM) from a full wave on, four (four per SM) below that.  Steps without full windows, eight /
+  // four / two heads, us: 250 x 128 heads 92.9 / 97.5 / 141, 64 x 80 16.8 / 19.1 / 27.
+  const bool eight = (i64)d.b * d.G * ((p.hpg + 7) / 8) >= 3 * sms;
+  const ssdi8_status_t s = eight ? pick(std::integral_constant<int, 8>{}) : pick(std::integral_constant<int, 4>{});
+  if (s != SSDI8_OK) return s;
   const FoldParams f = {p.c, a.A, a.s_x, a.s_B, a.slots, a.pos, d.b, d.H, d.G};
   auto go_fold = [&](auto kernel, int N, size_t smem) {
     const i64 heads = (i64)d.b * d.H, most = (i64)sms * (768 / (2 * N));

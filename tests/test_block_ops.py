@@ -411,7 +411,7 @@ def _token_params(rng, H, N, G, W):
 @pytest.mark.gpu
 @pytest.mark.parametrize("B,H,N,G,W,dtype,ydt,steps", [
     (1, 1, 64, 1, 4, "bfloat16", "float32", 34), (1, 3, 128, 1, 3, "float16", "float16", 18), (5, 4, 64, 2, 2, "float32", "float32", 18),
-    (3, 24, 128, 1, 4, "bfloat16", "bfloat16", 17), (4, 9, 128, 3, 4, "bfloat16", "float32", 17), (2, 16, 64, 8, 4, "bfloat16", "bfloat16", 17),
+    (3, 24, 128, 1, 4, "bfloat16", "bfloat16", 17), (150, 20, 64, 1, 4, "bfloat16", "float32", 3), (60, 60, 128, 4, 4, "float16", "float32", 2), (4, 9, 128, 3, 4, "bfloat16", "float32", 17), (2, 16, 64, 8, 4, "bfloat16", "bfloat16", 17),
 ])
 def test_token_steps(B, H, N, G, W, dtype, ydt, steps):
     """sequences at different positions (0 among them, and one whose slot was written in the middle of a window), step after step:
