@@ -18,6 +18,8 @@ constexpr int kMaxWarps = 16;
 constexpr int kMaxChunks = kMaxNormWidth / 128;
 
 struct None {};   // no gate
+template <typename Z> struct GateRaw { typedef typename Elem<Z>::raw4 raw4; };
+template <> struct GateRaw<None> { struct raw4 {}; };
 
 template <typename T, typename Z>
 struct NormParams {
@@ -32,19 +34,24 @@ struct NormParams {
 };
 
 template <typename T>
-__device__ __forceinline__ float4 load_row4(const T* p, bool aligned) {
-  return Elem<T>::cvt(aligned ? load4<T, true>(p) : load4<T, false>(p));
+__device__ __forceinline__ typename Elem<T>::raw4 load_row4(const T* p, bool aligned) {
+  return aligned ? load4<T, true>(p) : load4<T, false>(p);
+}
+template <>
+__device__ __forceinline__ float4 load_row4<float>(const float* p, bool aligned) {
+  return aligned ? load4<float, true>(p) : load4<float, false>(p);
 }
 
-// z / (1 + exp(-z)), 9 eps: ex2's argument as a rounded product and its remainder
-__device__ __forceinline__ float silu_compensated(float z) {
-  const float L = -1.44269504f, L_LO = -1.92596299e-8f;   // -log2(e) as two numbers
-  const float t = z * L;
-  const float lo = fmaf(z, L_LO, fmaf(z, L, -t));
-  float e = ex2_approx(t);
-  // (from 2^127 on the value would be 0 for something that is not: NaN, which sends the row to binary64)
-  e = t < 127.0f ? fmaf(e, lo * 0.693147181f, e) : __uint_as_float(0x7fffffffu);
-  return z * rcp_approx(1.0f + e);
+// z / (1 + exp(-z)) of two, 9 eps: ex2's argument as a rounded product and its remainder.  Not for z below kLeastGate, where exp(-z)
+// leaves binary32's range.
+constexpr float kLeastGate = -86.0f;
+__device__ __forceinline__ float2 silu2(float2 z) {
+  auto both = [](float v) { return make_float2(v, v); };
+  const float2 L = both(-1.44269504f), t = __fmul2_rn(z, L);   // -log2(e) z; its rest below, times ln 2
+  const float2 rest = __ffma2_rn(z, both(-1.33497567e-8f), __fmul2_rn(__ffma2_rn(z, L, make_float2(-t.x, -t.y)), both(0.693147181f)));
+  const float2 e = make_float2(ex2_approx(t.x), ex2_approx(t.y));
+  const float2 d = __fadd2_rn(__ffma2_rn(e, rest, e), both(1.0f));
+  return __fmul2_rn(z, make_float2(rcp_approx(d.x), rcp_approx(d.y)));
 }
 
 // u w of column i in binary64
@@ -59,49 +66,142 @@ __device__ __noinline__ double gated_exact(const NormParams<T, Z>& p, i64 row, i
   return p.weight ? v * (double)p.weight[i] : v;
 }
 
+// Codes of a row in binary64: those of the chunks in `near`, or all of them (and the row's step size) if the row is out of binary32's range.
+// The absmax in binary64 is that of the chunks in `cand`.  All threads call it, behind their stores.
+template <typename T, typename Z, int NCH>
+__device__ __noinline__ void exact_row(const NormParams<T, Z>& p, i64 row, uint32_t near, uint32_t cand, bool range, bool zero, double* sum64,
+                                       double* top64) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nwarps = blockDim.x >> 5;
+  const int D = p.D, nchunks = (D + 127) / 128, cpg = p.groups > 1 ? nchunks / p.groups : nchunks;
+  const bool many = p.groups > 1, dynamic = p.static_scale == nullptr;
+  auto col_of = [&](int k) { return ((warp + k * nwarps) * 32 + lane) * 4; };
+  if (zero) {
+    // a row of zeros (padding) needs none of it; x that underflowed does
+    bool any = false;
+#pragma unroll 1
+    for (int k = 0; k < NCH; ++k)
+      if (col_of(k) < D) {
+        const float4 v = Elem<T>::cvt(load_row4<T>(p.x + row * p.sx + col_of(k), p.valigned));
+        any |= v.x != 0.f || v.y != 0.f || v.z != 0.f || v.w != 0.f;
+      }
+    if (!__syncthreads_or(any)) {
+#pragma unroll 1
+      for (int k = 0; k < NCH; ++k)
+        if (col_of(k) < D) *reinterpret_cast<uint32_t*>(p.xq + row * D + col_of(k)) = 0u;
+      if (dynamic && p.scale && threadIdx.x == 0) p.scale[row] = 1.0f;
+      return;
+    }
+  }
+  const bool norms = many || !dynamic || !range;
+  if (norms) {
+#pragma unroll 1
+    for (int k = 0; k < NCH; ++k) {
+      double s = 0.0;
+      if (col_of(k) < D)
+#pragma unroll 1
+        for (int e = 0; e < 4; ++e) {
+          double u;
+          gated_exact(p, row, col_of(k) + e, &u);
+          s += u * u;
+        }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+      if (lane == 0 && warp + k * nwarps < nchunks) sum64[warp + k * nwarps] = s;
+    }
+    __syncthreads();
+  }
+  auto rnorm = [&](int k) {   // 1 / sqrt(mean + eps) of chunk k's group, or 1 where it cancels
+    const int c = warp + k * nwarps;
+    if (!norms || c >= nchunks) return 1.0;
+    double s = 0.0;
+    for (int i = c / cpg * cpg; i < c / cpg * cpg + cpg; ++i) s += sum64[i];
+    return 1.0 / sqrt(s / (double)(many ? cpg * 128 : D) + (double)p.eps);
+  };
+  double m64 = 0.0;
+  if (dynamic) {
+#pragma unroll 1
+    for (int k = 0; k < NCH; ++k)
+      if (col_of(k) < D && (!range || (cand >> k & 1u))) {
+        const double r = rnorm(k);
+#pragma unroll 1
+        for (int e = 0; e < 4; ++e) {
+          double u;
+          m64 = fmax(m64, fabs(gated_exact(p, row, col_of(k) + e, &u) * r));   // (a NaN counts for nothing)
+        }
+      }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m64 = fmax(m64, __shfl_xor_sync(0xffffffffu, m64, o));
+    if (lane == 0) top64[warp] = m64;
+    __syncthreads();
+    for (int i = 0; i < nwarps; ++i) m64 = fmax(m64, top64[i]);
+    if (!range && p.scale && threadIdx.x == 0) p.scale[row] = m64 > 0.0 ? (float)(m64 / 127.0) : 1.0f;
+  }
+#pragma unroll 1
+  for (int k = 0; k < NCH; ++k)
+    if (col_of(k) < D && (!range || (near >> k & 1u))) {
+      const double r = rnorm(k);
+#pragma unroll 1
+      for (int e = 0; e < 4; ++e) {
+        double u;
+        const double v = gated_exact(p, row, col_of(k) + e, &u) * r;
+        const double q = !dynamic ? v / (double)*p.static_scale : m64 > 0.0 ? 127.0 * v / m64 : v;   // (exact ties stay ties)
+        p.xq[row * D + col_of(k) + e] = (int8_t)__double2int_rn(fmax(fmin(q, 127.0), -127.0));        // (fmin(NaN, 127) = 127)
+      }
+    }
+}
+
 // NCH chunks of 128 columns per warp: chunk c = warp + k * warps
 template <typename T, typename Z, int NCH>
-__global__ void __launch_bounds__(32 * kMaxWarps) norm_kernel(const __grid_constant__ NormParams<T, Z> p) {
+__global__ void __launch_bounds__(NCH == 5 ? 416 : 512, NCH == 5 ? 2 : NCH == 2 ? 2 : 1) norm_kernel(const __grid_constant__ NormParams<T, Z> p) {
   constexpr bool GATE = !std::is_same<Z, None>::value;
-  __shared__ float part[2][kMaxWarps];
-  __shared__ float csum[kMaxChunks], cmax[kMaxChunks];   // of chunks, where the row has several groups
-  __shared__ double dsum[kMaxChunks], dmax[kMaxWarps];
+  __shared__ struct {
+    float part[2][kMaxWarps];
+    float csum[kMaxChunks], cmax[kMaxChunks];   // of chunks, where the row has several groups
+    double sum64[kMaxChunks], top64[kMaxWarps];
+  } S;
   pdl_launch_dependents();
   pdl_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nwarps = blockDim.x >> 5;
   const i64 row = blockIdx.x;
   const int D = p.D, nchunks = (D + 127) / 128, cpg = p.groups > 1 ? nchunks / p.groups : nchunks;
   const bool many = p.groups > 1, dynamic = p.static_scale == nullptr;
-  float4 t[NCH];
-  float cs[NCH], mx[NCH];
+  float2 t[NCH][2];   // u w
+  float cs[NCH], mx[NCH], least = 0.f;
   {
-    float4 zv[GATE ? NCH : 1];
+    typename Elem<T>::raw4 xr[NCH];
+    typename GateRaw<Z>::raw4 zr[NCH];
 #pragma unroll
     for (int k = 0; k < NCH; ++k) {
       const int col = ((warp + k * nwarps) * 32 + lane) * 4;
-      t[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (GATE) zv[GATE ? k : 0] = t[k];
+      xr[k] = {};
+      zr[k] = {};
       if (col < D) {
-        t[k] = load_row4<T>(p.x + row * p.sx + col, p.valigned);
-        if constexpr (GATE) zv[k] = load_row4<Z>(p.z + row * p.sz + col, p.zaligned);
+        xr[k] = load_row4<T>(p.x + row * p.sx + col, p.valigned);
+        if constexpr (GATE) zr[k] = load_row4<Z>(p.z + row * p.sz + col, p.zaligned);
       }
     }
 #pragma unroll
     for (int k = 0; k < NCH; ++k) {
       const int col = ((warp + k * nwarps) * 32 + lane) * 4;
+      const float4 v = Elem<T>::cvt(xr[k]);
+      t[k][0] = make_float2(v.x, v.y);
+      t[k][1] = make_float2(v.z, v.w);
       if constexpr (GATE) {
-        t[k].x *= silu_compensated(zv[k].x);
-        t[k].y *= silu_compensated(zv[k].y);
-        t[k].z *= silu_compensated(zv[k].z);
-        t[k].w *= silu_compensated(zv[k].w);
+        const float4 z = Elem<Z>::cvt(zr[k]);
+        least = fminf(fminf(least, fminf(z.x, z.y)), fminf(z.z, z.w));   // (a NaN shows in the sums)
+        t[k][0] = __fmul2_rn(t[k][0], silu2(make_float2(z.x, z.y)));
+        t[k][1] = __fmul2_rn(t[k][1], silu2(make_float2(z.z, z.w)));
       }
-      cs[k] = fmaf(t[k].x, t[k].x, t[k].y * t[k].y) + fmaf(t[k].z, t[k].z, t[k].w * t[k].w);
+      const float2 sq = __ffma2_rn(t[k][0], t[k][0], __fmul2_rn(t[k][1], t[k][1]));
+      cs[k] = sq.x + sq.y;
       if (p.weight && col < D) {
         const float4 w = *reinterpret_cast<const float4*>(p.weight + col);
-        t[k] = make_float4(t[k].x * w.x, t[k].y * w.y, t[k].z * w.z, t[k].w * w.w);
+        t[k][0] = __fmul2_rn(t[k][0], make_float2(w.x, w.y));
+        t[k][1] = __fmul2_rn(t[k][1], make_float2(w.z, w.w));
       }
-      mx[k] = fmaxf(fmaxf(fabsf(t[k].x), fabsf(t[k].y)), fmaxf(fabsf(t[k].z), fabsf(t[k].w)));
+      mx[k] = fmaxf(fmaxf(fabsf(t[k][0].x), fabsf(t[k][0].y)), fmaxf(fabsf(t[k][1].x), fabsf(t[k][1].y)));
     }
+    if (least < kLeastGate) cs[0] = __uint_as_float(0x7fffffffu);   // (sends the row to binary64)
   }
   // sum of squares and absmax of the row, or of its groups (whole chunks each)
   float r = 0.f, rk[NCH], top = 0.f, total = 0.f;   // 1 / sqrt(mean + eps) of the row or of each chunk's group; absmax of o; sum of squares
@@ -116,10 +216,10 @@ __global__ void __launch_bounds__(32 * kMaxWarps) norm_kernel(const __grid_const
       s += __shfl_xor_sync(0xffffffffu, s, o);
       m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
     }
-    if (lane == 0) { part[0][warp] = s; part[1][warp] = m; }
+    if (lane == 0) { S.part[0][warp] = s; S.part[1][warp] = m; }
     __syncthreads();
-    s = lane < nwarps ? part[0][lane] : 0.f;
-    m = lane < nwarps ? part[1][lane] : 0.f;
+    s = lane < nwarps ? S.part[0][lane] : 0.f;
+    m = lane < nwarps ? S.part[1][lane] : 0.f;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
       s += __shfl_xor_sync(0xffffffffu, s, o);
@@ -141,13 +241,13 @@ __global__ void __launch_bounds__(32 * kMaxWarps) norm_kernel(const __grid_const
         m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
       }
       const int c = warp + k * nwarps;
-      if (lane == 0 && c < nchunks) { csum[c] = s; cmax[c] = m; }
+      if (lane == 0 && c < nchunks) { S.csum[c] = s; S.cmax[c] = m; }
     }
     __syncthreads();
     const float n = (float)(cpg * 128);
     for (int g = 0; g < p.groups; ++g) {
       float s = 0.f, m = 0.f;
-      for (int c = lane; c < cpg; c += 32) { s += csum[g * cpg + c]; m = fmaxf(m, cmax[g * cpg + c]); }
+      for (int c = lane; c < cpg; c += 32) { s += S.csum[g * cpg + c]; m = fmaxf(m, S.cmax[g * cpg + c]); }
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) {
         s += __shfl_xor_sync(0xffffffffu, s, o);
@@ -167,113 +267,38 @@ __global__ void __launch_bounds__(32 * kMaxWarps) norm_kernel(const __grid_const
   const float inv = 1.0f / step;
   const float rel = (dynamic ? (many ? 80.f : 28.f) : 42.f) * kEps;
   uint32_t code[NCH];
-  uint32_t near = 0;   // bit 4 k + c: the quotient lies near the middle of two integers
+  uint32_t near = 0;   // bit k: one of the four quotients lies near the middle of two integers
+  const float f_row = 127.0f / (top / r);
 #pragma unroll
   for (int k = 0; k < NCH; ++k) {
-    const float f = (dynamic && !many) ? 127.0f / (top / r) : rk[k] * inv;
-    const float v[4] = {t[k].x, t[k].y, t[k].z, t[k].w};
-    float m[4];
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      float q;
-      asm("min.xorsign.abs.f32 %0, %1, %2;" : "=f"(q) : "f"(v[c] * f), "f"(127.0f));
-      m[c] = __fadd_rn(q, kMagicOut);
-      const float off = fabsf(q - __fadd_rn(m[c], -kMagicOut));
-      near |= (!(fmaf(rel, fabsf(q), off) <= 0.5f) ? 1u : 0u) << (4 * k + c);
-    }
-    code[k] = pack4_bits(__float_as_uint(m[0]), __float_as_uint(m[1]), __float_as_uint(m[2]), __float_as_uint(m[3]));
-    if (((warp + k * nwarps) * 32 + lane) * 4 >= D) near &= ~(15u << (4 * k));
+    const float f = dynamic && !many ? f_row : rk[k] * inv;
+    const float2 v0 = __fmul2_rn(t[k][0], make_float2(f, f)), v1 = __fmul2_rn(t[k][1], make_float2(f, f));
+    float2 q0, q1;
+    asm("min.xorsign.abs.f32 %0, %1, %2;" : "=f"(q0.x) : "f"(v0.x), "f"(127.0f));
+    asm("min.xorsign.abs.f32 %0, %1, %2;" : "=f"(q0.y) : "f"(v0.y), "f"(127.0f));
+    asm("min.xorsign.abs.f32 %0, %1, %2;" : "=f"(q1.x) : "f"(v1.x), "f"(127.0f));
+    asm("min.xorsign.abs.f32 %0, %1, %2;" : "=f"(q1.y) : "f"(v1.y), "f"(127.0f));
+    const float2 mg = make_float2(kMagicOut, kMagicOut), mn = make_float2(-kMagicOut, -kMagicOut);
+    const float2 m0 = __fadd2_rn(q0, mg), m1 = __fadd2_rn(q1, mg);
+    const float2 i0 = __fadd2_rn(m0, mn), i1 = __fadd2_rn(m1, mn);
+    // how far from the integer, and how far off at most
+    const float a = fmaf(rel, fabsf(q0.x), fabsf(q0.x - i0.x)), b = fmaf(rel, fabsf(q0.y), fabsf(q0.y - i0.y));
+    const float c = fmaf(rel, fabsf(q1.x), fabsf(q1.x - i1.x)), d = fmaf(rel, fabsf(q1.y), fabsf(q1.y - i1.y));
+    near |= (!(fmaxf(fmaxf(a, b), fmaxf(c, d)) <= 0.5f) ? 1u : 0u) << k;   // (rows with a NaN are out of range)
+    code[k] = pack4_bits(__float_as_uint(m0.x), __float_as_uint(m0.y), __float_as_uint(m1.x), __float_as_uint(m1.y));
+    if (((warp + k * nwarps) * 32 + lane) * 4 >= D) near &= ~(1u << k);
   }
-  float scale_out = step;
-  bool exact = __syncthreads_or(near != 0 || !range);
-  if (exact && total == 0.f) {
-    // a row of zeros (padding) needs none of it; x that underflowed does
-    bool any = false;
+  // chunks that hold an element which can be the row's absmax
+  uint32_t cand = 0;
 #pragma unroll
-    for (int k = 0; k < NCH; ++k) {
-      const int col = ((warp + k * nwarps) * 32 + lane) * 4;
-      if (col < D) {
-        const float4 v = load_row4<T>(p.x + row * p.sx + col, p.valigned);
-        any |= v.x != 0.f || v.y != 0.f || v.z != 0.f || v.w != 0.f;
-        code[k] = 0u;
-      }
-    }
-    exact = __syncthreads_or(any);
-    if (!exact) scale_out = 1.0f;
-  }
-  if (exact) {
-    // binary64, for what is near (or for all of a row outside the safe range)
-    double rd[NCH];
-#pragma unroll
-    for (int k = 0; k < NCH; ++k) rd[k] = 1.0;
-    if (many || !dynamic || !range) {
-#pragma unroll 1
-      for (int k = 0; k < NCH; ++k) {
-        const int c = warp + k * nwarps, col = (c * 32 + lane) * 4;
-        double s = 0.0;
-        if (col < D)
-#pragma unroll 1
-          for (int e = 0; e < 4; ++e) {
-            double u;
-            gated_exact(p, row, col + e, &u);
-            s += u * u;
-          }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-        if (lane == 0 && c < nchunks) dsum[c] = s;
-      }
-      __syncthreads();
-#pragma unroll
-      for (int k = 0; k < NCH; ++k) {
-        const int c = warp + k * nwarps;
-        if (c < nchunks) {
-          double s = 0.0;
-          for (int i = c / cpg * cpg; i < c / cpg * cpg + cpg; ++i) s += dsum[i];
-          rd[k] = 1.0 / sqrt(s / (double)(many ? cpg * 128 : D) + (double)p.eps);
-        }
-      }
-    }
-    double m64 = 0.0;
-    if (dynamic) {
-#pragma unroll
-      for (int k = 0; k < NCH; ++k) {
-        const int col = ((warp + k * nwarps) * 32 + lane) * 4;
-        const float v[4] = {t[k].x, t[k].y, t[k].z, t[k].w};
-#pragma unroll 1
-        for (int e = 0; e < 4; ++e)
-          if (col < D && (!range || fabsf(v[e]) * rk[k] >= top * (1.0f - 160.0f * kEps))) {
-            double u;
-            m64 = fmax(m64, fabs(gated_exact(p, row, col + e, &u) * rd[k]));   // (a NaN counts for nothing)
-          }
-      }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) m64 = fmax(m64, __shfl_xor_sync(0xffffffffu, m64, o));
-      if (lane == 0) dmax[warp] = m64;
-      __syncthreads();
-      for (int i = 0; i < nwarps; ++i) m64 = fmax(m64, dmax[i]);
-    }
-    const double sd = dynamic ? (m64 > 0.0 ? m64 / 127.0 : 1.0) : (double)*p.static_scale;
-    if (!range && dynamic) scale_out = (float)sd;
-#pragma unroll
-    for (int k = 0; k < NCH; ++k) {
-      const int col = ((warp + k * nwarps) * 32 + lane) * 4;
-#pragma unroll 1
-      for (int e = 0; e < 4; ++e)
-        if (col < D && (!range || (near >> (4 * k + e) & 1u))) {
-          double u;
-          const double v = gated_exact(p, row, col + e, &u) * rd[k];
-          const double q = dynamic && m64 > 0.0 ? 127.0 * v / m64 : v / sd;   // (exact ties stay ties)
-          const uint32_t c = (uint32_t)__double2int_rn(fmax(fmin(q, 127.0), -127.0)) & 0xffu;   // (fmin(NaN, 127) = 127)
-          code[k] = (code[k] & ~(0xffu << (8 * e))) | c << (8 * e);
-        }
-    }
-  }
+  for (int k = 0; k < NCH; ++k) cand |= (mx[k] * rk[k] >= top * (1.0f - 160.0f * kEps) ? 1u : 0u) << k;
 #pragma unroll
   for (int k = 0; k < NCH; ++k) {
     const int col = ((warp + k * nwarps) * 32 + lane) * 4;
     if (col < D) *reinterpret_cast<uint32_t*>(p.xq + row * D + col) = code[k];
   }
-  if (p.scale && threadIdx.x == 0) p.scale[row] = scale_out;
+  if (dynamic && p.scale && threadIdx.x == 0) p.scale[row] = step;
+  if (__syncthreads_or(near != 0 || !range)) exact_row<T, Z, NCH>(p, row, near, cand, range, total == 0.f, S.sum64, S.top64);
 }
 
 template <typename T, typename Z>
