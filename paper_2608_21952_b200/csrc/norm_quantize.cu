@@ -29,7 +29,7 @@ struct NormParams {
   int8_t* xq;
   float* scale;
   const float* static_scale;
-  int D, groups, valigned, zaligned;
+  int D, groups, valigned, zaligned, fast;
   float eps;
 };
 
@@ -74,7 +74,8 @@ __device__ __noinline__ void exact_row(const NormParams<T, Z>& p, i64 row, uint3
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nwarps = blockDim.x >> 5;
   const int D = p.D, nchunks = (D + 127) / 128, cpg = p.groups > 1 ? nchunks / p.groups : nchunks;
   const bool many = p.groups > 1, dynamic = p.static_scale == nullptr;
-  auto col_of = [&](int k) { return ((warp + k * nwarps) * 32 + lane) * 4; };
+  const int c0 = warp * NCH;   // this warp's chunks
+  auto col_of = [&](int k) { return ((c0 + k) * 32 + lane) * 4; };
   if (zero) {
     // a row of zeros (padding) needs none of it; x that underflowed does
     bool any = false;
@@ -106,12 +107,12 @@ __device__ __noinline__ void exact_row(const NormParams<T, Z>& p, i64 row, uint3
         }
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-      if (lane == 0 && warp + k * nwarps < nchunks) sum64[warp + k * nwarps] = s;
+      if (lane == 0 && c0 + k < nchunks) sum64[c0 + k] = s;
     }
     __syncthreads();
   }
   auto rnorm = [&](int k) {   // 1 / sqrt(mean + eps) of chunk k's group, or 1 where it cancels
-    const int c = warp + k * nwarps;
+    const int c = c0 + k;
     if (!norms || c >= nchunks) return 1.0;
     double s = 0.0;
     for (int i = c / cpg * cpg; i < c / cpg * cpg + cpg; ++i) s += sum64[i];
@@ -150,10 +151,57 @@ __device__ __noinline__ void exact_row(const NormParams<T, Z>& p, i64 row, uint3
     }
 }
 
-// NCH chunks of 128 columns per warp: chunk c = warp + k * warps
-template <typename T, typename Z, int NCH>
-__global__ void __launch_bounds__(NCH == 5 ? 416 : 512, NCH == 5 ? 2 : NCH == 2 ? 2 : 1) norm_kernel(const __grid_constant__ NormParams<T, Z> p) {
+// u w of a warp's chunks, their sums of u^2 and absmax.  ALL: every chunk lies in the row and is aligned, so loads stand at fixed
+// distances from one address.
+template <typename T, typename Z, int NCH, bool ALL>
+__device__ __forceinline__ void row_values(const NormParams<T, Z>& p, i64 row, int col0, float2 (&t)[NCH][2], float (&cs)[NCH], float (&mx)[NCH]) {
   constexpr bool GATE = !std::is_same<Z, None>::value;
+  const T* const x = p.x + row * p.sx + col0;
+  const float* const w = p.weight + col0;
+  typename Elem<T>::raw4 xr[NCH];
+  typename GateRaw<Z>::raw4 zr[NCH];
+#pragma unroll
+  for (int k = 0; k < NCH; ++k) {
+    xr[k] = {};
+    zr[k] = {};
+    if (ALL || col0 + 128 * k < p.D) {
+      xr[k] = load_row4<T>(x + 128 * k, ALL || p.valigned);
+      if constexpr (GATE) zr[k] = load_row4<Z>(p.z + row * p.sz + col0 + 128 * k, ALL || p.zaligned);
+    }
+  }
+  float least = 0.f;
+#pragma unroll
+  for (int k = 0; k < NCH; ++k) {
+    const float4 v = Elem<T>::cvt(xr[k]);
+    t[k][0] = make_float2(v.x, v.y);
+    t[k][1] = make_float2(v.z, v.w);
+    if constexpr (GATE) {
+      const float4 z = Elem<Z>::cvt(zr[k]);
+      least = fminf(fminf(least, fminf(z.x, z.y)), fminf(z.z, z.w));   // (a NaN shows in the sums)
+      t[k][0] = __fmul2_rn(t[k][0], silu2(make_float2(z.x, z.y)));
+      t[k][1] = __fmul2_rn(t[k][1], silu2(make_float2(z.z, z.w)));
+    }
+    const float2 sq = __ffma2_rn(t[k][0], t[k][0], __fmul2_rn(t[k][1], t[k][1]));
+    cs[k] = sq.x + sq.y;
+    if (p.weight && (ALL || col0 + 128 * k < p.D)) {
+      const float4 f = *reinterpret_cast<const float4*>(w + 128 * k);
+      t[k][0] = __fmul2_rn(t[k][0], make_float2(f.x, f.y));
+      t[k][1] = __fmul2_rn(t[k][1], make_float2(f.z, f.w));
+    }
+    mx[k] = fmaxf(fmaxf(fabsf(t[k][0].x), fabsf(t[k][0].y)), fmaxf(fabsf(t[k][1].x), fabsf(t[k][1].y)));
+  }
+  if (least < kLeastGate) cs[0] = __uint_as_float(0x7fffffffu);   // (sends the row to binary64)
+}
+
+__device__ __forceinline__ float warp_max(float v) {   // of numbers >= 0; a NaN counts for nothing
+  float m;
+  asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(v));
+  return m;
+}
+
+// A warp has NCH chunks of 128 columns, one after the other.
+template <typename T, typename Z, int NCH>
+__global__ void __launch_bounds__(NCH == 5 ? 416 : 512, NCH == 8 ? 1 : 2) norm_kernel(const __grid_constant__ NormParams<T, Z> p) {
   __shared__ struct {
     float part[2][kMaxWarps];
     float csum[kMaxChunks], cmax[kMaxChunks];   // of chunks, where the row has several groups
@@ -163,68 +211,30 @@ __global__ void __launch_bounds__(NCH == 5 ? 416 : 512, NCH == 5 ? 2 : NCH == 2 
   pdl_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nwarps = blockDim.x >> 5;
   const i64 row = blockIdx.x;
-  const int D = p.D, nchunks = (D + 127) / 128, cpg = p.groups > 1 ? nchunks / p.groups : nchunks;
-  const bool many = p.groups > 1, dynamic = p.static_scale == nullptr;
-  float2 t[NCH][2];   // u w
-  float cs[NCH], mx[NCH], least = 0.f;
-  {
-    typename Elem<T>::raw4 xr[NCH];
-    typename GateRaw<Z>::raw4 zr[NCH];
-#pragma unroll
-    for (int k = 0; k < NCH; ++k) {
-      const int col = ((warp + k * nwarps) * 32 + lane) * 4;
-      xr[k] = {};
-      zr[k] = {};
-      if (col < D) {
-        xr[k] = load_row4<T>(p.x + row * p.sx + col, p.valigned);
-        if constexpr (GATE) zr[k] = load_row4<Z>(p.z + row * p.sz + col, p.zaligned);
-      }
-    }
-#pragma unroll
-    for (int k = 0; k < NCH; ++k) {
-      const int col = ((warp + k * nwarps) * 32 + lane) * 4;
-      const float4 v = Elem<T>::cvt(xr[k]);
-      t[k][0] = make_float2(v.x, v.y);
-      t[k][1] = make_float2(v.z, v.w);
-      if constexpr (GATE) {
-        const float4 z = Elem<Z>::cvt(zr[k]);
-        least = fminf(fminf(least, fminf(z.x, z.y)), fminf(z.z, z.w));   // (a NaN shows in the sums)
-        t[k][0] = __fmul2_rn(t[k][0], silu2(make_float2(z.x, z.y)));
-        t[k][1] = __fmul2_rn(t[k][1], silu2(make_float2(z.z, z.w)));
-      }
-      const float2 sq = __ffma2_rn(t[k][0], t[k][0], __fmul2_rn(t[k][1], t[k][1]));
-      cs[k] = sq.x + sq.y;
-      if (p.weight && col < D) {
-        const float4 w = *reinterpret_cast<const float4*>(p.weight + col);
-        t[k][0] = __fmul2_rn(t[k][0], make_float2(w.x, w.y));
-        t[k][1] = __fmul2_rn(t[k][1], make_float2(w.z, w.w));
-      }
-      mx[k] = fmaxf(fmaxf(fabsf(t[k][0].x), fabsf(t[k][0].y)), fmaxf(fabsf(t[k][1].x), fabsf(t[k][1].y)));
-    }
-    if (least < kLeastGate) cs[0] = __uint_as_float(0x7fffffffu);   // (sends the row to binary64)
-  }
+  const int D = p.D, nchunks = (D + 127) / 128, c0 = warp * NCH, col0 = (c0 * 32 + lane) * 4;
+  const bool many = p.groups > 1, dynamic = p.static_scale == nullptr, all = p.fast && (c0 + NCH) * 128 <= D;
+  float2 t[NCH][2];
+  float cs[NCH], mx[NCH];
+  if (all) row_values<T, Z, NCH, true>(p, row, col0, t, cs, mx);
+  else row_values<T, Z, NCH, false>(p, row, col0, t, cs, mx);
   // sum of squares and absmax of the row, or of its groups (whole chunks each)
   float r = 0.f, rk[NCH], top = 0.f, total = 0.f;   // 1 / sqrt(mean + eps) of the row or of each chunk's group; absmax of o; sum of squares
-  bool range = true;                   // the sums are where binary32 is safe
+  bool range = true;                                // the sums are where binary32 is safe
   auto safe = [](float v) { return v > 1e-30f && v < 1e37f; };
   if (!many) {
     float s = cs[0], m = mx[0];
 #pragma unroll
     for (int k = 1; k < NCH; ++k) { s += cs[k]; m = fmaxf(m, mx[k]); }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      s += __shfl_xor_sync(0xffffffffu, s, o);
-      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    }
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    m = warp_max(m);
     if (lane == 0) { S.part[0][warp] = s; S.part[1][warp] = m; }
     __syncthreads();
-    s = lane < nwarps ? S.part[0][lane] : 0.f;
+    s = (lane & 15) < nwarps ? S.part[0][lane & 15] : 0.f;
     m = lane < nwarps ? S.part[1][lane] : 0.f;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      s += __shfl_xor_sync(0xffffffffu, s, o);
-      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    }
+    for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    m = warp_max(m);
     range = safe(s) && safe(m);
     total = s;
     r = 1.0f / sqrtf(s / (float)D + p.eps);
@@ -232,16 +242,15 @@ __global__ void __launch_bounds__(NCH == 5 ? 416 : 512, NCH == 5 ? 2 : NCH == 2 
 #pragma unroll
     for (int k = 0; k < NCH; ++k) rk[k] = r;
   } else {
+    const int cpg = nchunks / p.groups;
 #pragma unroll
     for (int k = 0; k < NCH; ++k) {
-      float s = cs[k], m = mx[k];
+      float s = cs[k];
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) {
-        s += __shfl_xor_sync(0xffffffffu, s, o);
-        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-      }
-      const int c = warp + k * nwarps;
-      if (lane == 0 && c < nchunks) { S.csum[c] = s; S.cmax[c] = m; }
+      for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+      const float m = warp_max(mx[k]);
+      if (lane == 0 && c0 + k < nchunks) { S.csum[c0 + k] = s; S.cmax[c0 + k] = m; }
+      rk[k] = 0.f;
     }
     __syncthreads();
     const float n = (float)(cpg * 128);
@@ -249,26 +258,24 @@ __global__ void __launch_bounds__(NCH == 5 ? 416 : 512, NCH == 5 ? 2 : NCH == 2 
       float s = 0.f, m = 0.f;
       for (int c = lane; c < cpg; c += 32) { s += S.csum[g * cpg + c]; m = fmaxf(m, S.cmax[g * cpg + c]); }
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) {
-        s += __shfl_xor_sync(0xffffffffu, s, o);
-        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-      }
+      for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+      m = warp_max(m);
       const float rg = 1.0f / sqrtf(s / n + p.eps);
       range &= safe(s) && safe(m);
       total += s;
       top = fmaxf(top, m * rg);
 #pragma unroll
       for (int k = 0; k < NCH; ++k)
-        if ((warp + k * nwarps) / cpg == g) rk[k] = rg;
+        if (c0 + k >= g * cpg && c0 + k < (g + 1) * cpg) rk[k] = rg;
     }
   }
   const float step = dynamic ? top / 127.0f : *p.static_scale;
   range &= safe(step);
   const float inv = 1.0f / step;
   const float rel = (dynamic ? (many ? 80.f : 28.f) : 42.f) * kEps;
-  uint32_t code[NCH];
-  uint32_t near = 0;   // bit k: one of the four quotients lies near the middle of two integers
   const float f_row = 127.0f / (top / r);
+  uint32_t near = 0, cand = 0;   // bit k: one of the four quotients lies near the middle of two integers; one element can be the row's absmax
+  int8_t* const xq = p.xq + row * D + col0;
 #pragma unroll
   for (int k = 0; k < NCH; ++k) {
     const float f = dynamic && !many ? f_row : rk[k] * inv;
@@ -284,18 +291,12 @@ __global__ void __launch_bounds__(NCH == 5 ? 416 : 512, NCH == 5 ? 2 : NCH == 2 
     // how far from the integer, and how far off at most
     const float a = fmaf(rel, fabsf(q0.x), fabsf(q0.x - i0.x)), b = fmaf(rel, fabsf(q0.y), fabsf(q0.y - i0.y));
     const float c = fmaf(rel, fabsf(q1.x), fabsf(q1.x - i1.x)), d = fmaf(rel, fabsf(q1.y), fabsf(q1.y - i1.y));
-    near |= (!(fmaxf(fmaxf(a, b), fmaxf(c, d)) <= 0.5f) ? 1u : 0u) << k;   // (rows with a NaN are out of range)
-    code[k] = pack4_bits(__float_as_uint(m0.x), __float_as_uint(m0.y), __float_as_uint(m1.x), __float_as_uint(m1.y));
-    if (((warp + k * nwarps) * 32 + lane) * 4 >= D) near &= ~(1u << k);
-  }
-  // chunks that hold an element which can be the row's absmax
-  uint32_t cand = 0;
-#pragma unroll
-  for (int k = 0; k < NCH; ++k) cand |= (mx[k] * rk[k] >= top * (1.0f - 160.0f * kEps) ? 1u : 0u) << k;
-#pragma unroll
-  for (int k = 0; k < NCH; ++k) {
-    const int col = ((warp + k * nwarps) * 32 + lane) * 4;
-    if (col < D) *reinterpret_cast<uint32_t*>(p.xq + row * D + col) = code[k];
+    const uint32_t code = pack4_bits(__float_as_uint(m0.x), __float_as_uint(m0.y), __float_as_uint(m1.x), __float_as_uint(m1.y));
+    if (all || col0 + 128 * k < D) {
+      if (!(fmaxf(fmaxf(a, b), fmaxf(c, d)) <= 0.5f)) near |= 1u << k;   // (rows with a NaN are out of range)
+      if (mx[k] * rk[k] >= top * (1.0f - 160.0f * kEps)) cand |= 1u << k;
+      *reinterpret_cast<uint32_t*>(xq + 128 * k) = code;
+    }
   }
   if (dynamic && p.scale && threadIdx.x == 0) p.scale[row] = step;
   if (__syncthreads_or(near != 0 || !range)) exact_row<T, Z, NCH>(p, row, near, cand, range, total == 0.f, S.sum64, S.top64);
@@ -310,6 +311,7 @@ ssdi8_status_t launch(const ssdi8_norm_args_t& a, cudaStream_t st) {
   p.D = a.width; p.groups = a.groups; p.eps = a.eps;
   p.valigned = reinterpret_cast<uintptr_t>(a.x) % (4 * sizeof(T)) == 0 && a.stride_x % 4 == 0;
   p.zaligned = a.z && reinterpret_cast<uintptr_t>(a.z) % (4 * sizeof(Z)) == 0 && a.stride_z % 4 == 0;
+  p.fast = p.valigned && (!a.z || p.zaligned);
   const int chunks = (a.width + 127) / 128;
   auto go = [&](auto n) -> ssdi8_status_t {
     constexpr int NCH = decltype(n)::value;
