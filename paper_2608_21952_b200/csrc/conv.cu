@@ -42,14 +42,80 @@ __device__ __forceinline__ int sequence(const ConvParams<T>& p, int b, bool firs
   return len;
 }
 
+// largest magnitude of so many raw elements, as floats: magnitudes are ordered as their bits are
+template <typename T> struct RawMax;
+template <> struct RawMax<float> {
+  uint4 m = make_uint4(0u, 0u, 0u, 0u);
+  __device__ __forceinline__ void add(const float4& v) {
+    m = make_uint4(max(m.x, __float_as_uint(v.x) & 0x7fffffffu), max(m.y, __float_as_uint(v.y) & 0x7fffffffu),
+                   max(m.z, __float_as_uint(v.z) & 0x7fffffffu), max(m.w, __float_as_uint(v.w) & 0x7fffffffu));
+  }
+  __device__ __forceinline__ float4 get() const {
+    return make_float4(__uint_as_float(m.x), __uint_as_float(m.y), __uint_as_float(m.z), __uint_as_float(m.w));
+  }
+};
+template <typename T> struct RawMax16 {
+  uint2 m = make_uint2(0u, 0u);
+  __device__ __forceinline__ void add(const uint2& v) { m = make_uint2(__vmaxu2(m.x, v.x & 0x7fff7fffu), __vmaxu2(m.y, v.y & 0x7fff7fffu)); }
+  __device__ __forceinline__ float4 get() const { return Elem<T>::cvt(m); }
+};
+template <> struct RawMax<__half> : RawMax16<__half> {};
+template <> struct RawMax<__nv_bfloat16> : RawMax16<__nv_bfloat16> {};
+
+// The code of token t, channel ch, where it lies near the middle of two integers, in binary64, from the inputs (the ring still holds what
+// it held before the call).  Whether it does is seen once more, with room to spare.
+template <typename T, int W>
+__device__ __noinline__ void code_exact(const ConvParams<T>& p, int b, int t, int ch, int slot, int pos) {
+  const int Ch = p.D + 2 * p.GN, at = ch - p.D;
+  float x[W], w[W];
+#pragma unroll
+  for (int k = 0; k < W; ++k) {
+    const int tk = t - (W - 1) + k;
+    x[k] = 0.f;
+    if (tk >= 0) x[k] = Elem<T>::get(p.xBC[b * p.sb + tk * p.stok + ch]);
+    else if (slot >= 0 && pos + tk >= 0) x[k] = Elem<T>::get(p.ring[((i64)slot * W + ((uint32_t)pos + tk) % W) * Ch + ch]);
+    w[k] = p.weight[(i64)ch * W + k];
+  }
+  const float bias = p.bias ? p.bias[ch] : 0.f;
+  const float step = at < 0 ? p.s_x[ch] : at < p.GN ? p.s_B[at / p.N] : p.s_C[(at - p.GN) / p.N];
+  float v = bias, m = fabsf(bias);
+#pragma unroll
+  for (int k = 0; k < W; ++k) {
+    v = fmaf(w[k], x[k], v);
+    m = fmaf(fabsf(w[k]), fabsf(x[k]), m);
+  }
+  const float q = v / (1.0f + __expf(-v)) / step;
+  // (twice the bound in block.cuh; |v| <= m)
+  if (fabsf(q - rintf(q)) + 2.0f * kEps * (5.0f * m / step + (14.0f + 2.0f * m) * fabsf(q)) < 0.5f && step >= 1e-30f && step <= 1e30f) return;
+  double e = (double)bias;
+#pragma unroll
+  for (int k = 0; k < W; ++k) e = __fma_rn((double)w[k], (double)x[k], e);
+  const double r = e / (1.0 + exp(-e)) / (double)step;
+  int8_t* const out = reinterpret_cast<int8_t*>(at < 0 ? p.xq : at < p.GN ? p.Bq : p.Cq);
+  const int width = at < 0 ? p.D : p.GN, col = at < 0 ? ch : at < p.GN ? at : at - p.GN;
+  out[((i64)b * p.L + t) * width + col] = (int8_t)__double2int_rn(fmax(fmin(r, 127.0), -127.0));   // (fmin(NaN, 127) = 127)
+}
+
+// Groups of four quotients (a token, four channels) one of which may lie near the middle of two integers: they wait for the end of the
+// block, whose threads then have a quotient each.  (Each at once by the lane that met it, its warp waiting: 157 us where
+// 8 x 2048 x 80 heads with a longer and narrower test took 119.)
+constexpr int kQueue = 256;
+struct Queue {
+  uint32_t item[kQueue];   // token of the slab << 8 | thread
+  int count;
+};
+
 template <typename T, int W, bool CODES, bool ALIGNED>
-__device__ __forceinline__ void conv_block(const ConvParams<T>& p, int b, int slab, int cblock) {
+__device__ __forceinline__ void conv_block(const ConvParams<T>& p, int b, int slab, int cblock, Queue& queue) {
   typedef typename Elem<T>::raw4 raw4;
   const int Ch = p.D + 2 * p.GN;
   int slot, pos;
+  if (CODES && threadIdx.x == 0) queue.count = 0;
   const int len = sequence(p, b, cblock == 0 && slab == 0, &slot, &pos);
-  const int col = 4 * (cblock * CT + threadIdx.x);
-  if (col >= Ch) return;
+  if (CODES) __syncthreads();
+  const int own_col = 4 * (cblock * CT + threadIdx.x);
+  const bool active = own_col < Ch;
+  const int col = active ? own_col : 0;   // (the others come along for the end of the block)
   float2 w01[W], w23[W];   // taps of channels 0, 1 and 2, 3
   float wsum[4];
 #pragma unroll
@@ -71,12 +137,14 @@ __device__ __forceinline__ void conv_block(const ConvParams<T>& p, int b, int sl
   }
   const float4 bias = p.bias ? make_float4(p.bias[col], p.bias[col + 1], p.bias[col + 2], p.bias[col + 3])
                              : make_float4(0.f, 0.f, 0.f, 0.f);
-  float4 step = make_float4(1.f, 1.f, 1.f, 1.f), inv = step;
+  float2 step01 = make_float2(1.f, 1.f), step23 = step01;
+  float fac[4];   // 5 eps / step
   uint32_t* out = nullptr;
   int ow4 = 0;
   bool usable = true;
   if (CODES) {
     int oq;
+    float4 step;
     if (col < p.D) {
       step = *reinterpret_cast<const float4*>(p.s_x + col);
       out = p.xq; ow4 = p.D / 4; oq = col / 4;
@@ -88,103 +156,138 @@ __device__ __forceinline__ void conv_block(const ConvParams<T>& p, int b, int sl
       out = isC ? p.Cq : p.Bq; ow4 = p.GN / 4; oq = at / 4;
     }
     out += (i64)b * p.L * ow4 + oq;
-    inv = make_float4(__frcp_rn(step.x), __frcp_rn(step.y), __frcp_rn(step.z), __frcp_rn(step.w));
+    step01 = make_float2(step.x, step.y);
+    step23 = make_float2(step.z, step.w);
+    fac[0] = 5.1f * kEps / step.x; fac[1] = 5.1f * kEps / step.y; fac[2] = 5.1f * kEps / step.z; fac[3] = 5.1f * kEps / step.w;
     auto normal = [](float x) { return x >= 1e-30f && x <= 1e30f; };
     usable = normal(step.x) && normal(step.y) && normal(step.z) && normal(step.w);
   }
   const int t0 = slab * p.slab, t1 = min(t0 + p.slab, p.L);
-  const int live = min(t1, len);
+  const int live = active ? min(t1, len) : t0;
   const T* src = p.xBC + b * p.sb + col;
-  T* ring = slot >= 0 ? p.ring + (i64)slot * W * Ch + col : nullptr;
-  float4 h[W + CROWS - 1];   // the W - 1 tokens ahead and the eight at hand
+  T* const ring = slot >= 0 ? p.ring + (i64)slot * W * Ch + col : nullptr;
+  raw4 past[W - 1];   // the W - 1 tokens ahead
 #pragma unroll
   for (int k = 0; k < W - 1; ++k) {
     const int t = t0 - (W - 1) + k;
-    h[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    past[k] = {};
     if (t0 < live) {
-      if (t >= 0) h[k] = Elem<T>::cvt(load4<T, ALIGNED>(src + t * p.stok));
-      else if (ring && pos + t >= 0) h[k] = Elem<T>::cvt(*reinterpret_cast<const raw4*>(ring + (i64)(((uint32_t)pos + t) % W) * Ch));
+      if (t >= 0) past[k] = load4<T, ALIGNED>(src + t * p.stok);
+      else if (ring && pos + t >= 0) past[k] = *reinterpret_cast<const raw4*>(ring + (i64)(((uint32_t)pos + t) % W) * Ch);
     }
   }
-  // the last W tokens stay in the ring (its rows ahead of this call have been read above, by this very thread: only the first slab does)
-  if (ring && slab == 0) {
-#pragma unroll
-    for (int k = 0; k < W; ++k) {
-      const int t = len - 1 - k;
-      if (t >= 0) *reinterpret_cast<raw4*>(ring + (i64)(((uint32_t)pos + t) % W) * Ch) = load4<T, ALIGNED>(src + t * p.stok);
-    }
-  }
-  for (int t = t0; t < live; t += CROWS) {
+  src += t0 * p.stok;
+  if (CODES) out += (i64)t0 * ow4;
+  // eight tokens from t on; WHOLE: all of them live
+  auto eight = [&](auto whole, int t) {
+    constexpr bool WHOLE = decltype(whole)::value;
     raw4 raw[CROWS];
 #pragma unroll
-    for (int u = 0; u < CROWS; ++u)
-      if (t + u < live) raw[u] = load4<T, ALIGNED>(src + (t + u) * p.stok);
-    float4 mx = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int u = 0; u < CROWS; ++u) h[W - 1 + u] = t + u < live ? Elem<T>::cvt(raw[u]) : make_float4(0.f, 0.f, 0.f, 0.f);
-    float4 d0;   // 5 eps M / step, M from the largest |x| at hand
-    if (CODES) {
-#pragma unroll
-      for (int u = 0; u < W + CROWS - 1; ++u)
-        mx = make_float4(fmaxf(mx.x, fabsf(h[u].x)), fmaxf(mx.y, fabsf(h[u].y)), fmaxf(mx.z, fabsf(h[u].z)), fmaxf(mx.w, fabsf(h[u].w)));
-      d0 = make_float4(5.f * kEps * fmaf(wsum[0], mx.x, fabsf(bias.x)) * inv.x, 5.f * kEps * fmaf(wsum[1], mx.y, fabsf(bias.y)) * inv.y,
-                       5.f * kEps * fmaf(wsum[2], mx.z, fabsf(bias.z)) * inv.z, 5.f * kEps * fmaf(wsum[3], mx.w, fabsf(bias.w)) * inv.w);
+    for (int u = 0; u < CROWS; ++u) {
+      if (!WHOLE) raw[u] = {};
+      if (WHOLE || t + u < live) raw[u] = load4<T, ALIGNED>(src + u * p.stok);
     }
+    // the nearest to an integer's middle that a quotient may come: 5 eps M / step + (12 + 2 |v|) eps |q| off, M from the largest |x| at
+    // hand, |v| <= M, |q| <= 127
+    float least[4];
+    if (CODES) {
+      RawMax<T> top;
+#pragma unroll
+      for (int k = 0; k < W - 1; ++k) top.add(past[k]);
+#pragma unroll
+      for (int u = 0; u < CROWS; ++u) top.add(raw[u]);
+      const float4 m = top.get();
+      const float M[4] = {fmaf(wsum[0], m.x, fabsf(bias.x)), fmaf(wsum[1], m.y, fabsf(bias.y)), fmaf(wsum[2], m.z, fabsf(bias.z)),
+                          fmaf(wsum[3], m.w, fabsf(bias.w))};
+#pragma unroll
+      for (int c = 0; c < 4; ++c) least[c] = fmaf(M[c], -(fac[c] + 2.0f * 127.0f * kEps), 0.5f - 12.0f * 127.0f * kEps);
+    }
+    float2 h01[W], h23[W];   // the window, oldest first
+#pragma unroll
+    for (int k = 0; k < W - 1; ++k) {
+      const float4 v = Elem<T>::cvt(past[k]);
+      h01[k + 1] = make_float2(v.x, v.y);
+      h23[k + 1] = make_float2(v.z, v.w);
+    }
+    uint32_t near = 0;   // bit u: one of the token's quotients comes nearer
 #pragma unroll
     for (int u = 0; u < CROWS; ++u) {
-      if (t + u < live) {
-        float2 v01 = make_float2(bias.x, bias.y), v23 = make_float2(bias.z, bias.w);
+      const float4 own = Elem<T>::cvt(raw[u]);
 #pragma unroll
-        for (int k = 0; k < W; ++k) {
-          v01 = __ffma2_rn(w01[k], make_float2(h[u + k].x, h[u + k].y), v01);
-          v23 = __ffma2_rn(w23[k], make_float2(h[u + k].z, h[u + k].w), v23);
-        }
-        const float v[4] = {v01.x, v01.y, v23.x, v23.y};
-        float s[4];
+      for (int k = 0; k < W - 1; ++k) { h01[k] = h01[k + 1]; h23[k] = h23[k + 1]; }
+      h01[W - 1] = make_float2(own.x, own.y);
+      h23[W - 1] = make_float2(own.z, own.w);
+      float2 v01 = make_float2(bias.x, bias.y), v23 = make_float2(bias.z, bias.w);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) s[c] = v[c] * rcp_approx(1.0f + ex2_approx(v[c] * -1.44269504f));
-        if (CODES) {
-          const float iv[4] = {inv.x, inv.y, inv.z, inv.w}, dd[4] = {d0.x, d0.y, d0.z, d0.w};
-          float m[4];
-          bool near[4], any = !usable;
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            const float q = s[c] * iv[c];
-            float cl;
-            asm("min.xorsign.abs.f32 %0, %1, %2;" : "=f"(cl) : "f"(q), "f"(127.0f));
-            m[c] = __fadd_rn(cl, kMagicOut);
-            const float off = fabsf(cl - __fadd_rn(m[c], -kMagicOut));
-            near[c] = !(fmaf(fmaf(2.0f * kEps, fabsf(v[c]), 12.0f * kEps), fabsf(cl), off + dd[c]) <= 0.5f) || !usable;
-            any |= near[c];
-          }
-          if (any) {
-            const float st[4] = {step.x, step.y, step.z, step.w}, bi[4] = {bias.x, bias.y, bias.z, bias.w};
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              float x[4] = {0.f, 0.f, 0.f, 0.f}, w[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-              for (int k = 0; k < W; ++k) {
-                const float4& hv = h[u + k];
-                x[k] = c == 0 ? hv.x : c == 1 ? hv.y : c == 2 ? hv.z : hv.w;
-                w[k] = c == 0 ? w01[k].x : c == 1 ? w01[k].y : c == 2 ? w23[k].x : w23[k].y;
-              }
-              if (near[c])
-                m[c] = __uint_as_float(rne_clamp_bits(
-                    silu_quotient_exact<W>(x[0], x[1], x[2], x[3], w[0], w[1], w[2], w[3], bi[c], st[c])));
-            }
-          }
-          out[(i64)(t + u) * ow4] = pack4_bits(__float_as_uint(m[0]), __float_as_uint(m[1]), __float_as_uint(m[2]), __float_as_uint(m[3]));
-        } else {
-          *reinterpret_cast<raw4*>(p.out + ((i64)b * p.L + t + u) * Ch + col) = Elem<T>::pack(make_float4(s[0], s[1], s[2], s[3]));
-        }
+      for (int k = 0; k < W; ++k) {
+        v01 = __ffma2_rn(w01[k], h01[k], v01);
+        v23 = __ffma2_rn(w23[k], h23[k], v23);
+      }
+      const float2 L = make_float2(-1.44269504f, -1.44269504f);
+      const float2 a01 = __fmul2_rn(v01, L), a23 = __fmul2_rn(v23, L);
+      const float2 e01 = make_float2(ex2_approx(a01.x), ex2_approx(a01.y)), e23 = make_float2(ex2_approx(a23.x), ex2_approx(a23.y));
+      const float2 d01 = __ffma2_rn(e01, step01, step01), d23 = __ffma2_rn(e23, step23, step23);   // (1 + e) step
+      const float2 p01 = __fmul2_rn(v01, make_float2(rcp_approx(d01.x), rcp_approx(d01.y))), p23 = __fmul2_rn(v23, make_float2(rcp_approx(d23.x), rcp_approx(d23.y)));
+      if (CODES) {
+        float2 q01, q23;
+        asm("min.xorsign.abs.f32 %0, %1, %2;" : "=f"(q01.x) : "f"(p01.x), "f"(127.0f));
+        asm("min.xorsign.abs.f32 %0, %1, %2;" : "=f"(q01.y) : "f"(p01.y), "f"(127.0f));
+        asm("min.xorsign.abs.f32 %0, %1, %2;" : "=f"(q23.x) : "f"(p23.x), "f"(127.0f));
+        asm("min.xorsign.abs.f32 %0, %1, %2;" : "=f"(q23.y) : "f"(p23.y), "f"(127.0f));
+        const float2 mg = make_float2(kMagicOut, kMagicOut), mn = make_float2(-kMagicOut, -kMagicOut), neg = make_float2(-1.f, -1.f);
+        const float2 m01 = __fadd2_rn(q01, mg), m23 = __fadd2_rn(q23, mg);
+        const float2 f01 = __ffma2_rn(__fadd2_rn(m01, mn), neg, q01), f23 = __ffma2_rn(__fadd2_rn(m23, mn), neg, q23);   // from the integer (exact)
+        // (a NaN among the bounds: not below)
+        const bool far = fabsf(f01.x) <= least[0] && fabsf(f01.y) <= least[1] && fabsf(f23.x) <= least[2] && fabsf(f23.y) <= least[3];
+        if (!far) near |= 1u << u;
+        if (WHOLE || t + u < live) out[(i64)u * ow4] = pack4_bits(__float_as_uint(m01.x), __float_as_uint(m01.y), __float_as_uint(m23.x), __float_as_uint(m23.y));
+      } else if (WHOLE || t + u < live) {
+        *reinterpret_cast<raw4*>(p.out + ((i64)b * p.L + t + u) * Ch + col) = Elem<T>::pack(make_float4(p01.x, p01.y, p23.x, p23.y));
       }
     }
 #pragma unroll
-    for (int k = 0; k < W - 1; ++k) h[k] = h[CROWS + k];
-  }
-  for (int t = max(t0, live); t < t1; ++t) {
-    if (CODES) out[(i64)t * ow4] = 0u;
+    for (int k = 0; k < W - 1; ++k) past[k] = raw[CROWS - (W - 1) + k];
+    src += CROWS * p.stok;
+    if (CODES) {
+      out += (i64)CROWS * ow4;
+      if (!usable) near = (1u << CROWS) - 1u;
+#pragma unroll 1
+      for (; near; near &= near - 1) {
+        const int at = t + __ffs(near) - 1;
+        if (at >= live) break;
+        const int k = atomicAdd(&queue.count, 1);
+        if (k < kQueue) queue.item[k] = (uint32_t)(at - t0) << 8 | threadIdx.x;
+        else   // (no room: at once)
+          for (int c = 0; c < 4; ++c) code_exact<T, W>(p, b, at, col + c, slot, pos);
+      }
+    }
+  };
+  int t = t0;
+#pragma unroll 1
+  for (; t + CROWS <= live; t += CROWS) eight(std::true_type{}, t);
+  if (t < live) eight(std::false_type{}, t);
+  // (`out` stands behind the last eight tokens that were begun)
+  const int begun = t0 + (max(live - t0, 0) + CROWS - 1) / CROWS * CROWS;
+  for (t = max(t0, live); t < t1 && active; ++t) {
+    if (CODES) out[(i64)(t - begun) * ow4] = 0u;
     else *reinterpret_cast<raw4*>(p.out + ((i64)b * p.L + t) * Ch + col) = Elem<T>::pack(make_float4(0.f, 0.f, 0.f, 0.f));
+  }
+  if (CODES) {
+    __syncthreads();   // (single codes go over the words)
+    const int n = 4 * min(queue.count, kQueue);
+    for (int k = threadIdx.x; k < n; k += CT) {
+      const uint32_t item = queue.item[k >> 2];
+      code_exact<T, W>(p, b, t0 + (int)(item >> 8), 4 * (cblock * CT + (int)(item & 255u)) + (k & 3), slot, pos);
+    }
+    if (ring && slab == 0) __syncthreads();   // (what the ring held before the call has been read)
+  }
+  // the last W tokens stay in the ring
+  if (ring && slab == 0 && active) {
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+      t = len - 1 - k;
+      if (t >= 0) *reinterpret_cast<raw4*>(ring + (i64)(((uint32_t)pos + t) % W) * Ch) = load4<T, ALIGNED>(p.xBC + b * p.sb + t * p.stok + col);
+    }
   }
 }
 
@@ -215,12 +318,13 @@ __device__ __forceinline__ void dt_block(const ConvParams<T>& p, int b, int slab
 }
 
 template <typename T, int W, bool CODES, bool ALIGNED>
-__global__ void __launch_bounds__(CT) conv_kernel(const __grid_constant__ ConvParams<T> p) {
+__global__ void __launch_bounds__(CT, sizeof(T) == 4 ? 4 : 5) conv_kernel(const __grid_constant__ ConvParams<T> p) {
   pdl_launch_dependents();
   pdl_wait();
   const int nx = p.cblocks + (p.dt ? 1 : 0), cblock = blockIdx.x % nx, at = blockIdx.x / nx;
   const int b = at / p.nslab, slab = at % p.nslab;
-  if (cblock < p.cblocks) conv_block<T, W, CODES, ALIGNED>(p, b, slab, cblock);
+  __shared__ Queue queue;
+  if (cblock < p.cblocks) conv_block<T, W, CODES, ALIGNED>(p, b, slab, cblock, queue);
   else dt_block(p, b, slab);
 }
 

@@ -201,7 +201,7 @@ __device__ __forceinline__ float warp_max(float v) {   // of numbers >= 0; a NaN
 
 // A warp has NCH chunks of 128 columns, one after the other.
 template <typename T, typename Z, int NCH>
-__global__ void __launch_bounds__(NCH == 5 ? 416 : 512, NCH == 8 ? 1 : 2) norm_kernel(const __grid_constant__ NormParams<T, Z> p) {
+__global__ void __launch_bounds__(512, NCH == 8 ? 1 : 2) norm_kernel(const __grid_constant__ NormParams<T, Z> p) {
   __shared__ struct {
     float part[2][kMaxWarps];
     float csum[kMaxChunks], cmax[kMaxChunks];   // of chunks, where the row has several groups
