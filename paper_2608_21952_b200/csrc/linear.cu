@@ -38,12 +38,79 @@ __device__ __forceinline__ float activate(float v, int act) {
   return v;
 }
 
-// tile -> (row block, column block): eight row blocks at a time, so that the tiles in flight share rows of x and of w in L2
+// tile -> (row block, column block): GROUP row blocks at a time, so that the tiles in flight share rows of x and of w in L2
+template <int GROUP>
 __device__ __forceinline__ void tile_of(int tile, int mtiles, int ntiles, int* m, int* n) {
-  const int per = 8 * ntiles, group = tile / per, rest = tile % per;
-  const int rows = min(8, mtiles - group * 8);
-  *m = group * 8 + rest % rows;
+  const int per = GROUP * ntiles, group = tile / per, rest = tile % per;
+  const int rows = min(GROUP, mtiles - group * GROUP);
+  *m = group * GROUP + rest % rows;
   *n = rest / rows;
+}
+
+// A quarter's 32 rows (lanes) of an accumulator of BN columns: t is this lane's row, n0 the tile's first column, cw and cb the
+// columns' step sizes and biases; `drained` is called once the last column has been read.
+template <typename T, int BN, typename F>
+__device__ __forceinline__ void epilogue(const LinearParams& p, uint32_t tmem, int t, int n0, const float* cw, const float* cb, F drained) {
+  const float sr = t < p.T ? (p.s_row ? p.s_row[t] : 1.0f) : 0.f;
+#pragma unroll 1
+  for (int c0 = 0; c0 < BN; c0 += 32) {
+    int v[32];
+    __syncwarp();   // (lanes beyond the last row skip the stores)
+    tmem_ld32(tmem + c0, v);
+    tmem_ld_wait();
+    if (c0 + 32 == BN) {
+      tc_fence_before();
+      drained();
+    }
+    const int o0 = n0 + c0;
+    if (t >= p.T || o0 >= p.O) continue;
+    T* dst = static_cast<T*>(p.out) + t * p.out_stride + o0;
+    const T* res = p.residual ? static_cast<const T*>(p.residual) + t * p.res_stride + o0 : nullptr;
+    const bool whole = o0 + 32 <= p.O;
+    if (whole && p.vec_out && (!res || p.vec_res)) {
+      constexpr int V = 16 / sizeof(T), NV = 32 / V;   // elements of a 16-byte vector, vectors of 32 elements
+      uint4 raw[NV];
+      if (res) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) raw[i] = reinterpret_cast<const uint4*>(res)[i];
+      }
+#pragma unroll
+      for (int c = 0; c < 32; c += 8) {
+        float f[8];
+        const float4 w0 = *reinterpret_cast<const float4*>(cw + c0 + c), w1 = *reinterpret_cast<const float4*>(cw + c0 + c + 4);
+        const float4 b0 = *reinterpret_cast<const float4*>(cb + c0 + c), b1 = *reinterpret_cast<const float4*>(cb + c0 + c + 4);
+        const float ws[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w}, bs[8] = {b0.x, b0.y, b0.z, b0.w, b1.x, b1.y, b1.z, b1.w};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = activate(fmaf((float)v[c + e] * sr, ws[e], bs[e]), p.act);
+        uint4* const at = raw + c / V;
+        if (res) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) f[e] += Elem<T>::get(reinterpret_cast<const T*>(at)[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) reinterpret_cast<T*>(at)[e] = Elem<T>::put(f[e]);
+#pragma unroll
+        for (int i = 0; i < 8 / V; ++i) reinterpret_cast<uint4*>(dst + c)[i] = at[i];
+      }
+    } else {
+#pragma unroll
+      for (int c = 0; c < 32; ++c)
+        if (o0 + c < p.O) {
+          float f = activate(fmaf((float)v[c] * sr, cw[c0 + c], cb[c0 + c]), p.act);
+          if (res) f += Elem<T>::get(res[c]);
+          dst[c] = Elem<T>::put(f);
+        }
+    }
+  }
+}
+// step sizes and biases of a tile's columns into shared memory, by the 128 epilogue threads
+template <int BN>
+__device__ __forceinline__ void columns(const LinearParams& p, int n0, float* cw, float* cb, int et) {
+  for (int c = et; c < BN; c += 128) {
+    const int o = n0 + c;
+    cw[c] = o < p.O ? p.s_w[o] : 0.f;
+    cb[c] = o < p.O && p.bias ? p.bias[o] : 0.f;
+  }
 }
 
 template <typename T, int BN>
@@ -84,7 +151,7 @@ __global__ void __launch_bounds__(LT, 1) linear_kernel(const __grid_constant__ C
     int it = 0;
     for (int tile = blockIdx.x; tile < ntotal; tile += gridDim.x) {
       int m, n;
-      tile_of(tile, p.mtiles, p.ntiles, &m, &n);
+      tile_of<8>(tile, p.mtiles, p.ntiles, &m, &n);
       for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
         const int s = it % S::kStages;
         if (it >= S::kStages) mbar_wait(&empty[s], (it / S::kStages - 1) & 1, p.status);
@@ -124,64 +191,14 @@ __global__ void __launch_bounds__(LT, 1) linear_kernel(const __grid_constant__ C
     for (int tile = blockIdx.x; tile < ntotal; tile += gridDim.x, ++at) {
       const int buf = at & 1;
       int m, n;
-      tile_of(tile, p.mtiles, p.ntiles, &m, &n);
+      tile_of<8>(tile, p.mtiles, p.ntiles, &m, &n);
       float* cw = cols + buf * 2 * BN;
-      float* cb = cw + BN;
-      for (int c = et; c < BN; c += 128) {
-        const int o = n * BN + c;
-        cw[c] = o < p.O ? p.s_w[o] : 0.f;
-        cb[c] = o < p.O && p.bias ? p.bias[o] : 0.f;
-      }
-      const int t = m * BM + quarter * 32 + lane;
-      const float sr = t < p.T ? (p.s_row ? p.s_row[t] : 1.0f) : 0.f;
+      columns<BN>(p, n * BN, cw, cw + BN, et);
       named_bar_sync(1, 128);   // (and nobody is still reading the columns of the tile before the last)
       mbar_wait(&acc_full[buf], (at >> 1) & 1, p.status);
       tc_fence_after();
-      for (int c0 = 0; c0 < BN; c0 += 32) {
-        int v[32];
-        tmem_ld32(tmem + ((uint32_t)(quarter * 32) << 16) + buf * BN + c0, v);
-        tmem_ld_wait();
-        if (c0 + 32 == BN) {
-          tc_fence_before();
-          mbar_arrive(&acc_empty[buf]);
-        }
-        const int o0 = n * BN + c0;
-        if (t >= p.T || o0 >= p.O) continue;
-        T* dst = static_cast<T*>(p.out) + t * p.out_stride + o0;
-        const T* res = p.residual ? static_cast<const T*>(p.residual) + t * p.res_stride + o0 : nullptr;
-        const bool whole = o0 + 32 <= p.O;
-        if (whole && p.vec_out && (!res || p.vec_res)) {
-#pragma unroll
-          for (int c = 0; c < 32; c += 8) {
-            constexpr int V = 16 / sizeof(T), NV = 8 / V;   // elements of a 16-byte vector, vectors of eight elements
-            float f[8];
-            const float4 w0 = *reinterpret_cast<const float4*>(cw + c0 + c), w1 = *reinterpret_cast<const float4*>(cw + c0 + c + 4);
-            const float4 b0 = *reinterpret_cast<const float4*>(cb + c0 + c), b1 = *reinterpret_cast<const float4*>(cb + c0 + c + 4);
-            const float ws[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w}, bs[8] = {b0.x, b0.y, b0.z, b0.w, b1.x, b1.y, b1.z, b1.w};
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = activate(fmaf((float)v[c + e] * sr, ws[e], bs[e]), p.act);
-            uint4 raw[NV];
-            if (res) {
-#pragma unroll
-              for (int i = 0; i < NV; ++i) raw[i] = reinterpret_cast<const uint4*>(res + c)[i];
-#pragma unroll
-              for (int e = 0; e < 8; ++e) f[e] += Elem<T>::get(reinterpret_cast<const T*>(raw)[e]);
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) reinterpret_cast<T*>(raw)[e] = Elem<T>::put(f[e]);
-#pragma unroll
-            for (int i = 0; i < NV; ++i) reinterpret_cast<uint4*>(dst + c)[i] = raw[i];
-          }
-        } else {
-#pragma unroll
-          for (int c = 0; c < 32; ++c)
-            if (o0 + c < p.O) {
-              float f = activate(fmaf((float)v[c] * sr, cw[c0 + c], cb[c0 + c]), p.act);
-              if (res) f += Elem<T>::get(res[c]);
-              dst[c] = Elem<T>::put(f);
-            }
-        }
-      }
+      epilogue<T, BN>(p, tmem + ((uint32_t)(quarter * 32) << 16) + buf * BN, m * BM + quarter * 32 + lane, n * BN, cw, cw + BN,
+                      [&] { mbar_arrive(&acc_empty[buf]); });
     }
   }
   tc_fence_before();
@@ -190,6 +207,151 @@ __global__ void __launch_bounds__(LT, 1) linear_kernel(const __grid_constant__ C
   if (warp == 2) {
     tc_fence_after();
     tmem_dealloc(tmem, 2 * BN);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ pairs of SMs
+// The same on tiles of 256 x 256 for two SMs (cta_group::2): each CTA of a pair loads 128 rows of x and 128 of w, the first one issues the
+// MMAs, and each drains its 128 rows of the accumulator.  32 KB per CTA and 128 of K where a lone tile of 128 x 256 takes 48: what the
+// operands' way from L2 bounds (16384 x 2560 x 5120: 238 us with lone tiles, 155 with pairs).
+constexpr int PBN = 256;
+struct PairLayout {
+  static constexpr int kStages = 6;
+  static constexpr uint32_t kA = BM * BK, kStage = 2 * kA;
+  static constexpr uint32_t kBars = kStages * kStage;
+  static constexpr uint32_t kCols = kBars + 256;
+  static constexpr uint32_t kBytes = kCols + 2 * 2 * PBN * 4;
+  static constexpr uint32_t kAlloc = kBytes + 1024;
+};
+
+__device__ __forceinline__ uint32_t in_first(const void* p) {   // the same place in the pair's first CTA
+  uint32_t a;
+  asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(a) : "r"(smem_u32(p)));
+  return a;
+}
+__device__ __forceinline__ void pair_load(void* dst, const CUtensorMap* tm, uint32_t bar, int x, int y) {   // bar: of the first CTA
+  asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+               ::"r"(smem_u32(dst)), "l"(tm), "r"(bar), "r"(x), "r"(y)
+               : "memory");
+}
+__device__ __forceinline__ void pair_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+               : "memory");
+}
+__device__ __forceinline__ void pair_commit(uint64_t* bar) {   // arrives at this place in both CTAs
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+               ::"r"(smem_u32(bar)), "h"((uint16_t)3)
+               : "memory");
+}
+__device__ __forceinline__ void arrive_at(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+template <typename T>
+__global__ void __launch_bounds__(LT, 1) linear_pair_kernel(const __grid_constant__ CUtensorMap tx, const __grid_constant__ CUtensorMap tw,
+                                                            const __grid_constant__ LinearParams p) {
+  typedef PairLayout S;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::kBars);   // (waited for in the first CTA; the second's loads arrive there too)
+  uint64_t* empty = full + S::kStages;
+  uint64_t* acc_full = empty + S::kStages;
+  uint64_t* acc_empty = acc_full + 2;                              // (waited for in the first CTA)
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
+  float* cols = reinterpret_cast<float*>(smem + S::kCols);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rank = blockIdx.x & 1, pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
+  if (tid == 0) {
+    for (int i = 0; i < S::kStages; ++i) {
+      mbar_init(&full[i], 1);
+      mbar_init(&empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&acc_full[i], 1);
+      mbar_init(&acc_empty[i], 8);   // the epilogue warps of both
+    }
+    fence_mbar_init();
+    tma_prefetch_desc(&tx);
+    tma_prefetch_desc(&tw);
+  }
+  if (warp == 2) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();   // (the other CTA's barriers are there)
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  pdl_launch_dependents();
+  pdl_wait();
+  const int ntotal = p.mtiles * p.ntiles;
+  if (warp == 0) {
+    int it = 0;
+    for (int tile = pair; tile < ntotal; tile += npairs) {
+      int m, n;
+      tile_of<4>(tile, p.mtiles, p.ntiles, &m, &n);
+      for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
+        const int s = it % S::kStages;
+        if (it >= S::kStages) mbar_wait(&empty[s], (it / S::kStages - 1) & 1, p.status);
+        if (elect_one()) {
+          if (rank == 0) mbar_expect_tx(&full[s], 2 * S::kStage);
+          const uint32_t bar = in_first(&full[s]);
+          pair_load(smem + s * S::kStage, &tx, bar, kb * BK, m * 256 + rank * 128);
+          pair_load(smem + s * S::kStage + S::kA, &tw, bar, kb * BK, n * PBN + rank * 128);
+        }
+        __syncwarp();
+      }
+    }
+    // (the last commits have arrived here before this CTA ends)
+    for (int k = it > S::kStages ? it - S::kStages : 0; k < it; ++k) mbar_wait(&empty[k % S::kStages], (k / S::kStages) & 1, p.status);
+  } else if (warp == 1 && rank == 0) {
+    constexpr uint32_t idesc = idesc_s8(256, PBN, 0, 0);
+    int it = 0, at = 0;
+    for (int tile = pair; tile < ntotal; tile += npairs, ++at) {
+      const int buf = at & 1;
+      if (at >= 2) mbar_wait(&acc_empty[buf], ((at >> 1) - 1) & 1, p.status);
+      tc_fence_after();
+      for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
+        const int s = it % S::kStages;
+        mbar_wait(&full[s], (it / S::kStages) & 1, p.status);
+        tc_fence_after();
+        if (elect_one()) {
+          const uint64_t da = tile_desc(smem_u32(smem + s * S::kStage), 128), db = tile_desc(smem_u32(smem + s * S::kStage + S::kA), 128);
+#pragma unroll
+          for (int k = 0; k < BK / 32; ++k) pair_mma(tmem + buf * PBN, da + 2 * k, db + 2 * k, idesc, kb > 0 || k > 0);
+          pair_commit(&empty[s]);
+          if (kb + 1 == p.kblocks) pair_commit(&acc_full[buf]);
+        }
+        __syncwarp();
+      }
+    }
+  } else if (warp >= 4) {
+    const int quarter = warp & 3, et = tid - 128;
+    int at = 0;
+    for (int tile = pair; tile < ntotal; tile += npairs, ++at) {
+      const int buf = at & 1;
+      int m, n;
+      tile_of<4>(tile, p.mtiles, p.ntiles, &m, &n);
+      float* cw = cols + buf * 2 * PBN;
+      columns<PBN>(p, n * PBN, cw, cw + PBN, et);
+      named_bar_sync(1, 128);
+      mbar_wait(&acc_full[buf], (at >> 1) & 1, p.status);
+      tc_fence_after();
+      epilogue<T, PBN>(p, tmem + ((uint32_t)(quarter * 32) << 16) + buf * PBN, m * 256 + rank * 128 + quarter * 32 + lane, n * PBN, cw, cw + PBN, [&] {
+        __syncwarp();
+        if (lane == 0) arrive_at(in_first(&acc_empty[buf]));
+      });
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  drain_after_timeout(p.status);
+  cluster_sync();   // (nothing of the other CTA's is on its way here any more: its commits and arrivals have been waited for or precede this)
+  if (warp == 2) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
   }
 }
 
@@ -221,8 +383,24 @@ ssdi8_status_t launch_linear(const ssdi8_linear_args_t& a, int dtype, cudaStream
     if (sms <= 0) return SSDI8_ERR_CUDA;
     return launch_configured(linear_kernel<E, BN>, dim3((unsigned)(tiles < sms ? tiles : sms)), dim3(LT), Layout<BN>::kAlloc, -1, false, st, tx, tw, p);
   };
+  auto go_pair = [&](auto t) -> ssdi8_status_t {
+    using E = decltype(t);
+    p.mtiles = (a.rows + 255) / 256;
+    p.ntiles = (a.outs + PBN - 1) / PBN;
+    const i64 tiles = (i64)p.mtiles * p.ntiles;
+    if (tiles > 0x3fffffff) return SSDI8_ERR_SHAPE;
+    CUtensorMap tx, tw;
+    const uint64_t dx[2] = {(uint64_t)a.inner, (uint64_t)a.rows}, dw[2] = {(uint64_t)a.inner, (uint64_t)a.outs}, stride[1] = {(uint64_t)a.inner};
+    const uint32_t box[2] = {BK, 128};
+    if (!encode_tensor_map(&tx, a.xq, 1, 2, dx, stride, box, 128) || !encode_tensor_map(&tw, a.wq, 1, 2, dw, stride, box, 128)) return SSDI8_ERR_CUDA;
+    const i64 pairs = sm_count() / 2;
+    if (pairs <= 0) return SSDI8_ERR_CUDA;
+    return launch_any(linear_pair_kernel<E>, dim3((unsigned)(2 * (tiles < pairs ? tiles : pairs))), 2, dim3(LT), PairLayout::kAlloc, PairLayout::kAlloc, -1,
+                      false, st, tx, tw, p);
+  };
   // Tiles of 256 columns where they fill the SMs, else of 128.
   auto pick = [&](auto t) -> ssdi8_status_t {
+    if ((i64)((a.rows + 255) / 256) * ((a.outs + 255) / 256) >= sm_count() / 2) return go_pair(t);
     const i64 wide = (i64)((a.rows + BM - 1) / BM) * ((a.outs + 255) / 256);
     return wide >= sm_count() ? go(std::integral_constant<int, 256>{}, t) : go(std::integral_constant<int, 128>{}, t);
   };
