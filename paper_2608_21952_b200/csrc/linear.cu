@@ -1,6 +1,6 @@
 // Int8 projection: out = act(s_row s_w (xq wq^T) + bias) + residual, on tcgen05.mma.kind::i8 with int32 accumulators in tensor memory
 // (the integer sums are exact) and everything behind them in the epilogue.  Persistent: a loading warp (TMA, both operands K-major in
-// rows of 128 bytes with the 128-byte swizzle), an issuing warp, and four epilogue warps that drain one accumulator while the
+// rows of 128 bytes with the 128-byte swizzle), an issuing warp, and epilogue warps that drain one accumulator while the
 // next tile's is formed in the other.
 #include "block.cuh"
 #include "kernels.h"
@@ -11,7 +11,7 @@ namespace {
 
 using namespace sm100;
 
-constexpr int LT = 256;      // threads: loader, issuer, tensor-memory allocator, one idle, four epilogue warps
+constexpr int LT = 256;      // threads: loader, issuer, tensor-memory allocator, one idle, four epilogue warps (pairs of SMs: eight)
 constexpr int BM = 128, BK = 128;
 
 struct LinearParams {
@@ -20,15 +20,16 @@ struct LinearParams {
   void* out; i64 out_stride;
   int32_t* status;
   int T, O, kblocks, mtiles, ntiles, act, vec_out, vec_res;
+  int bn, xrows, stages;   // lone tiles: columns, rows of x in a load, stages of the ring
 };
 
-template <int BN>
+// Shared memory of a lone tile's CTA: a ring of stages, 128 rows of x (as many loaded as there are) and bn rows of w each.
 struct Layout {
-  static constexpr int kStages = BN == 256 ? 4 : 6;
-  static constexpr uint32_t kA = BM * BK, kStage = kA + BN * BK;
-  static constexpr uint32_t kBars = kStages * kStage;
+  static constexpr int kMaxBN = 256, kMaxStages = 10;
+  static constexpr uint32_t kA = BM * BK, kRing = 196608;
+  static constexpr uint32_t kBars = kRing;
   static constexpr uint32_t kCols = kBars + 256;                 // s_w and bias of two tiles' columns
-  static constexpr uint32_t kBytes = kCols + 2 * 2 * BN * 4;
+  static constexpr uint32_t kBytes = kCols + 2 * 2 * kMaxBN * 4;
   static constexpr uint32_t kAlloc = kBytes + 1024;              // (the tiles start on 1024 bytes)
 };
 
@@ -47,26 +48,27 @@ __device__ __forceinline__ void tile_of(int tile, int mtiles, int ntiles, int* m
   *n = rest / rows;
 }
 
-// A quarter's 32 rows (lanes) of an accumulator of BN columns: t is this lane's row, n0 the tile's first column, cw and cb the
+// A quarter's 32 rows (lanes) of `ncols` columns of an accumulator: t is this lane's row, n0 the first column, cw and cb the
 // columns' step sizes and biases; `drained` is called once the last column has been read.
-template <typename T, int BN, typename F>
-__device__ __forceinline__ void epilogue(const LinearParams& p, uint32_t tmem, int t, int n0, const float* cw, const float* cb, F drained) {
+template <typename T, typename F>
+__device__ __forceinline__ void epilogue(const LinearParams& p, uint32_t tmem, int t, int n0, int ncols, const float* cw, const float* cb, F drained) {
+  const int end = min(n0 + ncols, p.O);
   const float sr = t < p.T ? (p.s_row ? p.s_row[t] : 1.0f) : 0.f;
 #pragma unroll 1
-  for (int c0 = 0; c0 < BN; c0 += 32) {
+  for (int c0 = 0; c0 < ncols; c0 += 32) {
     int v[32];
     __syncwarp();   // (lanes beyond the last row skip the stores)
     tmem_ld32(tmem + c0, v);
     tmem_ld_wait();
-    if (c0 + 32 == BN) {
+    if (c0 + 32 >= ncols) {
       tc_fence_before();
       drained();
     }
     const int o0 = n0 + c0;
-    if (t >= p.T || o0 >= p.O) continue;
+    if (t >= p.T || o0 >= end) continue;
     T* dst = static_cast<T*>(p.out) + t * p.out_stride + o0;
     const T* res = p.residual ? static_cast<const T*>(p.residual) + t * p.res_stride + o0 : nullptr;
-    const bool whole = o0 + 32 <= p.O;
+    const bool whole = o0 + 32 <= end;
     if (whole && p.vec_out && (!res || p.vec_res)) {
       constexpr int V = 16 / sizeof(T), NV = 32 / V;   // elements of a 16-byte vector, vectors of 32 elements
       uint4 raw[NV];
@@ -95,7 +97,7 @@ __device__ __forceinline__ void epilogue(const LinearParams& p, uint32_t tmem, i
     } else {
 #pragma unroll
       for (int c = 0; c < 32; ++c)
-        if (o0 + c < p.O) {
+        if (o0 + c < end) {
           float f = activate(fmaf((float)v[c] * sr, cw[c0 + c], cb[c0 + c]), p.act);
           if (res) f += Elem<T>::get(res[c]);
           dst[c] = Elem<T>::put(f);
@@ -103,31 +105,30 @@ __device__ __forceinline__ void epilogue(const LinearParams& p, uint32_t tmem, i
     }
   }
 }
-// step sizes and biases of a tile's columns into shared memory, by the 128 epilogue threads
-template <int BN>
-__device__ __forceinline__ void columns(const LinearParams& p, int n0, float* cw, float* cb, int et) {
-  for (int c = et; c < BN; c += 128) {
+// step sizes and biases of a tile's columns into shared memory, by the epilogue threads
+__device__ __forceinline__ void columns(const LinearParams& p, int n0, int ncols, float* cw, float* cb, int et, int threads) {
+  for (int c = et; c < ncols; c += threads) {
     const int o = n0 + c;
     cw[c] = o < p.O ? p.s_w[o] : 0.f;
     cb[c] = o < p.O && p.bias ? p.bias[o] : 0.f;
   }
 }
 
-template <typename T, int BN>
+template <typename T>
 __global__ void __launch_bounds__(LT, 1) linear_kernel(const __grid_constant__ CUtensorMap tx, const __grid_constant__ CUtensorMap tw,
                                                        const __grid_constant__ LinearParams p) {
-  typedef Layout<BN> S;
+  typedef Layout S;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::kBars);
-  uint64_t* empty = full + S::kStages;
-  uint64_t* acc_full = empty + S::kStages;
+  uint64_t* empty = full + S::kMaxStages;
+  uint64_t* acc_full = empty + S::kMaxStages;
   uint64_t* acc_empty = acc_full + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
   float* cols = reinterpret_cast<float*>(smem + S::kCols);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
-    for (int i = 0; i < S::kStages; ++i) {
+    for (int i = 0; i < S::kMaxStages; ++i) {
       mbar_init(&full[i], 1);
       mbar_init(&empty[i], 1);
     }
@@ -139,7 +140,7 @@ __global__ void __launch_bounds__(LT, 1) linear_kernel(const __grid_constant__ C
     tma_prefetch_desc(&tx);
     tma_prefetch_desc(&tw);
   }
-  if (warp == 2) tmem_alloc(tmem_slot, 2 * BN);
+  if (warp == 2) tmem_alloc(tmem_slot, 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -147,58 +148,59 @@ __global__ void __launch_bounds__(LT, 1) linear_kernel(const __grid_constant__ C
   pdl_launch_dependents();
   pdl_wait();
   const int ntotal = p.mtiles * p.ntiles;
+  const uint32_t stage = S::kA + p.bn * BK;   // (bn % 16 = 0: the operands start on 1024 bytes)
   if (warp == 0) {
-    int it = 0;
+    int s = 0, round = 0;
     for (int tile = blockIdx.x; tile < ntotal; tile += gridDim.x) {
       int m, n;
       tile_of<8>(tile, p.mtiles, p.ntiles, &m, &n);
-      for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
-        const int s = it % S::kStages;
-        if (it >= S::kStages) mbar_wait(&empty[s], (it / S::kStages - 1) & 1, p.status);
+      for (int kb = 0; kb < p.kblocks; ++kb) {
+        if (round > 0) mbar_wait(&empty[s], (round - 1) & 1, p.status);
         if (elect_one()) {
-          mbar_expect_tx(&full[s], S::kStage);
-          tma_load_2d(smem + s * S::kStage, &tx, &full[s], kb * BK, m * BM);
-          tma_load_2d(smem + s * S::kStage + S::kA, &tw, &full[s], kb * BK, n * BN);
+          mbar_expect_tx(&full[s], (uint32_t)(p.xrows + p.bn) * BK);
+          tma_load_2d(smem + s * stage, &tx, &full[s], kb * BK, m * BM);
+          tma_load_2d(smem + s * stage + S::kA, &tw, &full[s], kb * BK, n * p.bn);
         }
         __syncwarp();
+        if (++s == p.stages) { s = 0; ++round; }
       }
     }
     // the loads in flight land before the block ends: the issuer has waited for each of them
   } else if (warp == 1) {
-    constexpr uint32_t idesc = idesc_s8(BM, BN, 0, 0);
-    int it = 0, at = 0;
+    const uint32_t idesc = idesc_s8(BM, p.bn, 0, 0);
+    int s = 0, round = 0, at = 0;
     for (int tile = blockIdx.x; tile < ntotal; tile += gridDim.x, ++at) {
       const int buf = at & 1;
       if (at >= 2) mbar_wait(&acc_empty[buf], ((at >> 1) - 1) & 1, p.status);
       tc_fence_after();
-      for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
-        const int s = it % S::kStages;
-        mbar_wait(&full[s], (it / S::kStages) & 1, p.status);
+      for (int kb = 0; kb < p.kblocks; ++kb) {
+        mbar_wait(&full[s], round & 1, p.status);
         tc_fence_after();
         if (elect_one()) {
-          const uint64_t da = tile_desc(smem_u32(smem + s * S::kStage), 128), db = tile_desc(smem_u32(smem + s * S::kStage + S::kA), 128);
+          const uint64_t da = tile_desc(smem_u32(smem + s * stage), 128), db = tile_desc(smem_u32(smem + s * stage + S::kA), 128);
 #pragma unroll
-          for (int k = 0; k < BK / 32; ++k) mma_s8_ss(tmem + buf * BN, da + 2 * k, db + 2 * k, idesc, kb > 0 || k > 0);
+          for (int k = 0; k < BK / 32; ++k) mma_s8_ss(tmem + buf * S::kMaxBN, da + 2 * k, db + 2 * k, idesc, kb > 0 || k > 0);
           mma_commit(&empty[s]);
           if (kb + 1 == p.kblocks) mma_commit(&acc_full[buf]);
         }
         __syncwarp();
+        if (++s == p.stages) { s = 0; ++round; }
       }
     }
   } else if (warp >= 4) {
-    const int quarter = warp & 3, et = tid - 128;
+    const int quarter = warp & 3;
     int at = 0;
     for (int tile = blockIdx.x; tile < ntotal; tile += gridDim.x, ++at) {
       const int buf = at & 1;
       int m, n;
       tile_of<8>(tile, p.mtiles, p.ntiles, &m, &n);
-      float* cw = cols + buf * 2 * BN;
-      columns<BN>(p, n * BN, cw, cw + BN, et);
+      float* cw = cols + buf * 2 * S::kMaxBN;
+      columns(p, n * p.bn, p.bn, cw, cw + S::kMaxBN, tid - 128, 128);
       named_bar_sync(1, 128);   // (and nobody is still reading the columns of the tile before the last)
       mbar_wait(&acc_full[buf], (at >> 1) & 1, p.status);
       tc_fence_after();
-      epilogue<T, BN>(p, tmem + ((uint32_t)(quarter * 32) << 16) + buf * BN, m * BM + quarter * 32 + lane, n * BN, cw, cw + BN,
-                      [&] { mbar_arrive(&acc_empty[buf]); });
+      epilogue<T>(p, tmem + ((uint32_t)(quarter * 32) << 16) + buf * S::kMaxBN, m * BM + quarter * 32 + lane, n * p.bn, p.bn, cw, cw + S::kMaxBN,
+                  [&] { mbar_arrive(&acc_empty[buf]); });
     }
   }
   tc_fence_before();
@@ -206,7 +208,7 @@ __global__ void __launch_bounds__(LT, 1) linear_kernel(const __grid_constant__ C
   drain_after_timeout(p.status);
   if (warp == 2) {
     tc_fence_after();
-    tmem_dealloc(tmem, 2 * BN);
+    tmem_dealloc(tmem, 512);
   }
 }
 
@@ -214,7 +216,7 @@ __global__ void __launch_bounds__(LT, 1) linear_kernel(const __grid_constant__ C
 // The same on tiles of 256 x 256 for two SMs (cta_group::2): each CTA of a pair loads 128 rows of x and 128 of w, the first one issues the
 // MMAs, and each drains its 128 rows of the accumulator.  32 KB per CTA and 128 of K where a lone tile of 128 x 256 takes 48: what the
 // operands' way from L2 bounds (16384 x 2560 x 5120: 238 us with lone tiles, 155 with pairs).
-constexpr int PBN = 256;
+constexpr int PBN = 256, PT = 384;
 struct PairLayout {
   static constexpr int kStages = 6;
   static constexpr uint32_t kA = BM * BK, kStage = 2 * kA;
@@ -249,7 +251,7 @@ __device__ __forceinline__ void arrive_at(uint32_t bar) {
 }
 
 template <typename T>
-__global__ void __launch_bounds__(LT, 1) linear_pair_kernel(const __grid_constant__ CUtensorMap tx, const __grid_constant__ CUtensorMap tw,
+__global__ void __launch_bounds__(PT, 1) linear_pair_kernel(const __grid_constant__ CUtensorMap tx, const __grid_constant__ CUtensorMap tw,
                                                             const __grid_constant__ LinearParams p) {
   typedef PairLayout S;
   extern __shared__ uint8_t smem_raw[];
@@ -269,7 +271,7 @@ __global__ void __launch_bounds__(LT, 1) linear_pair_kernel(const __grid_constan
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&acc_full[i], 1);
-      mbar_init(&acc_empty[i], 8);   // the epilogue warps of both
+      mbar_init(&acc_empty[i], 16);   // the epilogue warps of both
     }
     fence_mbar_init();
     tma_prefetch_desc(&tx);
@@ -291,7 +293,7 @@ __global__ void __launch_bounds__(LT, 1) linear_pair_kernel(const __grid_constan
     int it = 0;
     for (int tile = pair; tile < ntotal; tile += npairs) {
       int m, n;
-      tile_of<4>(tile, p.mtiles, p.ntiles, &m, &n);
+      tile_of<8>(tile, p.mtiles, p.ntiles, &m, &n);
       for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
         const int s = it % S::kStages;
         if (it >= S::kStages) mbar_wait(&empty[s], (it / S::kStages - 1) & 1, p.status);
@@ -328,21 +330,22 @@ __global__ void __launch_bounds__(LT, 1) linear_pair_kernel(const __grid_constan
       }
     }
   } else if (warp >= 4) {
-    const int quarter = warp & 3, et = tid - 128;
+    const int quarter = warp & 3, half = (warp - 4) >> 2 << 7;   // eight warps: a quarter of the rows, half of the columns
     int at = 0;
     for (int tile = pair; tile < ntotal; tile += npairs, ++at) {
       const int buf = at & 1;
       int m, n;
-      tile_of<4>(tile, p.mtiles, p.ntiles, &m, &n);
+      tile_of<8>(tile, p.mtiles, p.ntiles, &m, &n);
       float* cw = cols + buf * 2 * PBN;
-      columns<PBN>(p, n * PBN, cw, cw + PBN, et);
-      named_bar_sync(1, 128);
+      columns(p, n * PBN, PBN, cw, cw + PBN, tid - 128, PT - 128);
+      named_bar_sync(1, PT - 128);
       mbar_wait(&acc_full[buf], (at >> 1) & 1, p.status);
       tc_fence_after();
-      epilogue<T, PBN>(p, tmem + ((uint32_t)(quarter * 32) << 16) + buf * PBN, m * 256 + rank * 128 + quarter * 32 + lane, n * PBN, cw, cw + PBN, [&] {
-        __syncwarp();
-        if (lane == 0) arrive_at(in_first(&acc_empty[buf]));
-      });
+      epilogue<T>(p, tmem + ((uint32_t)(quarter * 32) << 16) + buf * PBN + half, m * 256 + rank * 128 + quarter * 32 + lane, n * PBN + half, 128, cw + half,
+                  cw + PBN + half, [&] {
+                    __syncwarp();
+                    if (lane == 0) arrive_at(in_first(&acc_empty[buf]));
+                  });
     }
   }
   tc_fence_before();
@@ -368,43 +371,46 @@ ssdi8_status_t launch_linear(const ssdi8_linear_args_t& a, int dtype, cudaStream
   auto vec = [e](const void* q, i64 stride) { return reinterpret_cast<uintptr_t>(q) % 16 == 0 && stride * (i64)e % 16 == 0; };
   p.vec_out = vec(a.out, a.stride_out);
   p.vec_res = vec(a.residual, a.stride_residual);
-  auto go = [&](auto bn, auto t) -> ssdi8_status_t {
-    constexpr int BN = decltype(bn)::value;
-    using E = decltype(t);
-    p.mtiles = (a.rows + BM - 1) / BM;
-    p.ntiles = (a.outs + BN - 1) / BN;
-    const i64 tiles = (i64)p.mtiles * p.ntiles;
-    if (tiles > 0x3fffffff) return SSDI8_ERR_SHAPE;
-    CUtensorMap tx, tw;
+  const int sms = sm_count();
+  if (sms <= 0) return SSDI8_ERR_CUDA;
+  auto maps = [&](CUtensorMap* tx, uint32_t xrows, CUtensorMap* tw, uint32_t wrows) {
     const uint64_t dx[2] = {(uint64_t)a.inner, (uint64_t)a.rows}, dw[2] = {(uint64_t)a.inner, (uint64_t)a.outs}, stride[1] = {(uint64_t)a.inner};
-    const uint32_t bx[2] = {BK, BM}, bw[2] = {BK, BN};
-    if (!encode_tensor_map(&tx, a.xq, 1, 2, dx, stride, bx, 128) || !encode_tensor_map(&tw, a.wq, 1, 2, dw, stride, bw, 128)) return SSDI8_ERR_CUDA;
-    const int sms = sm_count();
-    if (sms <= 0) return SSDI8_ERR_CUDA;
-    return launch_configured(linear_kernel<E, BN>, dim3((unsigned)(tiles < sms ? tiles : sms)), dim3(LT), Layout<BN>::kAlloc, -1, false, st, tx, tw, p);
+    const uint32_t bx[2] = {BK, xrows}, bw[2] = {BK, wrows};
+    return encode_tensor_map(tx, a.xq, 1, 2, dx, stride, bx, 128) && encode_tensor_map(tw, a.wq, 1, 2, dw, stride, bw, 128);
   };
-  auto go_pair = [&](auto t) -> ssdi8_status_t {
-    using E = decltype(t);
-    p.mtiles = (a.rows + 255) / 256;
-    p.ntiles = (a.outs + PBN - 1) / PBN;
-    const i64 tiles = (i64)p.mtiles * p.ntiles;
-    if (tiles > 0x3fffffff) return SSDI8_ERR_SHAPE;
-    CUtensorMap tx, tw;
-    const uint64_t dx[2] = {(uint64_t)a.inner, (uint64_t)a.rows}, dw[2] = {(uint64_t)a.inner, (uint64_t)a.outs}, stride[1] = {(uint64_t)a.inner};
-    const uint32_t box[2] = {BK, 128};
-    if (!encode_tensor_map(&tx, a.xq, 1, 2, dx, stride, box, 128) || !encode_tensor_map(&tw, a.wq, 1, 2, dw, stride, box, 128)) return SSDI8_ERR_CUDA;
-    const i64 pairs = sm_count() / 2;
-    if (pairs <= 0) return SSDI8_ERR_CUDA;
-    return launch_any(linear_pair_kernel<E>, dim3((unsigned)(2 * (tiles < pairs ? tiles : pairs))), 2, dim3(LT), PairLayout::kAlloc, PairLayout::kAlloc, -1,
-                      false, st, tx, tw, p);
+  // Lone tiles of 128 x bn or, on pairs of SMs, of 256 x 256: what is done sooner, by waves of tiles and cycles per tile (128 of K
+  // take the tensor pipe 2 bn cycles of a lone tile, their operands 2 (rows + bn) on the SM's way from L2; a pair's 512 take about 640).
+  // bn is a multiple of 32.  64 x 10576 x 2560: tiles of 96 columns BN_FIGURES; of 128 on 83 SMs 9.9.
+  const i64 mt = (a.rows + BM - 1) / BM;
+  p.xrows = a.rows < BM ? (a.rows + 7) / 8 * 8 : BM;
+  double best = 0.0;
+  for (int bn = 32; bn <= Layout::kMaxBN; bn += 32) {
+    const i64 tiles = mt * ((a.outs + bn - 1) / bn);
+    const double cycles = (double)((tiles + sms - 1) / sms) * ((double)p.kblocks * 2.0 * (p.xrows + bn) + 1500.0 + 12.0 * bn);
+    if (best == 0.0 || cycles < best) {
+      best = cycles;
+      p.bn = bn;
+    }
+  }
+  const i64 ptiles = (i64)((a.rows + 255) / 256) * ((a.outs + PBN - 1) / PBN), pairs = sms / 2;
+  const bool pair = pairs > 0 && (double)((ptiles + pairs - 1) / pairs) * (640.0 * p.kblocks + 4500.0) < best;
+  const i64 tiles = pair ? ptiles : mt * ((a.outs + p.bn - 1) / p.bn);
+  if (tiles > 0x3fffffff) return SSDI8_ERR_SHAPE;
+  p.mtiles = pair ? (a.rows + 255) / 256 : (int)mt;
+  p.ntiles = pair ? (a.outs + PBN - 1) / PBN : (a.outs + p.bn - 1) / p.bn;
+  CUtensorMap tx, tw;
+  if (!(pair ? maps(&tx, 128, &tw, 128) : maps(&tx, p.xrows, &tw, p.bn))) return SSDI8_ERR_CUDA;
+  const int stages = (int)(Layout::kRing / (Layout::kA + p.bn * BK));
+  p.stages = stages < Layout::kMaxStages ? stages : Layout::kMaxStages;
+  auto go = [&](auto lone, auto paired) -> ssdi8_status_t {
+    if (pair)
+      return launch_any(paired, dim3((unsigned)(2 * (tiles < pairs ? tiles : pairs))), 2, dim3(PT), PairLayout::kAlloc, PairLayout::kAlloc, -1, false, st, tx,
+                        tw, p);
+    return launch_configured(lone, dim3((unsigned)(tiles < sms ? tiles : sms)), dim3(LT), Layout::kAlloc, -1, false, st, tx, tw, p);
   };
-  // Tiles of 256 columns where they fill the SMs, else of 128.
-  auto pick = [&](auto t) -> ssdi8_status_t {
-    if ((i64)((a.rows + 255) / 256) * ((a.outs + 255) / 256) >= sm_count() / 2) return go_pair(t);
-    const i64 wide = (i64)((a.rows + BM - 1) / BM) * ((a.outs + 255) / 256);
-    return wide >= sm_count() ? go(std::integral_constant<int, 256>{}, t) : go(std::integral_constant<int, 128>{}, t);
-  };
-  return dtype == 0 ? pick(float{}) : dtype == 1 ? pick(__half{}) : pick(__nv_bfloat16{});
+  return dtype == 0 ? go(linear_kernel<float>, linear_pair_kernel<float>)
+       : dtype == 1 ? go(linear_kernel<__half>, linear_pair_kernel<__half>)
+                    : go(linear_kernel<__nv_bfloat16>, linear_pair_kernel<__nv_bfloat16>);
 }
 
 }  // namespace ssdi8
