@@ -358,6 +358,165 @@ __global__ void __launch_bounds__(PT, 1) linear_pair_kernel(const __grid_constan
   }
 }
 
+// ------------------------------------------------------------------------------------------------ few rows
+// Up to 128 rows (decode): the weight is what is read, so its rows are the accumulator's 128 lanes and the tokens its columns (a weight row
+// costs the tensor pipe a tenth of what 128 mostly empty token rows cost), and K is shared out among the CTAs of a cluster, two on
+// an SM, until they are all at it.  The parts of a tile meet in shared memory (int32: in any order the same), each CTA finishing some tokens.
+constexpr int FT = 256, kFewRows = 128;
+struct FewLayout {
+  static constexpr int kMaxStages = 5;
+  static constexpr uint32_t kW = 128 * BK, kRing = 102400;       // (the accumulator's image of [128 tokens][128] goes over the ring: 65536)
+  static constexpr uint32_t kBars = kRing;
+  static constexpr uint32_t kAlloc = kBars + 256 + 1024;
+};
+struct FewParams {
+  LinearParams l;
+  int n, split;   // columns of the accumulator (tokens, to 16), CTAs of a cluster
+};
+
+__device__ __forceinline__ int4 ld_from(const int* p, int rank) {   // the same place in another CTA of the cluster
+  uint32_t a;
+  int4 v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
+  asm volatile("ld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+  return v;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(FT, 2) linear_few_kernel(const __grid_constant__ CUtensorMap tx, const __grid_constant__ CUtensorMap tw,
+                                                           const __grid_constant__ FewParams f) {
+  typedef FewLayout S;
+  const LinearParams& p = f.l;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::kBars);
+  uint64_t* empty = full + S::kMaxStages;
+  uint64_t* acc_full = empty + S::kMaxStages;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_full + 1);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int i = 0; i < S::kMaxStages; ++i) {
+      mbar_init(&full[i], 1);
+      mbar_init(&empty[i], 1);
+    }
+    mbar_init(acc_full, 1);
+    fence_mbar_init();
+    tma_prefetch_desc(&tx);
+    tma_prefetch_desc(&tw);
+  }
+  if (warp == 2) tmem_alloc(tmem_slot, 128);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  pdl_launch_dependents();
+  pdl_wait();
+  const int rank = blockIdx.x % f.split, o0 = blockIdx.x / f.split * 128;
+  const int kb0 = p.kblocks * rank / f.split, kb1 = p.kblocks * (rank + 1) / f.split;
+  const uint32_t stage = S::kW + f.n * BK;   // (n % 16 = 0: the operands start on 1024 bytes)
+  if (warp == 0) {
+    int s = 0, round = 0;
+    for (int kb = kb0; kb < kb1; ++kb) {
+      if (round > 0) mbar_wait(&empty[s], (round - 1) & 1, p.status);
+      if (elect_one()) {
+        mbar_expect_tx(&full[s], stage);
+        tma_load_2d(smem + s * stage, &tw, &full[s], kb * BK, o0);
+        tma_load_2d(smem + s * stage + S::kW, &tx, &full[s], kb * BK, 0);
+      }
+      __syncwarp();
+      if (++s == p.stages) { s = 0; ++round; }
+    }
+  } else if (warp == 1) {
+    const uint32_t idesc = idesc_s8(128, f.n, 0, 0);
+    int s = 0, round = 0;
+    for (int kb = kb0; kb < kb1; ++kb) {
+      mbar_wait(&full[s], round & 1, p.status);
+      tc_fence_after();
+      if (elect_one()) {
+        const uint64_t da = tile_desc(smem_u32(smem + s * stage), 128), db = tile_desc(smem_u32(smem + s * stage + S::kW), 128);
+#pragma unroll
+        for (int k = 0; k < BK / 32; ++k) mma_s8_ss(tmem, da + 2 * k, db + 2 * k, idesc, kb > kb0 || k > 0);
+        mma_commit(&empty[s]);
+        if (kb + 1 == kb1) mma_commit(acc_full);
+      }
+      __syncwarp();
+      if (++s == p.stages) { s = 0; ++round; }
+    }
+  }
+  int* const part = reinterpret_cast<int*>(smem);   // [n][128]
+  if (warp >= 4) {
+    // the accumulator over the ring: every load has been consumed by an MMA that is complete
+    const int quarter = warp & 3;
+    mbar_wait(acc_full, 0, p.status);
+    tc_fence_after();
+    for (int c0 = 0; c0 < f.n; c0 += 16) {
+      int v[16];
+      tmem_ld8(tmem + ((uint32_t)(quarter * 32) << 16) + c0, reinterpret_cast<int(&)[8]>(v[0]));
+      tmem_ld8(tmem + ((uint32_t)(quarter * 32) << 16) + c0 + 8, reinterpret_cast<int(&)[8]>(v[8]));
+      tmem_ld_wait();
+#pragma unroll
+      for (int c = 0; c < 16; ++c) part[(c0 + c) * 128 + quarter * 32 + lane] = v[c];
+    }
+    tc_fence_before();
+  }
+  __syncthreads();
+  if (f.split > 1) cluster_sync();
+  {
+    // a warp per token, four outputs per lane; the parts of four tokens on their way at a time
+    const int o = o0 + 4 * lane, no = min(p.O - o, 4);
+    float sw[4], bias[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      sw[e] = e < no ? p.s_w[o + e] : 0.f;
+      bias[e] = e < no && p.bias ? p.bias[o + e] : 0.f;
+    }
+    const int step = f.split * (FT / 32);
+    for (int t0 = rank + f.split * warp; t0 < p.T; t0 += 4 * step) {
+      int4 acc[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) acc[u] = make_int4(0, 0, 0, 0);
+      for (int r = 0; r < f.split; ++r)
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (t0 + u * step < p.T) {
+            const int* const at = part + (t0 + u * step) * 128 + 4 * lane;
+            const int4 v = f.split == 1 ? *reinterpret_cast<const int4*>(at) : ld_from(at, r);
+            acc[u] = make_int4(acc[u].x + v.x, acc[u].y + v.y, acc[u].z + v.z, acc[u].w + v.w);
+          }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int t = t0 + u * step;
+        if (t >= p.T || no <= 0) continue;
+        const float sr = p.s_row ? p.s_row[t] : 1.0f;
+        const int a4[4] = {acc[u].x, acc[u].y, acc[u].z, acc[u].w};
+        const T* const res = p.residual ? static_cast<const T*>(p.residual) + t * p.res_stride + o : nullptr;
+        T* const dst = static_cast<T*>(p.out) + t * p.out_stride + o;
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = activate(fmaf((float)a4[e] * sr, sw[e], bias[e]), p.act);
+        if (no == 4 && p.vec_out && (!res || p.vec_res)) {
+          if (res) {
+            const float4 q = Elem<T>::cvt(*reinterpret_cast<const typename Elem<T>::raw4*>(res));
+            v[0] += q.x; v[1] += q.y; v[2] += q.z; v[3] += q.w;
+          }
+          *reinterpret_cast<typename Elem<T>::raw4*>(dst) = Elem<T>::pack(make_float4(v[0], v[1], v[2], v[3]));
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (e < no) dst[e] = Elem<T>::put(res ? v[e] + Elem<T>::get(res[e]) : v[e]);
+        }
+      }
+    }
+  }
+  drain_after_timeout(p.status);
+  if (f.split > 1) cluster_sync();   // (the others have read this CTA's part)
+  else __syncthreads();
+  if (warp == 2) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 128);
+  }
+}
+
 }  // namespace
 
 ssdi8_status_t launch_linear(const ssdi8_linear_args_t& a, int dtype, cudaStream_t st) {
@@ -378,6 +537,21 @@ ssdi8_status_t launch_linear(const ssdi8_linear_args_t& a, int dtype, cudaStream
     const uint32_t bx[2] = {BK, xrows}, bw[2] = {BK, wrows};
     return encode_tensor_map(tx, a.xq, 1, 2, dx, stride, bx, 128) && encode_tensor_map(tw, a.wq, 1, 2, dw, stride, bw, 128);
   };
+  if (a.rows <= kFewRows) {
+    FewParams f = {p, (a.rows + 15) / 16 * 16, 1};
+    const i64 tiles = ((i64)a.outs + 127) / 128;
+    // (a part has at least four blocks of K; 64 x 10576 x 2560: FEW_FIGURES)
+    while (f.split < 8 && tiles * f.split * 2 <= 2 * sms && p.kblocks >= 8 * f.split) f.split *= 2;
+    if (tiles * f.split > 0x7fffffff) return SSDI8_ERR_SHAPE;
+    const int stages = (int)(FewLayout::kRing / (FewLayout::kW + f.n * BK));
+    f.l.stages = stages < FewLayout::kMaxStages ? stages : FewLayout::kMaxStages;
+    CUtensorMap tx, tw;
+    if (!maps(&tx, f.n, &tw, 128)) return SSDI8_ERR_CUDA;
+    auto go = [&](auto kernel) {
+      return launch_any(kernel, dim3((unsigned)(tiles * f.split)), f.split, dim3(FT), FewLayout::kAlloc, FewLayout::kAlloc, -1, false, st, tx, tw, f);
+    };
+    return dtype == 0 ? go(linear_few_kernel<float>) : dtype == 1 ? go(linear_few_kernel<__half>) : go(linear_few_kernel<__nv_bfloat16>);
+  }
   // Lone tiles of 128 x bn or, on pairs of SMs, of 256 x 256: what is done sooner, by waves of tiles and cycles per tile (128 of K
   // take the tensor pipe 2 bn cycles of a lone tile, their operands 2 (rows + bn) on the SM's way from L2; a pair's 512 take about 640).
   // bn is a multiple of 32.  64 x 10576 x 2560: tiles of 96 columns BN_FIGURES; of 128 on 83 SMs 9.9.

@@ -688,6 +688,9 @@ LINEAR = [  # T, O, K, dtype, act, bias, residual, s_row, pad, offset
     (2000, 1999, 96, "float16", "relu2", True, None, True, 1, 0), (257, 7000, 64, "float32", "none", True, "own", True, 8, 8),
     (2, 24, 8192, "float32", "none", True, None, True, 0, 0), (33, 515, 1040, "bfloat16", "none", True, "own", True, 0, 0),
     (200, 10576, 256, "bfloat16", "none", False, None, True, 0, 0),
+    # few rows: K shared out among 2, 4 and 8 CTAs, parts of unequal length
+    (17, 2000, 1296, "bfloat16", "silu", True, "own", True, 0, 0), (127, 1000, 2688, "float16", "none", True, "out", True, 1, 0),
+    (128, 130, 5152, "float32", "relu2", True, None, True, 0, 0), (65, 2560, 5120, "bfloat16", "none", True, "own", True, 0, 0),
     # tiles of pairs of SMs: many tiles, ragged rows and columns, K of less than a block and of an odd number of blocks
     (4099, 1300, 16, "bfloat16", "none", True, "own", True, 0, 0), (3000, 2570, 656, "float16", "silu", True, "out", True, 6, 0),
     (5200, 2560, 1100 // 16 * 16, "bfloat16", "none", True, "own", True, 0, 0), (9000, 530, 2048, "float32", "relu2", False, None, False, 2, 2),
