@@ -413,6 +413,14 @@ __global__ void __launch_bounds__(FT, 2) linear_few_kernel(const __grid_constant
   pdl_wait();
   const int rank = blockIdx.x % f.split, o0 = blockIdx.x / f.split * 128;
   const int kb0 = p.kblocks * rank / f.split, kb1 = p.kblocks * (rank + 1) / f.split;
+  // a warp per token in the end, four outputs per lane
+  const int o = o0 + 4 * lane, no = min(p.O - o, 4), step = f.split * (FT / 32);
+  float sw[4], bias[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    sw[e] = e < no ? p.s_w[o + e] : 0.f;
+    bias[e] = e < no && p.bias ? p.bias[o + e] : 0.f;
+  }
   const uint32_t stage = S::kW + f.n * BK;   // (n % 16 = 0: the operands start on 1024 bytes)
   if (warp == 0) {
     int s = 0, round = 0;
@@ -462,19 +470,15 @@ __global__ void __launch_bounds__(FT, 2) linear_few_kernel(const __grid_constant
   __syncthreads();
   if (f.split > 1) cluster_sync();
   {
-    // a warp per token, four outputs per lane; the parts of four tokens on their way at a time
-    const int o = o0 + 4 * lane, no = min(p.O - o, 4);
-    float sw[4], bias[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      sw[e] = e < no ? p.s_w[o + e] : 0.f;
-      bias[e] = e < no && p.bias ? p.bias[o + e] : 0.f;
-    }
-    const int step = f.split * (FT / 32);
+    // (the parts of four tokens on their way at a time)
     for (int t0 = rank + f.split * warp; t0 < p.T; t0 += 4 * step) {
       int4 acc[4];
+      float srs[4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) acc[u] = make_int4(0, 0, 0, 0);
+      for (int u = 0; u < 4; ++u) {
+        acc[u] = make_int4(0, 0, 0, 0);
+        srs[u] = p.s_row && t0 + u * step < p.T ? p.s_row[t0 + u * step] : 1.0f;
+      }
       for (int r = 0; r < f.split; ++r)
 #pragma unroll
         for (int u = 0; u < 4; ++u)
@@ -487,13 +491,12 @@ __global__ void __launch_bounds__(FT, 2) linear_few_kernel(const __grid_constant
       for (int u = 0; u < 4; ++u) {
         const int t = t0 + u * step;
         if (t >= p.T || no <= 0) continue;
-        const float sr = p.s_row ? p.s_row[t] : 1.0f;
         const int a4[4] = {acc[u].x, acc[u].y, acc[u].z, acc[u].w};
         const T* const res = p.residual ? static_cast<const T*>(p.residual) + t * p.res_stride + o : nullptr;
         T* const dst = static_cast<T*>(p.out) + t * p.out_stride + o;
         float v[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = activate(fmaf((float)a4[e] * sr, sw[e], bias[e]), p.act);
+        for (int e = 0; e < 4; ++e) v[e] = activate(fmaf((float)a4[e] * srs[u], sw[e], bias[e]), p.act);
         if (no == 4 && p.vec_out && (!res || p.vec_res)) {
           if (res) {
             const float4 q = Elem<T>::cvt(*reinterpret_cast<const typename Elem<T>::raw4*>(res));
@@ -540,7 +543,7 @@ ssdi8_status_t launch_linear(const ssdi8_linear_args_t& a, int dtype, cudaStream
   if (a.rows <= kFewRows) {
     FewParams f = {p, (a.rows + 15) / 16 * 16, 1};
     const i64 tiles = ((i64)a.outs + 127) / 128;
-    // (a part has at least four blocks of K; 64 x 10576 x 2560: FEW_FIGURES)
+    // (a part has at least four blocks of K)
     while (f.split < 8 && tiles * f.split * 2 <= 2 * sms && p.kblocks >= 8 * f.split) f.split *= 2;
     if (tiles * f.split > 0x7fffffff) return SSDI8_ERR_SHAPE;
     const int stages = (int)(FewLayout::kRing / (FewLayout::kW + f.n * BK));
@@ -554,7 +557,7 @@ ssdi8_status_t launch_linear(const ssdi8_linear_args_t& a, int dtype, cudaStream
   }
   // Lone tiles of 128 x bn or, on pairs of SMs, of 256 x 256: what is done sooner, by waves of tiles and cycles per tile (128 of K
   // take the tensor pipe 2 bn cycles of a lone tile, their operands 2 (rows + bn) on the SM's way from L2; a pair's 512 take about 640).
-  // bn is a multiple of 32.  64 x 10576 x 2560: tiles of 96 columns BN_FIGURES; of 128 on 83 SMs 9.9.
+  // bn is a multiple of 32.
   const i64 mt = (a.rows + BM - 1) / BM;
   p.xrows = a.rows < BM ? (a.rows + 7) / 8 * 8 : BM;
   double best = 0.0;
