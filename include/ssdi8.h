@@ -421,7 +421,7 @@ ssdi8_status_t ssdi8_cache_write(const ssdi8_dims_t* dims, const ssdi8_cache_t* 
  *   S = E step code + sum_j (w_j s_x s_B x_j) B_j,  E = exp(A sum dt),  w_j = dt_j exp(A sum of the dt behind j)
  * over the waiting tokens j.  first[b] (NULL: as a slot is left by ssdi8_cache_write and ssdi8_token_step, above): position of the first
  * token that the codes do not hold; a window of more than 16 tokens or less than none is taken for padding.  A, s_x, s_B as for the step.
- * Padding leaves its rows of state alone. */
+ * Padding leaves its rows of state alone.  s_x and state 16-byte aligned. */
 ssdi8_status_t ssdi8_cache_read(const ssdi8_dims_t* dims, const ssdi8_cache_t* cache, const int32_t* slots, const int32_t* first,
                                 const int32_t* pos, const float* A, const float* s_x, const float* s_B, float* state, int32_t* status,
                                 void* stream);

@@ -19,7 +19,7 @@ bool heads_supported(const ssdi8_dims_t* d) {
 
 // the slots of a cache; ring: with the convolution's
 ssdi8_status_t cache_supported(const ssdi8_dims_t* d, const ssdi8_cache_t* c, const int32_t* slots, bool ring) {
-  if (!heads_supported(d) || c->nslots <= 0 || (!slots && c->nslots < d->batch) || (i64)d->batch * d->nheads > 0x7fffffff) return SSDI8_ERR_SHAPE;
+  if (!heads_supported(d) || c->nslots <= 0 || (!slots && c->nslots < d->batch) || (i64)d->batch * d->nheads > 0x3fffffff) return SSDI8_ERR_SHAPE;
   if (ring && (c->dtype < 0 || c->dtype > 2)) return SSDI8_ERR_UNSUPPORTED;
   if (ring && (c->width < 2 || c->width > 4)) return SSDI8_ERR_SHAPE;
   if (!c->codes || !c->scales || !c->xwin || !c->Bwin || !c->dtwin || !c->start || (ring && !c->ring)) return SSDI8_ERR_NULL;
@@ -70,7 +70,7 @@ ssdi8_status_t ssdi8_cache_read(const ssdi8_dims_t* dims, const ssdi8_cache_t* c
   ssdi8_status_t s = cache_supported(dims, cache, slots, false);
   if (s != SSDI8_OK) return s;
   if (!pos || !A || !s_x || !s_B || !state) return SSDI8_ERR_NULL;
-  if (!aligned16(state)) return SSDI8_ERR_ALIGN;
+  if (!aligned16(state) || !aligned16(s_x)) return SSDI8_ERR_ALIGN;
   if ((s = check_arch()) != SSDI8_OK) return s;
   return launch_cache_read(make_dims(dims), *cache, slots, first, pos, A, s_x, s_B, state, status, static_cast<cudaStream_t>(stream));
 }

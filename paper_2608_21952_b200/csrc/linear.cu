@@ -29,14 +29,34 @@ struct Layout {
   static constexpr uint32_t kA = BM * BK, kRing = 196608;
   static constexpr uint32_t kBars = kRing;
   static constexpr uint32_t kCols = kBars + 256;                 // s_w and bias of two tiles' columns
-  static constexpr uint32_t kBytes = kCols + 2 * 2 * kMaxBN * 4;
-  static constexpr uint32_t kAlloc = kBytes + 1024;              // (the tiles start on 1024 bytes)
+  static constexpr uint32_t kTurns = kCols + 2 * 2 * kMaxBN * 4;
+  static constexpr uint32_t kAlloc = kTurns + 4 * 32 * 17 * 4 + 1024;   // (the tiles start on 1024 bytes)
 };
 
 __device__ __forceinline__ float activate(float v, int act) {
   if (act == SSDI8_ACT_SILU) return v * rcp_approx(1.0f + ex2_approx(v * -1.44269504f));
   if (act == SSDI8_ACT_RELU2) return v > 0.f ? v * v : 0.f * v;   // (a NaN stays one)
   return v;
+}
+
+// Tensor memory for all warps but the loader's, by warp 2.  Behind the wait for the kernel before and ahead of the trigger for the next
+// one: a kernel that held some while it waits, or that still had to ask for some when the next one may be scheduled beside it, could
+// leave the two waiting for one another.
+template <int GROUP>
+__device__ __forceinline__ uint32_t allocated(uint32_t* slot, uint32_t columns, int warp, int threads) {
+  if (warp == 2) {
+    if (GROUP == 1) {
+      tmem_alloc(slot, columns);
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(slot)), "r"(columns) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    pdl_launch_dependents();
+  }
+  tc_fence_before();
+  named_bar_sync(2, threads - 32);
+  tc_fence_after();
+  return *slot;
 }
 
 // tile -> (row block, column block): GROUP row blocks at a time, so that the tiles in flight share rows of x and of w in L2
@@ -49,11 +69,43 @@ __device__ __forceinline__ void tile_of(int tile, int mtiles, int ntiles, int* m
 }
 
 // A quarter's 32 rows (lanes) of `ncols` columns of an accumulator: t is this lane's row, n0 the first column, cw and cb the
-// columns' step sizes and biases; `drained` is called once the last column has been read.
-template <typename T, typename F>
-__device__ __forceinline__ void epilogue(const LinearParams& p, uint32_t tmem, int t, int n0, int ncols, const float* cw, const float* cb, F drained) {
-  const int end = min(n0 + ncols, p.O);
+// columns' step sizes and biases; `drained` is called once the last column has been read.  Rows of out (and residual) on 16-byte
+// boundaries are written by their lane, 32 columns at a time; others, and a ragged end, go through `turn` (32 x 17 floats of the
+// warp's), 16 columns at a time, so that lanes stand beside one another in a row (3439 x 16470 x 1232, fp16, residual: 985 us one by one, 287).
+// The residual of 32 columns is on its way while the 32 before it are finished, the first of them while the accumulator is; `ready` waits
+// for that.
+constexpr int kTurn = 32 * 17;
+template <typename T, typename R, typename F>
+__device__ __forceinline__ void epilogue(const LinearParams& p, uint32_t tmem, int t, int n0, int ncols, const float* cw, const float* cb, float* turn,
+                                         R ready, F drained) {
+  typedef typename std::conditional<sizeof(T) == 4, uint32_t, uint16_t>::type Bits;
+  constexpr int V = 16 / sizeof(T), NV = 32 / V;   // elements of a 16-byte vector, vectors of 32 elements
+  const int end = min(n0 + ncols, p.O), lane = threadIdx.x & 31;
   const float sr = t < p.T ? (p.s_row ? p.s_row[t] : 1.0f) : 0.f;
+  const T* const residual = static_cast<const T*>(p.residual);
+  T* const out = static_cast<T*>(p.out);
+  const bool vectors = p.vec_out && (!residual || p.vec_res);
+  uint32_t res[32];   // this lane's 32 elements as 16-byte vectors, or one element of each 16 columns of 16 rows, twice
+  auto fetch = [&](int o0) {
+    if (!residual || o0 >= end) return;
+    if (vectors && o0 + 32 <= end) {
+      if (t < p.T) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          const uint4 q = reinterpret_cast<const uint4*>(residual + t * p.res_stride + o0)[i];
+          res[4 * i] = q.x; res[4 * i + 1] = q.y; res[4 * i + 2] = q.z; res[4 * i + 3] = q.w;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < 32; ++k) {
+        const int tt = t - lane + 2 * (k & 15) + (lane >> 4), o = o0 + (k & 16) + (lane & 15);
+        if (tt < p.T && o < end) res[k] = reinterpret_cast<const Bits*>(residual)[tt * p.res_stride + o];
+      }
+    }
+  };
+  fetch(n0);
+  ready();
 #pragma unroll 1
   for (int c0 = 0; c0 < ncols; c0 += 32) {
     int v[32];
@@ -65,43 +117,58 @@ __device__ __forceinline__ void epilogue(const LinearParams& p, uint32_t tmem, i
       drained();
     }
     const int o0 = n0 + c0;
-    if (t >= p.T || o0 >= end) continue;
-    T* dst = static_cast<T*>(p.out) + t * p.out_stride + o0;
-    const T* res = p.residual ? static_cast<const T*>(p.residual) + t * p.res_stride + o0 : nullptr;
-    const bool whole = o0 + 32 <= end;
-    if (whole && p.vec_out && (!res || p.vec_res)) {
-      constexpr int V = 16 / sizeof(T), NV = 32 / V;   // elements of a 16-byte vector, vectors of 32 elements
-      uint4 raw[NV];
-      if (res) {
+    if (o0 >= end) continue;
+    if (vectors && o0 + 32 <= end) {
+      uint32_t mine[NV * 4];
 #pragma unroll
-        for (int i = 0; i < NV; ++i) raw[i] = reinterpret_cast<const uint4*>(res)[i];
-      }
+      for (int i = 0; i < NV * 4; ++i) mine[i] = res[i];
+      fetch(o0 + 32);
+      if (t < p.T) {
+        T* const dst = out + t * p.out_stride + o0;
 #pragma unroll
-      for (int c = 0; c < 32; c += 8) {
-        float f[8];
-        const float4 w0 = *reinterpret_cast<const float4*>(cw + c0 + c), w1 = *reinterpret_cast<const float4*>(cw + c0 + c + 4);
-        const float4 b0 = *reinterpret_cast<const float4*>(cb + c0 + c), b1 = *reinterpret_cast<const float4*>(cb + c0 + c + 4);
-        const float ws[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w}, bs[8] = {b0.x, b0.y, b0.z, b0.w, b1.x, b1.y, b1.z, b1.w};
+        for (int c = 0; c < 32; c += 8) {
+          float f[8];
+          const float4 w0 = *reinterpret_cast<const float4*>(cw + c0 + c), w1 = *reinterpret_cast<const float4*>(cw + c0 + c + 4);
+          const float4 b0 = *reinterpret_cast<const float4*>(cb + c0 + c), b1 = *reinterpret_cast<const float4*>(cb + c0 + c + 4);
+          const float ws[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w}, bs[8] = {b0.x, b0.y, b0.z, b0.w, b1.x, b1.y, b1.z, b1.w};
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = activate(fmaf((float)v[c + e] * sr, ws[e], bs[e]), p.act);
-        uint4* const at = raw + c / V;
-        if (res) {
+          for (int e = 0; e < 8; ++e) f[e] = activate(fmaf((float)v[c + e] * sr, ws[e], bs[e]), p.act);
+          T* const at = reinterpret_cast<T*>(mine) + c;
+          if (residual) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) f[e] += Elem<T>::get(reinterpret_cast<const T*>(at)[e]);
+            for (int e = 0; e < 8; ++e) f[e] += Elem<T>::get(at[e]);
+          }
+#pragma unroll
+          for (int e = 0; e < 8; ++e) at[e] = Elem<T>::put(f[e]);
+#pragma unroll
+          for (int i = 0; i < 8 / V; ++i) {
+            const uint32_t* const w = mine + (c / V + i) * 4;
+            reinterpret_cast<uint4*>(dst + c)[i] = make_uint4(w[0], w[1], w[2], w[3]);
+          }
         }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) reinterpret_cast<T*>(at)[e] = Elem<T>::put(f[e]);
-#pragma unroll
-        for (int i = 0; i < 8 / V; ++i) reinterpret_cast<uint4*>(dst + c)[i] = at[i];
       }
     } else {
+      Bits mine[32];
 #pragma unroll
-      for (int c = 0; c < 32; ++c)
-        if (o0 + c < end) {
-          float f = activate(fmaf((float)v[c] * sr, cw[c0 + c], cb[c0 + c]), p.act);
-          if (res) f += Elem<T>::get(res[c]);
-          dst[c] = Elem<T>::put(f);
+      for (int k = 0; k < 32; ++k) mine[k] = (Bits)res[k];
+      fetch(o0 + 32);
+#pragma unroll
+      for (int h = 0; h < 32; h += 16) {
+#pragma unroll
+        for (int c = 0; c < 16; ++c) turn[lane * 17 + c] = activate(fmaf((float)v[h + c] * sr, cw[c0 + h + c], cb[c0 + h + c]), p.act);
+        __syncwarp();
+        const int o = o0 + h + (lane & 15);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int row = 2 * i + (lane >> 4), tt = t - lane + row;
+          if (tt < p.T && o < end) {
+            float f = turn[row * 17 + (lane & 15)];
+            if (residual) f += Elem<T>::get(*reinterpret_cast<const T*>(&mine[h + i]));
+            out[tt * p.out_stride + o] = Elem<T>::put(f);
+          }
         }
+        __syncwarp();
+      }
     }
   }
 }
@@ -140,13 +207,9 @@ __global__ void __launch_bounds__(LT, 1) linear_kernel(const __grid_constant__ C
     tma_prefetch_desc(&tx);
     tma_prefetch_desc(&tw);
   }
-  if (warp == 2) tmem_alloc(tmem_slot, 512);
-  tc_fence_before();
   __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem = *tmem_slot;
-  pdl_launch_dependents();
   pdl_wait();
+  const uint32_t tmem = warp == 0 ? 0u : allocated<1>(tmem_slot, 512, warp, LT);
   const int ntotal = p.mtiles * p.ntiles;
   const uint32_t stage = S::kA + p.bn * BK;   // (bn % 16 = 0: the operands start on 1024 bytes)
   if (warp == 0) {
@@ -197,10 +260,9 @@ __global__ void __launch_bounds__(LT, 1) linear_kernel(const __grid_constant__ C
       float* cw = cols + buf * 2 * S::kMaxBN;
       columns(p, n * p.bn, p.bn, cw, cw + S::kMaxBN, tid - 128, 128);
       named_bar_sync(1, 128);   // (and nobody is still reading the columns of the tile before the last)
-      mbar_wait(&acc_full[buf], (at >> 1) & 1, p.status);
-      tc_fence_after();
       epilogue<T>(p, tmem + ((uint32_t)(quarter * 32) << 16) + buf * S::kMaxBN, m * BM + quarter * 32 + lane, n * p.bn, p.bn, cw, cw + S::kMaxBN,
-                  [&] { mbar_arrive(&acc_empty[buf]); });
+                  reinterpret_cast<float*>(smem + S::kTurns) + quarter * kTurn,
+                  [&] { mbar_wait(&acc_full[buf], (at >> 1) & 1, p.status); tc_fence_after(); }, [&] { mbar_arrive(&acc_empty[buf]); });
     }
   }
   tc_fence_before();
@@ -222,8 +284,8 @@ struct PairLayout {
   static constexpr uint32_t kA = BM * BK, kStage = 2 * kA;
   static constexpr uint32_t kBars = kStages * kStage;
   static constexpr uint32_t kCols = kBars + 256;
-  static constexpr uint32_t kBytes = kCols + 2 * 2 * PBN * 4;
-  static constexpr uint32_t kAlloc = kBytes + 1024;
+  static constexpr uint32_t kTurns = kCols + 2 * 2 * PBN * 4;
+  static constexpr uint32_t kAlloc = kTurns + 8 * kTurn * 4 + 1024;
 };
 
 __device__ __forceinline__ uint32_t in_first(const void* p) {   // the same place in the pair's first CTA
@@ -277,17 +339,10 @@ __global__ void __launch_bounds__(PT, 1) linear_pair_kernel(const __grid_constan
     tma_prefetch_desc(&tx);
     tma_prefetch_desc(&tw);
   }
-  if (warp == 2) {
-    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-  }
-  tc_fence_before();
   __syncthreads();
   cluster_sync();   // (the other CTA's barriers are there)
-  tc_fence_after();
-  const uint32_t tmem = *tmem_slot;
-  pdl_launch_dependents();
   pdl_wait();
+  const uint32_t tmem = warp == 0 ? 0u : allocated<2>(tmem_slot, 512, warp, PT);
   const int ntotal = p.mtiles * p.ntiles;
   if (warp == 0) {
     int it = 0;
@@ -339,10 +394,9 @@ __global__ void __launch_bounds__(PT, 1) linear_pair_kernel(const __grid_constan
       float* cw = cols + buf * 2 * PBN;
       columns(p, n * PBN, PBN, cw, cw + PBN, tid - 128, PT - 128);
       named_bar_sync(1, PT - 128);
-      mbar_wait(&acc_full[buf], (at >> 1) & 1, p.status);
-      tc_fence_after();
       epilogue<T>(p, tmem + ((uint32_t)(quarter * 32) << 16) + buf * PBN + half, m * 256 + rank * 128 + quarter * 32 + lane, n * PBN + half, 128, cw + half,
-                  cw + PBN + half, [&] {
+                  cw + PBN + half, reinterpret_cast<float*>(smem + S::kTurns) + (warp - 4) * kTurn,
+                  [&] { mbar_wait(&acc_full[buf], (at >> 1) & 1, p.status); tc_fence_after(); }, [&] {
                     __syncwarp();
                     if (lane == 0) arrive_at(in_first(&acc_empty[buf]));
                   });
@@ -404,13 +458,9 @@ __global__ void __launch_bounds__(FT, 2) linear_few_kernel(const __grid_constant
     tma_prefetch_desc(&tx);
     tma_prefetch_desc(&tw);
   }
-  if (warp == 2) tmem_alloc(tmem_slot, 128);
-  tc_fence_before();
   __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem = *tmem_slot;
-  pdl_launch_dependents();
   pdl_wait();
+  const uint32_t tmem = warp == 0 ? 0u : allocated<1>(tmem_slot, 128, warp, FT);
   const int rank = blockIdx.x % f.split, o0 = blockIdx.x / f.split * 128;
   const int kb0 = p.kblocks * rank / f.split, kb1 = p.kblocks * (rank + 1) / f.split;
   // a warp per token in the end, four outputs per lane
