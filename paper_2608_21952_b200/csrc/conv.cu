@@ -299,21 +299,26 @@ __device__ __forceinline__ void dt_block(const ConvParams<T>& p, int b, int slab
   const int t0 = slab * p.slab, n = (min(t0 + p.slab, p.L) - t0) * p.H;
   const T* src = p.dt_raw + b * p.dt_sb;
   float* dst = p.dt + ((i64)b * p.L + t0) * p.H;
+  // (token and head go on by CT pairs without a division)
+  int t = threadIdx.x / p.H, hd = threadIdx.x % p.H;
+  const int dt = CT / p.H, dh = CT % p.H;
   for (int i0 = threadIdx.x; i0 < n; i0 += 4 * CT) {
     float v[4], o[4];
+    bool live[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const int i = i0 + u * CT, t = t0 + i / p.H, hd = i % p.H;
-      v[u] = i < n && t < len ? Elem<T>::get(src[t * p.dt_stok + hd]) : 0.f;
+      live[u] = i0 + u * CT < n && t0 + t < len;
+      v[u] = live[u] ? Elem<T>::get(src[(t0 + t) * p.dt_stok + hd]) : 0.f;
       if (p.softplus && p.dt_bias) v[u] = __fadd_rn(v[u], p.dt_bias[hd]);
       o[u] = v[u];
+      t += dt;
+      hd += dh;
+      if (hd >= p.H) { hd -= p.H; ++t; }
     }
     if (p.softplus) softplus_dt<4>(v, 0.f, o);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int i = i0 + u * CT;
-      if (i < n) dst[i] = t0 + i / p.H < len ? o[u] : 0.f;
-    }
+    for (int u = 0; u < 4; ++u)
+      if (i0 + u * CT < n) dst[i0 + u * CT] = live[u] ? o[u] : 0.f;
   }
 }
 
