@@ -62,8 +62,7 @@ template <typename T> struct RawMax16 {
 template <> struct RawMax<__half> : RawMax16<__half> {};
 template <> struct RawMax<__nv_bfloat16> : RawMax16<__nv_bfloat16> {};
 
-// The code of token t, channel ch, where it lies near the middle of two integers, in binary64, from the inputs (the ring still holds what
-// it held before the call).  Whether it does is seen once more, with room to spare.
+// The code of token t, channel ch, in binary64, from the inputs (the ring still holds what it held before the call).
 template <typename T, int W>
 __device__ __noinline__ void code_exact(const ConvParams<T>& p, int b, int t, int ch, int slot, int pos) {
   const int Ch = p.D + 2 * p.GN, at = ch - p.D;
@@ -78,19 +77,10 @@ __device__ __noinline__ void code_exact(const ConvParams<T>& p, int b, int t, in
   }
   const float bias = p.bias ? p.bias[ch] : 0.f;
   const float step = at < 0 ? p.s_x[ch] : at < p.GN ? p.s_B[at / p.N] : p.s_C[(at - p.GN) / p.N];
-  float v = bias, m = fabsf(bias);
-#pragma unroll
-  for (int k = 0; k < W; ++k) {
-    v = fmaf(w[k], x[k], v);
-    m = fmaf(fabsf(w[k]), fabsf(x[k]), m);
-  }
-  const float q = v / (1.0f + __expf(-v)) / step;
-  // (twice the bound in block.cuh; |v| <= m)
-  if (fabsf(q - rintf(q)) + 2.0f * kEps * (5.0f * m / step + (14.0f + 2.0f * m) * fabsf(q)) < 0.5f && step >= 1e-30f && step <= 1e30f) return;
   double e = (double)bias;
 #pragma unroll
   for (int k = 0; k < W; ++k) e = __fma_rn((double)w[k], (double)x[k], e);
-  const double r = e / (1.0 + exp(-e)) / (double)step;
+  const double r = e / ((1.0 + exp(-e)) * (double)step);
   int8_t* const out = reinterpret_cast<int8_t*>(at < 0 ? p.xq : at < p.GN ? p.Bq : p.Cq);
   const int width = at < 0 ? p.D : p.GN, col = at < 0 ? ch : at < p.GN ? at : at - p.GN;
   out[((i64)b * p.L + t) * width + col] = (int8_t)__double2int_rn(fmax(fmin(r, 127.0), -127.0));   // (fmin(NaN, 127) = 127)
@@ -109,42 +99,28 @@ template <typename T, int W, bool CODES, bool ALIGNED>
 __device__ __forceinline__ void conv_block(const ConvParams<T>& p, int b, int slab, int cblock, Queue& queue) {
   typedef typename Elem<T>::raw4 raw4;
   const int Ch = p.D + 2 * p.GN;
-  int slot, pos;
-  if (CODES && threadIdx.x == 0) queue.count = 0;
-  const int len = sequence(p, b, cblock == 0 && slab == 0, &slot, &pos);
-  if (CODES) __syncthreads();
   const int own_col = 4 * (cblock * CT + threadIdx.x);
   const bool active = own_col < Ch;
   const int col = active ? own_col : 0;   // (the others come along for the end of the block)
-  float2 w01[W], w23[W];   // taps of channels 0, 1 and 2, 3
-  float wsum[4];
+  // what does not depend on the sequence is on its way while the slot is looked up
+  float w[4][W];
 #pragma unroll
   for (int c = 0; c < 4; ++c) {
-    float w[W];
     if (W == 4) {
       const float4 v = *reinterpret_cast<const float4*>(p.weight + (i64)(col + c) * W);
-      w[0] = v.x; w[1] = v.y; w[W - 2] = v.z; w[W - 1] = v.w;
+      w[c][0] = v.x; w[c][1] = v.y; w[c][W - 2] = v.z; w[c][W - 1] = v.w;
     } else {
 #pragma unroll
-      for (int k = 0; k < W; ++k) w[k] = p.weight[(i64)(col + c) * W + k];
-    }
-    wsum[c] = 0.f;
-#pragma unroll
-    for (int k = 0; k < W; ++k) {
-      (c < 2 ? (c == 0 ? w01[k].x : w01[k].y) : (c == 2 ? w23[k].x : w23[k].y)) = w[k];
-      wsum[c] += fabsf(w[k]);
+      for (int k = 0; k < W; ++k) w[c][k] = p.weight[(i64)(col + c) * W + k];
     }
   }
   const float4 bias = p.bias ? make_float4(p.bias[col], p.bias[col + 1], p.bias[col + 2], p.bias[col + 3])
                              : make_float4(0.f, 0.f, 0.f, 0.f);
-  float2 step01 = make_float2(1.f, 1.f), step23 = step01;
-  float fac[4];   // 5 eps / step
+  float4 step = make_float4(1.f, 1.f, 1.f, 1.f);
   uint32_t* out = nullptr;
   int ow4 = 0;
-  bool usable = true;
   if (CODES) {
     int oq;
-    float4 step;
     if (col < p.D) {
       step = *reinterpret_cast<const float4*>(p.s_x + col);
       out = p.xq; ow4 = p.D / 4; oq = col / 4;
@@ -156,12 +132,29 @@ __device__ __forceinline__ void conv_block(const ConvParams<T>& p, int b, int sl
       out = isC ? p.Cq : p.Bq; ow4 = p.GN / 4; oq = at / 4;
     }
     out += (i64)b * p.L * ow4 + oq;
-    step01 = make_float2(step.x, step.y);
-    step23 = make_float2(step.z, step.w);
-    fac[0] = 5.1f * kEps / step.x; fac[1] = 5.1f * kEps / step.y; fac[2] = 5.1f * kEps / step.z; fac[3] = 5.1f * kEps / step.w;
-    auto normal = [](float x) { return x >= 1e-30f && x <= 1e30f; };
-    usable = normal(step.x) && normal(step.y) && normal(step.z) && normal(step.w);
   }
+  int slot, pos;
+  if (CODES && threadIdx.x == 0) queue.count = 0;
+  const int len = sequence(p, b, cblock == 0 && slab == 0, &slot, &pos);
+  if (CODES) __syncthreads();
+  float2 w01[W], w23[W];   // taps of channels 0, 1 and 2, 3
+  float wsum[4];
+#pragma unroll
+  for (int k = 0; k < W; ++k) {
+    w01[k] = make_float2(w[0][k], w[1][k]);
+    w23[k] = make_float2(w[2][k], w[3][k]);
+  }
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    wsum[c] = 0.f;
+#pragma unroll
+    for (int k = 0; k < W; ++k) wsum[c] += fabsf(w[c][k]);
+  }
+  const float2 step01 = make_float2(step.x, step.y), step23 = make_float2(step.z, step.w);
+  auto normal = [](float x) { return x >= 1e-30f && x <= 1e30f; };
+  const bool usable = normal(step.x) && normal(step.y) && normal(step.z) && normal(step.w);
+  const float fac[4] = {5.1f * kEps * rcp_approx(step.x), 5.1f * kEps * rcp_approx(step.y), 5.1f * kEps * rcp_approx(step.z),
+                        5.1f * kEps * rcp_approx(step.w)};   // 5 eps / step
   const int t0 = slab * p.slab, t1 = min(t0 + p.slab, p.L);
   const int live = active ? min(t1, len) : t0;
   const T* src = p.xBC + b * p.sb + col;
