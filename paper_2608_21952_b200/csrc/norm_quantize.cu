@@ -8,6 +8,10 @@
 // the sum, halved; 3).  A quotient that lies nearer than that to the middle of two integers is formed again in binary64, from the row's
 // absmax in binary64 (of the few elements that can be it) and, where it does not cancel, the norm in binary64.  Rows whose sums leave
 // binary32's range have all of their codes formed so.
+//
+// What bounds it: 16384 rows of 5120 (fp32 and a bf16 gate, 587 MB: 90 us at the copy rate) take 129 us: 33 instructions an element, two of them
+// on the quarter-rate pipe (the exponential and the reciprocal), with two to four blocks of eight warps to an SM (64 registers; 48 spill: 140 us).
+// Codes and exact path in one body took 292 us, one element after the other; pairs, with the exact path out of line, 144; chunks of a warp side by side 135.
 #include "block.cuh"
 #include "kernels.h"
 

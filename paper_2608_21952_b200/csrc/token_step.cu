@@ -2,7 +2,12 @@
 // the slot's window.  The state is read once, as codes, and not written: with the tokens since its last fold beside it,
 //   y = s_C (E scale sum_n C q + s_x s_B sum_j w_j (C . B_j) x_j) + D s_x x + corr,   E = exp(A sum dt), w_j = dt_j exp(A sum behind j)
 // (ChunkScan1 and ChunkScan2 of Algorithm 2 for a single row, with int8 dot products), a quarter of the fp32 state's bytes one way
-// instead of two.  Once in 16 tokens the full window is folded into the codes, in binary64.
+// instead of two.  Once in 16 tokens the full window is folded into the codes, as in binary64, by a second kernel.
+//
+// What bounds it: 64 sequences x 80 heads (53 MB, 8.2 us at the copy rate) take 16.5 us without full windows, 250 x 128 (335 MB, 51 us) 94: about
+// 760 instructions a warp, half of them the convolution of B and C, which every block of heads does for itself, and the chain of a block (slot, ring,
+// codes, weights of the window, y: 10 thousand cycles) with 27 warps to an SM.  The fp32 state's step (ssd_step.cu) with its two
+// kernels ahead takes 58.8 for the first.  With one sequence in 16 folding, 31 and 145 us: a fold is about 1700 instructions a warp.
 #include "kernels.h"
 #include "sm100.cuh"
 #include "state_cache.cuh"
