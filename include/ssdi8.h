@@ -373,7 +373,8 @@ ssdi8_status_t ssdi8_softplus_dt(const float* dt_raw, const float* dt_bias, int6
  * kept, slots ignored.  slots = NULL: slot b.  Rows from lens[b] on get codes, out and dt of 0, which pass through the chunk scan without
  * a trace (pad seqlen to a multiple of the chunk); a padding sequence has no tokens at all.
  * dims.chunk is ignored; seqlen may be 0.  weight [Ch][width], bias [Ch] or NULL, Ch = H*P + 2*G*N; dt_raw has xBC's type.
- * weight, s_x, xq, Bq, Cq, out and ring 16-byte aligned, xBC and dt_raw at an element's alignment, any strides of tokens and sequences. */
+ * weight, s_x, xq, Bq, Cq, out and ring 16-byte aligned, xBC and dt_raw at an element's alignment, any strides of tokens and
+ * sequences; out is another tensor than xBC. */
 typedef struct {
   const void* xBC; int64_t stride_b, stride_t;               /* [B][L][Ch]                       */
   const float* weight; const float* bias;                    /* [Ch][width], [Ch]                */
@@ -468,7 +469,7 @@ ssdi8_status_t ssdi8_norm_quantize(const ssdi8_norm_args_t* args, int32_t dtype,
  * in binary32, rounded once to out's type.  act: SSDI8_ACT_NONE, v / (1 + exp(-v)) (_SILU), max(v, 0)^2 (_RELU2).  xq [rows][inner],
  * wq [outs][inner] (step sizes s_w per output), dense and 16-byte aligned; inner % 16 = 0, 16 <= inner <= 131072 (the sums stay in
  * 32 bits).  s_row, bias, residual may be NULL (1, 0, 0): the paper adds its mean correction at the out-proj (Section 4.3), which is `bias`
- * here.  out, residual: type dtype, any strides of rows (overlapping rows aside); residual may be out itself.  rows may be 0. */
+ * here.  out, residual: type dtype, any strides of rows (out's at least outs); residual may be out itself.  rows may be 0. */
 enum { SSDI8_ACT_NONE = 0, SSDI8_ACT_SILU = 1, SSDI8_ACT_RELU2 = 2 };
 typedef struct {
   const int8_t* xq; const int8_t* wq;

@@ -43,7 +43,7 @@ ssdi8_status_t ssdi8_conv_fwd(const ssdi8_dims_t* dims, const ssdi8_conv_args_t*
   if (a->ring && !a->slots && a->nslots < dims->batch) return SSDI8_ERR_SHAPE;
   if (!a->xBC || !a->weight || (a->dt && !a->dt_raw)) return SSDI8_ERR_NULL;
   if (a->xq ? !a->Bq || !a->Cq || !a->s_x || !a->s_B || !a->s_C : !a->out) return SSDI8_ERR_NULL;
-  if (a->xq && a->out) return SSDI8_ERR_UNSUPPORTED;
+  if ((a->xq && a->out) || a->out == a->xBC) return SSDI8_ERR_UNSUPPORTED;
   const void* ptrs[] = {a->weight, a->ring, a->s_x, a->xq, a->Bq, a->Cq, a->out};
   for (const void* p : ptrs)
     if (!aligned16(p)) return SSDI8_ERR_ALIGN;
@@ -109,6 +109,7 @@ ssdi8_status_t ssdi8_norm_quantize(const ssdi8_norm_args_t* a, int32_t dtype, in
 ssdi8_status_t ssdi8_linear(const ssdi8_linear_args_t* a, int32_t dtype, void* stream) {
   if (!a) return SSDI8_ERR_NULL;
   if (dtype < 0 || dtype > 2 || a->act < SSDI8_ACT_NONE || a->act > SSDI8_ACT_RELU2) return SSDI8_ERR_UNSUPPORTED;
+  if (a->rows > 1 && a->stride_out < a->outs) return SSDI8_ERR_SHAPE;   // (rows that overlap)
   if (a->rows < 0 || a->outs <= 0 || a->inner < 16 || a->inner > 131072 || a->inner % 16 != 0) return SSDI8_ERR_SHAPE;
   if (a->rows == 0) return SSDI8_OK;
   if (!a->xq || !a->wq || !a->s_w || !a->out) return SSDI8_ERR_NULL;

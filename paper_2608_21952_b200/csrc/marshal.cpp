@@ -95,7 +95,20 @@ struct LayerArg : Struct {
 };
 
 struct CacheArg : Struct {
-  explicit CacheArg(PyObject* o) : Struct(o, g_types.cache, sizeof(ssdi8_cache_t)) {}
+  explicit CacheArg(PyObject* o) : Struct(o, g_types.cache, sizeof(ssdi8_cache_t)) {
+    PyObject* d = PyObject_GetAttrString(o, "device");   // (of cache_of; a structure filled by hand has none)
+    if (!d) {
+      PyErr_Clear();
+      return;
+    }
+    const long index = PyLong_AsLong(d);
+    Py_DECREF(d);
+    if (index == -1 && PyErr_Occurred()) throw BadArgument{};
+    if (index != c10::cuda::current_device()) {
+      PyErr_SetString(PyExc_ValueError, "the cache lives on another device than the current one");
+      throw BadArgument{};
+    }
+  }
   const ssdi8_cache_t* get() const { return static_cast<const ssdi8_cache_t*>(b.buf); }
 };
 

@@ -574,7 +574,7 @@ ssdi8_status_t launch(const Dims& d, const ssdi8_cache_t& c, const ssdi8_token_a
   if (sms <= 0) return SSDI8_ERR_CUDA;
   // Eight heads to a block (three of them per SM) from a full wave on, four (four per SM) below that.  Steps without full windows, eight /
   // four / two heads, us: 250 x 128 heads 92.9 / 97.5 / 141, 64 x 80 16.8 / 19.1 / 27.
-  const bool eight = (i64)d.b * d.G * ((p.hpg + 7) / 8) >= 3 * sms;
+  const bool eight = p.hpg > 4 && (i64)d.b * d.G * ((p.hpg + 7) / 8) >= 3 * sms;
   const ssdi8_status_t s = eight ? pick(std::integral_constant<int, 8>{}) : pick(std::integral_constant<int, 4>{});
   if (s != SSDI8_OK) return s;
   const FoldParams f = {p.c, a.A, a.s_x, a.s_B, a.slots, a.pos, d.b, d.H, d.G};

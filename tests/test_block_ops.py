@@ -58,6 +58,7 @@ def _conv_args(**kw):
     ("ERR_UNSUPPORTED", {}, {}, 3, 4, 0),
     ("ERR_UNSUPPORTED", {}, {}, 2, 4, 1 << 1),
     ("ERR_UNSUPPORTED", {}, {"out": ADDR}, 2, 4, 0),                 # codes or a tensor, not both
+    ("ERR_UNSUPPORTED", {}, {"xq": None, "out": ADDR}, 2, 4, 0),     # not in place: tokens ahead would be read behind their change
     ("ERR_SHAPE", {}, {}, 2, 1, 0),
     ("ERR_SHAPE", {}, {}, 2, 5, 0),
     ("ERR_SHAPE", {"headdim": 32}, {}, 2, 4, 0),
@@ -621,7 +622,7 @@ class LinearArgs(C.Structure):
 
 @pytest.mark.parametrize("want,args,dtype", [
     ("ERR_UNSUPPORTED", {}, 3), ("ERR_UNSUPPORTED", {"act": 3}, 0), ("ERR_UNSUPPORTED", {"act": -1}, 0), ("ERR_SHAPE", {"rows": -1}, 0),
-    ("ERR_SHAPE", {"outs": 0}, 0), ("ERR_SHAPE", {"inner": 0}, 0), ("ERR_SHAPE", {"inner": 24}, 0), ("ERR_SHAPE", {"inner": 131088}, 0),
+    ("ERR_SHAPE", {"outs": 0}, 0), ("ERR_SHAPE", {"stride_out": 63}, 0), ("ERR_SHAPE", {"inner": 0}, 0), ("ERR_SHAPE", {"inner": 24}, 0), ("ERR_SHAPE", {"inner": 131088}, 0),
     ("ERR_NULL", {"xq": None}, 0), ("ERR_NULL", {"wq": None}, 0), ("ERR_NULL", {"s_w": None}, 0), ("ERR_NULL", {"out": None}, 0),
     ("ERR_ALIGN", {"xq": ADDR + 8}, 0), ("ERR_ALIGN", {"wq": ADDR + 1}, 0), ("ERR_ALIGN", {"out": ADDR + 2}, 0), ("ERR_ALIGN", {"residual": ADDR + 1}, 1),
     ("OK", {"rows": 0, "out": None}, 0),
@@ -730,3 +731,71 @@ def test_linear_on_two_streams_and_in_a_graph():
         bd.ssdi8_linear(x, w, sw, c, residual=c)
     graph.replay()
     assert torch.equal(a, want) and torch.equal(b, want) and torch.equal(c, 2 * want)
+
+
+# ------------------------------------------------------------------------------------------------ the binding's own checks
+@pytest.mark.gpu
+def test_binding_refuses_what_tensors_tell():
+    """shapes are SSDi8Error(ERR_SHAPE), element types TypeError, host or strided tensors AssertionError, another device ValueError"""
+    torch = pytest.importorskip("torch")
+    from paper_2608_21952_b200 import binding as bd
+    e = lambda *s, dtype=torch.int8, device="cuda": torch.empty(*s, dtype=dtype, device=device)  # noqa: E731
+    x, w, sw, out = e(4, 64), e(32, 64), e(32, dtype=torch.float32), e(4, 32, dtype=torch.float32)
+    for bad in (dict(wq=e(32, 48)), dict(s_w=e(31, dtype=torch.float32)), dict(out=e(5, 32, dtype=torch.float32)), dict(xq=e(4, 64, 1))):
+        with pytest.raises(bd.SSDi8Error) as err:
+            bd.ssdi8_linear(**{**dict(xq=x, wq=w, s_w=sw, out=out), **bad})
+        assert err.value.code == bd.ERR_SHAPE
+    for bad in (dict(xq=e(4, 64, dtype=torch.float32)), dict(out=e(4, 32)), dict(residual=e(4, 32, dtype=torch.bfloat16)), dict(s_w=None)):
+        with pytest.raises(TypeError):
+            bd.ssdi8_linear(**{**dict(xq=x, wq=w, s_w=sw, out=out), **bad})
+    for bad in (dict(xq=e(4, 64, device="cpu")), dict(wq=e(64, 32).t()), dict(out=e(32, 4, dtype=torch.float32).t())):
+        with pytest.raises(AssertionError):
+            bd.ssdi8_linear(**{**dict(xq=x, wq=w, s_w=sw, out=out), **bad})
+    dims = bd.Dims(1, 1, 2, 64, 64, 1, 0)
+    cache = bd.make_cache(dims, 2)
+    cache.device = 7
+    with pytest.raises(ValueError):
+        bd.ssdi8_cache_write(dims, cache, None, None, None)
+    good = {k: t for k, t in cache.tensors.items()}
+    for bad, kind in ((dict(codes=good["codes"][:1].contiguous()), bd.SSDi8Error), (dict(start=good["start"].float()), TypeError),
+                      (dict(ring=good["ring"].to(torch.int16)), TypeError), (dict(xwin=good["xwin"].cpu()), ValueError)):
+        with pytest.raises(kind):
+            bd.cache_of(dims, **{**good, **bad})
+
+
+@pytest.mark.gpu
+def test_offsets_beyond_32_bits():
+    """a slot and a row whose elements lie more than 2^31 into their tensors"""
+    torch = pytest.importorskip("torch")
+    from paper_2608_21952_b200 import binding as bd
+    H, N, n = 128, 128, 2100   # codes: 2100 x 1 MB
+    dims = bd.Dims(2, 1, H, 64, N, 1, 0)
+    cache = bd.make_cache(dims, n)
+    assert cache.tensors["codes"].numel() > 2 ** 31
+    slots, pos = torch.tensor([n - 1, 3], dtype=torch.int32, device="cuda"), torch.tensor([15, 15], dtype=torch.int32, device="cuda")
+    S = torch.randn(1, H, 64, N, device="cuda").expand(2, -1, -1, -1).contiguous()
+    bd.ssdi8_cache_write(dims, cache, slots, pos, S)
+    rng = np.random.default_rng(1)
+    p = {k: _t(v) for k, v in _token_params(rng, H, N, 1, 4).items()}
+    x = _t(rng.standard_normal((1, 64 * H + 2 * N)).astype(np.float32), "bfloat16").expand(2, -1)
+    raw, y = _t(rng.standard_normal((1, H)).astype(np.float32), "bfloat16").expand(2, -1), torch.empty(2, 64 * H, device="cuda")
+    cache.tensors["ring"][n - 1].copy_(cache.tensors["ring"][3].normal_())
+    bd.ssdi8_token_step(dims, cache, x, p["w"], p["bias"], raw, p["dt_bias"], p["A"], p["D"], p["corr"], p["s_x"], p["s_B"], p["s_C"], slots, pos, y,
+                        flags=bd.FLAG_DT_SOFTPLUS)
+    assert torch.equal(y[0], y[1]) and y.isfinite().all()
+    for k in ("codes", "scales", "xwin", "Bwin", "dtwin", "ring"):   # (folded, too)
+        assert torch.equal(cache.tensors[k][n - 1], cache.tensors[k][3]), k
+    out = torch.empty(2, H, 64, N, device="cuda")
+    bd.ssdi8_cache_read(dims, cache, slots, pos + 1, p["A"], p["s_x"], p["s_B"], out)
+    assert torch.equal(out[0], out[1]) and (out[0] - cache.tensors["scales"][3][..., None] * cache.tensors["codes"][3]).abs().max() == 0
+    del cache, out, S
+    # rows of the projection and the norm: 2^31 elements apart and more
+    T, O = 70000, 32768
+    wide = torch.empty(T, O, dtype=torch.bfloat16, device="cuda")
+    xq, wq, sw = torch.randint(-127, 128, (T, 64), dtype=torch.int8, device="cuda"), torch.randint(-127, 128, (O, 64), dtype=torch.int8, device="cuda"), torch.rand(O, device="cuda")
+    xq[-300:] = xq[:300]
+    bd.ssdi8_linear(xq, wq, sw, wide)
+    assert torch.equal(wide[-300:], wide[:300])
+    codes, sc = torch.empty(T, 16384, dtype=torch.int8, device="cuda"), torch.empty(T, device="cuda")
+    bd.ssdi8_norm_quantize(wide[:, 16384:], codes, z=wide[:, :16384], scale=sc)
+    assert torch.equal(codes[-300:], codes[:300]) and torch.equal(sc[-300:], sc[:300])
