@@ -3,10 +3,11 @@
 // width - 1 tokens in registers and walks a slab of tokens, eight loads in flight, so that every element is read once (and
 // width - 1 of a slab's tokens once more, from L2) and leaves as one byte.
 //
-// What bounds it: instructions.  8 x 2048 tokens x 80 heads (bf16, 272 MB in and out: 42 us at the copy rate) takes 108 us, 58 M warp
-// instructions (20 an element: the convolution, the SiLU, the code, and the test whether binary32 may decide it); without that test and
-// the time steps it takes 77.  Five blocks of four warps to an SM: four or six take 126 and 118; loads of the next eight tokens ahead of the
-// present ones 117 to 135; slabs of 48 or 32 tokens 115 and 122, of 128 128.
+// What bounds it: instructions, with the latencies around them.  8 x 2048 tokens x 80 heads (bf16, 272 MB in and out: 42 us at the copy
+// rate) takes 97 us, 60 % of the issue slots, the quarter-rate pipe busy for 46 % of the time (two exponentials and two reciprocals a
+// pair).  Without the test whether binary32 may decide a code and without the time steps it takes 77.  Nine blocks of four warps to an
+// SM: eight 100, seven 104, six 117, ten 104 us; slabs of 32 tokens 105, of 96 and 128 98 and 101, but 32 and 39 where 64 take 28
+// (5 x 1787 tokens x 50 heads, ragged).  One channel a thread, in arithmetic of single elements, took 108.
 #include "block.cuh"
 #include "kernels.h"
 
@@ -114,8 +115,8 @@ __device__ __noinline__ void code_exact(const ConvParams<T>& p, int b, int t, in
 }
 
 // Pairs of quotients (a token, two channels) one of which may lie near the middle of two integers: they wait for the end of the
-// block, whose threads then have a quotient each.  (Each at once by the lane that met it, its warp waiting: 157 us where
-// 8 x 2048 x 80 heads with a longer and narrower test took 119.)
+// block, whose threads then have a quotient each.  (Each at once by the lane that met it, its warp waiting, took 119 us
+// where the queue took 111, with one channel a thread.)
 constexpr int kQueue = 256;
 struct Queue {
   uint32_t item[kQueue];   // token of the slab << 8 | thread
