@@ -218,6 +218,18 @@ def test_conv_values_that_are_not_finite_and_step_sizes_at_the_ends():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype,H,L,W", [("bfloat16", 3, 150, 4), ("float32", 5, 64, 3), ("float16", 1, 9, 2)])
+def test_conv_where_binary32_decides_next_to_nothing(dtype, H, L, W):
+    """step sizes outside the normal range in most channels, and inputs far above the steps in others, going on from a ring"""
+    c = _conv_case(8, 3, L, H, 64, 1, W, dtype, 0)
+    c["s_x"][: 40 * H] = 1e-33
+    c["s_x"][40 * H : 60 * H] = 1e-8
+    lens, pos, slots = np.array([L, L - 1, 0], np.int32), np.array([5, 1, 2], np.int32), np.array([4, 0, 2], np.int32)
+    ring = c["ring"].clone()
+    _conv_check(c, _conv_run(c, True, lens=lens, slots=slots, pos=pos, ring=ring), True, lens=lens, slots=slots, pos=pos, ring=ring, ring_before=c["ring"])
+
+
+@pytest.mark.gpu
 def test_conv_on_a_side_stream_and_in_a_graph():
     torch = pytest.importorskip("torch")
     from paper_2608_21952_b200 import binding as bd
