@@ -72,9 +72,13 @@ __device__ __noinline__ double gated_exact(const NormParams<T, Z>& p, i64 row, i
 
 // Codes of a row in binary64: those of the chunks in `near`, or all of them (and the row's step size) if the row is out of binary32's range.
 // The absmax in binary64 is that of the chunks in `cand`.  All threads call it, behind their stores.
+// In a row of several groups the quotient is 127 v / v_m times the ratio of the two norms: 1 in the group of the absmax, where ties stay ties.
+struct Top {
+  double o, v, r;   // |u w| r, |u w|, r = 1 / sqrt(mean + eps)
+};
 template <typename T, typename Z, int NCH>
 __device__ __noinline__ void exact_row(const NormParams<T, Z>& p, i64 row, uint32_t near, uint32_t cand, bool range, bool zero, double* sum64,
-                                       double* top64) {
+                                       Top* top64) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nwarps = blockDim.x >> 5;
   const int D = p.D, nchunks = (D + 127) / 128, cpg = p.groups > 1 ? nchunks / p.groups : nchunks;
   const bool many = p.groups > 1, dynamic = p.static_scale == nullptr;
@@ -122,7 +126,7 @@ __device__ __noinline__ void exact_row(const NormParams<T, Z>& p, i64 row, uint3
     for (int i = c / cpg * cpg; i < c / cpg * cpg + cpg; ++i) s += sum64[i];
     return 1.0 / sqrt(s / (double)(many ? cpg * 128 : D) + (double)p.eps);
   };
-  double m64 = 0.0;
+  Top m = {0.0, 0.0, 1.0};
   if (dynamic) {
 #pragma unroll 1
     for (int k = 0; k < NCH; ++k)
@@ -131,15 +135,21 @@ __device__ __noinline__ void exact_row(const NormParams<T, Z>& p, i64 row, uint3
 #pragma unroll 1
         for (int e = 0; e < 4; ++e) {
           double u;
-          m64 = fmax(m64, fabs(gated_exact(p, row, col_of(k) + e, &u) * r));   // (a NaN counts for nothing)
+          const double v = fabs(gated_exact(p, row, col_of(k) + e, &u));
+          if (v * r > m.o) m = {v * r, v, r};   // (a NaN counts for nothing)
         }
       }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m64 = fmax(m64, __shfl_xor_sync(0xffffffffu, m64, o));
-    if (lane == 0) top64[warp] = m64;
+    for (int o = 16; o > 0; o >>= 1) {
+      const Top t = {__shfl_xor_sync(0xffffffffu, m.o, o), __shfl_xor_sync(0xffffffffu, m.v, o), __shfl_xor_sync(0xffffffffu, m.r, o)};
+      if (t.o > m.o) m = t;
+    }
+    if (lane == 0) top64[warp] = m;
     __syncthreads();
-    for (int i = 0; i < nwarps; ++i) m64 = fmax(m64, top64[i]);
-    if (!range && p.scale && threadIdx.x == 0) p.scale[row] = m64 > 0.0 ? (float)(m64 / 127.0) : 1.0f;
+    m = top64[0];   // (the same of equal ones for all threads)
+    for (int i = 1; i < nwarps; ++i)
+      if (top64[i].o > m.o) m = top64[i];
+    if (!range && p.scale && threadIdx.x == 0) p.scale[row] = m.o > 0.0 ? (float)(m.o / 127.0) : 1.0f;
   }
 #pragma unroll 1
   for (int k = 0; k < NCH; ++k)
@@ -148,8 +158,8 @@ __device__ __noinline__ void exact_row(const NormParams<T, Z>& p, i64 row, uint3
 #pragma unroll 1
       for (int e = 0; e < 4; ++e) {
         double u;
-        const double v = gated_exact(p, row, col_of(k) + e, &u) * r;
-        const double q = !dynamic ? v / (double)*p.static_scale : m64 > 0.0 ? 127.0 * v / m64 : v;   // (exact ties stay ties)
+        const double v = gated_exact(p, row, col_of(k) + e, &u);
+        const double q = !dynamic ? v * r / (double)*p.static_scale : m.o > 0.0 ? 127.0 * v / m.v * (r / m.r) : v * r;
         p.xq[row * D + col_of(k) + e] = (int8_t)__double2int_rn(fmax(fmin(q, 127.0), -127.0));        // (fmin(NaN, 127) = 127)
       }
     }
@@ -209,7 +219,8 @@ __global__ void __launch_bounds__(512, NCH == 8 ? 1 : 2) norm_kernel(const __gri
   __shared__ struct {
     float part[2][kMaxWarps];
     float csum[kMaxChunks], cmax[kMaxChunks];   // of chunks, where the row has several groups
-    double sum64[kMaxChunks], top64[kMaxWarps];
+    double sum64[kMaxChunks];
+    Top top64[kMaxWarps];
   } S;
   pdl_launch_dependents();
   pdl_wait();

@@ -138,6 +138,14 @@ class Slots:
         return bound
 
 
+def parts(x, z, weight, groups, eps):
+    """u w, and each element's sqrt(mean + eps)"""
+    T, D = x.shape
+    u = x.astype(np.float64) if z is None else x.astype(np.float64) * silu(z.astype(np.float64))
+    root = np.sqrt((u.reshape(T, groups, D // groups) ** 2).mean(-1) + eps)
+    return u if weight is None else u * weight.astype(np.float64), np.repeat(root, D // groups, -1)
+
+
 def norm(x, z, weight, groups, eps):
     """o of the gated RMS norm, and the same without the norm where the row is one group (it cancels out of 127 o / absmax)"""
     T, D = x.shape
@@ -158,4 +166,10 @@ def norm_codes(x, z, weight, groups, eps, static=None):
             return code(o / np.float64(static)), None
         top, of = np.nan_to_num(np.fmax.reduce(np.abs(v), -1), nan=0.0, posinf=np.inf), np.nan_to_num(np.fmax.reduce(np.abs(o), -1), nan=0.0, posinf=np.inf)
         q = np.where(top[:, None] > 0, 127.0 * v / np.where(top > 0, top, 1)[:, None], v)
+        if groups > 1:
+            # the same with the ratio of the norms by itself, which is 1 in the group of the absmax: exact ties stay ties there
+            v, root = parts(x, z, weight, groups, eps)
+            at = np.where(np.isnan(o), -1.0, np.abs(o)).argmax(-1)[:, None]
+            ratio = 127.0 * v / np.abs(np.take_along_axis(v, at, -1)) * (np.take_along_axis(root, at, -1) / root)
+            q = np.where((top > 0)[:, None] & np.isfinite(root).all(-1, keepdims=True), ratio, q)
         return code(q), np.where(of > 0, of / 127.0, 1.0)

@@ -563,7 +563,7 @@ def _norm_check(x, z, weight, groups, eps, static=None, scale=True):
     sc = torch.full((T,), 7.0, device="cuda") if scale else None
     bd.ssdi8_norm_quantize(x, xq, weight=None if weight is None else _t(weight), z=z, groups=groups, eps=eps, scale=sc,
                            static_scale=None if static is None else _t(np.array([static], np.float32)))
-    want, step = ref.norm_codes(_np(x), None if z is None else _np(z), weight, groups, eps, static)
+    want, step = ref.norm_codes(_np(x), None if z is None else _np(z), weight, groups, eps, None if static is None else np.float32(static))
     np.testing.assert_array_equal(_np(xq), want)
     if scale and static is None:
         # binary32: 12 eps of u w, 24 of the norm, and the quotient
@@ -623,6 +623,31 @@ def test_norm_ties_go_to_the_even_code():
     x[:, 127], x[1] = 127, -x[1]
     x[1, 200] = -127
     _norm_check(torch.from_numpy(x).cuda(), None, None, 1, 1e-5)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("gate", [None, "float32"])
+def test_norm_ties_in_the_group_of_the_absmax(gate):
+    """rows of several groups: quotients of k + 1/2 in the group of the absmax, where the norm cancels, and beside groups of other norms"""
+    import torch
+    from paper_2608_21952_b200 import binding as bd
+    rng = np.random.default_rng(12)
+    x = 0.01 * rng.standard_normal((254, 4, 128)).astype(np.float32)
+    at, f = rng.integers(0, 4, 254), rng.uniform(0.5, 2, 254).astype(np.float32)
+    k = rng.integers(-20, 20, (254, 127)).astype(np.float32)   # (the absmax is six times the root mean square and more; the others' is four)
+    f = np.float32(2.0) ** -12 * np.round(f * 4096)   # (13 bits: products with k + 1/2 are exact)
+    for t in range(254):
+        x[t, at[t], 1:] = (k[t] + 0.5) * f[t]
+        x[t, at[t], 0] = (-127.0 if t % 2 else 127.0) * f[t]
+    z = None if gate is None else _t(np.full((254, 512), 40, np.float32))   # (SiLU(40) = 40 to 17 digits)
+    rms = np.sqrt((x.astype(np.float64) ** 2).mean(-1))
+    assert np.array_equal((np.abs(x).max(-1) / rms).argmax(-1), at)
+    xq = torch.empty(254, 512, dtype=torch.int8, device="cuda")
+    bd.ssdi8_norm_quantize(_t(x.reshape(254, 512)), xq, z=z, groups=4, eps=1e-5)
+    got = _np(xq).reshape(254, 4, 128)
+    for t in range(254):
+        np.testing.assert_array_equal(got[t, at[t], 1:], np.rint(k[t] + 0.5))
+        assert got[t, at[t], 0] == (-127 if t % 2 else 127)
 
 
 # ------------------------------------------------------------------------------------------------ int8 projection
