@@ -9,9 +9,11 @@
 // absmax in binary64 (of the few elements that can be it) and, where it does not cancel, the norm in binary64.  Rows whose sums leave
 // binary32's range have all of their codes formed so.
 //
-// What bounds it: 16384 rows of 5120 (fp32 and a bf16 gate, 587 MB: 90 us at the copy rate) take 129 us: 33 instructions an element, two of them
-// on the quarter-rate pipe (the exponential and the reciprocal), with two to four blocks of eight warps to an SM (64 registers; 48 spill: 140 us).
-// Codes and exact path in one body took 292 us, one element after the other; pairs, with the exact path out of line, 144; chunks of a warp side by side 135.
+// What bounds it: 16384 rows of 5120 (fp32 and a bf16 gate, 587 MB: 90 us at the copy rate) take 122 us: 33 instructions an element, two of them
+// on the quarter-rate pipe (the exponential and the reciprocal), with three to five blocks to an SM (80 registers; 64 take 129 us with five
+// chunks to a warp, 48 spill: 140).
+// Codes and exact path in one body took 292 us, one element after the other; pairs, with the exact path out of line, 144; chunks of a warp side
+// by side 135.
 #include "block.cuh"
 #include "kernels.h"
 
@@ -213,9 +215,9 @@ __device__ __forceinline__ float warp_max(float v) {   // of numbers >= 0; a NaN
   return m;
 }
 
-// A warp has NCH chunks of 128 columns, one after the other.
-template <typename T, typename Z, int NCH>
-__global__ void __launch_bounds__(512, NCH == 8 ? 1 : 2) norm_kernel(const __grid_constant__ NormParams<T, Z> p) {
+// A warp has NCH chunks of 128 columns, one after the other; WARPS at most.
+template <typename T, typename Z, int NCH, int WARPS>
+__global__ void __launch_bounds__(32 * WARPS, WARPS == 16 ? 1 : NCH == 2 ? 4 : 3) norm_kernel(const __grid_constant__ NormParams<T, Z> p) {
   __shared__ struct {
     float part[2][kMaxWarps];
     float csum[kMaxChunks], cmax[kMaxChunks];   // of chunks, where the row has several groups
@@ -328,13 +330,23 @@ ssdi8_status_t launch(const ssdi8_norm_args_t& a, cudaStream_t st) {
   p.zaligned = a.z && reinterpret_cast<uintptr_t>(a.z) % (4 * sizeof(Z)) == 0 && a.stride_z % 4 == 0;
   p.fast = p.valigned && (!a.z || p.zaligned);
   const int chunks = (a.width + 127) / 128;
-  auto go = [&](auto n) -> ssdi8_status_t {
-    constexpr int NCH = decltype(n)::value;
-    return launch_configured(norm_kernel<T, Z, NCH>, dim3((unsigned)a.rows), dim3(32 * ((chunks + NCH - 1) / NCH)), 0, -1, false, st, p);
+  auto go = [&](auto n, auto warps) -> ssdi8_status_t {
+    constexpr int NCH = decltype(n)::value, WARPS = decltype(warps)::value;
+    return launch_configured(norm_kernel<T, Z, NCH, WARPS>, dim3((unsigned)a.rows), dim3(32 * ((chunks + NCH - 1) / NCH)), 0, -1, false, st, p);
   };
-  if (chunks <= 32) return go(std::integral_constant<int, 2>{});
-  if (chunks <= 64) return go(std::integral_constant<int, 5>{});
-  return go(std::integral_constant<int, 8>{});
+  typedef std::integral_constant<int, 2> Two;
+  typedef std::integral_constant<int, 5> Five;
+  typedef std::integral_constant<int, 8> Eight;
+  typedef std::integral_constant<int, 16> Sixteen;
+  // Few rows want many warps, many rows few warps with much each: a warp's share of the reductions is the same for two chunks as for
+  // eight (fp32 and a bf16 gate, us with 2, 5, 8 chunks to a warp: 600 rows of 2048 8.2, 9.3, 9.9, of 5120 -, 11.1, 11.4; 4096 rows
+  // of 512 9.9, 11.3, 12.4, of 2048 22.8, 20.9, 18.8, of 2560 28.7, 21.6, 24.3, of 4096 44.5, 37.3, 29.5, of 8192 -, 70.5, 55.2).  Five
+  // where eight leave more of the last warp idle.
+  if (chunks > 64) return go(Eight(), Sixteen());
+  const bool few = a.rows <= 1024;
+  if (chunks <= 4 || (few && chunks <= 16)) return go(Two(), Eight());
+  if (chunks <= 40 && (few || (chunks + 4) / 5 * 5 < (chunks + 7) / 8 * 8)) return go(Five(), Eight());
+  return go(Eight(), Eight());
 }
 
 template <typename T>

@@ -593,6 +593,21 @@ def test_norm(T, D, groups, dtype, gate, offset):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("T,D,groups,dtype,gate,offset", [
+    (1024, 2064, 1, "bfloat16", None, 0), (1025, 512, 1, "float32", "bfloat16", 0), (1025, 528, 1, "bfloat16", "float16", 1),
+    (1030, 1024, 8, "float16", "bfloat16", 0), (1030, 2560, 2, "float32", None, 0), (1030, 4096, 1, "bfloat16", "float32", 0),
+    (1030, 5136, 1, "bfloat16", "bfloat16", 0), (1030, 8192, 4, "bfloat16", None, 2),
+])
+def test_norm_of_many_rows(T, D, groups, dtype, gate, offset):
+    """the widths and row counts at which a warp's share changes; rows of zeros, of one value and out of binary32's range among them"""
+    test_norm(T, D, groups, dtype, gate, offset)
+    rng = np.random.default_rng(D)
+    x = rng.standard_normal((T, D)).astype(np.float32)
+    x[5], x[T - 1], x[T - 2, 1:], x[17] = 0, 1, 0, x[17] * (1e-25 if dtype != "float16" else 1e-4)
+    _norm_check(_t(x, dtype), None, None, groups, 1e-5)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("groups", [1, 2])
 @pytest.mark.parametrize("gate", [None, "float32"])
 def test_norm_of_extreme_rows(groups, gate):
