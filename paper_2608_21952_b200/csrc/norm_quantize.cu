@@ -9,7 +9,7 @@
 // absmax in binary64 (of the few elements that can be it) and, where it does not cancel, the norm in binary64.  Rows whose sums leave
 // binary32's range have all of their codes formed so.
 //
-// What bounds it: 16384 rows of 5120 (fp32 and a bf16 gate, 587 MB: 90 us at the copy rate) take 122 us: 33 instructions an element, two of them
+// What bounds it: 16384 rows of 5120 (fp32 and a bf16 gate, 587 MB: 90 us at the copy rate) take 122 us: 30 instructions an element, two of them
 // on the quarter-rate pipe (the exponential and the reciprocal), with three to five blocks to an SM (80 registers; 64 take 129 us with five
 // chunks to a warp, 48 spill: 140).
 // Codes and exact path in one body took 292 us, one element after the other; pairs, with the exact path out of line, 144; chunks of a warp side
