@@ -396,7 +396,8 @@ ssdi8_status_t ssdi8_conv_fwd(const ssdi8_dims_t* dims, const ssdi8_conv_args_t*
  * Re-quantising the state at every token would keep small updates from ever moving a code; with the window the step reads the codes
  * and writes one window row, and the codes are formed anew once in 16 tokens.
  * A slot at position pos (tokens of the sequence so far) has the tokens from max(start, pos - pos mod 16) on in its window and all
- * earlier ones in its codes.
+ * earlier ones in its codes.  A call's nheads, headdim, dstate and ngroups are those that the arrays were laid out for (the binding
+ * refuses others; here nothing tells), its batch any number of slots.
  * codes, scales, xwin, Bwin, dtwin, ring: 16-byte aligned. */
 #define SSDI8_CACHE_WINDOW 16
 typedef struct {

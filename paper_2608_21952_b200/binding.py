@@ -326,7 +326,8 @@ def cache_of(dims: Dims, codes, scales, xwin, Bwin, dtwin, start, ring=None) -> 
         setattr(c, name, _ptr(t))
     if ring is not None:
         c.width, c.dtype = ring.shape[1], _ENTRY_DTYPES[ring.dtype]
-    c.device = codes.device.index   # (compared with the current device by every call)
+    c.heads = (H, P, N, G)          # (compared with the call's dims,
+    c.device = codes.device.index   # and this with the current device, by every call)
     c.tensors = {name: t for name, (t, _, _) in want.items()}   # (the struct holds raw pointers: they stay alive with it)
     return c
 

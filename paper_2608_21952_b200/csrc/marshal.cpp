@@ -94,15 +94,31 @@ struct LayerArg : Struct {
   const ssdi8_layer_args_t* get() const { return static_cast<const ssdi8_layer_args_t*>(b.buf); }
 };
 
+// A cache as cache_of leaves it says what its arrays were laid out for (`heads`: H, P, N, G) and where they live (`device`); a structure
+// filled by hand says neither, and its caller answers for both.  A call with other dims would read and write past the arrays: it is
+// refused as a tensor of another shape is.
+struct BadShape {};
+PyObject* const kHeads = PyUnicode_InternFromString("heads");
+PyObject* const kDevice = PyUnicode_InternFromString("device");
 struct CacheArg : Struct {
-  explicit CacheArg(PyObject* o) : Struct(o, g_types.cache, sizeof(ssdi8_cache_t)) {
-    PyObject* d = PyObject_GetAttrString(o, "device");   // (of cache_of; a structure filled by hand has none)
-    if (!d) {
+  CacheArg(PyObject* o, const ssdi8_dims_t& d) : Struct(o, g_types.cache, sizeof(ssdi8_cache_t)) {
+    if (PyObject* h = PyObject_GetAttr(o, kHeads)) {
+      const int32_t want[4] = {d.nheads, d.headdim, d.dstate, d.ngroups};
+      bool same = PyTuple_Check(h) && PyTuple_GET_SIZE(h) == 4;
+      for (int i = 0; same && i < 4; ++i) same = PyLong_AsLong(PyTuple_GET_ITEM(h, i)) == want[i];
+      Py_DECREF(h);
+      if (PyErr_Occurred()) throw BadArgument{};
+      if (!same) throw BadShape{};
+    } else {
+      PyErr_Clear();
+    }
+    PyObject* v = PyObject_GetAttr(o, kDevice);
+    if (!v) {
       PyErr_Clear();
       return;
     }
-    const long index = PyLong_AsLong(d);
-    Py_DECREF(d);
+    const long index = PyLong_AsLong(v);
+    Py_DECREF(v);
     if (index == -1 && PyErr_Occurred()) throw BadArgument{};
     if (index != c10::cuda::current_device()) {
       PyErr_SetString(PyExc_ValueError, "the cache lives on another device than the current one");
@@ -128,7 +144,6 @@ void* stream(PyObject* o) {
 // current one (the stream's) a ValueError.
 constexpr int kInt8 = -1, kInt32 = -2;   // beside the library's 0 = fp32, 1 = fp16, 2 = bf16
 constexpr int kAnyFloat = -3;
-struct BadShape {};
 struct Tensor {
   const at::Tensor* t = nullptr;
   int dtype = 0;
@@ -366,7 +381,7 @@ ENTRY(conv_fwd, 21) {
 
 ENTRY(cache_write, 7) {   // dims, cache, slots, pos, state, status, stream
   DimsArg d(a[0]);
-  CacheArg c(a[1]);
+  CacheArg c(a[1], *d.get());
   const int64_t B = d.get()->batch;
   const int32_t* slots = tensor(a[2], "slots", kInt32, {B}, true).as<int32_t>();
   const int32_t* pos = tensor(a[3], "pos", kInt32, {B}, true).as<int32_t>();
@@ -378,7 +393,7 @@ ENTRY(cache_write, 7) {   // dims, cache, slots, pos, state, status, stream
 
 ENTRY(cache_read, 11) {   // dims, cache, slots, first, pos, A, s_x, s_B, state, status, stream
   DimsArg d(a[0]);
-  CacheArg c(a[1]);
+  CacheArg c(a[1], *d.get());
   const int64_t B = d.get()->batch, H = d.get()->nheads, P = d.get()->headdim;
   const int32_t* slots = tensor(a[2], "slots", kInt32, {B}, true).as<int32_t>();
   const int32_t* first = tensor(a[3], "first", kInt32, {B}, true).as<int32_t>();
@@ -395,7 +410,7 @@ ENTRY(cache_read, 11) {   // dims, cache, slots, first, pos, A, s_x, s_B, state,
 // dims, cache, xBC, weight, bias, dt_raw, dt_bias, A, D, corr, s_x, s_B, s_C, slots, pos, y, status, flags, stream
 ENTRY(token_step, 19) {
   DimsArg d(a[0]);
-  CacheArg c(a[1]);
+  CacheArg c(a[1], *d.get());
   const int64_t B = d.get()->batch, H = d.get()->nheads, G = d.get()->ngroups, HP = H * d.get()->headdim,
                 Ch = HP + 2 * G * d.get()->dstate;
   const int dtype = c.get()->dtype;

@@ -1,0 +1,52 @@
+"""The operators around the layer at the edges of what they take: values that are not finite, rows and groups of zeros, step sizes
+at the ends of the range, status words in use, arguments that contradict one another."""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+import block_reference as ref
+from test_block_ops import ADDR, LinearArgs, _cache, _dims, _lib, _np, _t, _token_params
+
+
+# ------------------------------------------------------------------------------------------------ cache and token step
+def _other_dims(bd):
+    """other heads, other groups, another state size: what a cache of 4 heads of 64 x 64 in 2 groups was not laid out for"""
+    return [_dims(bd, nheads=8), _dims(bd, nheads=2), _dims(bd, ngroups=4), _dims(bd, ngroups=1), _dims(bd, dstate=128)]
+
+
+def test_calls_refuse_a_cache_of_other_dims(monkeypatch):
+    """without a device: the cache is looked at ahead of every other argument (and never with the dims that it has)"""
+    import torch
+    bd, _ = _lib()
+    monkeypatch.setattr(bd, "_ptr", lambda t: t.data_ptr())
+    own = _dims(bd)
+    z = lambda *s, dtype=torch.int8: torch.zeros(s, dtype=dtype)  # noqa: E731
+    c = bd.cache_of(own, codes=z(4, 4, 64, 64), scales=z(4, 4, 64, dtype=torch.float32), xwin=z(4, 4, 16, 64), Bwin=z(4, 2, 16, 64),
+                    dtwin=z(4, 4, 16, dtype=torch.float32), start=z(4, dtype=torch.int32), ring=z(4, 4, 512, dtype=torch.bfloat16))
+    for d in _other_dims(bd):
+        for call in (lambda: bd.ssdi8_cache_write(d, c, None, None, None), lambda: bd.ssdi8_cache_read(d, c, *[None] * 6),
+                     lambda: bd.ssdi8_token_step(d, c, *[None] * 14)):
+            with pytest.raises(bd.SSDi8Error) as err:
+                call()
+            assert err.value.code == bd.ERR_SHAPE
+
+
+@pytest.mark.gpu
+def test_a_cache_of_other_dims_stays_as_it_was():
+    from paper_2608_21952_b200 import binding as bd
+    import torch
+    c, a, _ = _cache(np.random.default_rng(1), 4, 4, 64, 2)
+    for d in _other_dims(bd):
+        B, H, G, N = d.batch, d.nheads, d.ngroups, d.dstate
+        state, f = torch.ones(B, H, 64, N, device="cuda"), lambda *s: torch.ones(s, device="cuda")  # noqa: E731
+        pos = torch.zeros(B, dtype=torch.int32, device="cuda")
+        with pytest.raises(bd.SSDi8Error):
+            bd.ssdi8_cache_write(d, c, None, None, state)
+        with pytest.raises(bd.SSDi8Error):
+            bd.ssdi8_cache_read(d, c, None, pos, f(H), f(H * 64), f(G), state)
+    for k, t in c.tensors.items():
+        np.testing.assert_array_equal(_np(t), a[k])
+    d = _dims(bd, batch=3, seqlen=77)   # (sequences and lengths are the call's own)
+    bd.ssdi8_cache_write(d, c, None, None, torch.ones(3, 4, 64, 64, device="cuda"))
+    assert np.all(_np(c.tensors["codes"])[:3] == 127)
