@@ -41,19 +41,23 @@ __device__ __forceinline__ bool mbar_try_wait(uint64_t* bar, uint32_t parity) {
   return ok != 0;
 }
 // Bounded wait.  Every try_wait blocks for up to its suspend-time hint, so the cap is of the
-// order of a second.  On expiry the caller's status word is set and the wait returns; once
-// the word is set, every later wait of the grid gives up after a few polls, so the kernel runs
-// to its normal end (tensor memory is freed) quickly, with undefined results.
+// order of a second.  On expiry the caller's status word becomes SSDI8_ERR_DEVICE_TIMEOUT and the wait
+// returns; once it is that, every later wait of the grid gives up after a few polls, so the kernel runs
+// to its normal end (tensor memory is freed) quickly, with undefined results.  Another error in the word
+// (a bad row of this call or an earlier one) is no reason to give up.
 // The polling loop is one out-of-line function: a call site is the first attempt and a branch, so
 // the many waits of a warp-specialised kernel do not bloat its instruction footprint.
 constexpr uint32_t kWaitCap = 1u << 17;
+__device__ __forceinline__ bool timed_out(const int32_t* status) {
+  return status && *reinterpret_cast<const volatile int32_t*>(status) == (int32_t)SSDI8_ERR_DEVICE_TIMEOUT;
+}
 // (CAP is a template parameter only so that the library's self-test can run this very loop with a
 // cap of a few dozen polls on a barrier nobody arrives on; every kernel of the layer uses kWaitCap.)
 template <uint32_t CAP = kWaitCap>
 static __device__ __noinline__ void mbar_wait_slow(uint64_t* bar, uint32_t parity, int32_t* status) {
   for (uint32_t it = 0; it < CAP; ++it) {
     if (mbar_try_wait(bar, parity)) return;
-    if ((it & 255u) == 255u && status && *reinterpret_cast<volatile int32_t*>(status) != 0) return;
+    if ((it & 255u) == 255u && timed_out(status)) return;
   }
   if (status) atomicExch(status, (int32_t)SSDI8_ERR_DEVICE_TIMEOUT);
 }
@@ -66,11 +70,11 @@ __device__ __forceinline__ void named_bar_sync(uint32_t id, uint32_t nthreads) {
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(nthreads) : "memory");
 }
 
-// At the end of a kernel whose waits are bounded: if some wait of the grid gave up (the status word is
-// set), the handshakes of this CTA may be broken and copies into its shared memory may still be in
+// At the end of a kernel whose waits are bounded: if some wait of the grid gave up (the status word says
+// so), the handshakes of this CTA may be broken and copies into its shared memory may still be in
 // flight; give them a bounded time to land before the CTA retires and its shared memory is handed on.
 __device__ __forceinline__ void drain_after_timeout(const int32_t* status) {
-  if (status && *reinterpret_cast<const volatile int32_t*>(status) != 0)
+  if (timed_out(status))
     for (int i = 0; i < 50; ++i) __nanosleep(1000);
 }
 
@@ -81,7 +85,7 @@ __device__ __forceinline__ bool mbar_wait_inline(uint64_t* bar, uint32_t parity,
   for (uint32_t it = 0; it < kWaitCap; ++it) {
     if (mbar_try_wait(bar, parity)) return true;
     if (SLEEP_NS) __nanosleep(SLEEP_NS);
-    if ((it & 255u) == 255u && status && *reinterpret_cast<volatile int32_t*>(status) != 0) return false;
+    if ((it & 255u) == 255u && timed_out(status)) return false;
   }
   if (status) atomicExch(status, (int32_t)SSDI8_ERR_DEVICE_TIMEOUT);
   return false;

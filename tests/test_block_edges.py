@@ -50,3 +50,37 @@ def test_a_cache_of_other_dims_stays_as_it_was():
     d = _dims(bd, batch=3, seqlen=77)   # (sequences and lengths are the call's own)
     bd.ssdi8_cache_write(d, c, None, None, torch.ones(3, 4, 64, 64, device="cuda"))
     assert np.all(_np(c.tensors["codes"])[:3] == 127)
+
+
+# ------------------------------------------------------------------------------------------------ status words
+def _us(torch, f, n=20, rounds=5):
+    f()
+    best = 1e9
+    for _ in range(rounds):
+        a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        torch.cuda.synchronize()
+        a.record()
+        for _ in range(n):
+            f()
+        b.record()
+        b.synchronize()
+        best = min(best, 1000 * a.elapsed_time(b) / n)
+    return best
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,O,K", [(16, 256, 1024), (300, 300, 1024), (3000, 2570, 656)])
+def test_linear_with_a_status_word_that_holds_another_calls_error(T, O, K):
+    """SSDI8_ERR_SHAPE of a bad row elsewhere is no time-out: same outputs, no copies waited for at the end (50 us a block), the word kept"""
+    import torch
+    from paper_2608_21952_b200 import binding as bd
+    rng = np.random.default_rng(T)
+    x, w = (_t(rng.integers(-127, 128, s).astype(np.int8)) for s in ((T, K), (O, K)))
+    sw = _t(rng.uniform(0.5, 1.5, O).astype(np.float32))
+    want, out = (torch.empty(T, O, device="cuda") for _ in range(2))
+    clear, bad = (torch.tensor([v], dtype=torch.int32, device="cuda") for v in (0, bd.ERR_SHAPE))
+    bd.ssdi8_linear(x, w, sw, want, status=clear)
+    bd.ssdi8_linear(x, w, sw, out, status=bad)
+    assert torch.equal(out, want) and int(bad.item()) == bd.ERR_SHAPE and int(clear.item()) == 0
+    quick, slow = (_us(torch, lambda: bd.ssdi8_linear(x, w, sw, out, status=s)) for s in (clear, bad))
+    assert slow < quick + 25, (quick, slow)
