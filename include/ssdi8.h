@@ -359,8 +359,9 @@ ssdi8_status_t ssdi8_softplus_dt(const float* dt_raw, const float* dt_bias, int6
 /* Slots.  A serving program keeps one slot per sequence (ring rows of the convolution, state cache).  slots[b] names the slot of
  * the call's sequence b; a negative one marks a sequence of padding, whose slot data and outputs are left alone (or cleared,
  * where an entry says so).  A slot or position that no call may have (slots[b] >= nslots, pos[b] < 0) and a slot that an earlier
- * sequence of the same call names already are taken for padding, and *status (if given) becomes SSDI8_ERR_SHAPE; it is not
- * written otherwise. */
+ * sequence of the same call names already are taken for padding, and *status (if given) becomes SSDI8_ERR_SHAPE, unless it holds
+ * SSDI8_ERR_DEVICE_TIMEOUT, which it keeps; it is not written otherwise.  One word may serve calls of every kind; one that
+ * holds a time-out is cleared before its next use (waits that meet it give up early). */
 
 /* Causal convolution of a prompt: depthwise, `width` taps (2, 3 or 4), bias, SiLU, and the entry quantiser (Section 4.2,
  * "Quantization of B,C") in one pass over xBC.

@@ -90,6 +90,13 @@ __device__ __noinline__ float silu_quotient_exact(float x0, float x1, float x2, 
   return (float)rint(fmax(fmin(q, 127.0), -127.0));   // (fmin(NaN, 127) = 127)
 }
 
+// A slot or position that no call may have: the status word becomes SSDI8_ERR_SHAPE.  A time-out stays one (then there is more amiss
+// than a row), whichever of the two a call meets first.
+__device__ __forceinline__ void bad_row(int32_t* status) {
+  constexpr int32_t timeout = (int32_t)SSDI8_ERR_DEVICE_TIMEOUT;
+  if (status && atomicExch(status, (int32_t)SSDI8_ERR_SHAPE) == timeout) atomicExch(status, timeout);
+}
+
 // The slot of sequence b, or -1 (padding) with *bad set where the call names one that it may not: out of range, a negative
 // position, or the slot of an earlier sequence.  All threads of the block call it.
 __device__ __forceinline__ int slot_of(const int32_t* slots, const int32_t* pos, int nslots, int b, bool* bad) {

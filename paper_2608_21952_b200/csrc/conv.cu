@@ -43,7 +43,7 @@ __device__ __forceinline__ int sequence(const ConvParams<T>& p, int b, bool firs
     *slot = slot_of(p.slots, p.pos, p.nslots, b, &bad);
     *pos = p.pos && *slot >= 0 ? p.pos[b] : 0;
     if (*slot < 0) len = 0;
-    if (bad && first_block && threadIdx.x == 0 && p.status) atomicExch(p.status, (int32_t)SSDI8_ERR_SHAPE);
+    if (bad && first_block && threadIdx.x == 0) bad_row(p.status);
   }
   return len;
 }

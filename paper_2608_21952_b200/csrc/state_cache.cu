@@ -27,7 +27,7 @@ __global__ void __launch_bounds__(SC_T) cache_write_kernel(CacheView c, const in
     v[r] = state ? __ldcs(state + (((i64)b * H + h) * 64 + p0 + r * RPP) * N4 + lane) : make_float4(0.f, 0.f, 0.f, 0.f);
   bool bad;
   const int slot = slot_of(slots, pos, c.nslots, b, &bad);
-  if (bad && h == 0 && threadIdx.x == 0 && status) atomicExch(status, (int32_t)SSDI8_ERR_SHAPE);
+  if (bad && h == 0 && threadIdx.x == 0) bad_row(status);
   if (slot < 0) return;
   if (h == 0 && p0 == 0 && lane == 0) c.start[slot] = pos ? pos[b] : 0;
   const i64 row0 = ((i64)slot * H + h) * 64 + p0;
@@ -68,7 +68,7 @@ __global__ void __launch_bounds__(SC_T, 4) cache_read_kernel(CacheView c, const 
     bad = f < 0 || f > p || p - f > kWin;
     n = bad ? 0 : p - f;
   }
-  if (bad && h == 0 && threadIdx.x == 0 && status) atomicExch(status, (int32_t)SSDI8_ERR_SHAPE);
+  if (bad && h == 0 && threadIdx.x == 0) bad_row(status);
   if (slot < 0 || bad) return;
   const i64 sh = (i64)slot * H + h;
   uint32_t q[R];

@@ -154,7 +154,7 @@ __global__ void __launch_bounds__(TS_ALL, HPC == 8 ? 3 : 4) token_kernel(const _
   bool bad;
   const int slot = slot_of(p.slots, p.pos, p.c.nslots, b, &bad);
   const int pos = slot >= 0 ? p.pos[b] : 0;
-  if (bad && hb == 0 && g == 0 && tid == 0 && p.status) atomicExch(p.status, (int32_t)SSDI8_ERR_SHAPE);
+  if (bad && hb == 0 && g == 0 && tid == 0) bad_row(p.status);
   if (slot < 0) return;
   const int start = p.c.start[slot], now = pos % kWin, f = max(start, pos - now);
   const i64 sh0 = (i64)slot * p.H + h0;
@@ -170,7 +170,7 @@ __global__ void __launch_bounds__(TS_ALL, HPC == 8 ? 3 : 4) token_kernel(const _
     for (int k = 0; k < N / 64; ++k) Bv[k] = reinterpret_cast<const uint32_t*>(Bw + j * N)[piece * (N / 64) + k];
   }
   if (start > pos) {   // the slot was written behind this position
-    if (hb == 0 && g == 0 && tid == 0 && p.status) atomicExch(p.status, (int32_t)SSDI8_ERR_SHAPE);
+    if (hb == 0 && g == 0 && tid == 0) bad_row(p.status);
     return;
   }
   if (tid >= TS_T && lane < nh) {

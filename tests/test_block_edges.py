@@ -52,6 +52,20 @@ def test_a_cache_of_other_dims_stays_as_it_was():
     assert np.all(_np(c.tensors["codes"])[:3] == 127)
 
 
+def _token_case(seed, B, H, N, G, n=None, start=None):
+    rng = np.random.default_rng(seed)
+    c, a, torch = _cache(rng, n or B, H, N, G, start=start)
+    p = _token_params(rng, H, N, G, 4)
+    x = _t(rng.standard_normal((B, 64 * H + 2 * G * N)).astype(np.float32), "bfloat16")
+    raw = _t(rng.standard_normal((B, H)).astype(np.float32), "bfloat16")
+    return c, a, p, {k: _t(v) for k, v in p.items()}, x, raw, torch
+
+
+def _token(bd, c, dev, x, raw, pos, y, dims, slots=None, status=None, flags=0):
+    bd.ssdi8_token_step(dims, c, x, dev["w"], dev["bias"], raw, dev["dt_bias"], dev["A"], dev["D"], dev["corr"], dev["s_x"], dev["s_B"], dev["s_C"],
+                        slots, pos, y, status=status, flags=bd.FLAG_DT_SOFTPLUS | flags)
+
+
 # ------------------------------------------------------------------------------------------------ status words
 def _us(torch, f, n=20, rounds=5):
     f()
@@ -84,3 +98,22 @@ def test_linear_with_a_status_word_that_holds_another_calls_error(T, O, K):
     assert torch.equal(out, want) and int(bad.item()) == bd.ERR_SHAPE and int(clear.item()) == 0
     quick, slow = (_us(torch, lambda: bd.ssdi8_linear(x, w, sw, out, status=s)) for s in (clear, bad))
     assert slow < quick + 25, (quick, slow)
+
+
+@pytest.mark.gpu
+def test_bad_rows_do_not_hide_a_time_out():
+    """a word that holds a time-out keeps it; one that holds nothing or another error becomes SSDI8_ERR_SHAPE"""
+    from paper_2608_21952_b200 import binding as bd
+    c, a, p, dev, x, raw, torch = _token_case(4, 2, 2, 64, 1)
+    d, pos, slots = _dims(bd, 2, 1, 2, 64, 64, 1), torch.tensor([3, 0], dtype=torch.int32, device="cuda"), torch.tensor([0, 9], dtype=torch.int32, device="cuda")
+    y, state = torch.empty(2, 128, device="cuda"), torch.zeros(2, 2, 64, 64, device="cuda")
+    conv = lambda st: bd.ssdi8_conv_fwd(d, x[:, None], dev["w"], dev["bias"], out=torch.empty(2, 1, x.shape[1], dtype=torch.bfloat16, device="cuda"),  # noqa: E731
+                                        ring=c.tensors["ring"], slots=slots, pos=pos, status=st)
+    calls = {"conv": conv, "write": lambda st: bd.ssdi8_cache_write(d, c, slots, pos, state, status=st),
+             "read": lambda st: bd.ssdi8_cache_read(d, c, slots, pos, dev["A"], dev["s_x"], dev["s_B"], state, status=st),
+             "token": lambda st: _token(bd, c, dev, x, raw, pos, y, d, slots=slots, status=st)}
+    for name, call in calls.items():
+        for held, want in ((0, bd.ERR_SHAPE), (bd.ERR_SHAPE, bd.ERR_SHAPE), (bd.ERR_DEVICE_TIMEOUT, bd.ERR_DEVICE_TIMEOUT)):
+            status = torch.tensor([held], dtype=torch.int32, device="cuda")
+            call(status)
+            assert int(status.item()) == want, (name, held)
