@@ -40,7 +40,7 @@ struct Layout {
 
 __device__ __forceinline__ float activate(float v, int act) {
   if (act == SSDI8_ACT_SILU) return v * rcp_approx(1.0f + ex2_approx(v * -1.44269504f));
-  if (act == SSDI8_ACT_RELU2) return v > 0.f ? v * v : 0.f * v;   // (a NaN stays one)
+  if (act == SSDI8_ACT_RELU2) return v < 0.f ? 0.f : v * v;   // (-inf is 0, a NaN stays one)
   return v;
 }
 

@@ -9,6 +9,35 @@ import block_reference as ref
 from test_block_ops import ADDR, LinearArgs, _cache, _dims, _lib, _np, _t, _token_params
 
 
+# ------------------------------------------------------------------------------------------------ projection
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("T,O,K", [(3, 40, 64), (200, 72, 144), (3000, 2570, 656)])   # few rows, lone tiles, pairs of SMs
+def test_squared_relu_of_values_that_are_not_finite(T, O, K, dtype):
+    """max(v, 0)^2 is 0 for -inf (of a bias that closes an output, of a product that overflows), inf for inf and NaN for NaN alone"""
+    import torch
+    from paper_2608_21952_b200 import binding as bd
+    x, w = np.ones((T, K), np.int8), np.ones((O, K), np.int8)
+    w[5] = -1
+    sw, bias = np.full(O, 2.0 ** -10, np.float32), np.zeros(O, np.float32)
+    bias[1], bias[2], bias[3], bias[4] = -np.inf, np.inf, np.nan, -3.0
+    sw[5] = 3e38   # (K products of -1: beyond binary32)
+    sw[6] = 3e38
+    want = np.full(O, (K * 2.0 ** -10) ** 2)
+    want[[1, 2, 3, 4, 5, 6]] = [0, np.inf, np.nan, 0, 0, np.inf]
+    for residual in (None, 0.5):
+        out = torch.full((T, O), 7.0, device="cuda").to(getattr(torch, dtype))
+        res = None if residual is None else torch.full_like(out, residual)
+        bd.ssdi8_linear(_t(x), _t(w), _t(sw), out, bias=_t(bias), residual=res, act=bd.ACT_RELU2)
+        got = _np(out).astype(np.float64)
+        exact = np.broadcast_to(want + (residual or 0), got.shape)
+        np.testing.assert_array_equal(got[:, 1:7], exact[:, 1:7])
+        assert residual is not None or not np.signbit(got[:, [1, 4, 5]]).any()
+        # (K 2^-10, its square and the sum: one rounding each at most, and that of the type)
+        half = 2.0 ** -24 if dtype == "float32" else 2.0 ** -8
+        np.testing.assert_allclose(got[:, 7:], exact[:, 7:], rtol=half + 4 * 2.0 ** -24)
+
+
 # ------------------------------------------------------------------------------------------------ cache and token step
 def _other_dims(bd):
     """other heads, other groups, another state size: what a cache of 4 heads of 64 x 64 in 2 groups was not laid out for"""
