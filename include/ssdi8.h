@@ -471,7 +471,8 @@ ssdi8_status_t ssdi8_norm_quantize(const ssdi8_norm_args_t* args, int32_t dtype,
  * in binary32, rounded once to out's type.  act: SSDI8_ACT_NONE, v / (1 + exp(-v)) (_SILU), max(v, 0)^2 (_RELU2).  xq [rows][inner],
  * wq [outs][inner] (step sizes s_w per output), dense and 16-byte aligned; inner % 16 = 0, 16 <= inner <= 131072 (the sums stay in
  * 32 bits).  s_row, bias, residual may be NULL (1, 0, 0): the paper adds its mean correction at the out-proj (Section 4.3), which is `bias`
- * here.  out, residual: type dtype, any strides of rows (out's at least outs); residual may be out itself.  rows may be 0. */
+ * here.  out, residual: type dtype, any strides of rows (out's at least outs); residual may be out itself.  rows may be 0; rows and outs
+ * up to 2^31 - 256. */
 enum { SSDI8_ACT_NONE = 0, SSDI8_ACT_SILU = 1, SSDI8_ACT_RELU2 = 2 };
 typedef struct {
   const int8_t* xq; const int8_t* wq;

@@ -110,6 +110,7 @@ ssdi8_status_t ssdi8_linear(const ssdi8_linear_args_t* a, int32_t dtype, void* s
   if (!a) return SSDI8_ERR_NULL;
   if (dtype < 0 || dtype > 2 || a->act < SSDI8_ACT_NONE || a->act > SSDI8_ACT_RELU2) return SSDI8_ERR_UNSUPPORTED;
   if (a->rows > 1 && a->stride_out < a->outs) return SSDI8_ERR_SHAPE;   // (rows that overlap)
+  if (a->rows > kMaxLinearRows || a->outs > kMaxLinearRows) return SSDI8_ERR_SHAPE;
   if (a->rows < 0 || a->outs <= 0 || a->inner < 16 || a->inner > 131072 || a->inner % 16 != 0) return SSDI8_ERR_SHAPE;
   if (a->rows == 0) return SSDI8_OK;
   if (!a->xq || !a->wq || !a->s_w || !a->out) return SSDI8_ERR_NULL;

@@ -182,6 +182,7 @@ ssdi8_status_t launch_cache_read(const Dims& d, const ssdi8_cache_t& c, const in
 ssdi8_status_t launch_token_step(const Dims& d, const ssdi8_cache_t& c, const ssdi8_token_args_t& a, bool softplus, int ydt, cudaStream_t st);
 constexpr int kMaxNormWidth = 16384;
 ssdi8_status_t launch_norm_quantize(const ssdi8_norm_args_t& a, int dtype, int zdtype, cudaStream_t st);
+constexpr int kMaxLinearRows = 0x7fffff00;   // (and outputs: a tile's last ones are counted in 32 bits)
 ssdi8_status_t launch_linear(const ssdi8_linear_args_t& a, int dtype, cudaStream_t st);
 
 // measurement aid and self-test (selftest.cu): `nbatch` batches of int8_mma_peak_batch() MMAs of

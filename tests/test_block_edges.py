@@ -38,6 +38,13 @@ def test_squared_relu_of_values_that_are_not_finite(T, O, K, dtype):
         np.testing.assert_allclose(got[:, 7:], exact[:, 7:], rtol=half + 4 * 2.0 ** -24)
 
 
+@pytest.mark.parametrize("args", [{"rows": 0x7fffff01}, {"rows": 0x7fffffff}, {"outs": 0x7fffff01, "stride_out": 1 << 31}])
+def test_linear_refuses_counts_that_a_tile_would_carry_beyond_32_bits(args):
+    bd, lib = _lib()
+    a = LinearArgs(**{**dict(xq=ADDR, wq=ADDR, s_w=ADDR, out=ADDR, stride_out=64, rows=4, outs=64, inner=64), **args})
+    assert lib.ssdi8_linear(C.byref(a), 0, None) == bd.ERR_SHAPE
+
+
 # ------------------------------------------------------------------------------------------------ cache and token step
 def _other_dims(bd):
     """other heads, other groups, another state size: what a cache of 4 heads of 64 x 64 in 2 groups was not laid out for"""
