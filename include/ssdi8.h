@@ -454,6 +454,8 @@ ssdi8_status_t ssdi8_token_step(const ssdi8_dims_t* dims, const ssdi8_cache_t* c
  *   u = x z / (1 + exp(-z)) (z = NULL: u = x);  o = u w / sqrt(mean over the channel's group of u^2 + eps) (w = NULL: 1)
  *   static_scale = NULL: step = absmax of the row's o / 127 (1 if that is 0), code = rne(127 o / absmax), scale[row] = (float)step
  *   else:                code = rne(o / *static_scale) saturated; scale is not written
+ * A group whose mean of u^2 and eps are both 0 has o = 0 w: without eps, too, its codes are 0 (under weights that are finite), beside
+ * other groups as in a row of zeros, whose step size is 1.
  * A NaN counts for nothing in the absmax and has the code +127.  A row of width channels is `groups` groups of consecutive ones: groups = 1
  * and width % 16 = 0, or groups of a multiple of 128; width <= 16384.  x has type dtype, z zdtype (ignored without z), any strides of rows;
  * xq [rows][width]; weight and xq 16-byte aligned, x and z at an element's alignment.  rows may be 0. */

@@ -72,7 +72,8 @@ __device__ __noinline__ double gated_exact(const NormParams<T, Z>& p, i64 row, i
   return p.weight ? v * (double)p.weight[i] : v;
 }
 
-// Codes of a row in binary64: those of the chunks in `near`, or all of them (and the row's step size) if the row is out of binary32's range.
+// Codes of a row in binary64: those of the chunks in `near`, or all of them (and the row's step size) if the row is out of binary32's range
+// (one with a group of zeros is).
 // The absmax in binary64 is that of the chunks in `cand`.  All threads call it, behind their stores.
 // In a row of several groups the quotient is 127 v / v_m times the ratio of the two norms: 1 in the group of the absmax, where ties stay ties.
 struct Top {
@@ -126,7 +127,8 @@ __device__ __noinline__ void exact_row(const NormParams<T, Z>& p, i64 row, uint3
     if (!norms || c >= nchunks) return 1.0;
     double s = 0.0;
     for (int i = c / cpg * cpg; i < c / cpg * cpg + cpg; ++i) s += sum64[i];
-    return 1.0 / sqrt(s / (double)(many ? cpg * 128 : D) + (double)p.eps);
+    const double m = s / (double)(many ? cpg * 128 : D) + (double)p.eps;
+    return m == 0.0 ? 0.0 : 1.0 / sqrt(m);   // (zeros without eps: o = 0)
   };
   Top m = {0.0, 0.0, 1.0};
   if (dynamic) {

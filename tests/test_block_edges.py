@@ -45,6 +45,42 @@ def test_linear_refuses_counts_that_a_tile_would_carry_beyond_32_bits(args):
     assert lib.ssdi8_linear(C.byref(a), 0, None) == bd.ERR_SHAPE
 
 
+# ------------------------------------------------------------------------------------------------ norm
+def _norm(x, z, weight, groups, eps, static=None):
+    import torch
+    from paper_2608_21952_b200 import binding as bd
+    T, D = x.shape
+    xq, sc = torch.full((T, D), 99, dtype=torch.int8, device="cuda"), torch.full((T,), 7.0, device="cuda")
+    bd.ssdi8_norm_quantize(_t(x), xq, weight=None if weight is None else _t(weight), z=None if z is None else _t(z), groups=groups, eps=eps,
+                           scale=sc, static_scale=None if static is None else _t(np.array([static], np.float32)))
+    return _np(xq), _np(sc)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("gate", [False, True])
+@pytest.mark.parametrize("static", [None, 0.03])
+@pytest.mark.parametrize("groups,D", [(1, 512), (2, 512), (4, 8192)])
+def test_norm_without_eps_of_rows_and_groups_of_zeros(groups, D, static, gate):
+    """a group of zeros has o = 0: codes of 0, alone in its row and beside others alike; a whole row of them the step size 1"""
+    rng = np.random.default_rng(D + groups)
+    T = 7
+    x, z = rng.standard_normal((T, D)).astype(np.float32), rng.standard_normal((T, D)).astype(np.float32)
+    weight = rng.uniform(0.5, 1.5, D).astype(np.float32)
+    w = D // groups
+    x[0], x[2, :w], x[3, -w:], x[6, ::2] = 0, 0, 0, 0
+    x[5] *= 1e-30   # (beyond binary32's squares, but no zeros)
+    dead = np.repeat((x.reshape(T, groups, w) == 0).all(-1), w, -1)
+    got, step = _norm(x, z if gate else None, weight, groups, 0.0, static)
+    want, top = ref.norm_codes(x, z if gate else None, weight, groups, 0.0, None if static is None else np.float32(static))
+    want[dead] = 0
+    np.testing.assert_array_equal(got, want)
+    if static is None:
+        top[dead.all(-1)] = 1
+        np.testing.assert_allclose(step, top, rtol=40 * 2.0 ** -24)
+    else:
+        assert np.all(step == 7.0)
+
+
 # ------------------------------------------------------------------------------------------------ cache and token step
 def _other_dims(bd):
     """other heads, other groups, another state size: what a cache of 4 heads of 64 x 64 in 2 groups was not laid out for"""
