@@ -88,13 +88,17 @@ __device__ __noinline__ void exact_row(const NormParams<T, Z>& p, i64 row, uint3
   const int c0 = warp * NCH;   // this warp's chunks
   auto col_of = [&](int k) { return ((c0 + k) * 32 + lane) * 4; };
   if (zero) {
-    // a row of zeros (padding) needs none of it; x that underflowed does
-    bool any = false;
+    // a row of zeros (padding) needs none of it; x that underflowed does, and so does 0 times a weight or over a step that makes it NaN
+    bool any = !dynamic && !(fabsf(*p.static_scale) > 0.f);
 #pragma unroll 1
     for (int k = 0; k < NCH; ++k)
       if (col_of(k) < D) {
         const float4 v = Elem<T>::cvt(load_row4<T>(p.x + row * p.sx + col_of(k), p.valigned));
         any |= v.x != 0.f || v.y != 0.f || v.z != 0.f || v.w != 0.f;
+        if (p.weight) {
+          const float4 w = *reinterpret_cast<const float4*>(p.weight + col_of(k));
+          any |= !(0.f * w.x + 0.f * w.y + 0.f * w.z + 0.f * w.w == 0.f);
+        }
       }
     if (!__syncthreads_or(any)) {
 #pragma unroll 1

@@ -81,6 +81,30 @@ def test_norm_without_eps_of_rows_and_groups_of_zeros(groups, D, static, gate):
         assert np.all(step == 7.0)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("groups", [1, 2])
+def test_norm_of_zeros_under_weights_and_steps_that_are_not_finite(groups):
+    """0 times an infinite or missing weight is NaN, code +127, in a row of zeros as in any other; so is 0 over a step of 0 or NaN"""
+    rng = np.random.default_rng(5)
+    x = rng.standard_normal((4, 256)).astype(np.float32)
+    x[0], x[1, :128] = 0, 0
+    weight = rng.uniform(0.5, 1.5, 256).astype(np.float32)
+    weight[7], weight[9] = np.nan, np.inf
+    got, step = _norm(x[:2], None, weight, groups, 1e-5)
+    want = np.zeros(256, np.int8)
+    want[[7, 9]] = 127
+    np.testing.assert_array_equal(got[0], want)
+    assert step[0] == 1.0 and np.all(got[1, [7, 9]] == 127)
+    got, _ = _norm(x, None, weight, groups, 1e-5, 0.03)
+    with np.errstate(all="ignore"):
+        np.testing.assert_array_equal(got, ref.norm_codes(x, None, weight, groups, 1e-5, np.float32(0.03))[0])
+    for odd in (0.0, np.nan):
+        got, _ = _norm(x, None, None, groups, 1e-5, odd)
+        with np.errstate(all="ignore"):
+            np.testing.assert_array_equal(got, ref.norm_codes(x, None, None, groups, 1e-5, np.float32(odd))[0])
+        assert np.all(got[0] == 127)
+
+
 # ------------------------------------------------------------------------------------------------ cache and token step
 def _other_dims(bd):
     """other heads, other groups, another state size: what a cache of 4 heads of 64 x 64 in 2 groups was not laid out for"""
