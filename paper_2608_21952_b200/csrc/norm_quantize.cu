@@ -241,7 +241,7 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 16 ? 1 : NCH == 2 ? 4 : 3
   if (all) row_values<T, Z, NCH, true>(p, row, col0, t, cs, mx);
   else row_values<T, Z, NCH, false>(p, row, col0, t, cs, mx);
   // sum of squares and absmax of the row, or of its groups (whole chunks each)
-  float r = 0.f, rk[NCH], top = 0.f, total = 0.f;   // 1 / sqrt(mean + eps) of the row or of each chunk's group; absmax of o; sum of squares
+  float r = 0.f, rk[NCH], top = 0.f, total = 0.f;   // 1 / sqrt(mean + eps) of the row (or its groups' largest) or of each chunk's group; absmax of o; sum of squares
   bool range = true;                                // the sums are where binary32 is safe
   auto safe = [](float v) { return v > 1e-30f && v < 1e37f; };
   if (!many) {
@@ -287,14 +287,15 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 16 ? 1 : NCH == 2 ? 4 : 3
       range &= safe(s) && safe(m);
       total += s;
       top = fmaxf(top, m * rg);
+      r = fmaxf(r, rg);
 #pragma unroll
       for (int k = 0; k < NCH; ++k)
         if (c0 + k >= g * cpg && c0 + k < (g + 1) * cpg) rk[k] = rg;
     }
   }
   const float step = dynamic ? top / 127.0f : *p.static_scale;
-  range &= safe(step);
   const float inv = 1.0f / step;
+  range &= safe(step) && r * inv < 1e37f;   // (a larger factor could make infinities of products that are subnormal)
   const float rel = (dynamic ? (many ? 80.f : 28.f) : 42.f) * kEps;
   const float f_row = 127.0f / (top / r);
   uint32_t near = 0, cand = 0;   // bit k: one of the four quotients lies near the middle of two integers; one element can be the row's absmax

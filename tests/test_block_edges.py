@@ -105,6 +105,21 @@ def test_norm_of_zeros_under_weights_and_steps_that_are_not_finite(groups):
         assert np.all(got[0] == 127)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("groups", [1, 2])
+def test_norm_whose_factor_leaves_binary32(groups):
+    """1 / (norm step) of 1e45: the small products are codes between the ends nevertheless"""
+    rng = np.random.default_rng(6)
+    x = (1e-15 * rng.uniform(0.5, 1.5, (3, 512)) * rng.choice([-1, 1], (3, 512))).astype(np.float32)
+    weight = np.ones(512, np.float32)
+    weight[::4] = 1e-28
+    static = np.float32(1.5e-30)
+    want, _ = ref.norm_codes(x, None, weight, groups, 0.0, static)
+    assert np.abs(want[:, ::4]).max() < 127 and np.all(np.abs(want[:, 1::4]) == 127)
+    got, _ = _norm(x, None, weight, groups, 0.0, static)
+    np.testing.assert_array_equal(got, want)
+
+
 # ------------------------------------------------------------------------------------------------ cache and token step
 def _other_dims(bd):
     """other heads, other groups, another state size: what a cache of 4 heads of 64 x 64 in 2 groups was not laid out for"""
