@@ -433,8 +433,10 @@ ENTRY(token_step, 19) {
   const Tensor y = tensor(a[15], "y", kAnyFloat, {B, HP});
   t.y = y.data();
   t.status = tensor(a[16], "status", kInt32, {1}, true).as<int32_t>();
-  const uint32_t fl = flags | (y.dtype == 1 ? SSDI8_FLAG_Y_FP16 : y.dtype == 2 ? SSDI8_FLAG_Y_BF16 : 0);
+  // (y's type comes from the tensor: a flag that says another one is refused, with two of them by the library)
+  const uint32_t own = y.dtype == 1 ? SSDI8_FLAG_Y_FP16 : y.dtype == 2 ? SSDI8_FLAG_Y_BF16 : 0, fl = flags | own;
   void* st = stream(a[18]);
+  if (!own && (flags & (SSDI8_FLAG_Y_FP16 | SSDI8_FLAG_Y_BF16))) return PyLong_FromLong(SSDI8_ERR_UNSUPPORTED);
   return call([&] { return ssdi8_token_step(d.get(), c.get(), &t, fl, st); });
 } END
 

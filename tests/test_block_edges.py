@@ -177,6 +177,25 @@ def _token(bd, c, dev, x, raw, pos, y, dims, slots=None, status=None, flags=0):
                         slots, pos, y, status=status, flags=bd.FLAG_DT_SOFTPLUS | flags)
 
 
+@pytest.mark.gpu
+def test_token_step_refuses_a_type_of_y_that_the_tensor_has_not():
+    """an fp32 y with a flag of 16 bits would hold pairs of values; a flag that says what the tensor is passes"""
+    from paper_2608_21952_b200 import binding as bd
+    c, a, p, dev, x, raw, torch = _token_case(2, 2, 2, 64, 1)
+    pos, d = torch.zeros(2, dtype=torch.int32, device="cuda"), _dims(bd, 2, 1, 2, 64, 64, 1)
+    for t, flag in (("float32", bd.FLAG_Y_BF16), ("float32", bd.FLAG_Y_FP16), ("bfloat16", bd.FLAG_Y_FP16), ("float16", bd.FLAG_Y_BF16)):
+        y = torch.full((2, 128), 5.0, device="cuda").to(getattr(torch, t))
+        with pytest.raises(bd.SSDi8Error) as err:
+            _token(bd, c, dev, x, raw, pos, y, d, flags=flag)
+        assert err.value.code == bd.ERR_UNSUPPORTED and torch.all(y == 5.0)
+    for k, t in c.tensors.items():
+        np.testing.assert_array_equal(_np(t), a[k])
+    same = [torch.empty(2, 128, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    _token(bd, c, dev, x, raw, pos, same[0], d, flags=bd.FLAG_Y_BF16)
+    _token(bd, c, dev, x, raw, pos, same[1], d)
+    assert torch.equal(*same)
+
+
 # ------------------------------------------------------------------------------------------------ status words
 def _us(torch, f, n=20, rounds=5):
     f()
