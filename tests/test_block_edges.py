@@ -196,6 +196,48 @@ def test_token_step_refuses_a_type_of_y_that_the_tensor_has_not():
     assert torch.equal(*same)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("N,G,H", [(64, 2, 6), (128, 1, 9)])
+def test_token_step_adds_a_rows_products_as_integers(N, G, H):
+    """rows whose products cancel: y is off by binary32's error of the sum, not of the products (E scale sum_n C code is exact up to its factors)"""
+    from paper_2608_21952_b200 import binding as bd
+    B = 5
+    c, a, p, dev, x, raw, torch = _token_case(3, B, H, N, G)
+    p["D"][:], p["corr"][:], dev["D"], dev["corr"] = 0, 0, None, None
+    pos = np.array([0, 16, 32, 48, 160], np.int32)   # (the token alone is in the window)
+    u = ref.conv(_np(x)[:, None], p["w"], p["bias"], None, a["ring"].copy(), None, pos)[:, 0]
+    HP, GN = 64 * H, G * N
+    Cq = ref.code(u[:, HP + GN:].reshape(B, G, N) / p["s_C"].astype(np.float64)[:, None]).astype(np.int64)
+    Bq = ref.code(u[:, HP:HP + GN].reshape(B, G, N) / p["s_B"].astype(np.float64)[:, None]).astype(np.int64)
+    xq = ref.code(u[:, :HP] / p["s_x"].astype(np.float64)).reshape(B, H, 64).astype(np.int64)
+    group = np.arange(H) // (H // G)
+    # the code under the largest one of C is what brings a row's sum nearest to 0
+    codes = a["codes"].astype(np.int64)
+    at = np.abs(Cq).argmax(-1)   # [B, G]
+    for b in range(B):
+        for h in range(H):
+            k = at[b, group[h]]
+            big = Cq[b, group[h], k]
+            if big:
+                rest = codes[b, h] @ Cq[b, group[h]] - codes[b, h, :, k] * big
+                codes[b, h, :, k] = np.clip(np.rint(-rest / big), -127, 127)
+    c.tensors["codes"].copy_(_t(codes.astype(np.int8)))
+    y = torch.empty(B, HP, device="cuda")
+    _token(bd, c, dev, x, raw, _t(pos), y, _dims(bd, B, 1, H, 64, N, G))
+    dt = np.stack([_np(c.tensors["dtwin"])[b, :, 0] for b in range(B)]).astype(np.float64)
+    f = lambda k: p[k].astype(np.float64)  # noqa: E731
+    exponent = np.abs(f("A")) * dt
+    sums = np.einsum("bhpn,bhn->bhp", codes, Cq[:, group])
+    off = np.exp(f("A") * dt)[..., None] * a["scales"].astype(np.float64) * sums
+    own = f("s_x").reshape(H, 64) * f("s_B")[group][:, None] * (dt * (Cq * Bq).sum(-1)[:, group])[..., None] * xq
+    sC = f("s_C")[group][:, None]
+    want, size = sC * (off + own), sC * (np.abs(off) + np.abs(own))
+    naive = sC * np.exp(f("A") * dt)[..., None] * a["scales"] * np.einsum("bhpn,bhn->bhp", np.abs(codes), np.abs(Cq[:, group]))
+    bound = 2.0 ** -24 * (32 + exponent)[..., None] * size
+    assert np.median(naive / np.maximum(np.abs(off * sC), 1e-30)) > 50   # (the case is what it says)
+    assert np.all(np.abs(_np(y).reshape(B, H, 64) - want) <= bound)
+
+
 # ------------------------------------------------------------------------------------------------ status words
 def _us(torch, f, n=20, rounds=5):
     f()
