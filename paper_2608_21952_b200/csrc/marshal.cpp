@@ -9,6 +9,8 @@
 
 #include <c10/cuda/CUDAStream.h>
 
+#include <limits>
+
 #include "../../include/ssdi8.h"
 
 namespace {
@@ -45,6 +47,16 @@ long long integer(PyObject* o) {
   const long long v = PyLong_AsLongLong(o);
   if (v == -1 && PyErr_Occurred()) throw BadArgument{};
   return v;
+}
+// a count or a set of flags of 32 bits: what is beyond them is not cut off
+template <typename T>
+T integer32(PyObject* o) {
+  const long long v = integer(o);
+  if (v < (long long)std::numeric_limits<T>::min() || v > (long long)std::numeric_limits<T>::max()) {
+    PyErr_SetString(PyExc_OverflowError, "a number of 32 bits is expected");
+    throw BadArgument{};
+  }
+  return (T)v;
 }
 float real(PyObject* o) {
   const double v = PyFloat_AsDouble(o);
@@ -374,7 +386,7 @@ ENTRY(conv_fwd, 21) {
   c.slots = tensor(a[16], "slots", kInt32, {B}, true).as<int32_t>();
   c.pos = tensor(a[17], "pos", kInt32, {B}, true).as<int32_t>();
   c.status = tensor(a[18], "status", kInt32, {1}, true).as<int32_t>();
-  const uint32_t flags = (uint32_t)integer(a[19]);
+  const uint32_t flags = integer32<uint32_t>(a[19]);
   void* st = stream(a[20]);
   return call([&] { return ssdi8_conv_fwd(d.get(), &c, x.dtype, width, flags, st); });
 } END
@@ -414,7 +426,7 @@ ENTRY(token_step, 19) {
   const int64_t B = d.get()->batch, H = d.get()->nheads, G = d.get()->ngroups, HP = H * d.get()->headdim,
                 Ch = HP + 2 * G * d.get()->dstate;
   const int dtype = c.get()->dtype;
-  const uint32_t flags = (uint32_t)integer(a[17]);
+  const uint32_t flags = integer32<uint32_t>(a[17]);
   ssdi8_token_args_t t = {};
   const Tensor x = tensor(a[2], "xBC", dtype, {B, Ch}, false, true), raw = tensor(a[5], "dt_raw", dtype, {B, H}, false, true);
   t.xBC = x.data(); t.stride_b = x.stride(0);
@@ -450,7 +462,7 @@ ENTRY(norm_quantize, 9) {   // x, xq, weight, z, groups, eps, scale, static_scal
   n.weight = tensor(a[2], "weight", 0, {D}, true).as<float>();
   const Tensor z = tensor(a[3], "z", kAnyFloat, {T, D}, true, true);
   if (z) { n.z = z.data(); n.stride_z = z.stride(0); }
-  n.groups = (int32_t)integer(a[4]);
+  n.groups = integer32<int32_t>(a[4]);
   n.eps = real(a[5]);
   n.scale = tensor(a[6], "scale", 0, {T}, true).as<float>();
   n.static_scale = tensor(a[7], "static_scale", 0, {1}, true).as<float>();
@@ -475,7 +487,7 @@ ENTRY(linear, 10) {   // xq, wq, s_w, out, s_row, bias, residual, act, status, s
   const Tensor r = tensor(a[6], "residual", out.dtype, {T, O}, true, true);
   if (r) { l.residual = r.data(); l.stride_residual = r.stride(0); }
   l.rows = (int32_t)T; l.outs = (int32_t)O; l.inner = (int32_t)K;
-  l.act = (int32_t)integer(a[7]);
+  l.act = integer32<int32_t>(a[7]);
   l.status = tensor(a[8], "status", kInt32, {1}, true).as<int32_t>();
   void* st = stream(a[9]);
   return call([&] { return ssdi8_linear(&l, out.dtype, st); });

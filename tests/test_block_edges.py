@@ -289,3 +289,21 @@ def test_bad_rows_do_not_hide_a_time_out():
             status = torch.tensor([held], dtype=torch.int32, device="cuda")
             call(status)
             assert int(status.item()) == want, (name, held)
+
+
+# ------------------------------------------------------------------------------------------------ the binding
+@pytest.mark.gpu
+def test_numbers_beyond_32_bits_are_refused():
+    """2^32 + 1 groups are not one, nor is a flag or an activation what is left of its low bits"""
+    import torch
+    from paper_2608_21952_b200 import binding as bd
+    x, xq = torch.ones(2, 256, device="cuda"), torch.full((2, 256), 9, dtype=torch.int8, device="cuda")
+    sw, out = torch.ones(2, device="cuda"), torch.full((2, 2), 9.0, device="cuda")
+    c, a, p, dev, t, raw, _ = _token_case(2, 2, 2, 64, 1)
+    pos, y, d = torch.zeros(2, dtype=torch.int32, device="cuda"), torch.full((2, 128), 9.0, device="cuda"), _dims(bd, 2, 1, 2, 64, 64, 1)
+    for call in (lambda: bd.ssdi8_norm_quantize(x, xq, groups=2 ** 32 + 1), lambda: bd.ssdi8_linear(xq, xq, sw, out, act=2 ** 32),
+                 lambda: _token(bd, c, dev, t, raw, pos, y, d, flags=1 << 32),
+                 lambda: bd.ssdi8_conv_fwd(d, t[:, None], dev["w"], out=torch.empty_like(t)[:, None], flags=-(1 << 32))):
+        with pytest.raises(OverflowError):
+            call()
+    assert torch.all(xq == 9) and torch.all(out == 9.0) and torch.all(y == 9.0)
