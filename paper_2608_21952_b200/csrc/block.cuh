@@ -72,23 +72,12 @@ __device__ __forceinline__ float rcp_approx(float x) {
 // The code of SiLU(v) is decided in binary32 wherever that is safe.  With M = |bias| + sum |w_k x_k| and eps = 2^-24:
 //   v, a chain of W <= 4 fused multiply-adds, is off by at most 4 eps M, and SiLU's slope is below 1.1;
 //   exp2(-v log2e): the product is off by 1.5 eps |v log2e|, ex2.approx by 4 eps; 1 + e, rcp.approx, the product with v, the
-//   reciprocal of the step size and the product with it add 1, 2, 1, 1 and 1 eps
-// so the quotient q is off by at most delta = 4.4 eps M / step + (10 + 1.5 |v|) eps |q|.  The kernels allow for
-// 5 eps M / step + (12 + 2 |v|) eps |q|; a quotient that lies nearer than that to the middle of two integers is formed again in
-// binary64.  Step sizes outside [1e-30, 1e30] always are.
+//   reciprocal of the step size and the product with it add 1, 2, 1, 2 and 1 eps
+// so the quotient q is off by at most delta = 4.4 eps M / step + (11 + 1.5 |v|) eps |q|.  A quotient that lies nearer than that to the
+// middle of two integers is formed again in binary64.  What each kernel allows for stands beside it (conv.cu: M and |q| of several
+// tokens at once, a step size that is multiplied into 1 + e; token_step.cu: 5 eps M / step + (14 + 2 |v|) eps |q|).  Step sizes outside
+// [1e-30, 1e30] always go that way.
 constexpr float kEps = 5.9604645e-8f;   // 2^-24
-// out of line: the quotient of a code in binary64.  x, w: W taps
-template <int W>
-__device__ __noinline__ float silu_quotient_exact(float x0, float x1, float x2, float x3, float w0, float w1, float w2, float w3,
-                                                  float bias, float step) {
-  const float x[4] = {x0, x1, x2, x3}, w[4] = {w0, w1, w2, w3};
-  double v = (double)bias;
-#pragma unroll
-  for (int k = 0; k < W; ++k) v = __fma_rn((double)w[k], (double)x[k], v);
-  const double q = v / (1.0 + exp(-v)) / (double)step;
-  // (rounded to an integer here: a second rounding to binary32 must not decide)
-  return (float)rint(fmax(fmin(q, 127.0), -127.0));   // (fmin(NaN, 127) = 127)
-}
 
 // A slot or position that no call may have: the status word becomes SSDI8_ERR_SHAPE.  A time-out stays one (then there is more amiss
 // than a row), whichever of the two a call meets first.

@@ -25,10 +25,10 @@ struct LinearParams {
   void* out; i64 out_stride;
   int32_t* status;
   int T, O, kblocks, mtiles, ntiles, act, vec_out, vec_res;
-  int bn, xrows, stages;   // lone tiles: columns, rows of x in a load, stages of the ring
+  int bn, stages;   // lone tiles: columns, stages of the ring
 };
 
-// Shared memory of a lone tile's CTA: a ring of stages, 128 rows of x (as many loaded as there are) and bn rows of w each.
+// Shared memory of a lone tile's CTA: a ring of stages, 128 rows of x and bn rows of w each.
 struct Layout {
   static constexpr int kMaxBN = 256, kMaxStages = 10;
   static constexpr uint32_t kA = BM * BK, kRing = 196608;
@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(LT, 1) linear_kernel(const __grid_constant__ C
       for (int kb = 0; kb < p.kblocks; ++kb) {
         if (round > 0) mbar_wait(&empty[s], (round - 1) & 1, p.status);
         if (elect_one()) {
-          mbar_expect_tx(&full[s], (uint32_t)(p.xrows + p.bn) * BK);
+          mbar_expect_tx(&full[s], (uint32_t)(BM + p.bn) * BK);
           tma_load_2d(smem + s * stage, &tx, &full[s], kb * BK, m * BM);
           tma_load_2d(smem + s * stage + S::kA, &tw, &full[s], kb * BK, n * p.bn);
         }
@@ -611,14 +611,13 @@ ssdi8_status_t launch_linear(const ssdi8_linear_args_t& a, int dtype, cudaStream
     return dtype == 0 ? go(linear_few_kernel<float>) : dtype == 1 ? go(linear_few_kernel<__half>) : go(linear_few_kernel<__nv_bfloat16>);
   }
   // Lone tiles of 128 x bn or, on pairs of SMs, of 256 x 256: what is done sooner, by waves of tiles and cycles per tile (128 of K
-  // take the tensor pipe 2 bn cycles of a lone tile, their operands 2 (rows + bn) on the SM's way from L2; a pair's 512 take about 640).
+  // take the tensor pipe 2 bn cycles of a lone tile, their operands 2 (128 + bn) on the SM's way from L2; a pair's 512 take about 640).
   // bn is a multiple of 32.
   const i64 mt = (a.rows + BM - 1) / BM;
-  p.xrows = a.rows < BM ? (a.rows + 7) / 8 * 8 : BM;
   double best = 0.0;
   for (int bn = 32; bn <= Layout::kMaxBN; bn += 32) {
     const i64 tiles = mt * ((a.outs + bn - 1) / bn);
-    const double cycles = (double)((tiles + sms - 1) / sms) * ((double)p.kblocks * 2.0 * (p.xrows + bn) + 1500.0 + 12.0 * bn);
+    const double cycles = (double)((tiles + sms - 1) / sms) * ((double)p.kblocks * 2.0 * (BM + bn) + 1500.0 + 12.0 * bn);
     if (best == 0.0 || cycles < best) {
       best = cycles;
       p.bn = bn;
@@ -631,7 +630,7 @@ ssdi8_status_t launch_linear(const ssdi8_linear_args_t& a, int dtype, cudaStream
   p.mtiles = pair ? (a.rows + 255) / 256 : (int)mt;
   p.ntiles = pair ? (a.outs + PBN - 1) / PBN : (a.outs + p.bn - 1) / p.bn;
   CUtensorMap tx, tw;
-  if (!(pair ? maps(&tx, 128, &tw, 128) : maps(&tx, p.xrows, &tw, p.bn))) return SSDI8_ERR_CUDA;
+  if (!(pair ? maps(&tx, 128, &tw, 128) : maps(&tx, BM, &tw, p.bn))) return SSDI8_ERR_CUDA;
   const int stages = (int)(Layout::kRing / (Layout::kA + p.bn * BK));
   p.stages = stages < Layout::kMaxStages ? stages : Layout::kMaxStages;
   auto go = [&](auto lone, auto paired) -> ssdi8_status_t {

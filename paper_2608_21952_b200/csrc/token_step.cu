@@ -38,6 +38,17 @@ struct TokenParams {
   int H, G, hpg, softplus, ydt, b0;   // hpg: heads per group; b0: the launch's first sequence
 };
 
+// The code of a channel in binary64, out of line, by the operations of a prompt's (conv.cu).  Four taps: of fewer, the first ones are 0.
+__device__ __noinline__ float code_exact(float x0, float x1, float x2, float x3, float w0, float w1, float w2, float w3, float bias, float step) {
+  const float x[4] = {x0, x1, x2, x3}, w[4] = {w0, w1, w2, w3};
+  double v = (double)bias;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v = __fma_rn((double)w[k], (double)x[k], v);
+  const double q = v / ((1.0 + exp(-v)) * (double)step);
+  // (rounded to an integer here: a second rounding to binary32 must not decide)
+  return (float)rint(fmax(fmin(q, 127.0), -127.0));   // (fmin(NaN, 127) = 127)
+}
+
 // Two channels of the token, ch and ch + 1 (ch even): what does not depend on the slot, loaded while the slot is on its way
 template <typename T>
 struct alignas(2 * sizeof(T)) Pair { T a, b; };
@@ -83,7 +94,7 @@ struct ChannelPair {
       v = __ffma2_rn(w[k], x, v);
       m = make_float2(fmaf(fabsf(w[k].x), fabsf(x.x), m.x), fmaf(fabsf(w[k].y), fabsf(x.y), m.y));
     }
-    // true: near the middle of two integers (see block.cuh; M is the token's own here, and the step size's reciprocal is off by 2 eps)
+    // true: near the middle of two integers, by 5 eps M / step + (14 + 2 |v|) eps |q| (see block.cuh)
     auto one = [&](float v, float m, float step, float* r) -> bool {
       const float inv = rcp_approx(step);
       const float q = v * rcp_approx(1.0f + ex2_approx(v * -1.44269504f)) * inv;
@@ -95,9 +106,9 @@ struct ChannelPair {
     };
     float r0, r1;
     if (one(v.x, m.x, step.x, &r0))
-      r0 = __uint_as_float(rne_clamp_bits(silu_quotient_exact<4>(xs[0].x, xs[1].x, xs[2].x, x3.x, w[0].x, w[1].x, w[2].x, w[3].x, bias.x, step.x)));
+      r0 = __uint_as_float(rne_clamp_bits(code_exact(xs[0].x, xs[1].x, xs[2].x, x3.x, w[0].x, w[1].x, w[2].x, w[3].x, bias.x, step.x)));
     if (one(v.y, m.y, step.y, &r1))
-      r1 = __uint_as_float(rne_clamp_bits(silu_quotient_exact<4>(xs[0].y, xs[1].y, xs[2].y, x3.y, w[0].y, w[1].y, w[2].y, w[3].y, bias.y, step.y)));
+      r1 = __uint_as_float(rne_clamp_bits(code_exact(xs[0].y, xs[1].y, xs[2].y, x3.y, w[0].y, w[1].y, w[2].y, w[3].y, bias.y, step.y)));
     return __byte_perm(__float_as_uint(r0), __float_as_uint(r1), 0x0040u) & 0xffffu;
   }
 };
