@@ -360,14 +360,16 @@ ssdi8_status_t ssdi8_softplus_dt(const float* dt_raw, const float* dt_bias, int6
  * the call's sequence b; a negative one marks a sequence of padding, whose slot data and outputs are left alone (or cleared,
  * where an entry says so).  A slot or position that no call may have (slots[b] >= nslots, pos[b] < 0) and a slot that an earlier
  * sequence of the same call names already are taken for padding, and *status (if given) becomes SSDI8_ERR_SHAPE, unless it holds
- * SSDI8_ERR_DEVICE_TIMEOUT, which it keeps; it is not written otherwise.  One word may serve calls of every kind; one that
- * holds a time-out is cleared before its next use (waits that meet it give up early). */
+ * SSDI8_ERR_DEVICE_TIMEOUT, which it keeps; a wait that runs out writes that, nothing else is written.  One word may serve
+ * calls of every kind; one that holds a time-out is cleared before its next use (waits that meet it give up early).  Sequences named
+ * twice are found by looking through all slots ahead of each, the batch squared in all. */
 
 /* Causal convolution of a prompt: depthwise, `width` taps (2, 3 or 4), bias, SiLU, and the entry quantiser (Section 4.2,
  * "Quantization of B,C") in one pass over xBC.
  *   v[t,ch] = bias[ch] + sum_k weight[ch][k] xBC[t - width + 1 + k, ch];  u = v / (1 + exp(-v))
  *   codes: xq = rne(u / s_x[ch]), Bq = rne(u / s_B[g]), Cq = rne(u / s_C[g]);  or out = u in xBC's type (xq = NULL)
  *   dt (if given): float(dt_raw), with SSDI8_FLAG_DT_SOFTPLUS softplus(dt_raw + dt_bias) as ssdi8_softplus_dt forms it
+ * out is formed in binary32: within 5 x 2^-24 of |bias| + sum |weight xBC| and (20 + 2 |v|) x 2^-24 of u, ahead of its type's rounding.
  * Sequence b has lens[b] tokens (clamped to [0, seqlen]; NULL: all), the first at position pos[b] (NULL: 0) of the sequence.
  * Tokens ahead of the call come from the ring, row t mod width of its slot for token t; those of negative positions are zeros, so
  * a slot needs no clearing for a new sequence.  The last `width` tokens are left there.  ring = NULL: zeros ahead, nothing is
@@ -424,18 +426,21 @@ ssdi8_status_t ssdi8_cache_write(const ssdi8_dims_t* dims, const ssdi8_cache_t* 
  *   S = E step code + sum_j (w_j s_x s_B x_j) B_j,  E = exp(A sum dt),  w_j = dt_j exp(A sum of the dt behind j)
  * over the waiting tokens j.  first[b] (NULL: as a slot is left by ssdi8_cache_write and ssdi8_token_step, above): position of the first
  * token that the codes do not hold; a window of more than 16 tokens or less than none is taken for padding.  A, s_x, s_B as for the step.
+ * E and w_j are formed in binary64; products and sums are binary32, S within 24 x 2^-24 of the sum of its terms' magnitudes.
  * Padding leaves its rows of state alone.  s_x and state 16-byte aligned. */
 ssdi8_status_t ssdi8_cache_read(const ssdi8_dims_t* dims, const ssdi8_cache_t* cache, const int32_t* slots, const int32_t* first,
                                 const int32_t* pos, const float* A, const float* s_x, const float* s_B, float* state, int32_t* status,
                                 void* stream);
 
 /* One token for every sequence of the batch: the convolution of ssdi8_conv_fwd on the ring, its codes and time step, and the
- * recurrence of ssdi8_ssd_step on the cache, in one launch.  pos[b] tokens of the sequence came before.
+ * recurrence of ssdi8_ssd_step on the cache, in one kernel, and behind it one that folds the windows that have become full (above 65535
+ * sequences, a kernel more for so many).  pos[b] tokens of the sequence came before.
  *   x, B, C: codes as in ssdi8_conv_fwd; the token goes into row pos mod width of the ring and row pos mod 16 of the window
  *   y = s_C (E scale sum_n C[n] code[p,n] + s_x s_B sum_j w_j (C . B_j) x_j[p]) + D s_x x + corr,  the token itself among the j
  *   if pos mod 16 = 15, behind that: S as in ssdi8_cache_read with all 16 tokens, in binary64; scale = (float)(absmax / 127)
  *   (1 if that is 0), code = rne(S / scale) saturated
- * E and w_j as in ssdi8_cache_read; the integer sums are exact.  y [B][H*P] is fp32, or 16-bit with SSDI8_FLAG_Y_FP16 / _BF16;
+ * E and w_j as in ssdi8_cache_read; the integer sums are exact.  In y the exponentials are binary32, of arguments rounded to it, like the
+ * products and sums behind them: within (32 + |A| sum dt) x 2^-24 of the sum of the terms' magnitudes, ahead of y's own rounding.  y [B][H*P] is fp32, or 16-bit with SSDI8_FLAG_Y_FP16 / _BF16;
  * SSDI8_FLAG_DT_SOFTPLUS as in ssdi8_conv_fwd.  Padding leaves its row of y alone.  A slot whose start lies behind pos is
  * taken for padding, with the status.  weight and s_x 16-byte aligned; bias, dt_bias, D, corr may be NULL. */
 typedef struct {
@@ -454,6 +459,7 @@ ssdi8_status_t ssdi8_token_step(const ssdi8_dims_t* dims, const ssdi8_cache_t* c
  *   u = x z / (1 + exp(-z)) (z = NULL: u = x);  o = u w / sqrt(mean over the channel's group of u^2 + eps) (w = NULL: 1)
  *   static_scale = NULL: step = absmax of the row's o / 127 (1 if that is 0), code = rne(127 o / absmax), scale[row] = (float)step
  *   else:                code = rne(o / *static_scale) saturated; scale is not written
+ * The codes are exact, scale[row] is formed in binary32 (within 40 x 2^-24 of step).
  * A group whose mean of u^2 and eps are both 0 has o = 0 w: without eps, too, its codes are 0 (under weights that are finite), beside
  * other groups as in a row of zeros, whose step size is 1.
  * A NaN counts for nothing in the absmax and has the code +127.  A row of width channels is `groups` groups of consecutive ones: groups = 1
@@ -470,9 +476,10 @@ ssdi8_status_t ssdi8_norm_quantize(const ssdi8_norm_args_t* args, int32_t dtype,
 
 /* Int8 projection (the in-proj and out-proj of the block, W8A8) with everything behind the product in its epilogue:
  *   acc[t,o] = sum_k xq[t,k] wq[o,k], INT32, exact;  out = act(s_row[t] s_w[o] acc + bias[o]) + residual[t,o]
- * in binary32, rounded once to out's type.  act: SSDI8_ACT_NONE, v / (1 + exp(-v)) (_SILU), max(v, 0)^2 (_RELU2).  xq [rows][inner],
- * wq [outs][inner] (step sizes s_w per output), dense and 16-byte aligned; inner % 16 = 0, 16 <= inner <= 131072 (the sums stay in
- * 32 bits).  s_row, bias, residual may be NULL (1, 0, 0): the paper adds its mean correction at the out-proj (Section 4.3), which is `bias`
+ * in binary32, rounded once to out's type (SiLU within (10 + 1.5 |v|) x 2^-24 of its value, 0 where exp(-v) leaves binary32, from about
+ * v = -87 down).  act: SSDI8_ACT_NONE, v / (1 + exp(-v)) (_SILU), max(v, 0)^2 (_RELU2).  xq [rows][inner],
+ * wq [outs][inner] (step sizes s_w per output), dense and 16-byte aligned; inner % 16 = 0, 16 <= inner <= 131072 (sums of codes from -127
+ * to 127, Eq. 1's, stay in 32 bits; -128 on both sides passes them by one at 131072).  s_row, bias, residual may be NULL (1, 0, 0): the paper adds its mean correction at the out-proj (Section 4.3), which is `bias`
  * here.  out, residual: type dtype, any strides of rows (out's at least outs); residual may be out itself.  rows may be 0; rows and outs
  * up to 2^31 - 256. */
 enum { SSDI8_ACT_NONE = 0, SSDI8_ACT_SILU = 1, SSDI8_ACT_RELU2 = 2 };

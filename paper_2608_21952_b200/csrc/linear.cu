@@ -4,9 +4,11 @@
 // next tile's is formed in the other.  Three forms: tiles for pairs of SMs where they are done sooner, lone tiles, and up to 128 rows.
 //
 // What bounds it: 16384 x 2560 x 5120 with bias and residual (95 us at the 4.5 POPS that the pipe reaches on resident operands, 41 us of bytes)
-// takes 145 to 153 us on inputs that stay (3.0 POPS; 135 without the residual) and 177 on inputs that do not, in a row of calls under the power limit: the
+// takes 145 to 153 us on inputs that stay (3.0 POPS; 135 without the residual) and 177 to 186 on inputs that do not, in a row of calls under the power limit: the
 // operands' 64 bytes a cycle and SM from L2, which is what an SM's port gives, and the clock.  64 x 10576 x 2560 (28.5 MB, 4.4 us): 9.0 us, 3.4 of them
 // operands from L2 at 11 TB/s (the tokens are read by every tile), then the parts' meeting and the epilogue, 2 us each.
+// From 129 to about 1000 rows a lone tile walks all of K on as many CTAs as there are tiles: 250 x 4096 x 8192 (5.8 us of bytes) 18.9 us, 250 x 18560 x
+// 4096 (13.4) 24, 600 x 2560 x 5120 (3.5) 15.  Rows of out off 16-byte boundaries leave as single elements: 3439 x 16470 x 1232, fp16, residual (39) 284.
 #include "block.cuh"
 #include "kernels.h"
 #include "sm100.cuh"
@@ -76,7 +78,7 @@ __device__ __forceinline__ void tile_of(int tile, int mtiles, int ntiles, int* m
 // A quarter's 32 rows (lanes) of `ncols` columns of an accumulator: t is this lane's row, n0 the first column, cw and cb the
 // columns' step sizes and biases; `drained` is called once the last column has been read.  Rows of out (and residual) on 16-byte
 // boundaries are written by their lane, 32 columns at a time; others, and a ragged end, go through `turn` (32 x 17 floats of the
-// warp's), 16 columns at a time, so that lanes stand beside one another in a row (3439 x 16470 x 1232, fp16, residual: 985 us one by one, 287).
+// warp's), 16 columns at a time, so that lanes stand beside one another in a row (3439 x 16470 x 1232, fp16, residual: 985 us one by one, 284).
 // The residual of 32 columns is on its way while the 32 before it are finished, the first of them while the accumulator is; `ready` waits
 // for that.
 constexpr int kTurn = 32 * 17;

@@ -1,6 +1,7 @@
 // Argument marshalling of the Python binding (paper_2608_21952_b200/binding.py): torch tensors and ctypes structures
 // to the pointers the C entry points take, the current stream, the call with the interpreter lock released.  No
-// arithmetic and no checks beyond the ones a pointer needs (a contiguous CUDA tensor, the right ctypes structure).
+// arithmetic and no checks beyond the ones a pointer needs (a contiguous CUDA tensor, the right ctypes structure; for the operators
+// around the layer, which take their sizes from the tensors and the cache, those too).
 // Why native: through ctypes a call with a dozen tensors took 9 to 13 us of host time (0.25 us per tensor for
 // its type checks and address, 3.4 us for the stream object) ahead of a launch of 3 us, more than the device time of
 // a decode step of one sequence (7 us for its three calls); from here a call takes 3.5 to 4 us, launch included, and

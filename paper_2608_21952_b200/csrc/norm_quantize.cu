@@ -8,8 +8,13 @@
 // the sum, halved; 3).  A quotient that lies nearer than that to the middle of two integers is formed again in binary64, from the row's
 // absmax in binary64 (of the few elements that can be it) and, where it does not cancel, the norm in binary64.  Rows whose sums leave
 // binary32's range have all of their codes formed so.
+// Such quotients are few, but one sends its row to binary64, whose norm (groups, static steps) is formed from all of the row's elements, one after
+// the other by each thread: of rows of 5120 in one group 2 % go there, with a static step 13 to 20 %, of rows of 8192 in 8 groups 11 to 17 %, with a
+// static step 25 % (normal values and 1 % outliers of 20, with the gate and without).  That is what bounds these: 16384 x 5120 with a
+// static step 219 us, 10000 x 8192 in 8 groups (fp32 and a bf16 gate, 89 us of bytes) 305, both 358; and of 64 x 5120 (bf16, gated), 8.1 us on
+// the device where a row of the 64 goes there (11 of 16 draws) and 2.7 where none does.
 //
-// What bounds it: 16384 rows of 5120 (fp32 and a bf16 gate, 587 MB: 90 us at the copy rate) take 122 us: 30 instructions an element, two of them
+// What bounds the others: 16384 rows of 5120 (fp32 and a bf16 gate, 587 MB: 91 us at the copy rate) take 122 to 129 us: 30 instructions an element, two of them
 // on the quarter-rate pipe (the exponential and the reciprocal), with three to five blocks to an SM (80 registers; 64 take 129 us with five
 // chunks to a warp, 48 spill: 140).
 // Codes and exact path in one body took 292 us, one element after the other; pairs, with the exact path out of line, 144; chunks of a warp side

@@ -1,7 +1,7 @@
 // Writing states into the 8-bit cache and reading them back.  Both stream: the fp32 state is 4 of the 5 bytes per element that
 // have to move (write: one pass, the row in registers between its absmax and its codes; read: codes in, fp32 out, with the
 // waiting tokens as up to 16 rank-one updates in registers).  Write, 8 sequences x 80 heads (26 MB, 4 us at the copy rate): 7.2 us, most of it one
-// round trip and the launch.  Read, 37 x 128 heads with half-filled windows (200 MB, 30 us): 48, the chain slot, window, weights, operands ahead of a
+// round trip and the launch.  Read, 37 x 128 heads with half-filled windows (198 MB, 31 us): 47, the chain slot, window, weights, operands ahead of a
 // block's stores with 32 warps to an SM (operands written by lanes of one bank 77; eight single loads of x a token where two do 57).
 #include "kernels.h"
 #include "state_cache.cuh"

@@ -4,10 +4,11 @@
 // (ChunkScan1 and ChunkScan2 of Algorithm 2 for a single row, with int8 dot products), a quarter of the fp32 state's bytes one way
 // instead of two.  Once in 16 tokens the full window is folded into the codes, as in binary64, by a second kernel.
 //
-// What bounds it: 64 sequences x 80 heads (53 MB, 8.2 us at the copy rate) take 16.5 us without full windows, 250 x 128 (335 MB, 51 us) 94: about
-// 760 instructions a warp, half of them the convolution of B and C, which every block of heads does for itself, and the chain of a block (slot, ring,
-// codes, weights of the window, y: 10 thousand cycles) with 27 warps to an SM.  The fp32 state's step (ssd_step.cu) with its two
-// kernels ahead takes 58.8 for the first.  With one sequence in 16 folding, 31 and 145 us: a fold is about 1700 instructions a warp.
+// What bounds it: 64 sequences x 80 heads (53 MB, 8.3 us at the copy rate) take 22 us without full windows (16 where the slots stay in L2 from call
+// to call), 250 x 128 (335 MB, 52 us) 93: about 760 instructions a warp, half of them the convolution of B and C, which every block of heads does for
+// itself, and the chain of a block (slot, ring, codes, weights of the window, y: 10 thousand cycles) with 27 warps to an SM.  The fp32 state's step (ssd_step.cu) with its two
+// kernels ahead takes 58.8 for the first.  With one sequence in 16 folding, 31 to 36 and 134 to 145 us
+// (all of them: 129 and 757): a fold is about 1700 instructions a warp, and its kernel starts when the last block of the step has ended.
 #include "kernels.h"
 #include "sm100.cuh"
 #include "state_cache.cuh"
@@ -584,7 +585,7 @@ ssdi8_status_t launch(const Dims& d, const ssdi8_cache_t& c, const ssdi8_token_a
   const int sms = sm_count();
   if (sms <= 0) return SSDI8_ERR_CUDA;
   // Eight heads to a block (three of them per SM) from a full wave on, four (four per SM) below that.  Steps without full windows, eight /
-  // four / two heads, us: 250 x 128 heads 92.9 / 97.5 / 141, 64 x 80 16.8 / 19.1 / 27.
+  // four / two heads, us: 250 x 128 heads 92.9 / 97.5 / 141, 64 x 80 (slots that stay in L2) 16.8 / 19.1 / 27.
   const bool eight = p.hpg > 4 && (i64)d.b * d.G * ((p.hpg + 7) / 8) >= 3 * sms;
   const ssdi8_status_t s = eight ? pick(std::integral_constant<int, 8>{}) : pick(std::integral_constant<int, 4>{});
   if (s != SSDI8_OK) return s;
