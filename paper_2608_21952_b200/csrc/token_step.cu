@@ -6,8 +6,8 @@
 //
 // What bounds it: 64 sequences x 80 heads (53 MB, 8.3 us at the copy rate) take 22 us without full windows (16 where the slots stay in L2 from call
 // to call), 250 x 128 (335 MB, 52 us) 93: about 760 instructions a warp, half of them the convolution of B and C, which every block of heads does for
-// itself, and the chain of a block (slot, ring, codes, weights of the window, y: 10 thousand cycles) with 27 warps to an SM.  The fp32 state's step (ssd_step.cu) with its two
-// kernels ahead takes 58.8 for the first.  With one sequence in 16 folding, 31 to 36 and 134 to 145 us
+// itself, and the chain of a block (slot, ring, codes, weights of the window, y: 10 thousand cycles) with 27 warps to an SM.  The fp32
+// state's step (ssd_step.cu) with its two kernels ahead takes 58.8 for the first.  With one sequence in 16 folding, 31 to 36 and 134 to 145 us
 // (all of them: 129 and 757): a fold is about 1700 instructions a warp, and its kernel starts when the last block of the step has ended.
 #include "kernels.h"
 #include "sm100.cuh"
