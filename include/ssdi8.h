@@ -441,8 +441,8 @@ ssdi8_status_t ssdi8_cache_read(const ssdi8_dims_t* dims, const ssdi8_cache_t* c
  *   (1 if that is 0), code = rne(S / scale) saturated
  * E and w_j as in ssdi8_cache_read; the integer sums are exact.  In y the exponentials are binary32, of arguments rounded to it, like the
  * products and sums behind them: within (32 + |A| sum dt) x 2^-24 of the sum of the terms' magnitudes, ahead of y's own rounding.
- * y [B][H*P] is fp32, or 16-bit with SSDI8_FLAG_Y_FP16 / _BF16; SSDI8_FLAG_DT_SOFTPLUS as in ssdi8_conv_fwd.  Padding leaves its row of y alone.  A slot whose start lies behind pos is
- * taken for padding, with the status.  weight and s_x 16-byte aligned; bias, dt_bias, D, corr may be NULL. */
+ * y [B][H*P] is fp32, or 16-bit with SSDI8_FLAG_Y_FP16 / _BF16; SSDI8_FLAG_DT_SOFTPLUS as in ssdi8_conv_fwd.  Padding leaves its row of
+ * y alone.  A slot whose start lies behind pos is taken for padding, with the status.  weight and s_x 16-byte aligned; bias, dt_bias, D, corr may be NULL. */
 typedef struct {
   const void* xBC; int64_t stride_b;          /* [B][Ch], the ring's type */
   const float* weight; const float* bias;     /* [Ch][width], [Ch]        */
@@ -480,7 +480,8 @@ ssdi8_status_t ssdi8_norm_quantize(const ssdi8_norm_args_t* args, int32_t dtype,
  * v = -87 down).  act: SSDI8_ACT_NONE, v / (1 + exp(-v)) (_SILU), max(v, 0)^2 (_RELU2).  xq [rows][inner],
  * wq [outs][inner] (step sizes s_w per output), dense and 16-byte aligned; inner % 16 = 0, 16 <= inner <= 131072 (sums of codes from -127
  * to 127, Eq. 1's, stay in 32 bits; -128 on both sides passes them by one at 131072).  s_row, bias, residual may be NULL (1, 0, 0): the
- * paper adds its mean correction at the out-proj (Section 4.3), which is `bias` here.  out, residual: type dtype, any strides of rows (out's at least outs); residual may be out itself.  rows may be 0; rows and outs
+ * paper adds its mean correction at the out-proj (Section 4.3), which is `bias` here.
+ * out, residual: type dtype, any strides of rows (out's at least outs); residual may be out itself.  rows may be 0; rows and outs
  * up to 2^31 - 256. */
 enum { SSDI8_ACT_NONE = 0, SSDI8_ACT_SILU = 1, SSDI8_ACT_RELU2 = 2 };
 typedef struct {
