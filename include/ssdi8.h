@@ -494,6 +494,77 @@ typedef struct {
 } ssdi8_linear_args_t;
 ssdi8_status_t ssdi8_linear(const ssdi8_linear_args_t* args, int32_t dtype, void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Projections in four bits, and the norm ahead of a block's projection.  (The paper's weights and activations have 8 bits; its block,
+ * Figure 1(a), and Eq. 1's symmetric uniform step are what these follow, with a scale per block of columns in place of one per row.)
+ *
+ * A matrix in four bits: the value of column k of row t is  c scale[t][k / block] step[t]  with a code c of +-{0, 0.5, 1, 1.5, 2, 3, 4, 6} (e2m1:
+ * sign, two bits of exponent, one of fraction), two to a byte, the even column's in the low half.  block 16: scales in e4m3 (up to 448); block 32: powers
+ * of two (e8m0, 2^(byte - 127)).  Scales stand in tiles of 128 rows and 4 blocks, 512 bytes each, the tiles of a row block beside one another: the
+ * byte of row t and block b is at ((t / 128) ceil(width / block / 4) + b / 4) 512 + (t % 32) 16 + (t % 128 / 32) 4 + b % 4.  Tiles are
+ * whole: ssdi8_fp4_scales_bytes of them, more if the array was made for more rows.  Bytes of blocks behind a row's last one are 0 (the quantisers write
+ * them so; any number would do that is not the NaN of its type); those of rows behind the last are left alone.
+ * step NULL: 1.  rows >= 0; width % 32 = 0, 32 <= width <= 131072; codes, scales 16-byte aligned. */
+typedef struct {
+  int32_t rows, width, block;   /* block: 16 or 32                 */
+  uint8_t* codes;               /* [rows][width / 2]               */
+  uint8_t* scales;              /* tiles of 512 bytes              */
+  float* step;                  /* [rows] or NULL                  */
+} ssdi8_fp4_t;
+/* host, pure: bytes of a matrix's scales (0 if the sizes are unsupported, or without rows) */
+size_t ssdi8_fp4_scales_bytes(int32_t rows, int32_t width, int32_t block);
+
+/* Quantiser of rows p = x (type dtype, any stride of rows; an element's alignment) into q, e2m1 and e4m3 rounded to nearest, ties to even:
+ *   block 16: g = fdiv(absmax of the row, 2688) with the low 8 bits of its significand cleared (1 if that is 0; 2688 = 6 x 448)
+ *             scale = e4m3 of max(absmax of the block / (6 g), 2^-9), code = e2m1 of p / (g scale), step = g
+ *   block 32: scale = the least power of two s from 2^-127 to 2^127 with absmax of the block <= 6 s (1 if that absmax is 0),
+ *             code = e2m1 of p / scale, step = 1 (if given)
+ * Quotients are exact ones (g has 16 bits so that their middles are binary32 numbers; for rows whose absmax lies below 2e-32, where these are
+ * subnormal, g scale and the quotient are each rounded to binary32).  Beyond 6 a code is 6.  A NaN counts for nothing in an absmax and has the code
+ * +6; in a row (block 16) or block (32) with an infinity other codes are 0.  q.step is needed with block 16. */
+ssdi8_status_t ssdi8_fp4_quantize(const void* x, int64_t stride_x, int32_t dtype, const ssdi8_fp4_t* q, void* stream);
+/* The values of a matrix in four bits: out[t,k] = fmul(c scale, step), rounded once more to out's type (any stride of rows, at least width). */
+ssdi8_status_t ssdi8_fp4_dequantize(const ssdi8_fp4_t* q, void* out, int64_t stride_out, int32_t dtype, void* stream);
+
+/* The residual stream's addition and the RMS norm ahead of a block's projection, ending in the projection's operand:
+ *   h = fadd(x, residual), rounded to the stream's type and written to residual_out (either may be NULL: h = x, nothing is written; with neither,
+ *       h = x as it is);   p = fmul(h, w) (w = NULL: 1);   r = 1 / sqrt(mean over the row of h^2 + eps), in binary64
+ *   int8 (xq):          a = fdiv(absmax of p, 127) (1 if that is 0), code = rne(fdiv(p, a)) saturated, scale = (float)(a r) (1 if a was 0)
+ *   with static_scale:  code = rne(fdiv(fmul(p, (float)r), *static_scale)) saturated; scale is not written
+ *   four bits (fp4):    codes and scales of p as ssdi8_fp4_quantize has them, step = (float)(its step x r) (1 for a row of zeros)
+ * so the factor r, the same for a row, meets no code but the static ones.  A NaN has the code +127 (+6) and makes r one, and with it scale or step.
+ * x has type dtype; residual and residual_out rdtype: x's or fp32 (0); any strides of rows, an element's alignment.  residual_out may be residual, or x
+ * where their types are the same.  Exactly one of xq and fp4 is given; width <= 16384, and width % 16 = 0 (xq) or fp4's own (% 32).  weight and
+ * xq 16-byte aligned.  rows may be 0.  (The gated norm behind the scan is ssdi8_norm_quantize; a residual that the projection before has added
+ * already, in ssdi8_linear or ssdi8_fp4_linear, is not given here.) */
+typedef struct {
+  const void* x; int64_t stride_x;
+  const void* residual; int64_t stride_residual;
+  void* residual_out; int64_t stride_out;
+  const float* weight;            /* [width] or NULL                */
+  int8_t* xq; float* scale;       /* [rows][width], [rows] or NULL  */
+  const float* static_scale;      /* 1 word on the DEVICE, or NULL  */
+  const ssdi8_fp4_t* fp4;         /* HOST: of the same rows and width, with its step; or NULL */
+  int64_t rows; int32_t width; float eps;
+} ssdi8_add_norm_args_t;
+ssdi8_status_t ssdi8_add_norm_quantize(const ssdi8_add_norm_args_t* args, int32_t dtype, int32_t rdtype, void* stream);
+
+/* Projection in four bits with everything behind the product in its epilogue:
+ *   out[t,o] = act(step_x[t] step_w[o] sum_k x[t,k] w[o,k] + bias[o]) + residual[t,o],  x and w without their step sizes in the sum
+ * Products (codes and scales) are exact, their sums binary32 as the tensor cores form them (in an order that the sizes decide, the same on every call: within
+ * width x 2^-24 of the sum of the products' magnitudes); the rest is binary32, rounded once to out's type, act as in ssdi8_linear.
+ * x [rows][inner] and w [outs][inner] have the same width and block.  out, residual: type dtype, any strides of rows (out's at least outs), an
+ * element's alignment; residual may be out itself.  rows may be 0; rows and outs up to 2^31 - 256. */
+typedef struct {
+  const ssdi8_fp4_t* x; const ssdi8_fp4_t* w;                /* HOST: activations, weight */
+  const float* bias;                                         /* [outs] or NULL */
+  const void* residual; int64_t stride_residual;
+  void* out; int64_t stride_out;
+  int32_t act;
+  int32_t* status;                                           /* 1 word, or NULL: SSDI8_ERR_DEVICE_TIMEOUT if a wait ran out */
+} ssdi8_fp4_linear_args_t;
+ssdi8_status_t ssdi8_fp4_linear(const ssdi8_fp4_linear_args_t* args, int32_t dtype, void* stream);
+
 /* Measurement aid (the paper has no counterpart): what tcgen05.mma.kind::i8 sustains on the current
  * device, for the "fraction of the int8 tensor-pipe peak" a benchmark reports.  One CTA per SM issues
  * `mma_per_sm` (rounded down to a multiple of 128, at least 128) dense MMAs of M 128 x N 256 x K 32

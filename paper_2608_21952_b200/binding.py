@@ -49,7 +49,8 @@ EXPORTS = ("ssdi8_status_string", "ssdi8_workspace_bytes", "ssdi8_quantize_act",
            "ssdi8_layer_fwd_host", "ssdi8_layer_fwd_host_scratch_bytes",
            "ssdi8_int8_mma_peak", "ssdi8_selftest_bounded_wait", "ssdi8_softplus_dt",
            "ssdi8_conv_fwd", "ssdi8_cache_write", "ssdi8_cache_read", "ssdi8_token_step",
-           "ssdi8_norm_quantize", "ssdi8_linear")
+           "ssdi8_norm_quantize", "ssdi8_linear",
+           "ssdi8_fp4_scales_bytes", "ssdi8_fp4_quantize", "ssdi8_fp4_dequantize", "ssdi8_add_norm_quantize", "ssdi8_fp4_linear")
 STATIC_WORKSPACE_BYTES = 16 << 20
 CACHE_WINDOW = 16
 ACT_NONE, ACT_SILU, ACT_RELU2 = 0, 1, 2
@@ -87,7 +88,12 @@ class Cache(C.Structure):
         [(k, C.c_void_p) for k in ("codes", "scales", "xwin", "Bwin", "dtwin", "start", "ring")]
 
 
-_m.init(Dims, FwdArgs, LayerArgs, Cache, C.Structure.__base__, C.ArgumentError)
+class Fp4(C.Structure):
+    """A matrix in four bits (ssdi8_fp4_t); made by fp4_of or make_fp4, which keep the tensors with it."""
+    _fields_ = [(k, C.c_int32) for k in ("rows", "width", "block")] + [(k, C.c_void_p) for k in ("codes", "scales", "step")]
+
+
+_m.init(Dims, FwdArgs, LayerArgs, Cache, Fp4, C.Structure.__base__, C.ArgumentError)
 
 
 _lib.ssdi8_status_string.restype = C.c_char_p
@@ -378,6 +384,85 @@ def ssdi8_linear(xq, wq, s_w, out, s_row=None, bias=None, residual=None, act: in
     code = _m.linear(xq, wq, s_w, out, s_row, bias, residual, act, status, stream)
     if code:
         _check(code, "ssdi8_linear")
+
+
+# ---- projections in four bits
+_lib.ssdi8_fp4_scales_bytes.restype = C.c_size_t
+_lib.ssdi8_fp4_scales_bytes.argtypes = [C.c_int32] * 3
+
+
+def ssdi8_fp4_scales_bytes(rows: int, width: int, block: int = 16) -> int:
+    return int(_lib.ssdi8_fp4_scales_bytes(rows, width, block))
+
+
+def _fp4_tiles(rows: int, width: int, block: int):
+    """shape of a matrix's scales: tiles of 128 rows and 4 blocks, row 32 i + j of a tile with its four bytes at [j][i]"""
+    return -(-rows // 128), -(-(width // block) // 4), 32, 4, 4
+
+
+def fp4_of(codes, scales, step=None, block: int = 16) -> Fp4:
+    """The matrix in four bits that these tensors hold: codes uint8 [rows, width / 2], scales uint8 [tiles of rows (more are left alone),
+    tiles of blocks, 32, 4, 4], step fp32 [rows] or None for ones."""
+    if codes.dim() != 2 or block not in (16, 32):
+        raise SSDi8Error(ERR_SHAPE, "fp4_of: codes are [rows, width / 2], a block is 16 or 32 columns")
+    rows, width = codes.shape[0], 2 * codes.shape[1]
+    if width % 32 or not 32 <= width <= 131072:
+        raise SSDi8Error(ERR_SHAPE, f"fp4_of: a width of {width} is not a multiple of 32 up to 131072")
+    tiles = _fp4_tiles(rows, width, block)
+    if scales.dim() != 5 or scales.shape[0] < tiles[0] or tuple(scales.shape[1:]) != tiles[1:]:
+        raise SSDi8Error(ERR_SHAPE, f"fp4_of: scales is {tuple(scales.shape)}, not {tiles}")
+    if step is not None and tuple(step.shape) != (rows,):
+        raise SSDi8Error(ERR_SHAPE, f"fp4_of: step is {tuple(step.shape)}, not {(rows,)}")
+    q = Fp4(rows=rows, width=width, block=block)
+    for name, t, dtype in (("codes", codes, torch.uint8), ("scales", scales, torch.uint8), ("step", step, torch.float32)):
+        if t is None:
+            continue
+        if t.dtype != dtype:
+            raise TypeError(f"{name} has the wrong element type")
+        if t.device != codes.device:
+            raise ValueError(f"{name} lives on another device than codes")
+        setattr(q, name, _ptr(t))
+    q.device = codes.device.index   # (compared with the current device by every call)
+    q.tensors = {"codes": codes, "scales": scales, "step": step}   # (the struct holds raw pointers: they stay alive with it)
+    return q
+
+
+def make_fp4(rows: int, width: int, block: int = 16, device="cuda") -> Fp4:
+    """An empty matrix in four bits (zeros) with its tensors in `.tensors`."""
+    if width % 32 or width < 32 or block not in (16, 32):
+        raise SSDi8Error(ERR_SHAPE, "make_fp4")
+    z = lambda *shape: torch.zeros(shape, dtype=torch.uint8, device=device)  # noqa: E731
+    return fp4_of(z(rows, width // 2), z(*_fp4_tiles(rows, width, block)), torch.ones(rows, device=device), block)
+
+
+def ssdi8_fp4_quantize(x, q: Fp4, stream=None) -> None:
+    """x [rows, width] (rows of any stride; fp32, fp16 or bf16) into a matrix in four bits."""
+    code = _m.fp4_quantize(x, q, stream)
+    if code:
+        _check(code, "ssdi8_fp4_quantize")
+
+
+def ssdi8_fp4_dequantize(q: Fp4, out, stream=None) -> None:
+    """The values of a matrix in four bits into out [rows, width]."""
+    code = _m.fp4_dequantize(q, out, stream)
+    if code:
+        _check(code, "ssdi8_fp4_dequantize")
+
+
+def ssdi8_add_norm_quantize(x, residual=None, residual_out=None, weight=None, eps: float = 1e-5, xq=None, scale=None, static_scale=None,
+                            fp4=None, stream=None) -> None:
+    """h = x + residual [T, D] (rows of any stride) into residual_out, and the RMS norm of h to int8 codes xq with a step size per row in
+    `scale` (or under a static one), or to a matrix in four bits."""
+    code = _m.add_norm_quantize(x, residual, residual_out, weight, eps, xq, scale, static_scale, fp4, stream)
+    if code:
+        _check(code, "ssdi8_add_norm_quantize")
+
+
+def ssdi8_fp4_linear(x: Fp4, w: Fp4, out, bias=None, residual=None, act: int = ACT_NONE, status=None, stream=None) -> None:
+    """out [T, O] = act(x [T, K] w [O, K]^T + bias) + residual of matrices in four bits (rows of out and residual of any stride)."""
+    code = _m.fp4_linear(x, w, out, bias, residual, act, status, stream)
+    if code:
+        _check(code, "ssdi8_fp4_linear")
 
 
 def ssdi8_int8_mma_peak(mma_per_sm: int, status=None, stream=None) -> float:

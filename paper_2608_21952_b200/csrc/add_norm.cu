@@ -1,0 +1,341 @@
+// Rows to codes: the residual stream's addition and the RMS norm behind it, h = x + residual, p = h w, ending in int8 codes or in four bits;
+// the same without addition and norm (p = x) as the quantiser of matrices in four bits; and the values of such a matrix.
+//
+// One pass: every thread keeps eight columns of up to four chunks in registers between the row's two reductions (sum of squares in binary64,
+// absmax of p; one exchange through shared memory) and the codes.  The norm's factor r never meets a code: it is the same for the row, so it
+// goes into the row's step size (with a static step size it does, once per element).  So the sum need not be formed ahead of the codes' arithmetic, and codes
+// are functions of p alone.  In binary64 the sum cannot leave its range and costs no time that the loads do not: two instructions an element on
+// a pipe that nothing else uses.
+#include "fp4.cuh"
+#include "kernels.h"
+
+#include <type_traits>
+
+namespace ssdi8 {
+namespace {
+
+constexpr int kChunk = 256;   // columns of a chunk: a warp's lanes have eight each, so that a block of 16 is two lanes and one of 32 four
+
+struct None {};   // no residual stream
+
+struct RowParams {
+  const void* x; i64 sx;
+  const void* residual; i64 sr;
+  void* stream; i64 ss;
+  const float* weight;
+  const float* static_scale;
+  int8_t* xq; float* scale;                  // int8: codes, step sizes (or NULL)
+  uint8_t *codes, *scales; float* step;      // four bits
+  int D, block, tiles;
+  bool vx, vr, vs;                           // rows on 16 bytes (16-bit elements), 16 bytes (fp32)
+  float eps;
+};
+
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, bool aligned, float (&v)[8]) {
+  if (aligned) {
+    if constexpr (sizeof(T) == 4) {
+      const float4 a = __ldcs(reinterpret_cast<const float4*>(p)), b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
+      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    } else {
+      const uint4 q = __ldcs(reinterpret_cast<const uint4*>(p));
+      const float4 a = Elem<T>::cvt(make_uint2(q.x, q.y)), b = Elem<T>::cvt(make_uint2(q.z, q.w));
+      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = Elem<T>::get(p[i]);
+  }
+}
+// rounds to T, in place, and stores (p = NULL: does not)
+template <typename T>
+__device__ __forceinline__ void store8(T* p, bool aligned, float (&v)[8]) {
+  if constexpr (sizeof(T) == 4) {
+    if (!p) return;
+    if (aligned) {
+      reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+      reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) p[i] = v[i];
+    }
+  } else {
+    const uint2 a = Elem<T>::pack(make_float4(v[0], v[1], v[2], v[3])), b = Elem<T>::pack(make_float4(v[4], v[5], v[6], v[7]));
+    if (!p) {
+    } else if (aligned) {
+      *reinterpret_cast<uint4*>(p) = make_uint4(a.x, a.y, b.x, b.y);
+    } else {
+      const uint32_t w[4] = {a.x, a.y, b.x, b.y};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) reinterpret_cast<uint16_t*>(p)[i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+    }
+    const float4 f = Elem<T>::cvt(a), g = Elem<T>::cvt(b);
+    v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w; v[4] = g.x; v[5] = g.y; v[6] = g.z; v[7] = g.w;
+  }
+}
+
+__device__ __forceinline__ float warp_max(float v) {   // of numbers >= 0; a NaN counts for nothing
+  float m;
+  asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(v));
+  return m;
+}
+__device__ __forceinline__ float absmax8(const float (&v)[8]) {
+  float m = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(v[i]));
+  return m;
+}
+
+// Codes and scales in four bits of a chunk's eight columns of this lane (`live`: inside the row); m is their absmax, g the row's step size.
+// All lanes of the warp call it.  Bytes of a tile's blocks behind the row's end are 0.
+__device__ __forceinline__ void chunk_fp4(const RowParams& p, i64 row, int chunk, bool live, const float (&v)[8], float m, float g) {
+  const int lane = threadIdx.x & 31, col = chunk * kChunk + lane * 8;
+  m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
+  uint32_t s, word, codes;
+  int tile;
+  if (p.block == 16) {
+    s = fp4_scale16(m, g);
+    codes = fp4_codes16(v, __fmul_rn(g, e4m3_to(s)));
+    s = live ? s : 0u;
+    word = s | __shfl_down_sync(0xffffffffu, s, 2) << 8;
+    word |= __shfl_down_sync(0xffffffffu, word, 4) << 16;
+    tile = (lane & 7) == 0 ? chunk * 4 + (lane >> 3) : p.tiles;
+  } else {
+    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
+    s = fp4_scale32(m);
+    codes = fp4_codes32(v, s);
+    s = live ? s : 0u;
+    word = s | __shfl_down_sync(0xffffffffu, s, 4) << 8;
+    word |= __shfl_down_sync(0xffffffffu, word, 8) << 16;
+    tile = (lane & 15) == 0 ? chunk * 2 + (lane >> 4) : p.tiles;
+  }
+  if (live) *reinterpret_cast<uint32_t*>(p.codes + (row * p.D + col) / 2) = codes;
+  if (tile < p.tiles) *reinterpret_cast<uint32_t*>(p.scales + fp4_scale_at(row, tile, p.tiles)) = word;
+}
+
+// A block has a row, a warp NCH chunks of it, one after the other.  NORM: h, its norm and the weight; else p is x (four bits).
+template <typename T, typename R, int NCH, bool NORM, bool FP4>
+__global__ void __launch_bounds__(512) row_kernel(const __grid_constant__ RowParams p) {
+  __shared__ double sums[16];
+  __shared__ float maxima[16];
+  pdl_launch_dependents();
+  pdl_wait();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nwarps = blockDim.x >> 5;
+  const i64 row = blockIdx.x;
+  const int c0 = warp * NCH, col0 = c0 * kChunk + lane * 8;
+  float v[NCH][8], m[NCH];
+  double ss = 0.0;
+#pragma unroll
+  for (int k = 0; k < NCH; ++k) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[k][i] = 0.f;
+    if (col0 + k * kChunk < p.D) load8<T>(static_cast<const T*>(p.x) + row * p.sx + col0 + k * kChunk, p.vx, v[k]);
+  }
+  if constexpr (!std::is_same<R, None>::value) {
+    const R* const res = static_cast<const R*>(p.residual);
+    R* const out = static_cast<R*>(p.stream);
+    float r[NCH][8];
+#pragma unroll
+    for (int k = 0; k < NCH; ++k)
+      if (res && col0 + k * kChunk < p.D) load8<R>(res + row * p.sr + col0 + k * kChunk, p.vr, r[k]);
+#pragma unroll
+    for (int k = 0; k < NCH; ++k)
+      if (col0 + k * kChunk < p.D) {
+        if (res) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[k][i] = __fadd_rn(v[k][i], r[k][i]);
+        }
+        store8<R>(out ? out + row * p.ss + col0 + k * kChunk : nullptr, p.vs, v[k]);
+      }
+  }
+#pragma unroll
+  for (int k = 0; k < NCH; ++k) {
+    if constexpr (NORM) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) ss = fma((double)v[k][i], (double)v[k][i], ss);
+      if (p.weight && col0 + k * kChunk < p.D) {
+        const float4 a = reinterpret_cast<const float4*>(p.weight + col0 + k * kChunk)[0], b = reinterpret_cast<const float4*>(p.weight + col0 + k * kChunk)[1];
+        const float w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[k][i] = __fmul_rn(v[k][i], w[i]);
+      }
+    }
+    m[k] = absmax8(v[k]);
+  }
+  float top = 0.f;
+  if (NORM || p.block == 16) {
+#pragma unroll
+    for (int k = 0; k < NCH; ++k) top = fmaxf(top, m[k]);
+    top = warp_max(top);
+    if constexpr (NORM) {
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+    }
+    if (lane == 0) {
+      maxima[warp] = top;
+      if (NORM) sums[warp] = ss;
+    }
+    __syncthreads();
+    top = warp_max(lane < nwarps ? maxima[lane] : 0.f);
+  }
+  // 1 / sqrt(mean + eps), by the threads that need it
+  auto factor = [&] {
+    double s = 0.0;
+    for (int i = 0; i < nwarps; ++i) s += sums[i];
+    return 1.0 / sqrt(s / (double)p.D + (double)p.eps);
+  };
+  if constexpr (FP4) {
+    const float g = p.block == 16 ? fp4_row_step(top) : 1.0f;
+    if (p.step && threadIdx.x == 0) {
+      if constexpr (NORM) p.step[row] = top > 0.f ? (float)((double)g * factor()) : 1.0f;
+      else p.step[row] = g;
+    }
+#pragma unroll
+    for (int k = 0; k < NCH; ++k)
+      if ((c0 + k) * kChunk < p.D) chunk_fp4(p, row, c0 + k, col0 + k * kChunk < p.D, v[k], m[k], g);
+  } else {
+    float a;
+    if (p.static_scale) {
+      const float r = (float)factor();
+      a = *p.static_scale;
+#pragma unroll
+      for (int k = 0; k < NCH; ++k)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[k][i] = __fmul_rn(v[k][i], r);
+    } else {
+      a = __fdiv_rn(top, 127.0f);
+      const bool some = a > 0.f;
+      a = some ? a : 1.0f;
+      if (p.scale && threadIdx.x == 0) p.scale[row] = some ? (float)((double)a * factor()) : 1.0f;
+    }
+    const float4 a4 = make_float4(a, a, a, a);
+    const Step4 st = step4(a4);
+#pragma unroll
+    for (int k = 0; k < NCH; ++k)
+      if (col0 + k * kChunk < p.D) {
+        const float4 lo = make_float4(v[k][0], v[k][1], v[k][2], v[k][3]), hi = make_float4(v[k][4], v[k][5], v[k][6], v[k][7]);
+        const uint2 q = st.usable ? make_uint2(code4(lo, st), code4(hi, st)) : make_uint2(code4_by_division(lo, a4), code4_by_division(hi, a4));
+        *reinterpret_cast<uint2*>(p.xq + row * p.D + col0 + k * kChunk) = q;
+      }
+  }
+}
+
+// Rows wider than a block's registers: the row is read twice where its absmax is needed.
+template <typename T>
+__global__ void __launch_bounds__(512) wide_kernel(const __grid_constant__ RowParams p) {
+  __shared__ float maxima[16];
+  pdl_launch_dependents();
+  pdl_wait();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const i64 row = blockIdx.x;
+  const T* const x = static_cast<const T*>(p.x) + row * p.sx;
+  float v[8], g = 1.0f;
+  if (p.block == 16) {
+    float top = 0.f;
+    for (int c = threadIdx.x * 8; c < p.D; c += 512 * 8) {
+      load8<T>(x + c, p.vx, v);
+      top = fmaxf(top, absmax8(v));
+    }
+    top = warp_max(top);
+    if (lane == 0) maxima[warp] = top;
+    __syncthreads();
+    g = fp4_row_step(warp_max(lane < 16 ? maxima[lane] : 0.f));
+  }
+  if (p.step && threadIdx.x == 0) p.step[row] = g;
+  for (int c = warp; c * kChunk < p.D; c += 16) {
+    const int col = c * kChunk + lane * 8;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = 0.f;
+    if (col < p.D) load8<T>(x + col, p.vx, v);
+    chunk_fp4(p, row, c, col < p.D, v, absmax8(v), g);
+  }
+}
+
+// Values of a matrix in four bits, eight columns a thread
+template <typename T>
+__global__ void __launch_bounds__(256) values_kernel(const uint8_t* codes, const uint8_t* scales, const float* step, T* out, i64 stride, bool aligned,
+                                                     i64 groups, int per_row, int block, int tiles) {
+  pdl_launch_dependents();
+  pdl_wait();
+  for (i64 i = blockIdx.x * 256ll + threadIdx.x; i < groups; i += gridDim.x * 256ll) {
+    const i64 row = i / per_row;
+    const int col = (int)(i - row * per_row) * 8, b = col / block;
+    const uint32_t byte = scales[fp4_scale_at(row, b >> 2, tiles) + (b & 3)];
+    const float s = block == 16 ? e4m3_to(byte) : e8m0_to(byte), f = step ? step[row] : 1.0f;
+    float v[8];
+    e2m1_to8(__ldcs(reinterpret_cast<const uint32_t*>(codes) + i), v);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = __fmul_rn(__fmul_rn(v[k], s), f);
+    store8<T>(out + row * stride + col, aligned, v);
+  }
+}
+
+template <typename T, typename R, bool NORM, bool FP4>
+ssdi8_status_t launch(const RowParams& p, i64 rows, cudaStream_t st) {
+  const int chunks = (p.D + kChunk - 1) / kChunk;
+  auto go = [&](auto n) -> ssdi8_status_t {
+    constexpr int NCH = decltype(n)::value;
+    return launch_configured(row_kernel<T, R, NCH, NORM, FP4>, dim3((unsigned)rows), dim3(32 * ((chunks + NCH - 1) / NCH)), 0, -1, false, st, p);
+  };
+  if (chunks <= 8) return go(std::integral_constant<int, 1>());
+  if (chunks <= 16) return go(std::integral_constant<int, 2>());
+  return go(std::integral_constant<int, 4>());
+}
+
+template <typename T>
+bool rows_aligned(const void* p, i64 stride) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % (16 / (i64)sizeof(T)) == 0; }
+
+template <typename T, typename R>
+ssdi8_status_t norm_of(const ssdi8_add_norm_args_t& a, cudaStream_t st) {
+  RowParams p = {};
+  p.x = a.x; p.sx = a.stride_x; p.vx = rows_aligned<T>(a.x, a.stride_x);
+  if constexpr (!std::is_same<R, None>::value) {
+    p.residual = a.residual; p.sr = a.stride_residual; p.vr = rows_aligned<R>(a.residual, a.stride_residual);
+    p.stream = a.residual_out; p.ss = a.stride_out; p.vs = rows_aligned<R>(a.residual_out, a.stride_out);
+  }
+  p.weight = a.weight; p.static_scale = a.static_scale; p.xq = a.xq; p.scale = a.scale;
+  p.D = a.width; p.eps = a.eps;
+  if (!a.fp4) return launch<T, R, true, false>(p, a.rows, st);
+  p.codes = a.fp4->codes; p.scales = a.fp4->scales; p.step = a.fp4->step;
+  p.block = a.fp4->block; p.tiles = fp4_tiles(p.D, p.block);
+  return launch<T, R, true, true>(p, a.rows, st);
+}
+
+template <typename T>
+ssdi8_status_t quantize_of(const void* x, i64 stride, const ssdi8_fp4_t& q, cudaStream_t st) {
+  RowParams p = {};
+  p.x = x; p.sx = stride; p.vx = rows_aligned<T>(x, stride);
+  p.codes = q.codes; p.scales = q.scales; p.step = q.step;
+  p.D = q.width; p.block = q.block; p.tiles = fp4_tiles(q.width, q.block);
+  if (q.width <= kMaxNormWidth) return launch<T, None, false, true>(p, q.rows, st);
+  return launch_configured(wide_kernel<T>, dim3((unsigned)q.rows), dim3(512), 0, -1, false, st, p);
+}
+
+}  // namespace
+
+ssdi8_status_t launch_add_norm(const ssdi8_add_norm_args_t& a, int dtype, int rdtype, cudaStream_t st) {
+  if (rdtype < 0)
+    return dtype == 0 ? norm_of<float, None>(a, st) : dtype == 1 ? norm_of<__half, None>(a, st) : norm_of<__nv_bfloat16, None>(a, st);
+  if (rdtype == 0)
+    return dtype == 0 ? norm_of<float, float>(a, st) : dtype == 1 ? norm_of<__half, float>(a, st) : norm_of<__nv_bfloat16, float>(a, st);
+  return dtype == 1 ? norm_of<__half, __half>(a, st) : norm_of<__nv_bfloat16, __nv_bfloat16>(a, st);
+}
+
+ssdi8_status_t launch_fp4_quantize(const void* x, i64 stride, int dtype, const ssdi8_fp4_t& q, cudaStream_t st) {
+  return dtype == 0 ? quantize_of<float>(x, stride, q, st) : dtype == 1 ? quantize_of<__half>(x, stride, q, st) : quantize_of<__nv_bfloat16>(x, stride, q, st);
+}
+
+ssdi8_status_t launch_fp4_dequantize(const ssdi8_fp4_t& q, void* out, i64 stride, int dtype, cudaStream_t st) {
+  const int sms = sm_count();
+  if (sms <= 0) return SSDI8_ERR_CUDA;
+  const i64 groups = (i64)q.rows * (q.width / 8), blocks = (groups + 255) / 256, most = 16ll * sms;
+  auto go = [&](auto t) -> ssdi8_status_t {
+    typedef decltype(t) T;
+    return launch_configured(values_kernel<T>, dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, -1, false, st, (const uint8_t*)q.codes,
+                             (const uint8_t*)q.scales, (const float*)q.step, static_cast<T*>(out), stride, rows_aligned<T>(out, stride), groups,
+                             q.width / 8, q.block, fp4_tiles(q.width, q.block));
+  };
+  return dtype == 0 ? go(float()) : dtype == 1 ? go(__half()) : go(__nv_bfloat16());
+}
+
+}  // namespace ssdi8

@@ -9,9 +9,8 @@
 // operands from L2 at 11 TB/s (the tokens are read by every tile), then the parts' meeting and the epilogue, 2 us each.
 // From 129 to about 1000 rows a lone tile walks all of K on as many CTAs as there are tiles: 250 x 4096 x 8192 (5.8 us of bytes) 18.9 us, 250 x 18560 x
 // 4096 (13.4) 24, 600 x 2560 x 5120 (3.5) 15.  Rows of out off 16-byte boundaries leave as single elements: 3439 x 16470 x 1232, fp16, residual (39) 284.
-#include "block.cuh"
 #include "kernels.h"
-#include "sm100.cuh"
+#include "linear.cuh"
 
 namespace ssdi8 {
 namespace {
@@ -39,41 +38,6 @@ struct Layout {
   static constexpr uint32_t kTurns = kCols + 2 * 2 * kMaxBN * 4;
   static constexpr uint32_t kAlloc = kTurns + 4 * 32 * 17 * 4 + 1024;   // (the tiles start on 1024 bytes)
 };
-
-__device__ __forceinline__ float activate(float v, int act) {
-  if (act == SSDI8_ACT_SILU) return v * rcp_approx(1.0f + ex2_approx(v * -1.44269504f));
-  if (act == SSDI8_ACT_RELU2) return v < 0.f ? 0.f : v * v;   // (-inf is 0, a NaN stays one)
-  return v;
-}
-
-// Tensor memory for all warps but the loader's, by warp 2.  Behind the wait for the kernel before and ahead of the trigger for the next
-// one: a kernel that held some while it waits, or that still had to ask for some when the next one may be scheduled beside it, could
-// leave the two waiting for one another.
-template <int GROUP>
-__device__ __forceinline__ uint32_t allocated(uint32_t* slot, uint32_t columns, int warp, int threads) {
-  if (warp == 2) {
-    if (GROUP == 1) {
-      tmem_alloc(slot, columns);
-    } else {
-      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(slot)), "r"(columns) : "memory");
-      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-    }
-    pdl_launch_dependents();
-  }
-  tc_fence_before();
-  named_bar_sync(2, threads - 32);
-  tc_fence_after();
-  return *slot;
-}
-
-// tile -> (row block, column block): GROUP row blocks at a time, so that the tiles in flight share rows of x and of w in L2
-template <int GROUP>
-__device__ __forceinline__ void tile_of(int tile, int mtiles, int ntiles, int* m, int* n) {
-  const int per = GROUP * ntiles, group = tile / per, rest = tile % per;
-  const int rows = min(GROUP, mtiles - group * GROUP);
-  *m = group * GROUP + rest % rows;
-  *n = rest / rows;
-}
 
 // A quarter's 32 rows (lanes) of `ncols` columns of an accumulator: t is this lane's row, n0 the first column, cw and cb the
 // columns' step sizes and biases; `drained` is called once the last column has been read.  Rows of out (and residual) on 16-byte
@@ -295,30 +259,11 @@ struct PairLayout {
   static constexpr uint32_t kAlloc = kTurns + 8 * kTurn * 4 + 1024;
 };
 
-__device__ __forceinline__ uint32_t in_first(const void* p) {   // the same place in the pair's first CTA
-  uint32_t a;
-  asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(a) : "r"(smem_u32(p)));
-  return a;
-}
-__device__ __forceinline__ void pair_load(void* dst, const CUtensorMap* tm, uint32_t bar, int x, int y) {   // bar: of the first CTA
-  asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-               ::"r"(smem_u32(dst)), "l"(tm), "r"(bar), "r"(x), "r"(y)
-               : "memory");
-}
 __device__ __forceinline__ void pair_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
   asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}"
                ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
                : "memory");
 }
-__device__ __forceinline__ void pair_commit(uint64_t* bar) {   // arrives at this place in both CTAs
-  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-               ::"r"(smem_u32(bar)), "h"((uint16_t)3)
-               : "memory");
-}
-__device__ __forceinline__ void arrive_at(uint32_t bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-
 template <typename T>
 __global__ void __launch_bounds__(PT, 1) linear_pair_kernel(const __grid_constant__ CUtensorMap tx, const __grid_constant__ CUtensorMap tw,
                                                             const __grid_constant__ LinearParams p) {

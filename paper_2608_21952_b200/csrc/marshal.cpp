@@ -68,7 +68,7 @@ float real(PyObject* o) {
 // The binding's ctypes types, given once at its import (init): a structure of another type, or any other object with a
 // buffer, would be read as pointers and sizes that it does not hold.  The errors are those of ctypes' byref and argtypes.
 struct Types {
-  PyObject *dims = nullptr, *fwd = nullptr, *layer = nullptr, *cache = nullptr, *ctypes_base = nullptr, *argument_error = nullptr;
+  PyObject *dims = nullptr, *fwd = nullptr, *layer = nullptr, *cache = nullptr, *fp4 = nullptr, *ctypes_base = nullptr, *argument_error = nullptr;
 } g_types;
 
 // the memory of a ctypes structure
@@ -113,6 +113,20 @@ struct LayerArg : Struct {
 struct BadShape {};
 PyObject* const kHeads = PyUnicode_InternFromString("heads");
 PyObject* const kDevice = PyUnicode_InternFromString("device");
+void on_current_device(PyObject* o, const char* what) {
+  PyObject* v = PyObject_GetAttr(o, kDevice);
+  if (!v) {
+    PyErr_Clear();
+    return;
+  }
+  const long index = PyLong_AsLong(v);
+  Py_DECREF(v);
+  if (index == -1 && PyErr_Occurred()) throw BadArgument{};
+  if (index != c10::cuda::current_device()) {
+    PyErr_Format(PyExc_ValueError, "%s lives on another device than the current one", what);
+    throw BadArgument{};
+  }
+}
 struct CacheArg : Struct {
   CacheArg(PyObject* o, const ssdi8_dims_t& d) : Struct(o, g_types.cache, sizeof(ssdi8_cache_t)) {
     if (PyObject* h = PyObject_GetAttr(o, kHeads)) {
@@ -125,20 +139,15 @@ struct CacheArg : Struct {
     } else {
       PyErr_Clear();
     }
-    PyObject* v = PyObject_GetAttr(o, kDevice);
-    if (!v) {
-      PyErr_Clear();
-      return;
-    }
-    const long index = PyLong_AsLong(v);
-    Py_DECREF(v);
-    if (index == -1 && PyErr_Occurred()) throw BadArgument{};
-    if (index != c10::cuda::current_device()) {
-      PyErr_SetString(PyExc_ValueError, "the cache lives on another device than the current one");
-      throw BadArgument{};
-    }
+    on_current_device(o, "the cache");
   }
   const ssdi8_cache_t* get() const { return static_cast<const ssdi8_cache_t*>(b.buf); }
+};
+
+// a matrix in four bits as fp4_of leaves it, or filled by hand
+struct Fp4Arg : Struct {
+  Fp4Arg(PyObject* o, const char* what) : Struct(o, g_types.fp4, sizeof(ssdi8_fp4_t)) { on_current_device(o, what); }
+  const ssdi8_fp4_t* get() const { return static_cast<const ssdi8_fp4_t*>(b.buf); }
 };
 
 // the stream of a call: the current one of the current device for None, else a torch stream object's
@@ -232,15 +241,15 @@ PyObject* entry(Py_ssize_t n, F f) {
 #define ENTRY(NAME, N) PyObject* NAME(PyObject*, PyObject* const* a, Py_ssize_t n) { return entry<N>(n, [&]() -> PyObject*
 #define END ); }
 
-ENTRY(init, 6) {   // Dims, FwdArgs, LayerArgs, Cache, the base type of ctypes objects, ctypes.ArgumentError
-  for (int i = 0; i < 6; ++i) {
+ENTRY(init, 7) {   // Dims, FwdArgs, LayerArgs, Cache, Fp4, the base type of ctypes objects, ctypes.ArgumentError
+  for (int i = 0; i < 7; ++i) {
     if (!PyType_Check(a[i])) {
       PyErr_SetString(PyExc_TypeError, "a type is expected");
       throw BadArgument{};
     }
     Py_INCREF(a[i]);   // (kept for the life of the process, like the module)
   }
-  g_types = {a[0], a[1], a[2], a[3], a[4], a[5]};
+  g_types = {a[0], a[1], a[2], a[3], a[4], a[5], a[6]};
   Py_RETURN_NONE;
 } END
 
@@ -494,6 +503,60 @@ ENTRY(linear, 10) {   // xq, wq, s_w, out, s_row, bias, residual, act, status, s
   return call([&] { return ssdi8_linear(&l, out.dtype, st); });
 } END
 
+ENTRY(fp4_quantize, 3) {   // x, q, stream
+  Fp4Arg q(a[1], "q");
+  const Tensor x = tensor(a[0], "x", kAnyFloat, {q.get()->rows, q.get()->width}, false, true);
+  void* st = stream(a[2]);
+  return call([&] { return ssdi8_fp4_quantize(x.data(), x.stride(0), x.dtype, q.get(), st); });
+} END
+
+ENTRY(fp4_dequantize, 3) {   // q, out, stream
+  Fp4Arg q(a[0], "q");
+  const Tensor out = tensor(a[1], "out", kAnyFloat, {q.get()->rows, q.get()->width}, false, true);
+  void* st = stream(a[2]);
+  return call([&] { return ssdi8_fp4_dequantize(q.get(), out.data(), out.stride(0), out.dtype, st); });
+} END
+
+ENTRY(add_norm_quantize, 10) {   // x, residual, residual_out, weight, eps, xq, scale, static_scale, fp4, stream
+  const Tensor x = tensor(a[0], "x", kAnyFloat, {-1, -1}, false, true);
+  const int64_t T = x.size(0), D = x.size(1);
+  if (D > 0x7fffffff) throw BadShape{};
+  ssdi8_add_norm_args_t n = {};
+  n.x = x.data(); n.stride_x = x.stride(0);
+  const Tensor r = tensor(a[1], "residual", kAnyFloat, {T, D}, true, true);
+  const Tensor o = tensor(a[2], "residual_out", r ? r.dtype : kAnyFloat, {T, D}, true, true);
+  if (r) { n.residual = r.data(); n.stride_residual = r.stride(0); }
+  if (o) { n.residual_out = o.data(); n.stride_out = o.stride(0); }
+  n.weight = tensor(a[3], "weight", 0, {D}, true).as<float>();
+  n.eps = real(a[4]);
+  n.xq = tensor(a[5], "xq", kInt8, {T, D}, true).as<int8_t>();
+  n.scale = tensor(a[6], "scale", 0, {T}, true).as<float>();
+  n.static_scale = tensor(a[7], "static_scale", 0, {1}, true).as<float>();
+  n.rows = T; n.width = (int32_t)D;
+  const int rdtype = r ? r.dtype : o ? o.dtype : 0;
+  void* st = stream(a[9]);
+  if (a[8] == Py_None) return call([&] { return ssdi8_add_norm_quantize(&n, x.dtype, rdtype, st); });
+  Fp4Arg q(a[8], "fp4");
+  n.fp4 = q.get();
+  return call([&] { return ssdi8_add_norm_quantize(&n, x.dtype, rdtype, st); });
+} END
+
+ENTRY(fp4_linear, 8) {   // x, w, out, bias, residual, act, status, stream
+  Fp4Arg x(a[0], "x"), w(a[1], "w");
+  const int64_t T = x.get()->rows, O = w.get()->rows;
+  ssdi8_fp4_linear_args_t l = {};
+  l.x = x.get(); l.w = w.get();
+  const Tensor out = tensor(a[2], "out", kAnyFloat, {T, O}, false, true);
+  l.out = out.data(); l.stride_out = out.stride(0);
+  l.bias = tensor(a[3], "bias", 0, {O}, true).as<float>();
+  const Tensor r = tensor(a[4], "residual", out.dtype, {T, O}, true, true);
+  if (r) { l.residual = r.data(); l.stride_residual = r.stride(0); }
+  l.act = integer32<int32_t>(a[5]);
+  l.status = tensor(a[6], "status", kInt32, {1}, true).as<int32_t>();
+  void* st = stream(a[7]);
+  return call([&] { return ssdi8_fp4_linear(&l, out.dtype, st); });
+} END
+
 #undef ENTRY
 #undef END
 
@@ -501,7 +564,8 @@ ENTRY(linear, 10) {   // xq, wq, s_w, out, s_row, bias, residual, act, status, s
 PyMethodDef kMethods[] = {METHOD(init), METHOD(quantize_act), METHOD(quantize_entry), METHOD(chunk_scan_fwd), METHOD(chunk_scan_fwd_static),
                           METHOD(layer_fwd), METHOD(layer_fwd_host), METHOD(calibrate), METHOD(mean_correction),
                           METHOD(state_passing), METHOD(ssd_step), METHOD(softplus_dt), METHOD(conv_fwd), METHOD(cache_write),
-                          METHOD(cache_read), METHOD(token_step), METHOD(norm_quantize), METHOD(linear), {nullptr, nullptr, 0, nullptr}};
+                          METHOD(cache_read), METHOD(token_step), METHOD(norm_quantize), METHOD(linear),
+                          METHOD(fp4_quantize), METHOD(fp4_dequantize), METHOD(add_norm_quantize), METHOD(fp4_linear), {nullptr, nullptr, 0, nullptr}};
 #undef METHOD
 
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
