@@ -63,15 +63,19 @@ __device__ __forceinline__ void issue_stage(uint32_t acc, uint32_t ts, uint32_t 
   typedef Scales<BLOCK> S;
   const uint64_t da = tile_desc(a, ROW), db = tile_desc(b, ROW);
 #pragma unroll
+  for (int tile = 0; tile < S::kTiles; ++tile) {
+    if (tile * BLOCK < 16 * steps) {
+      const uint32_t ca = ts + 4 * tile, cb = ts + 4 * S::kTiles + 4 * bgroups * tile;
+      scales_in<CTAS>(ca, sa + tile * kTileBytes);
+      scales_in<CTAS>(cb, sb + tile * kTileBytes);
+      if (bgroups == 2) scales_in<CTAS>(cb + 4, sb + S::kBytes + tile * kTileBytes);
+    }
+  }
+#pragma unroll
   for (int k = 0; k < BK / 64; ++k) {
     if (k < steps) {
       const int tile = BLOCK == 16 ? k : k >> 1, id = BLOCK == 16 ? 0 : 2 * (k & 1);
       const uint32_t ca = ts + 4 * tile, cb = ts + 4 * S::kTiles + 4 * bgroups * tile;
-      if (id == 0) {
-        scales_in<CTAS>(ca, sa + tile * kTileBytes);
-        scales_in<CTAS>(cb, sb + tile * kTileBytes);
-        if (bgroups == 2) scales_in<CTAS>(cb + 4, sb + S::kBytes + tile * kTileBytes);
-      }
       mma_fp4<CTAS, BLOCK>(acc, da + 2 * k, db + 2 * k, idesc_fp4(M, N, BLOCK, id), ca, cb, !first || k > 0);
     }
   }
@@ -83,144 +87,247 @@ __device__ __forceinline__ void issue_stage(uint32_t acc, uint32_t ts, uint32_t 
 // of 256 columns would be all of tensor memory: they share 48 columns, which the scales take at its end, and an epilogue reads
 // the shared ones first.
 constexpr int PBN = 256, PT = 384, kShared = 48;
-constexpr int kTurn = 32 * 17;
 struct PairLayout {
-  static constexpr int kStages = 5;
+  static constexpr int kStages = 4;
   static constexpr uint32_t kA = 128 * ROW, kScales = 2 * kA, kStage = kScales + 3 * Scales<16>::kBytes;
-  static constexpr uint32_t kBars = kStages * kStage;
-  static constexpr uint32_t kCols = kBars + 256;
-  static constexpr uint32_t kTurns = kCols + 2 * 2 * PBN * 4;
-  static constexpr uint32_t kAlloc = kTurns + 8 * kTurn * 4 + 1024;
+  static constexpr uint32_t kSlabs = kStages * kStage;           // of each epilogue warp: twice 32 rows of 128 bytes on their way out
+  static constexpr uint32_t kCols = kSlabs + 8 * 2 * 4096;       // step sizes and biases of two tiles' columns
+  static constexpr uint32_t kBars = kCols + 2 * 2 * PBN * 4;
+  static constexpr uint32_t kAlloc = kBars + 256;
 };
 static_assert(PairLayout::kStage % 1024 == 0 && PairLayout::kAlloc <= 232448, "tiles start on 1024 bytes, and there are 227 KB");
 
-// step sizes and biases of a tile's columns into shared memory, by the epilogue threads
-__device__ __forceinline__ void columns(const Fp4Params& p, int n0, float* cw, float* cb, int et) {
-  const int o = n0 + et;   // (256 threads, 256 columns)
-  cw[et] = o < p.O ? (p.s_w ? p.s_w[o] : 1.0f) : 0.f;
-  cb[et] = o < p.O && p.bias ? p.bias[o] : 0.f;
+__device__ __forceinline__ void tma_store_wait_read_but_one() { asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); }
+// (relaxed: what it says is that reads of tensor memory are over, which they are before it is issued; a release would wait for stores)
+__device__ __forceinline__ void arrive_relaxed_at(uint32_t bar) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
-// A quarter's 32 rows (lanes) of 128 columns of an accumulator: t is this lane's row, n0 the first column, cw and cb the columns' step sizes and
-// biases; groups of 32 columns from the first on or (down) from the last on.  `drained` is called once half of the columns have been read, with
-// them in registers.  Rows of out (and residual) on 16-byte boundaries are written by their lane; others, and a ragged end, go through `turn`
-// (32 x 17 floats of the warp's), 16 columns at a time, so that lanes stand beside one another in a row.  The residual of 32 columns is on its way
-// while the 32 before it are finished.
-template <typename T, typename R, typename F>
-__device__ __forceinline__ void epilogue(const Fp4Params& p, uint32_t tmem, int t, int n0, bool down, const float* cw, const float* cb, float* turn, R ready,
-                                         F drained) {
+// One epilogue warp: a quarter's 32 rows (lanes) of 128 columns of an accumulator.  It works in units of 128 bytes of out's rows (64 columns, or 32 of
+// binary32), whose residual is on its way while the unit before is finished, and leaves them in one of its two slabs in shared memory.  Where out's rows
+// (and the residual's) lie on 16-byte boundaries a slab goes out by TMA, which leaves out what is beyond the last row and column.  Other
+// rows are read back from it as binary32, a row at a time by lanes that stand beside one another in it, and stored in words of four bytes: in
+// an odd row, one of 16-bit elements that starts in the middle of a word, lane j has elements 2 j + 1 and 2 j + 2, and the last lane both ends.
+template <typename T>
+struct Epilogue {
+  static constexpr int U = 128 / sizeof(T);   // columns of a unit
   typedef typename std::conditional<sizeof(T) == 4, uint32_t, uint16_t>::type Bits;
-  constexpr int V = 16 / sizeof(T), NV = 32 / V;   // elements of a 16-byte vector, vectors of 32 elements
-  const int end = min(n0 + 128, p.O), lane = threadIdx.x & 31;
-  const float sr = t < p.T ? (p.s_row ? p.s_row[t] : 1.0f) : 0.f;
-  const T* const residual = static_cast<const T*>(p.residual);
-  T* const out = static_cast<T*>(p.out);
-  const bool vectors = p.vec_out && (!residual || p.vec_res);
-  auto group = [&](int i) { return 32 * (down ? 3 - i : i); };
-  uint32_t res[32];   // this lane's 32 elements as 16-byte vectors, or one element of each 16 columns of 16 rows, twice
-  auto fetch = [&](int o0) {
-    if (!residual || o0 >= end) return;
-    if (vectors && o0 + 32 <= end) {
-      if (t < p.T) {
+
+  const Fp4Params& p;
+  const CUtensorMap* tout;
+  uint8_t* slab;
+  const int lane;
+  const bool vectors;
+  int slot = 0;
+  int t0, n0, end;       // the tile's first row of the warp, its first column, where its columns end
+  float sr;
+  uint32_t res[32];      // residual of a unit: this lane's row, or its word (two words' halves) of each of 32 rows
+
+  __device__ __forceinline__ Epilogue(const Fp4Params& p_, const CUtensorMap* tout_, uint8_t* slab_)
+      : p(p_), tout(tout_), slab(slab_), lane(threadIdx.x & 31), vectors(p_.vec_out && (!p_.residual || p_.vec_res)) {}
+
+  static __device__ __forceinline__ int odd_row(const void* q) { return (int)(reinterpret_cast<uintptr_t>(q) >> 1 & 1); }
+  // the residual of a tile into L2, ahead of its turn
+  __device__ __forceinline__ void prefetch(int t_first, int n_first) const {
+    const int t = t_first + lane;
+    if (!p.residual || t >= p.T || n_first >= p.O) return;
+    const uint8_t* const at = reinterpret_cast<const uint8_t*>(static_cast<const T*>(p.residual) + t * p.res_stride + n_first);
+    const int bytes = min(128, p.O - n_first) * (int)sizeof(T);
+    for (int o = 0; o < bytes; o += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(at + o));
+    asm volatile("prefetch.global.L2 [%0];" ::"l"(at + bytes - 1));
+  }
+  __device__ __forceinline__ void tile(int t_first, int n_first) {
+    t0 = t_first;
+    n0 = n_first;
+    end = min(n0 + 128, p.O);
+    sr = t0 + lane < p.T ? (p.s_row ? p.s_row[t0 + lane] : 1.0f) : 0.f;
+  }
+  __device__ __forceinline__ void fetch(int c0) {
+    const int o0 = n0 + c0;
+    if (!p.residual || o0 >= end) return;
+    const T* const residual = static_cast<const T*>(p.residual);
+    if (vectors) {
+      if (t0 + lane >= p.T) return;
+      const T* const at = residual + (t0 + lane) * p.res_stride + o0;
+      if (o0 + U <= end) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-          const uint4 q = reinterpret_cast<const uint4*>(residual + t * p.res_stride + o0)[i];
+        for (int i = 0; i < 8; ++i) {
+          const uint4 q = reinterpret_cast<const uint4*>(at)[i];
           res[4 * i] = q.x; res[4 * i + 1] = q.y; res[4 * i + 2] = q.z; res[4 * i + 3] = q.w;
         }
-      }
-    } else {
+      } else {
+        const Bits* const e = reinterpret_cast<const Bits*>(at);
 #pragma unroll
-      for (int k = 0; k < 32; ++k) {
-        const int tt = t - lane + 2 * (k & 15) + (lane >> 4), o = o0 + (k & 16) + (lane & 15);
-        if (tt < p.T && o < end) res[k] = reinterpret_cast<const Bits*>(residual)[tt * p.res_stride + o];
+        for (int i = 0; i < 32; ++i) {
+          constexpr int n = 4 / (int)sizeof(T);
+          uint32_t w = o0 + n * i < end ? (uint32_t)e[n * i] : 0u;
+          if (n == 2 && o0 + 2 * i + 1 < end) w |= (uint32_t)e[2 * i + 1] << 16;
+          res[i] = w;
+        }
       }
-    }
-  };
-  auto finish = [&](const int (&v)[32], int c0, int next) {
-    const int o0 = n0 + c0;
-    if (o0 >= end) {
-      if (next >= 0) fetch(n0 + next);
       return;
     }
-    if (vectors && o0 + 32 <= end) {
-      uint32_t mine[NV * 4];
+    const Bits* at = reinterpret_cast<const Bits*>(residual) + t0 * p.res_stride + o0;
+    const T* to = static_cast<const T*>(p.out) + t0 * p.out_stride + o0;
+    const int rows = min(32, p.T - t0);
 #pragma unroll
-      for (int i = 0; i < NV * 4; ++i) mine[i] = res[i];
-      if (next >= 0) fetch(n0 + next);
-      if (t < p.T) {
-        T* const dst = out + t * p.out_stride + o0;
-#pragma unroll
-        for (int c = 0; c < 32; c += 8) {
-          float f[8];
-          const float4 w0 = *reinterpret_cast<const float4*>(cw + c0 + c), w1 = *reinterpret_cast<const float4*>(cw + c0 + c + 4);
-          const float4 b0 = *reinterpret_cast<const float4*>(cb + c0 + c), b1 = *reinterpret_cast<const float4*>(cb + c0 + c + 4);
-          const float ws[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w}, bs[8] = {b0.x, b0.y, b0.z, b0.w, b1.x, b1.y, b1.z, b1.w};
-#pragma unroll
-          for (int e = 0; e < 8; ++e) f[e] = activate(fmaf(__int_as_float(v[c + e]) * sr, ws[e], bs[e]), p.act);
-          T* const at = reinterpret_cast<T*>(mine) + c;
-          if (residual) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] += Elem<T>::get(at[e]);
-          }
-#pragma unroll
-          for (int e = 0; e < 8; ++e) at[e] = Elem<T>::put(f[e]);
-#pragma unroll
-          for (int i = 0; i < 8 / V; ++i) {
-            const uint32_t* const w = mine + (c / V + i) * 4;
-            reinterpret_cast<uint4*>(dst + c)[i] = make_uint4(w[0], w[1], w[2], w[3]);
-          }
-        }
-      }
-    } else {
-      Bits mine[32];
-#pragma unroll
-      for (int k = 0; k < 32; ++k) mine[k] = (Bits)res[k];
-      if (next >= 0) fetch(n0 + next);
-#pragma unroll
-      for (int h = 0; h < 32; h += 16) {
-#pragma unroll
-        for (int c = 0; c < 16; ++c) turn[lane * 17 + c] = activate(fmaf(__int_as_float(v[h + c]) * sr, cw[c0 + h + c], cb[c0 + h + c]), p.act);
-        __syncwarp();
-        const int o = o0 + h + (lane & 15);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int row = 2 * i + (lane >> 4), tt = t - lane + row;
-          if (tt < p.T && o < end) {
-            float f = turn[row * 17 + (lane & 15)];
-            if (residual) f += Elem<T>::get(*reinterpret_cast<const T*>(&mine[h + i]));
-            out[tt * p.out_stride + o] = Elem<T>::put(f);
-          }
-        }
-        __syncwarp();
+    for (int r = 0; r < 32; ++r, at += p.res_stride, to += p.out_stride) {
+      if (r >= rows) break;
+      if constexpr (sizeof(T) == 4) {
+        if (o0 + lane < end) res[r] = at[lane];
+      } else {
+        const int odd = odd_row(to), a = 2 * lane + odd, b = (a + 1) & 63;
+        if (odd_row(at + odd) == 0 && b > a && o0 + b < end) res[r] = *reinterpret_cast<const uint32_t*>(at + a);
+        else res[r] = (o0 + a < end ? (uint32_t)at[a] : 0u) | (o0 + b < end ? (uint32_t)at[b] << 16 : 0u);
       }
     }
-  };
-  fetch(n0 + group(0));
-  ready();
-#pragma unroll 1
-  for (int i = 0; i < 4; i += 2) {
-    int v[32], u[32];
-    __syncwarp();   // (lanes beyond the last row skip the stores)
-    tmem_ld32(tmem + group(i), v);
-    tmem_ld32(tmem + group(i + 1), u);
-    tmem_ld_wait();
-    if (i == 0) {
-      tc_fence_before();
-      drained();
-    }
-    finish(v, group(i), group(i + 1));
-    finish(u, group(i + 1), i == 0 ? group(2) : -1);
   }
-}
+  // 32 columns of the accumulator, in pairs; one loop for each activation
+  __device__ __forceinline__ void values(const int (&v)[32], const float* cw, const float* cb, float2 (&f)[16]) const {
+    const float2 s2 = make_float2(sr, sr);
+#pragma unroll
+    for (int c = 0; c < 16; c += 2) {
+      const float4 w = *reinterpret_cast<const float4*>(cw + 2 * c), b = *reinterpret_cast<const float4*>(cb + 2 * c);
+      f[c] = __ffma2_rn(__fmul2_rn(make_float2(__int_as_float(v[2 * c]), __int_as_float(v[2 * c + 1])), s2), make_float2(w.x, w.y), make_float2(b.x, b.y));
+      f[c + 1] = __ffma2_rn(__fmul2_rn(make_float2(__int_as_float(v[2 * c + 2]), __int_as_float(v[2 * c + 3])), s2), make_float2(w.z, w.w),
+                            make_float2(b.z, b.w));
+    }
+    if (p.act == SSDI8_ACT_SILU) {
+#pragma unroll
+      for (int c = 0; c < 16; ++c) f[c] = make_float2(activate(f[c].x, SSDI8_ACT_SILU), activate(f[c].y, SSDI8_ACT_SILU));
+    } else if (p.act == SSDI8_ACT_RELU2) {
+#pragma unroll
+      for (int c = 0; c < 16; ++c) f[c] = make_float2(activate(f[c].x, SSDI8_ACT_RELU2), activate(f[c].y, SSDI8_ACT_RELU2));
+    }
+  }
+  // 32 columns, the first or second half of a unit of 16-bit elements, or all of one of binary32, into a slab
+  __device__ __forceinline__ void into(float2 (&f)[16], int half) {
+    if (vectors) {   // 16-byte chunks of a row of 128 bytes, as the 128-byte swizzle has them
+      uint8_t* const to = slab + slot * 4096;
+      if (p.residual) {
+#pragma unroll
+        for (int c = 0; c < 16; ++c) {
+          if constexpr (sizeof(T) == 4) {
+            f[c] = __fadd2_rn(f[c], make_float2(__uint_as_float(res[2 * c]), __uint_as_float(res[2 * c + 1])));
+          } else {
+            const T* const r = reinterpret_cast<const T*>(&res[16 * half + c]);
+            f[c] = __fadd2_rn(f[c], make_float2(Elem<T>::get(r[0]), Elem<T>::get(r[1])));
+          }
+        }
+      }
+      if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          *reinterpret_cast<uint4*>(to + swz_off(lane, i, 128)) = make_uint4(__float_as_uint(f[2 * i].x), __float_as_uint(f[2 * i].y),
+                                                                              __float_as_uint(f[2 * i + 1].x), __float_as_uint(f[2 * i + 1].y));
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint2 a = Elem<T>::pack(make_float4(f[4 * i].x, f[4 * i].y, f[4 * i + 1].x, f[4 * i + 1].y));
+          const uint2 b = Elem<T>::pack(make_float4(f[4 * i + 2].x, f[4 * i + 2].y, f[4 * i + 3].x, f[4 * i + 3].y));
+          *reinterpret_cast<uint4*>(to + swz_off(lane, 4 * half + i, 128)) = make_uint4(a.x, a.y, b.x, b.y);
+        }
+      }
+    } else {   // pairs of columns, at a place that depends on the row: no two lanes of a row or of a column meet in a bank
+      constexpr int pairs = U / 2;
+      float2* const to = reinterpret_cast<float2*>(slab) + lane * pairs;
+#pragma unroll
+      for (int c = 0; c < 16; ++c) to[(16 * half + c) ^ (lane & (pairs - 1))] = f[c];
+    }
+  }
+  __device__ __forceinline__ void take() {   // the slab's last store has been read
+    if (vectors) {
+      if (lane == 0) tma_store_wait_read_but_one();
+      __syncwarp();
+    }
+  }
+  __device__ __forceinline__ void leave(int c0) {
+    const int o0 = n0 + c0;
+    if (vectors) {
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        if (o0 < end && t0 < p.T) tma_store_2d(tout, slab + slot * 4096, o0, t0);
+        tma_store_commit();
+      }
+      slot ^= 1;
+      return;
+    }
+    __syncwarp();
+    if (o0 < end) {
+      constexpr int pairs = U / 2;
+      const float* const turn = reinterpret_cast<const float*>(slab);
+      T* at = static_cast<T*>(p.out) + t0 * p.out_stride + o0;
+      const int rows = min(32, p.T - t0);
+      auto column = [&](int r, int c) { return turn[r * U + (((c >> 1) ^ (r & (pairs - 1))) << 1) + (c & 1)]; };
+#pragma unroll
+      for (int r = 0; r < 32; ++r, at += p.out_stride) {
+        if (r >= rows) break;
+        if constexpr (sizeof(T) == 4) {
+          const float x = column(r, lane);
+          if (o0 + lane < end) at[lane] = p.residual ? x + __uint_as_float(res[r]) : x;
+        } else {
+          const int odd = odd_row(at), a = 2 * lane + odd, b = (a + 1) & 63;
+          float2 x;
+          if (odd) x = make_float2(column(r, a), column(r, b));
+          else x = reinterpret_cast<const float2*>(turn)[r * pairs + (lane ^ r)];
+          if (p.residual) {
+            const T* const m = reinterpret_cast<const T*>(&res[r]);
+            x = __fadd2_rn(x, make_float2(Elem<T>::get(m[0]), Elem<T>::get(m[1])));
+          }
+          const uint32_t w = Elem<T>::pack(make_float4(x.x, x.y, 0.f, 0.f)).x;
+          if (b > a && o0 + b < end) {
+            *reinterpret_cast<uint32_t*>(at + a) = w;
+          } else {
+            if (o0 + a < end) reinterpret_cast<uint16_t*>(at)[a] = (uint16_t)w;
+            if (o0 + b < end) reinterpret_cast<uint16_t*>(at)[b] = (uint16_t)(w >> 16);
+          }
+        }
+      }
+    }
+    __syncwarp();
+  }
+  // all 128 columns, the halves from the first or from the last on (down); `ready` waits for the accumulator, `drained` is called once the first half is
+  // in registers
+  template <typename R, typename F>
+  __device__ __forceinline__ void run(uint32_t tmem, bool down, const float* cw, const float* cb, R ready, F drained) {
+    int c0 = down ? 64 : 0;
+    fetch(c0);
+    ready();
+#pragma unroll 1
+    for (int i = 0; i < 2; ++i, c0 ^= 64) {
+      int v[32], u[32];
+      tmem_ld32(tmem + c0, v);
+      tmem_ld32(tmem + c0 + 32, u);
+      tmem_ld_wait();
+      if (i == 0) {
+        tc_fence_before();
+        drained();
+      }
+      float2 f[16];
+      take();
+      values(v, cw + c0, cb + c0, f);
+      into(f, 0);
+      if constexpr (sizeof(T) == 4) {
+        leave(c0);
+        fetch(c0 + 32);
+        take();
+      }
+      values(u, cw + c0 + 32, cb + c0 + 32, f);
+      into(f, sizeof(T) == 4 ? 0 : 1);
+      leave(sizeof(T) == 4 ? c0 + 32 : c0);
+      if (i == 0) fetch(c0 ^ 64);
+    }
+  }
+};
 
 template <typename T, int BLOCK>
 __global__ void __launch_bounds__(PT, 1) fp4_pair_kernel(const __grid_constant__ CUtensorMap tx, const __grid_constant__ CUtensorMap tw,
                                                          const __grid_constant__ CUtensorMap tsx, const __grid_constant__ CUtensorMap tsw,
-                                                         const __grid_constant__ Fp4Params p) {
+                                                         const __grid_constant__ CUtensorMap tout, const __grid_constant__ Fp4Params p) {
   typedef PairLayout S;
   constexpr uint32_t kSc = Scales<BLOCK>::kBytes;
-  extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  extern __shared__ __align__(1024) uint8_t smem[];   // (there is no static part: the window's base is on 1024 bytes)
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::kBars);   // (waited for in the first CTA; the second's loads arrive there too)
   uint64_t* empty = full + S::kStages;
   uint64_t* acc_full = empty + S::kStages;
@@ -243,6 +350,7 @@ __global__ void __launch_bounds__(PT, 1) fp4_pair_kernel(const __grid_constant__
     tma_prefetch_desc(&tw);
     tma_prefetch_desc(&tsx);
     tma_prefetch_desc(&tsw);
+    tma_prefetch_desc(&tout);
   }
   __syncthreads();
   cluster_sync();   // (the other CTA's barriers are there)
@@ -295,30 +403,46 @@ __global__ void __launch_bounds__(PT, 1) fp4_pair_kernel(const __grid_constant__
       }
     }
   } else if (warp >= 4) {
-    const int quarter = warp & 3, upper = (warp - 4) >> 2;   // eight warps: a quarter of the rows, half of the columns
-    int at = 0;
+    const int quarter = warp & 3, upper = (warp - 4) >> 2, et = tid & 127;   // eight warps: a quarter of the rows, half of the columns
+    Epilogue<T> ep(p, &tout, smem + S::kSlabs + (warp - 4) * 2 * 4096);
+    // a column's step size and bias, a tile ahead
+    float w = 0.f, b = 0.f;
+    auto column = [&](int n) {
+      const int o = n * PBN + upper * 128 + et;
+      w = o < p.O ? (p.s_w ? p.s_w[o] : 1.0f) : 0.f;
+      b = o < p.O && p.bias ? p.bias[o] : 0.f;
+    };
+    int at = 0, m, n;
+    tile_of<8>(pair, p.mtiles, p.ntiles, &m, &n);
+    column(n);
+    ep.prefetch(m * 256 + rank * 128 + quarter * 32, n * PBN + upper * 128);
     for (int tile = pair; tile < ntotal; tile += npairs, ++at) {
       const int buf = at & 1;
-      int m, n;
-      tile_of<8>(tile, p.mtiles, p.ntiles, &m, &n);
-      float* cw = cols + buf * 2 * PBN;
-      columns(p, n * PBN, cw, cw + PBN, tid - 128);
-      named_bar_sync(1, PT - 128);
+      float* const cw = cols + (buf * 2 + upper) * 256;
+      cw[et] = w;
+      cw[128 + et] = b;
+      ep.tile(m * 256 + rank * 128 + quarter * 32, n * PBN + upper * 128);
+      if (tile + npairs < ntotal) {
+        tile_of<8>(tile + npairs, p.mtiles, p.ntiles, &m, &n);
+        column(n);
+        ep.prefetch(m * 256 + rank * 128 + quarter * 32, n * PBN + upper * 128);
+      }
+      named_bar_sync(3 + upper, 128);   // the four warps of these columns (nobody is still reading those of the tile before the last)
       // The shared columns are the last of the first accumulator and the first of the second: the upper half's or the lower's.  The warps of the other
       // half have nothing there; what they say is that they are through with the tile before, which had the accumulator that the next tile gets.
       const bool shared = upper != buf;
       auto free = [&] {
         __syncwarp();
-        if (lane == 0) arrive_at(in_first(&acc_free[buf]));
+        if (lane == 0) arrive_relaxed_at(in_first(&acc_free[buf]));
       };
       if (!shared) free();
-      epilogue<T>(p, tmem + ((uint32_t)(quarter * 32) << 16) + buf * (PBN - kShared) + upper * 128, m * 256 + rank * 128 + quarter * 32 + lane,
-                  n * PBN + upper * 128, buf == 0, cw + upper * 128, cw + PBN + upper * 128, reinterpret_cast<float*>(smem + S::kTurns) + (warp - 4) * kTurn,
-                  [&] { mbar_wait(&acc_full[buf], (at >> 1) & 1, p.status); tc_fence_after(); }, [&] {
-                    if (shared) free();
-                  });
+      ep.run(tmem + ((uint32_t)(quarter * 32) << 16) + buf * (PBN - kShared) + upper * 128, buf == 0, cw, cw + 128,
+             [&] { mbar_wait(&acc_full[buf], (at >> 1) & 1, p.status); tc_fence_after(); }, [&] {
+               if (shared) free();
+             });
       tc_fence_before();   // (what the next tile's arrival vouches for)
     }
+    if (lane == 0) tma_store_wait_read();
   }
   tc_fence_before();
   __syncthreads();
@@ -551,8 +675,12 @@ ssdi8_status_t launch(const ssdi8_fp4_linear_args_t& a, cudaStream_t st) {
     p.mtiles = (int)((x.rows + 255ll) / 256);
     p.ntiles = (int)((w.rows + PBN - 1ll) / PBN);
     if (!codes(&tx, x, 128) || !codes(&tw, w, 128)) return SSDI8_ERR_CUDA;
+    CUtensorMap tout = tx;   // (where out's rows are not on 16 bytes it is not used)
+    const uint64_t dims[2] = {(uint64_t)p.O, (uint64_t)p.T}, stride[1] = {(uint64_t)(a.stride_out * e)};
+    const uint32_t box[2] = {(uint32_t)(128 / e), 32};
+    if (p.vec_out && !encode_tensor_map(&tout, a.out, (int)e, 2, dims, stride, box, 128)) p.vec_out = 0;
     return launch_any(fp4_pair_kernel<T, BLOCK>, dim3((unsigned)(2 * (ptiles < pairs ? ptiles : pairs))), 2, dim3(PT), PairLayout::kAlloc, PairLayout::kAlloc,
-                      -1, false, st, tx, tw, tsx, tsw, p);
+                      -1, true, st, tx, tw, tsx, tsw, tout, p);
   }
   f.l = p;
   f.l.mtiles = (int)mt;
