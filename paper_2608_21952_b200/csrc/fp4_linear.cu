@@ -23,10 +23,10 @@ struct Fp4Params {
   int T, O, steps, kblocks, tiles, mtiles, ntiles, act, vec_out, vec_res;   // steps: of 64 columns; tiles: of scales beside one another
 };
 
-// Instruction descriptor: e2m1 operands, K-major; scales e4m3 (blocks of 16) or e8m0 (32), whose byte of the word `id` names
-__host__ __device__ constexpr uint32_t idesc_fp4(int M, int N, int block, int id) {
-  return (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | (block == 32 ? 1u << 23 : 0u) | ((uint32_t)(M >> 4) << 24) |
-         ((uint32_t)id << 4) | ((uint32_t)id << 29);
+// Instruction descriptor: e2m1 operands, K-major; scales e4m3 (blocks of 16) or e8m0 (32; bits 4 and 29: the
+// word's byte that a step's first scale is in)
+__host__ __device__ constexpr uint32_t idesc_fp4(int M, int N, int block) {
+  return (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | (block == 32 ? 1u << 23 : 0u) | ((uint32_t)(M >> 4) << 24);
 }
 template <int CTAS, int BLOCK>
 __device__ __forceinline__ void mma_fp4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate) {
@@ -55,30 +55,34 @@ struct Scales {
   static constexpr uint32_t kBytes = kTiles * (uint32_t)kTileBytes;   // of 128 rows
 };
 
-// The MMAs of a stage (up to four steps of 64 columns), by one thread.  ts: columns for scales, 4 for each tile of a's and of b's.
-// Copies and MMAs of one thread are carried out in their order, so a tile's columns are free when the next stage's copies come.
-template <int CTAS, int BLOCK>
-__device__ __forceinline__ void issue_stage(uint32_t acc, uint32_t ts, uint32_t a, uint32_t b, uint32_t sa, uint32_t sb, int bgroups, int steps, int M, int N,
-                                            bool first) {
+// The MMAs of a stage, by one thread: `steps` of 64 columns, four (FULL) but in the last stage.  ts: columns for scales, 4 for each tile of a's and of
+// b's.  Copies and MMAs of one thread are carried out in their order, so a tile's columns are free when the next stage's copies come.
+template <int CTAS, int BLOCK, int BGROUPS, bool FULL>
+__device__ __forceinline__ void issue_steps(uint32_t acc, uint32_t ts, uint32_t a, uint32_t b, uint32_t sa, uint32_t idesc, int steps, bool first) {
   typedef Scales<BLOCK> S;
-  const uint64_t da = tile_desc(a, ROW), db = tile_desc(b, ROW);
 #pragma unroll
   for (int tile = 0; tile < S::kTiles; ++tile) {
-    if (tile * BLOCK < 16 * steps) {
-      const uint32_t ca = ts + 4 * tile, cb = ts + 4 * S::kTiles + 4 * bgroups * tile;
-      scales_in<CTAS>(ca, sa + tile * kTileBytes);
-      scales_in<CTAS>(cb, sb + tile * kTileBytes);
-      if (bgroups == 2) scales_in<CTAS>(cb + 4, sb + S::kBytes + tile * kTileBytes);
+    if (FULL || tile * BLOCK < 16 * steps) {
+      const uint32_t ca = ts + 4 * tile, cb = ts + 4 * S::kTiles + 4 * BGROUPS * tile, at = sa + tile * kTileBytes;
+      scales_in<CTAS>(ca, at);
+      scales_in<CTAS>(cb, at + S::kBytes);
+      if (BGROUPS == 2) scales_in<CTAS>(cb + 4, at + 2 * S::kBytes);
     }
   }
+  const uint64_t da = tile_desc(a, ROW), db = tile_desc(b, ROW);
 #pragma unroll
   for (int k = 0; k < BK / 64; ++k) {
-    if (k < steps) {
+    if (FULL || k < steps) {
       const int tile = BLOCK == 16 ? k : k >> 1, id = BLOCK == 16 ? 0 : 2 * (k & 1);
-      const uint32_t ca = ts + 4 * tile, cb = ts + 4 * S::kTiles + 4 * bgroups * tile;
-      mma_fp4<CTAS, BLOCK>(acc, da + 2 * k, db + 2 * k, idesc_fp4(M, N, BLOCK, id), ca, cb, !first || k > 0);
+      mma_fp4<CTAS, BLOCK>(acc, da + 2 * k, db + 2 * k, idesc | (uint32_t)id << 4 | (uint32_t)id << 29, ts + 4 * tile,
+                           ts + 4 * S::kTiles + 4 * BGROUPS * tile, !first || k > 0);
     }
   }
+}
+template <int CTAS, int BLOCK, int BGROUPS>
+__device__ __forceinline__ void issue_stage(uint32_t acc, uint32_t ts, uint32_t a, uint32_t b, uint32_t sa, uint32_t idesc, int steps, bool first) {
+  if (steps >= BK / 64) issue_steps<CTAS, BLOCK, BGROUPS, true>(acc, ts, a, b, sa, idesc, steps, first);
+  else issue_steps<CTAS, BLOCK, BGROUPS, false>(acc, ts, a, b, sa, idesc, steps, first);
 }
 
 // ------------------------------------------------------------------------------------------------ pairs of SMs
@@ -103,82 +107,92 @@ __device__ __forceinline__ void arrive_relaxed_at(uint32_t bar) {
   asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
-// One epilogue warp: a quarter's 32 rows (lanes) of 128 columns of an accumulator.  It works in units of 128 bytes of out's rows (64 columns, or 32 of
-// binary32), whose residual is on its way while the unit before is finished, and leaves them in one of its two slabs in shared memory.  Where out's rows
-// (and the residual's) lie on 16-byte boundaries a slab goes out by TMA, which leaves out what is beyond the last row and column.  Other
-// rows are read back from it as binary32, a row at a time by lanes that stand beside one another in it, and stored in words of four bytes: in
-// an odd row, one of 16-bit elements that starts in the middle of a word, lane j has elements 2 j + 1 and 2 j + 2, and the last lane both ends.
+// One epilogue warp: a quarter's 32 rows (lanes) of 128 columns of an accumulator, in units of 128 bytes of out's rows (64 columns, or 32 of
+// binary32), each through one of the warp's two slabs in shared memory.  Where out's rows (and the residual's) lie on 16-byte boundaries TMA brings the
+// residual of a unit into its slab, those of the next tile's first two while its accumulator is formed, and takes the unit from there; it leaves out
+// what is beyond the last row and column.  Other rows are read back from the slabs as binary32, a row at a time by lanes that stand beside
+// one another in it, and stored in words of four bytes: in an odd row, one of 16-bit elements that starts in the middle of a word,
+// lane j has elements 2 j + 1 and 2 j + 2, and the last lane both ends.
 template <typename T>
 struct Epilogue {
   static constexpr int U = 128 / sizeof(T);   // columns of a unit
   typedef typename std::conditional<sizeof(T) == 4, uint32_t, uint16_t>::type Bits;
 
   const Fp4Params& p;
-  const CUtensorMap* tout;
+  const CUtensorMap *tout, *tres;
   uint8_t* slab;
+  uint64_t* bar;         // of each slab's residual
   const int lane;
-  const bool vectors;
-  int slot = 0;
+  const bool vectors, even;   // even: every row of out starts on a word of four bytes, and the residual's
+  uint32_t phase = 0;    // of the barriers, a bit each
   int t0, n0, end;       // the tile's first row of the warp, its first column, where its columns end
   float sr;
-  uint32_t res[32];      // residual of a unit: this lane's row, or its word (two words' halves) of each of 32 rows
+  uint32_t res[32];      // rows on other boundaries: the residual of a unit, this lane's word (two words' halves) of each of 32 rows
 
-  __device__ __forceinline__ Epilogue(const Fp4Params& p_, const CUtensorMap* tout_, uint8_t* slab_)
-      : p(p_), tout(tout_), slab(slab_), lane(threadIdx.x & 31), vectors(p_.vec_out && (!p_.residual || p_.vec_res)) {}
+  __device__ __forceinline__ Epilogue(const Fp4Params& p_, const CUtensorMap* tout_, const CUtensorMap* tres_, uint8_t* slab_, uint64_t* bar_)
+      : p(p_), tout(tout_), tres(tres_), slab(slab_), bar(bar_), lane(threadIdx.x & 31), vectors(p_.vec_out && (!p_.residual || p_.vec_res)),
+        even(((reinterpret_cast<uintptr_t>(p_.out) >> 1 | (uintptr_t)p_.out_stride) & 1) == 0 &&
+             (!p_.residual || ((reinterpret_cast<uintptr_t>(p_.residual) >> 1 | (uintptr_t)p_.res_stride) & 1) == 0)) {}
 
-  static __device__ __forceinline__ int odd_row(const void* q) { return (int)(reinterpret_cast<uintptr_t>(q) >> 1 & 1); }
-  // the residual of a tile into L2, ahead of its turn
-  __device__ __forceinline__ void prefetch(int t_first, int n_first) const {
-    const int t = t_first + lane;
-    if (!p.residual || t >= p.T || n_first >= p.O) return;
-    const uint8_t* const at = reinterpret_cast<const uint8_t*>(static_cast<const T*>(p.residual) + t * p.res_stride + n_first);
-    const int bytes = min(128, p.O - n_first) * (int)sizeof(T);
-    for (int o = 0; o < bytes; o += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(at + o));
-    asm volatile("prefetch.global.L2 [%0];" ::"l"(at + bytes - 1));
-  }
   __device__ __forceinline__ void tile(int t_first, int n_first) {
     t0 = t_first;
     n0 = n_first;
     end = min(n0 + 128, p.O);
     sr = t0 + lane < p.T ? (p.s_row ? p.s_row[t0 + lane] : 1.0f) : 0.f;
   }
-  __device__ __forceinline__ void fetch(int c0) {
-    const int o0 = n0 + c0;
-    if (!p.residual || o0 >= end) return;
-    const T* const residual = static_cast<const T*>(p.residual);
-    if (vectors) {
-      if (t0 + lane >= p.T) return;
-      const T* const at = residual + (t0 + lane) * p.res_stride + o0;
-      if (o0 + U <= end) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const uint4 q = reinterpret_cast<const uint4*>(at)[i];
-          res[4 * i] = q.x; res[4 * i + 1] = q.y; res[4 * i + 2] = q.z; res[4 * i + 3] = q.w;
-        }
-      } else {
-        const Bits* const e = reinterpret_cast<const Bits*>(at);
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          constexpr int n = 4 / (int)sizeof(T);
-          uint32_t w = o0 + n * i < end ? (uint32_t)e[n * i] : 0u;
-          if (n == 2 && o0 + 2 * i + 1 < end) w |= (uint32_t)e[2 * i + 1] << 16;
-          res[i] = w;
-        }
+  static __device__ __forceinline__ int odd_row(const void* q) { return (int)(reinterpret_cast<uintptr_t>(q) >> 1 & 1); }
+
+  // the residual of the unit at (t, o) on its way into a slab, whose last store has been read but for the `later` ones behind it
+  __device__ __forceinline__ void arm(int slot, int t, int o, int later) {
+    if (lane == 0) {
+      if (later) tma_store_wait_read_but_one();
+      else tma_store_wait_read();
+      if (p.residual && t < p.T && o < p.O) {
+        mbar_expect_tx(&bar[slot], 4096);
+        tma_load_2d(slab + slot * 4096, tres, &bar[slot], o, t);
       }
-      return;
     }
-    const Bits* at = reinterpret_cast<const Bits*>(residual) + t0 * p.res_stride + o0;
-    const T* to = static_cast<const T*>(p.out) + t0 * p.out_stride + o0;
-    const int rows = min(32, p.T - t0);
+    __syncwarp();
+  }
+  // before the accumulator of the tile at (t, n) is there: what it needs of the residual
+  __device__ __forceinline__ void ahead(int t, int n, bool down) {
+    if (vectors) {
+      const int c0 = down ? 64 : 0;
+      arm(0, t, n + c0, 1);
+      arm(1, t, n + (sizeof(T) == 4 ? c0 + 32 : c0 ^ 64), 0);
+    } else if (p.residual && t + lane < p.T && n < p.O) {   // into L2
+      const uint8_t* const at = reinterpret_cast<const uint8_t*>(static_cast<const T*>(p.residual) + (t + lane) * p.res_stride + n);
+      const int bytes = min(128, p.O - n) * (int)sizeof(T);
+      for (int o = 0; o < bytes; o += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(at + o));
+      asm volatile("prefetch.global.L2 [%0];" ::"l"(at + bytes - 1));
+    }
+  }
+  // rows on other boundaries: whole units are read and written without a check, a batch of rows at a time; `same`: words of the residual are where out's are
+  __device__ __forceinline__ bool whole(int o0) const { return t0 + 32 <= p.T && o0 + U <= end; }
+  __device__ __forceinline__ void fetch(int o0) {
+    if (vectors || !p.residual || !whole(o0)) return;
+    const Bits* at = static_cast<const Bits*>(p.residual) + t0 * p.res_stride + o0;
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int r = 0; r < 32; ++r, at += p.res_stride, to += p.out_stride) {
-      if (r >= rows) break;
-      if constexpr (sizeof(T) == 4) {
-        if (o0 + lane < end) res[r] = at[lane];
+      for (int r = 0; r < 32; ++r, at += p.res_stride) res[r] = at[lane];
+    } else {
+      const T* to = static_cast<const T*>(p.out) + t0 * p.out_stride + o0;
+      if (even) {   // (o0 is a multiple of 32)
+#pragma unroll
+        for (int r = 0; r < 32; ++r, at += p.res_stride) res[r] = reinterpret_cast<const uint32_t*>(at)[lane];
+      } else if (odd_row(at) == odd_row(to) && (((p.out_stride ^ p.res_stride) & 1) == 0)) {
+#pragma unroll
+        for (int r = 0; r < 32; ++r, at += p.res_stride, to += p.out_stride) {
+          const int odd = odd_row(to);
+          if (lane < 31 || !odd) res[r] = *reinterpret_cast<const uint32_t*>(at + 2 * lane + odd);
+          else res[r] = (uint32_t)at[63] | (uint32_t)at[0] << 16;
+        }
       } else {
-        const int odd = odd_row(to), a = 2 * lane + odd, b = (a + 1) & 63;
-        if (odd_row(at + odd) == 0 && b > a && o0 + b < end) res[r] = *reinterpret_cast<const uint32_t*>(at + a);
-        else res[r] = (o0 + a < end ? (uint32_t)at[a] : 0u) | (o0 + b < end ? (uint32_t)at[b] << 16 : 0u);
+#pragma unroll
+        for (int r = 0; r < 32; ++r, at += p.res_stride, to += p.out_stride) {
+          const int a = 2 * lane + odd_row(to);
+          res[r] = (uint32_t)at[a] | (uint32_t)at[(a + 1) & 63] << 16;
+        }
       }
     }
   }
@@ -201,47 +215,48 @@ struct Epilogue {
     }
   }
   // 32 columns, the first or second half of a unit of 16-bit elements, or all of one of binary32, into a slab
-  __device__ __forceinline__ void into(float2 (&f)[16], int half) {
+  __device__ __forceinline__ void into(float2 (&f)[16], int slot, int half) {
     if (vectors) {   // 16-byte chunks of a row of 128 bytes, as the 128-byte swizzle has them
       uint8_t* const to = slab + slot * 4096;
-      if (p.residual) {
 #pragma unroll
-        for (int c = 0; c < 16; ++c) {
-          if constexpr (sizeof(T) == 4) {
-            f[c] = __fadd2_rn(f[c], make_float2(__uint_as_float(res[2 * c]), __uint_as_float(res[2 * c + 1])));
-          } else {
-            const T* const r = reinterpret_cast<const T*>(&res[16 * half + c]);
-            f[c] = __fadd2_rn(f[c], make_float2(Elem<T>::get(r[0]), Elem<T>::get(r[1])));
+      for (int i = 0; i < 32 / (16 / (int)sizeof(T)); ++i) {
+        uint4* const at = reinterpret_cast<uint4*>(to + swz_off(lane, (sizeof(T) == 4 ? 0 : 4 * half) + i, 128));
+        if constexpr (sizeof(T) == 4) {
+          float2 x = f[2 * i], y = f[2 * i + 1];
+          if (p.residual) {
+            const float4 r = *reinterpret_cast<const float4*>(at);
+            x = __fadd2_rn(x, make_float2(r.x, r.y));
+            y = __fadd2_rn(y, make_float2(r.z, r.w));
           }
-        }
-      }
-      if constexpr (sizeof(T) == 4) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          *reinterpret_cast<uint4*>(to + swz_off(lane, i, 128)) = make_uint4(__float_as_uint(f[2 * i].x), __float_as_uint(f[2 * i].y),
-                                                                              __float_as_uint(f[2 * i + 1].x), __float_as_uint(f[2 * i + 1].y));
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
+          *at = make_uint4(__float_as_uint(x.x), __float_as_uint(x.y), __float_as_uint(y.x), __float_as_uint(y.y));
+        } else {
+          if (p.residual) {
+            const uint4 r = *at;
+            const float4 a = Elem<T>::cvt(make_uint2(r.x, r.y)), b = Elem<T>::cvt(make_uint2(r.z, r.w));
+            f[4 * i] = __fadd2_rn(f[4 * i], make_float2(a.x, a.y));
+            f[4 * i + 1] = __fadd2_rn(f[4 * i + 1], make_float2(a.z, a.w));
+            f[4 * i + 2] = __fadd2_rn(f[4 * i + 2], make_float2(b.x, b.y));
+            f[4 * i + 3] = __fadd2_rn(f[4 * i + 3], make_float2(b.z, b.w));
+          }
           const uint2 a = Elem<T>::pack(make_float4(f[4 * i].x, f[4 * i].y, f[4 * i + 1].x, f[4 * i + 1].y));
           const uint2 b = Elem<T>::pack(make_float4(f[4 * i + 2].x, f[4 * i + 2].y, f[4 * i + 3].x, f[4 * i + 3].y));
-          *reinterpret_cast<uint4*>(to + swz_off(lane, 4 * half + i, 128)) = make_uint4(a.x, a.y, b.x, b.y);
+          *at = make_uint4(a.x, a.y, b.x, b.y);
         }
       }
     } else {   // pairs of columns, at a place that depends on the row: no two lanes of a row or of a column meet in a bank
       constexpr int pairs = U / 2;
       float2* const to = reinterpret_cast<float2*>(slab) + lane * pairs;
 #pragma unroll
-      for (int c = 0; c < 16; ++c) to[(16 * half + c) ^ (lane & (pairs - 1))] = f[c];
+      for (int c = 0; c < 16; ++c) to[((sizeof(T) == 4 ? 0 : 16 * half) + c) ^ (lane & (pairs - 1))] = f[c];
     }
   }
-  __device__ __forceinline__ void take() {   // the slab's last store has been read
-    if (vectors) {
-      if (lane == 0) tma_store_wait_read_but_one();
-      __syncwarp();
-    }
+  // the slab is there for a unit: with the residual in it, or its last store read
+  __device__ __forceinline__ void take(int slot, int c0) {
+    if (!vectors || n0 + c0 >= end || t0 >= p.T || !p.residual) return;
+    mbar_wait(&bar[slot], phase >> slot & 1u, p.status);
+    phase ^= 1u << slot;
   }
-  __device__ __forceinline__ void leave(int c0) {
+  __device__ __forceinline__ void leave(int slot, int c0) {
     const int o0 = n0 + c0;
     if (vectors) {
       fence_async_smem();
@@ -250,40 +265,65 @@ struct Epilogue {
         if (o0 < end && t0 < p.T) tma_store_2d(tout, slab + slot * 4096, o0, t0);
         tma_store_commit();
       }
-      slot ^= 1;
       return;
     }
     __syncwarp();
-    if (o0 < end) {
-      constexpr int pairs = U / 2;
-      const float* const turn = reinterpret_cast<const float*>(slab);
-      T* at = static_cast<T*>(p.out) + t0 * p.out_stride + o0;
-      const int rows = min(32, p.T - t0);
-      auto column = [&](int r, int c) { return turn[r * U + (((c >> 1) ^ (r & (pairs - 1))) << 1) + (c & 1)]; };
+    constexpr int pairs = U / 2;
+    const float* const turn = reinterpret_cast<const float*>(slab);
+    auto column = [&](int r, int c) { return turn[r * U + (((c >> 1) ^ (r & (pairs - 1))) << 1) + (c & 1)]; };
+    T* at = static_cast<T*>(p.out) + t0 * p.out_stride + o0;
+    if (sizeof(T) == 2 && even && whole(o0)) {
 #pragma unroll
       for (int r = 0; r < 32; ++r, at += p.out_stride) {
-        if (r >= rows) break;
-        if constexpr (sizeof(T) == 4) {
-          const float x = column(r, lane);
-          if (o0 + lane < end) at[lane] = p.residual ? x + __uint_as_float(res[r]) : x;
-        } else {
-          const int odd = odd_row(at), a = 2 * lane + odd, b = (a + 1) & 63;
-          float2 x;
-          if (odd) x = make_float2(column(r, a), column(r, b));
-          else x = reinterpret_cast<const float2*>(turn)[r * pairs + (lane ^ r)];
-          if (p.residual) {
-            const T* const m = reinterpret_cast<const T*>(&res[r]);
-            x = __fadd2_rn(x, make_float2(Elem<T>::get(m[0]), Elem<T>::get(m[1])));
-          }
-          const uint32_t w = Elem<T>::pack(make_float4(x.x, x.y, 0.f, 0.f)).x;
-          if (b > a && o0 + b < end) {
-            *reinterpret_cast<uint32_t*>(at + a) = w;
+        float2 x = reinterpret_cast<const float2*>(turn)[r * pairs + (lane ^ (r & (pairs - 1)))];
+        if (p.residual) {
+          const T* const m = reinterpret_cast<const T*>(&res[r]);
+          x = __fadd2_rn(x, make_float2(Elem<T>::get(m[0]), Elem<T>::get(m[1])));
+        }
+        if constexpr (sizeof(T) == 2) reinterpret_cast<uint32_t*>(at)[lane] = Elem<T>::pack(make_float4(x.x, x.y, 0.f, 0.f)).x;
+      }
+    } else if (whole(o0)) {
+#pragma unroll
+      for (int r0 = 0; r0 < 32; r0 += 8) {
+        float2 x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int r = r0 + i;
+          if constexpr (sizeof(T) == 4) {
+            x[i].x = column(r, lane);
+            if (p.residual) x[i].x += __uint_as_float(res[r]);
           } else {
-            if (o0 + a < end) reinterpret_cast<uint16_t*>(at)[a] = (uint16_t)w;
-            if (o0 + b < end) reinterpret_cast<uint16_t*>(at)[b] = (uint16_t)(w >> 16);
+            const int a = 2 * lane + odd_row(at + i * p.out_stride);
+            x[i] = make_float2(column(r, a), column(r, (a + 1) & 63));
+            if (p.residual) {
+              const T* const m = reinterpret_cast<const T*>(&res[r]);
+              x[i] = __fadd2_rn(x[i], make_float2(Elem<T>::get(m[0]), Elem<T>::get(m[1])));
+            }
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i, at += p.out_stride) {
+          if constexpr (sizeof(T) == 4) {
+            at[lane] = x[i].x;
+          } else {
+            const int odd = odd_row(at);
+            const uint32_t w = Elem<T>::pack(make_float4(x[i].x, x[i].y, 0.f, 0.f)).x;
+            if (lane < 31 || !odd) {
+              *reinterpret_cast<uint32_t*>(at + 2 * lane + odd) = w;
+            } else {
+              reinterpret_cast<uint16_t*>(at)[63] = (uint16_t)w;
+              reinterpret_cast<uint16_t*>(at)[0] = (uint16_t)(w >> 16);
+            }
           }
         }
       }
+    } else if (o0 < end) {
+      const T* rat = static_cast<const T*>(p.residual) + t0 * p.res_stride + o0;
+#pragma unroll 1
+      for (int r = 0; r < 32 && t0 + r < p.T; ++r, at += p.out_stride, rat += p.res_stride)
+#pragma unroll
+        for (int c = lane; c < U; c += 32)
+          if (o0 + c < end) at[c] = Elem<T>::put(p.residual ? column(r, c) + Elem<T>::get(rat[c]) : column(r, c));
     }
     __syncwarp();
   }
@@ -292,7 +332,7 @@ struct Epilogue {
   template <typename R, typename F>
   __device__ __forceinline__ void run(uint32_t tmem, bool down, const float* cw, const float* cb, R ready, F drained) {
     int c0 = down ? 64 : 0;
-    fetch(c0);
+    fetch(n0 + c0);
     ready();
 #pragma unroll 1
     for (int i = 0; i < 2; ++i, c0 ^= 64) {
@@ -305,18 +345,31 @@ struct Epilogue {
         drained();
       }
       float2 f[16];
-      take();
       values(v, cw + c0, cb + c0, f);
-      into(f, 0);
       if constexpr (sizeof(T) == 4) {
-        leave(c0);
-        fetch(c0 + 32);
-        take();
+        take(0, c0);
+        into(f, 0, 0);
+        leave(0, c0);
+        fetch(n0 + c0 + 32);
+        values(u, cw + c0 + 32, cb + c0 + 32, f);
+        take(1, c0 + 32);
+        into(f, 1, 0);
+        leave(1, c0 + 32);
+        if (i == 0) {
+          fetch(n0 + (c0 ^ 64));
+          if (vectors) {
+            arm(0, t0, n0 + (c0 ^ 64), 1);
+            arm(1, t0, n0 + (c0 ^ 64) + 32, 0);
+          }
+        }
+      } else {
+        take(i, c0);
+        into(f, i, 0);
+        values(u, cw + c0 + 32, cb + c0 + 32, f);
+        into(f, i, 1);
+        leave(i, c0);
+        if (i == 0) fetch(n0 + (c0 ^ 64));
       }
-      values(u, cw + c0 + 32, cb + c0 + 32, f);
-      into(f, sizeof(T) == 4 ? 0 : 1);
-      leave(sizeof(T) == 4 ? c0 + 32 : c0);
-      if (i == 0) fetch(c0 ^ 64);
     }
   }
 };
@@ -324,7 +377,8 @@ struct Epilogue {
 template <typename T, int BLOCK>
 __global__ void __launch_bounds__(PT, 1) fp4_pair_kernel(const __grid_constant__ CUtensorMap tx, const __grid_constant__ CUtensorMap tw,
                                                          const __grid_constant__ CUtensorMap tsx, const __grid_constant__ CUtensorMap tsw,
-                                                         const __grid_constant__ CUtensorMap tout, const __grid_constant__ Fp4Params p) {
+                                                         const __grid_constant__ CUtensorMap tout, const __grid_constant__ CUtensorMap tres,
+                                                         const __grid_constant__ Fp4Params p) {
   typedef PairLayout S;
   constexpr uint32_t kSc = Scales<BLOCK>::kBytes;
   extern __shared__ __align__(1024) uint8_t smem[];   // (there is no static part: the window's base is on 1024 bytes)
@@ -332,7 +386,8 @@ __global__ void __launch_bounds__(PT, 1) fp4_pair_kernel(const __grid_constant__
   uint64_t* empty = full + S::kStages;
   uint64_t* acc_full = empty + S::kStages;
   uint64_t* acc_free = acc_full + 2;                               // (waited for in the first CTA)
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_free + 2);
+  uint64_t* res_full = acc_free + 2;                               // of the epilogue warps' slabs
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(res_full + 16);
   float* cols = reinterpret_cast<float*>(smem + S::kCols);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = blockIdx.x & 1, pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
@@ -345,12 +400,14 @@ __global__ void __launch_bounds__(PT, 1) fp4_pair_kernel(const __grid_constant__
       mbar_init(&acc_full[i], 1);
       mbar_init(&acc_free[i], 16);   // the epilogue warps of both
     }
+    for (int i = 0; i < 16; ++i) mbar_init(&res_full[i], 1);
     fence_mbar_init();
     tma_prefetch_desc(&tx);
     tma_prefetch_desc(&tw);
     tma_prefetch_desc(&tsx);
     tma_prefetch_desc(&tsw);
     tma_prefetch_desc(&tout);
+    tma_prefetch_desc(&tres);
   }
   __syncthreads();
   cluster_sync();   // (the other CTA's barriers are there)
@@ -394,8 +451,8 @@ __global__ void __launch_bounds__(PT, 1) fp4_pair_kernel(const __grid_constant__
         tc_fence_after();
         if (elect_one()) {
           const uint32_t a = smem_u32(smem + s * S::kStage);
-          issue_stage<2, BLOCK>(tmem + buf * (PBN - kShared), tmem + 2 * PBN - kShared, a, a + S::kA, a + S::kScales, a + S::kScales + kSc, 2,
-                                p.steps - kb * (BK / 64), 256, PBN, kb == 0);
+          issue_stage<2, BLOCK, 2>(tmem + buf * (PBN - kShared), tmem + 2 * PBN - kShared, a, a + S::kA, a + S::kScales, idesc_fp4(256, PBN, BLOCK),
+                                   p.steps - kb * (BK / 64), kb == 0);
           pair_commit(&empty[s]);
           if (kb + 1 == p.kblocks) pair_commit(&acc_full[buf]);
         }
@@ -404,7 +461,7 @@ __global__ void __launch_bounds__(PT, 1) fp4_pair_kernel(const __grid_constant__
     }
   } else if (warp >= 4) {
     const int quarter = warp & 3, upper = (warp - 4) >> 2, et = tid & 127;   // eight warps: a quarter of the rows, half of the columns
-    Epilogue<T> ep(p, &tout, smem + S::kSlabs + (warp - 4) * 2 * 4096);
+    Epilogue<T> ep(p, &tout, &tres, smem + S::kSlabs + (warp - 4) * 2 * 4096, res_full + (warp - 4) * 2);
     // a column's step size and bias, a tile ahead
     float w = 0.f, b = 0.f;
     auto column = [&](int n) {
@@ -415,7 +472,7 @@ __global__ void __launch_bounds__(PT, 1) fp4_pair_kernel(const __grid_constant__
     int at = 0, m, n;
     tile_of<8>(pair, p.mtiles, p.ntiles, &m, &n);
     column(n);
-    ep.prefetch(m * 256 + rank * 128 + quarter * 32, n * PBN + upper * 128);
+    ep.ahead(m * 256 + rank * 128 + quarter * 32, n * PBN + upper * 128, true);
     for (int tile = pair; tile < ntotal; tile += npairs, ++at) {
       const int buf = at & 1;
       float* const cw = cols + (buf * 2 + upper) * 256;
@@ -425,7 +482,6 @@ __global__ void __launch_bounds__(PT, 1) fp4_pair_kernel(const __grid_constant__
       if (tile + npairs < ntotal) {
         tile_of<8>(tile + npairs, p.mtiles, p.ntiles, &m, &n);
         column(n);
-        ep.prefetch(m * 256 + rank * 128 + quarter * 32, n * PBN + upper * 128);
       }
       named_bar_sync(3 + upper, 128);   // the four warps of these columns (nobody is still reading those of the tile before the last)
       // The shared columns are the last of the first accumulator and the first of the second: the upper half's or the lower's.  The warps of the other
@@ -441,6 +497,7 @@ __global__ void __launch_bounds__(PT, 1) fp4_pair_kernel(const __grid_constant__
                if (shared) free();
              });
       tc_fence_before();   // (what the next tile's arrival vouches for)
+      if (tile + npairs < ntotal) ep.ahead(m * 256 + rank * 128 + quarter * 32, n * PBN + upper * 128, buf != 0);
     }
     if (lane == 0) tma_store_wait_read();
   }
@@ -455,14 +512,15 @@ __global__ void __launch_bounds__(PT, 1) fp4_pair_kernel(const __grid_constant__
 }
 
 // ------------------------------------------------------------------------------------------------ few rows
-// The weight's rows are the accumulator's 128 lanes and up to 256 tokens its columns, and K is shared out among the CTAs of a cluster until the SMs
-// are all at it.  The parts of a tile meet in shared memory, added in the order of their CTAs, each CTA finishing some tokens.
+// The weight's rows are the accumulator's 128 lanes and up to 256 tokens its columns, a tile to a CTA, and K is shared out among the CTAs of a cluster
+// until the SMs are all at it.  The parts of a tile meet in shared memory, added in the order of their CTAs, each CTA finishing some tokens.
 constexpr int FT = 256;
 struct FewLayout {
-  static constexpr int kMaxStages = 5;
+  static constexpr int kMaxStages = 10;
   static constexpr uint32_t kW = 128 * ROW;
-  static constexpr uint32_t kSmall = 101376, kLarge = 221184;    // the ring, two CTAs on an SM or one; the accumulator's image of [n][128] goes over it
-  static constexpr uint32_t kTail = 256 + 1024;                  // barriers; the tiles start on 1024 bytes
+  // the ring, two CTAs on an SM or one; the accumulator's image of [n][128] goes over it
+  static constexpr uint32_t kSmall = 101376, kLarge = 221184;
+  static constexpr uint32_t kRows = 256, kTail = kRows + 256 * 4 + 1024;   // barriers, step sizes of rows; the tiles start on 1024 bytes
 };
 static_assert(2 * (FewLayout::kSmall + FewLayout::kTail + 1024) <= 233472 && FewLayout::kLarge + FewLayout::kTail <= 232448, "");
 struct FewParams {
@@ -478,6 +536,68 @@ __device__ __forceinline__ float4 ld_from(const float* p, int rank) {   // the s
   asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
   return v;
 }
+// (relaxed: nothing was written for the others; a release would wait for stores to out)
+__device__ __forceinline__ void cluster_leave() {
+  asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
+  cluster_wait();
+}
+
+// A CTA's tokens, every split-th one, a warp to a token and four outputs to a lane: the parts of four tokens and their residuals on their way at a time
+template <typename T, int ACT>
+__device__ __forceinline__ void few_out(const FewParams& f, const float* part, const float* s_row, int rank, int tok0, int ntok, int o, int no,
+                                        const float (&sw)[4], const float (&bias)[4]) {
+  const Fp4Params& p = f.l;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, step = f.split * (FT / 32), first = rank + f.split * warp;
+  const bool vector = no == 4 && p.vec_out && (!p.residual || p.vec_res);
+  T* dst = static_cast<T*>(p.out) + (i64)(tok0 + first) * p.out_stride + o;
+  const T* res = static_cast<const T*>(p.residual) + (i64)(tok0 + first) * p.res_stride + o;
+  const i64 dstep = (i64)step * p.out_stride, rstep = (i64)step * p.res_stride;
+  const float2 w0 = make_float2(sw[0], sw[1]), w1 = make_float2(sw[2], sw[3]), b0 = make_float2(bias[0], bias[1]), b1 = make_float2(bias[2], bias[3]);
+#pragma unroll 1
+  for (int t0 = first; t0 < ntok; t0 += 4 * step, dst += 4 * dstep, res += 4 * rstep) {
+    float4 acc[4];
+    typename Elem<T>::raw4 q[4];
+    if (vector && p.residual) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (t0 + u * step < ntok) q[u] = *reinterpret_cast<const typename Elem<T>::raw4*>(res + u * rstep);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const float* const at = part + min(t0 + u * step, ntok - 1) * 128 + 4 * lane;
+      acc[u] = f.split == 1 ? *reinterpret_cast<const float4*>(at) : ld_from(at, 0);
+    }
+    for (int r = 1; r < f.split; ++r) {
+      float4 v[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) v[u] = ld_from(part + min(t0 + u * step, ntok - 1) * 128 + 4 * lane, r);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) acc[u] = make_float4(acc[u].x + v[u].x, acc[u].y + v[u].y, acc[u].z + v[u].z, acc[u].w + v[u].w);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (t0 + u * step >= ntok) break;
+      const float sr = s_row[t0 + u * step];
+      float2 x = __ffma2_rn(__fmul2_rn(make_float2(acc[u].x, acc[u].y), make_float2(sr, sr)), w0, b0);
+      float2 y = __ffma2_rn(__fmul2_rn(make_float2(acc[u].z, acc[u].w), make_float2(sr, sr)), w1, b1);
+      x = make_float2(activate(x.x, ACT), activate(x.y, ACT));
+      y = make_float2(activate(y.x, ACT), activate(y.y, ACT));
+      if (vector) {
+        if (p.residual) {
+          const float4 r = Elem<T>::cvt(q[u]);
+          x = __fadd2_rn(x, make_float2(r.x, r.y));
+          y = __fadd2_rn(y, make_float2(r.z, r.w));
+        }
+        *reinterpret_cast<typename Elem<T>::raw4*>(dst + u * dstep) = Elem<T>::pack(make_float4(x.x, x.y, y.x, y.y));
+      } else {
+        const float v[4] = {x.x, x.y, y.x, y.y};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (e < no) dst[u * dstep + e] = Elem<T>::put(p.residual ? v[e] + Elem<T>::get(res[u * rstep + e]) : v[e]);
+      }
+    }
+  }
+}
 
 template <typename T, int BLOCK>
 __global__ void __launch_bounds__(FT, 2) fp4_few_kernel(const __grid_constant__ CUtensorMap tx, const __grid_constant__ CUtensorMap tw,
@@ -492,6 +612,7 @@ __global__ void __launch_bounds__(FT, 2) fp4_few_kernel(const __grid_constant__ 
   uint64_t* empty = full + S::kMaxStages;
   uint64_t* acc_full = empty + S::kMaxStages;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_full + 1);
+  float* s_row = reinterpret_cast<float*>(smem + f.ring + S::kRows);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
     for (int i = 0; i < S::kMaxStages; ++i) {
@@ -507,19 +628,11 @@ __global__ void __launch_bounds__(FT, 2) fp4_few_kernel(const __grid_constant__ 
   }
   __syncthreads();
   pdl_wait();
-  const uint32_t tmem = warp == 0 ? 0u : allocated<1>(tmem_slot, f.columns, warp, FT);
+  if (warp != 0) allocated<1>(tmem_slot, f.columns, warp, FT);
   // CTAs of a cluster, then the tiles of tokens, then those of the weight (which their CTAs share in L2)
   const int rank = blockIdx.x % f.split, tile = blockIdx.x / f.split, m = tile / p.ntiles, n = tile % p.ntiles;
   const int o0 = m * 128, tok0 = n * f.n, ntok = min(f.n, p.T - tok0);
   const int kb0 = (int)((i64)p.kblocks * rank / f.split), kb1 = (int)((i64)p.kblocks * (rank + 1) / f.split);
-  // a warp per token in the end, four outputs per lane
-  const int o = o0 + 4 * lane, no = min(p.O - o, 4), step = f.split * (FT / 32);
-  float sw[4], bias[4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    sw[e] = e < no ? (p.s_w ? p.s_w[o + e] : 1.0f) : 0.f;
-    bias[e] = e < no && p.bias ? p.bias[o + e] : 0.f;
-  }
   // (n % 16 = 0: codes and scales start on 1024 bytes)
   const uint32_t scales = S::kW + f.n * ROW, stage = (scales + (1 + f.bgroups) * kSc + 1023) & ~1023u;
   if (warp == 0) {
@@ -539,84 +652,68 @@ __global__ void __launch_bounds__(FT, 2) fp4_few_kernel(const __grid_constant__ 
       if (++s == f.stages) { s = 0; ++round; }
     }
   } else if (warp == 1) {
-    int s = 0, round = 0;
-    for (int kb = kb0; kb < kb1; ++kb) {
-      mbar_wait(&full[s], round & 1, p.status);
-      tc_fence_after();
-      if (elect_one()) {
-        const uint32_t a = smem_u32(smem + s * stage);
-        issue_stage<1, BLOCK>(tmem, tmem + f.n, a, a + S::kW, a + scales, a + scales + kSc, f.bgroups, p.steps - kb * (BK / 64), 128, f.n, kb == kb0);
-        mma_commit(&empty[s]);
-        if (kb + 1 == kb1) mma_commit(acc_full);
+    const uint32_t tmem = *tmem_slot, idesc = idesc_fp4(128, f.n, BLOCK), base = smem_u32(smem);
+    const auto issue = [&](auto groups) {
+      int s = 0, round = 0;
+      for (int kb = kb0; kb < kb1; ++kb) {
+        mbar_wait(&full[s], round & 1, p.status);
+        tc_fence_after();
+        if (elect_one()) {
+          const uint32_t a = base + s * stage;
+          issue_stage<1, BLOCK, decltype(groups)::value>(tmem, tmem + f.n, a, a + S::kW, a + scales, idesc, p.steps - kb * (BK / 64), kb == kb0);
+          mma_commit(&empty[s]);
+          if (kb + 1 == kb1) mma_commit(acc_full);
+        }
+        __syncwarp();
+        if (++s == f.stages) { s = 0; ++round; }
       }
-      __syncwarp();
-      if (++s == f.stages) { s = 0; ++round; }
-    }
+    };
+    if (f.bgroups == 1) issue(std::integral_constant<int, 1>());
+    else issue(std::integral_constant<int, 2>());
+  } else if (warp == 3) {
+    for (int i = lane; i < ntok; i += 32) s_row[i] = p.s_row ? p.s_row[tok0 + i] : 1.0f;
+  }
+  // a warp per token in the end, four outputs per lane
+  const int o = o0 + 4 * lane, no = min(p.O - o, 4);
+  float sw[4], bias[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    sw[e] = e < no ? (p.s_w ? p.s_w[o + e] : 1.0f) : 0.f;
+    bias[e] = e < no && p.bias ? p.bias[o + e] : 0.f;
   }
   float* const part = reinterpret_cast<float*>(smem);   // [n][128]
-  if (warp >= 4) {
-    // the accumulator over the ring: every load has been consumed by an MMA that is complete
+  __syncthreads();
+  {
+    // the accumulator over the ring: every load has been consumed by an MMA that is complete.  Two warps to a quarter of the lanes.
     const int quarter = warp & 3;
     mbar_wait(acc_full, 0, p.status);
     tc_fence_after();
-    for (int c0 = 0; c0 < f.n; c0 += 16) {
+    const uint32_t at = *tmem_slot + ((uint32_t)(quarter * 32) << 16);
+    float* const to = part + quarter * 32 + lane;
+    for (int c0 = warp >> 2 << 4; c0 < f.n; c0 += 32) {
       int v[16];
-      tmem_ld8(tmem + ((uint32_t)(quarter * 32) << 16) + c0, reinterpret_cast<int(&)[8]>(v[0]));
-      tmem_ld8(tmem + ((uint32_t)(quarter * 32) << 16) + c0 + 8, reinterpret_cast<int(&)[8]>(v[8]));
+      tmem_ld8(at + c0, reinterpret_cast<int(&)[8]>(v[0]));
+      tmem_ld8(at + c0 + 8, reinterpret_cast<int(&)[8]>(v[8]));
       tmem_ld_wait();
 #pragma unroll
-      for (int c = 0; c < 16; ++c) part[(c0 + c) * 128 + quarter * 32 + lane] = __int_as_float(v[c]);
+      for (int c = 0; c < 16; ++c) to[(c0 + c) * 128] = __int_as_float(v[c]);
     }
     tc_fence_before();
   }
   __syncthreads();
   if (f.split > 1) cluster_sync();
-  // (the parts of four tokens on their way at a time)
-  for (int t0 = rank + f.split * warp; t0 < ntok; t0 += 4 * step) {
-    float4 acc[4];
-    float srs[4];
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      acc[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-      srs[u] = p.s_row && t0 + u * step < ntok ? p.s_row[tok0 + t0 + u * step] : 1.0f;
-    }
-    for (int r = 0; r < f.split; ++r)
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (t0 + u * step < ntok) {
-          const float* const at = part + (t0 + u * step) * 128 + 4 * lane;
-          const float4 v = f.split == 1 ? *reinterpret_cast<const float4*>(at) : ld_from(at, r);
-          acc[u] = make_float4(acc[u].x + v.x, acc[u].y + v.y, acc[u].z + v.z, acc[u].w + v.w);
-        }
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      if (t0 + u * step >= ntok || no <= 0) continue;
-      const i64 t = tok0 + t0 + u * step;
-      const float a4[4] = {acc[u].x, acc[u].y, acc[u].z, acc[u].w};
-      const T* const res = p.residual ? static_cast<const T*>(p.residual) + t * p.res_stride + o : nullptr;
-      T* const dst = static_cast<T*>(p.out) + t * p.out_stride + o;
-      float v[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = activate(fmaf(a4[e] * srs[u], sw[e], bias[e]), p.act);
-      if (no == 4 && p.vec_out && (!res || p.vec_res)) {
-        if (res) {
-          const float4 q = Elem<T>::cvt(*reinterpret_cast<const typename Elem<T>::raw4*>(res));
-          v[0] += q.x; v[1] += q.y; v[2] += q.z; v[3] += q.w;
-        }
-        *reinterpret_cast<typename Elem<T>::raw4*>(dst) = Elem<T>::pack(make_float4(v[0], v[1], v[2], v[3]));
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (e < no) dst[e] = Elem<T>::put(res ? v[e] + Elem<T>::get(res[e]) : v[e]);
-      }
-    }
+  if (no > 0) {
+    const auto finish = [&](auto act) { few_out<T, decltype(act)::value>(f, part, s_row, rank, tok0, ntok, o, no, sw, bias); };
+    if (p.act == SSDI8_ACT_SILU) finish(std::integral_constant<int, SSDI8_ACT_SILU>());
+    else if (p.act == SSDI8_ACT_RELU2) finish(std::integral_constant<int, SSDI8_ACT_RELU2>());
+    else finish(std::integral_constant<int, SSDI8_ACT_NONE>());
   }
   drain_after_timeout(p.status);
-  if (f.split > 1) cluster_sync();   // (the others have read this CTA's part)
+  if (f.split > 1) cluster_leave();   // (the others have read this CTA's part)
   else __syncthreads();
   if (warp == 2) {
     tc_fence_after();
-    tmem_dealloc(tmem, f.columns);
+    tmem_dealloc(*tmem_slot, f.columns);
   }
 }
 
@@ -650,26 +747,40 @@ ssdi8_status_t launch(const ssdi8_fp4_linear_args_t& a, cudaStream_t st) {
     return encode_tensor_map(tm, q.scales, 4, 2, dims, stride, box, 0);
   };
   if (!scales(&tsx, x) || !scales(&tsw, w)) return SSDI8_ERR_CUDA;
-  // What is done sooner, in cycles: an SM takes 60 bytes of operands a cycle.
+  // What is done sooner, in cycles (the figures are measured ones).  Few rows: 7200 for a launch, the first operands and the accumulator's way out, 46
+  // bytes of operands a cycle and SM in between, or where the ring does not hold all of a CTA's stages their latency of 1400 over those
+  // that it holds; the parts' meeting, the tokens.
   const i64 mt = (w.rows + 127ll) / 128;
   FewParams f = {};
   double best = 0.0;
   for (int n = x.rows <= 256 ? (x.rows + 15) / 16 * 16 : 128; n <= 256; n += x.rows <= 256 ? 256 : 128) {
     const i64 tiles = mt * ((x.rows + n - 1ll) / n);
-    const int per_sm = n <= 128 ? 2 : 1;
-    const double bytes = FewLayout::kW + n * ROW + (n <= 128 ? 2 : 3) * (double)Scales<BLOCK>::kBytes;
-    for (int split = 1; split <= 8 && split <= p.kblocks; split *= 2) {
-      const double waves = (double)((tiles * split + sms * per_sm - 1) / (sms * per_sm)), share = tiles * split < sms ? 1.0 : (double)per_sm;
-      const double cycles = waves * (share * ((p.kblocks + split - 1) / split * bytes / 60.0 + n * 8.0) + 3000.0 + (split > 1 ? 1000.0 : 0.0));
-      if (best == 0.0 || cycles < best) {
-        best = cycles;
-        f.n = n;
-        f.split = split;
+    const uint32_t bytes = (FewLayout::kW + n * ROW + (n <= 128 ? 2 : 3) * Scales<BLOCK>::kBytes + 1023) & ~1023u;
+    for (int per_sm = n <= 128 ? 2 : 1; per_sm >= 1; --per_sm) {
+      const int ring = (int)(per_sm == 2 ? FewLayout::kSmall : FewLayout::kLarge), stages = ring / (int)bytes < FewLayout::kMaxStages ? ring / (int)bytes : FewLayout::kMaxStages;
+      // (clusters of four take 7 of 8 SMs at best, 16 of a GPC's 18; of eight fewer: 64 x 2560 x 5120 8 us with four, 19 to 22 with eight)
+      for (int split = 1; split <= 4 && split <= p.kblocks; split *= 2) {
+        const i64 places = (i64)(split == 4 ? sms - sms / 8 : sms) * per_sm;
+        const double ctas = (double)tiles * split, waves = (double)((tiles * split + places - 1) / places), share = ctas <= sms ? 1.0 : (double)per_sm;
+        const int kb = (p.kblocks + split - 1) / split;
+        const double port = kb * (double)bytes * share / 46.0, latency = kb > stages ? (kb - stages) * 1400.0 / stages : 0.0;
+        const double cycles = 5000.0 + waves * (2200.0 + (port > latency ? port : latency) + n * 4.0 + (split > 1 ? 1300.0 : 0.0) + n / split * 8.0);
+        if (best == 0.0 || cycles < best) {
+          best = cycles;
+          f.n = n;
+          f.split = split;
+          f.ring = ring;
+          f.stages = stages;
+        }
       }
     }
   }
+  // Pairs: 11400 for a launch, the first operands and the last tile's way out, 570 for 256 of K where no epilogue is beside them and 760 where one is, 1700
+  // from one tile to the next; an epilogue's 7000 hide behind the next tile's product.  (One wave of each, us: 64 x 10576 x 2560 few rows 6.9, pairs 9.7;
+  // 512 x 2560 x 5120 11.3, 11.7; 250 x 18560 x 4096 17.2, 14.8; 1024 x 2560 x 5120 15.7, 12.7.)
   const i64 ptiles = (i64)((x.rows + 255ll) / 256) * ((w.rows + PBN - 1ll) / PBN), pairs = sms / 2;
-  const bool pair = pairs > 0 && (double)((ptiles + pairs - 1) / pairs) * (650.0 * p.kblocks + 800.0) + 5000.0 < best;
+  const double each = 760.0 * p.kblocks + 1700.0;
+  const bool pair = pairs > 0 && 11400.0 + 570.0 * p.kblocks + (double)((ptiles + pairs - 1) / pairs - 1) * (each > 7000.0 ? each : 7000.0) < best;
   if (pair) {
     if (ptiles > 0x3fffffff) return SSDI8_ERR_SHAPE;
     p.mtiles = (int)((x.rows + 255ll) / 256);
@@ -679,19 +790,18 @@ ssdi8_status_t launch(const ssdi8_fp4_linear_args_t& a, cudaStream_t st) {
     const uint64_t dims[2] = {(uint64_t)p.O, (uint64_t)p.T}, stride[1] = {(uint64_t)(a.stride_out * e)};
     const uint32_t box[2] = {(uint32_t)(128 / e), 32};
     if (p.vec_out && !encode_tensor_map(&tout, a.out, (int)e, 2, dims, stride, box, 128)) p.vec_out = 0;
+    CUtensorMap tres = tx;
+    const uint64_t rstride[1] = {(uint64_t)(a.stride_residual * e)};
+    if (a.residual && p.vec_res && !encode_tensor_map(&tres, a.residual, (int)e, 2, dims, rstride, box, 128)) p.vec_res = 0;
     return launch_any(fp4_pair_kernel<T, BLOCK>, dim3((unsigned)(2 * (ptiles < pairs ? ptiles : pairs))), 2, dim3(PT), PairLayout::kAlloc, PairLayout::kAlloc,
-                      -1, true, st, tx, tw, tsx, tsw, tout, p);
+                      -1, true, st, tx, tw, tsx, tsw, tout, tres, p);
   }
   f.l = p;
   f.l.mtiles = (int)mt;
   f.l.ntiles = (int)((x.rows + f.n - 1ll) / f.n);
   f.bgroups = f.n <= 128 ? 1 : 2;
-  f.ring = f.n <= 128 ? FewLayout::kSmall : FewLayout::kLarge;
   const int need = f.n + 4 * Scales<BLOCK>::kTiles * (1 + f.bgroups);
   f.columns = need <= 64 ? 64 : need <= 128 ? 128 : need <= 256 ? 256 : 512;
-  const uint32_t stage = (FewLayout::kW + f.n * ROW + (1 + f.bgroups) * Scales<BLOCK>::kBytes + 1023) & ~1023u;
-  const int stages = (int)(f.ring / stage);
-  f.stages = stages < FewLayout::kMaxStages ? stages : FewLayout::kMaxStages;
   const i64 grid = (i64)f.l.mtiles * f.l.ntiles * f.split;
   if (grid > 0x7fffffff) return SSDI8_ERR_SHAPE;
   if (!codes(&tx, x, f.n) || !codes(&tw, w, 128)) return SSDI8_ERR_CUDA;
