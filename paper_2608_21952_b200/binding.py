@@ -435,9 +435,9 @@ def make_fp4(rows: int, width: int, block: int = 16, device="cuda") -> Fp4:
     return fp4_of(z(rows, width // 2), z(*_fp4_tiles(rows, width, block)), torch.ones(rows, device=device), block)
 
 
-def ssdi8_fp4_quantize(x, q: Fp4, stream=None) -> None:
+def ssdi8_fp4_quantize(x, q: Fp4, status=None, stream=None) -> None:
     """x [rows, width] (rows of any stride; fp32, fp16 or bf16) into a matrix in four bits."""
-    code = _m.fp4_quantize(x, q, stream)
+    code = _m.fp4_quantize(x, q, status, stream)
     if code:
         _check(code, "ssdi8_fp4_quantize")
 
@@ -450,10 +450,10 @@ def ssdi8_fp4_dequantize(q: Fp4, out, stream=None) -> None:
 
 
 def ssdi8_add_norm_quantize(x, residual=None, residual_out=None, weight=None, eps: float = 1e-5, xq=None, scale=None, static_scale=None,
-                            fp4=None, stream=None) -> None:
+                            fp4=None, status=None, stream=None) -> None:
     """h = x + residual [T, D] (rows of any stride) into residual_out, and the RMS norm of h to int8 codes xq with a step size per row in
     `scale` (or under a static one), or to a matrix in four bits."""
-    code = _m.add_norm_quantize(x, residual, residual_out, weight, eps, xq, scale, static_scale, fp4, stream)
+    code = _m.add_norm_quantize(x, residual, residual_out, weight, eps, xq, scale, static_scale, fp4, status, stream)
     if code:
         _check(code, "ssdi8_add_norm_quantize")
 

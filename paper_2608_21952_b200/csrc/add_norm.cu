@@ -8,12 +8,14 @@
 // a pipe that nothing else uses.
 #include "fp4.cuh"
 #include "kernels.h"
+#include "sm100.cuh"
 
 #include <type_traits>
 
 namespace ssdi8 {
 namespace {
 
+constexpr int kMaxRing = 8;
 constexpr int kChunk = 256;   // columns of a chunk: a warp's lanes have eight each, so that a block of 16 is two lanes and one of 32 four
 
 struct None {};   // no residual stream
@@ -26,26 +28,34 @@ struct RowParams {
   const float* static_scale;
   int8_t* xq; float* scale;                  // int8: codes, step sizes (or NULL)
   uint8_t *codes, *scales; float* step;      // four bits
+  int32_t* status;
   int D, block, tiles;
   bool vx, vr, vs;                           // rows on 16 bytes (16-bit elements), 16 bytes (fp32)
   float eps;
 };
 
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, bool aligned, float (&v)[8]) {
+__device__ __forceinline__ void unpack8(const uint4& q, float (&v)[8]) {   // of 16-bit elements
+  const float4 a = Elem<T>::cvt(make_uint2(q.x, q.y)), b = Elem<T>::cvt(make_uint2(q.z, q.w));
+  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+__device__ __forceinline__ void spread8(const float4& a, const float4& b, float (&v)[8]) {
+  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, bool aligned, float (&v)[8]) {   // from global memory
   if (aligned) {
-    if constexpr (sizeof(T) == 4) {
-      const float4 a = __ldcs(reinterpret_cast<const float4*>(p)), b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
-      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-    } else {
-      const uint4 q = __ldcs(reinterpret_cast<const uint4*>(p));
-      const float4 a = Elem<T>::cvt(make_uint2(q.x, q.y)), b = Elem<T>::cvt(make_uint2(q.z, q.w));
-      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-    }
+    if constexpr (sizeof(T) == 4) spread8(__ldcs(reinterpret_cast<const float4*>(p)), __ldcs(reinterpret_cast<const float4*>(p) + 1), v);
+    else unpack8<T>(__ldcs(reinterpret_cast<const uint4*>(p)), v);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = Elem<T>::get(p[i]);
   }
+}
+template <typename T>
+__device__ __forceinline__ void load8_shared(const void* p, float (&v)[8]) {   // on 16 bytes
+  if constexpr (sizeof(T) == 4) spread8(static_cast<const float4*>(p)[0], static_cast<const float4*>(p)[1], v);
+  else unpack8<T>(*static_cast<const uint4*>(p), v);
 }
 // rounds to T, in place, and stores (p = NULL: does not)
 template <typename T>
@@ -74,6 +84,9 @@ __device__ __forceinline__ void store8(T* p, bool aligned, float (&v)[8]) {
   }
 }
 
+__device__ __forceinline__ void bulk_store(void* dst, const void* src, uint32_t bytes) {   // both on 16 bytes
+  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(sm100::smem_u32(src)), "r"(bytes) : "memory");
+}
 __device__ __forceinline__ float warp_max(float v) {   // of numbers >= 0; a NaN counts for nothing
   float m;
   asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(v));
@@ -113,41 +126,20 @@ __device__ __forceinline__ void chunk_fp4(const RowParams& p, i64 row, int chunk
   if (tile < p.tiles) *reinterpret_cast<uint32_t*>(p.scales + fp4_scale_at(row, tile, p.tiles)) = word;
 }
 
-// A block has a row, a warp NCH chunks of it, one after the other.  NORM: h, its norm and the weight; else p is x (four bits).
-template <typename T, typename R, int NCH, bool NORM, bool FP4>
-__global__ void __launch_bounds__(512) row_kernel(const __grid_constant__ RowParams p) {
-  __shared__ double sums[16];
-  __shared__ float maxima[16];
-  pdl_launch_dependents();
-  pdl_wait();
+// What a row's threads say to one another; two of each, so that a row's are read while the next one's are written
+struct Meeting {
+  double sums[2][16];
+  float maxima[2][16];
+};
+
+// A warp's chunks of a row from their h (v): p = h w, the row's sum of squares and absmax of p (the block's only barrier), step sizes and codes.
+// `behind` is called behind that barrier.
+template <int NCH, bool NORM, bool FP4, typename F>
+__device__ __forceinline__ void finish_row(const RowParams& p, Meeting& meet, int turn, i64 row, float (&v)[NCH][8], F behind) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nwarps = blockDim.x >> 5;
-  const i64 row = blockIdx.x;
   const int c0 = warp * NCH, col0 = c0 * kChunk + lane * 8;
-  float v[NCH][8], m[NCH];
+  float m[NCH];
   double ss = 0.0;
-#pragma unroll
-  for (int k = 0; k < NCH; ++k) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[k][i] = 0.f;
-    if (col0 + k * kChunk < p.D) load8<T>(static_cast<const T*>(p.x) + row * p.sx + col0 + k * kChunk, p.vx, v[k]);
-  }
-  if constexpr (!std::is_same<R, None>::value) {
-    const R* const res = static_cast<const R*>(p.residual);
-    R* const out = static_cast<R*>(p.stream);
-    float r[NCH][8];
-#pragma unroll
-    for (int k = 0; k < NCH; ++k)
-      if (res && col0 + k * kChunk < p.D) load8<R>(res + row * p.sr + col0 + k * kChunk, p.vr, r[k]);
-#pragma unroll
-    for (int k = 0; k < NCH; ++k)
-      if (col0 + k * kChunk < p.D) {
-        if (res) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) v[k][i] = __fadd_rn(v[k][i], r[k][i]);
-        }
-        store8<R>(out ? out + row * p.ss + col0 + k * kChunk : nullptr, p.vs, v[k]);
-      }
-  }
 #pragma unroll
   for (int k = 0; k < NCH; ++k) {
     if constexpr (NORM) {
@@ -172,16 +164,17 @@ __global__ void __launch_bounds__(512) row_kernel(const __grid_constant__ RowPar
       for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
     }
     if (lane == 0) {
-      maxima[warp] = top;
-      if (NORM) sums[warp] = ss;
+      meet.maxima[turn][warp] = top;
+      if (NORM) meet.sums[turn][warp] = ss;
     }
-    __syncthreads();
-    top = warp_max(lane < nwarps ? maxima[lane] : 0.f);
   }
+  __syncthreads();
+  behind();
+  if (NORM || p.block == 16) top = warp_max(lane < nwarps ? meet.maxima[turn][lane] : 0.f);
   // 1 / sqrt(mean + eps), by the threads that need it
   auto factor = [&] {
     double s = 0.0;
-    for (int i = 0; i < nwarps; ++i) s += sums[i];
+    for (int i = 0; i < nwarps; ++i) s += meet.sums[turn][i];
     return 1.0 / sqrt(s / (double)p.D + (double)p.eps);
   };
   if constexpr (FP4) {
@@ -220,6 +213,116 @@ __global__ void __launch_bounds__(512) row_kernel(const __grid_constant__ RowPar
   }
 }
 
+// A block has a row, a warp NCH chunks of it, one after the other.  NORM: h, its norm and the weight; else p is x (four bits).
+template <typename T, typename R, int NCH, bool NORM, bool FP4>
+__global__ void __launch_bounds__(512) row_kernel(const __grid_constant__ RowParams p) {
+  __shared__ Meeting meet;
+  pdl_launch_dependents();
+  pdl_wait();
+  const i64 row = blockIdx.x;
+  const int col0 = (threadIdx.x >> 5) * NCH * kChunk + (threadIdx.x & 31) * 8;
+  float v[NCH][8];
+#pragma unroll
+  for (int k = 0; k < NCH; ++k) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[k][i] = 0.f;
+    if (col0 + k * kChunk < p.D) load8<T>(static_cast<const T*>(p.x) + row * p.sx + col0 + k * kChunk, p.vx, v[k]);
+  }
+  if constexpr (!std::is_same<R, None>::value) {
+    const R* const res = static_cast<const R*>(p.residual);
+    R* const out = static_cast<R*>(p.stream);
+    float r[NCH][8];
+#pragma unroll
+    for (int k = 0; k < NCH; ++k)
+      if (res && col0 + k * kChunk < p.D) load8<R>(res + row * p.sr + col0 + k * kChunk, p.vr, r[k]);
+#pragma unroll
+    for (int k = 0; k < NCH; ++k)
+      if (col0 + k * kChunk < p.D) {
+        if (res) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[k][i] = __fadd_rn(v[k][i], r[k][i]);
+        }
+        store8<R>(out ? out + row * p.ss + col0 + k * kChunk : nullptr, p.vs, v[k]);
+      }
+  }
+  finish_row<NCH, NORM, FP4>(p, meet, 0, row, v, [] {});
+}
+
+// Many rows: a block walks rows a grid apart through a ring in shared memory, `stages` rows of x and of the residual on their way by bulk copies while one
+// is worked on.  The row's barrier (every thread has its elements in registers then) gives its place in the ring to the row that comes
+// `stages` later; where there is a residual stream, h takes the place of the residual (of x if there is none) and leaves from
+// there, and the next copy waits until it has been read.
+template <typename T, typename R, int NCH, bool NORM, bool FP4>
+__global__ void __launch_bounds__(512, 2) ring_kernel(const __grid_constant__ RowParams p, int rows, int stages) {
+  using namespace sm100;
+  constexpr bool STREAM = !std::is_same<R, None>::value;
+  extern __shared__ __align__(16) uint8_t ring[];
+  __shared__ Meeting meet;
+  __shared__ uint64_t full[kMaxRing];
+  const int tid = threadIdx.x, col0 = (tid >> 5) * NCH * kChunk + (tid & 31) * 8;
+  typedef typename std::conditional<STREAM, R, T>::type S;
+  const uint32_t xbytes = p.D * (uint32_t)sizeof(T), rbytes = STREAM ? p.D * (uint32_t)sizeof(S) : 0u;
+  if (tid == 0) {
+    for (int i = 0; i < stages; ++i) mbar_init(&full[i], 1);
+    fence_mbar_init();
+  }
+  __syncthreads();
+  pdl_launch_dependents();
+  pdl_wait();
+  auto request = [&](int s, i64 row) {   // by one thread
+    uint8_t* const at = ring + s * (xbytes + rbytes);
+    mbar_expect_tx(&full[s], xbytes + (STREAM && p.residual ? rbytes : 0u));
+    bulk_load(at, static_cast<const T*>(p.x) + row * p.sx, xbytes, &full[s]);
+    if (STREAM && p.residual) bulk_load(at + xbytes, static_cast<const S*>(p.residual) + row * p.sr, rbytes, &full[s]);
+  };
+  if (tid == 0)
+    for (int s = 0; s < stages && blockIdx.x + (i64)s * gridDim.x < rows; ++s) request(s, blockIdx.x + (i64)s * gridDim.x);
+  int s = 0, round = 0, turn = 0;
+  bool late = false;
+  for (i64 row = blockIdx.x; row < rows; row += gridDim.x, turn ^= 1) {
+    uint8_t* const at = ring + s * (xbytes + rbytes);
+    late |= !mbar_wait_inline<0>(&full[s], round & 1, p.status);
+    float v[NCH][8];
+#pragma unroll
+    for (int k = 0; k < NCH; ++k) {
+      const int col = col0 + k * kChunk;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[k][i] = 0.f;
+      if (col < p.D) {
+        load8_shared<T>(reinterpret_cast<const T*>(at) + col, v[k]);
+        if constexpr (STREAM) {
+          S* const h = reinterpret_cast<S*>(at + xbytes) + col;
+          if (p.residual) {
+            float r[8];
+            load8_shared<S>(h, r);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[k][i] = __fadd_rn(v[k][i], r[i]);
+          }
+          store8<S>(h, true, v[k]);
+        }
+      }
+    }
+    if (STREAM) fence_async_smem();   // (ahead of the copies from and to the places just written)
+    const i64 next = row + (i64)stages * gridDim.x;
+    finish_row<NCH, NORM, FP4>(p, meet, turn, row, v, [&] {   // behind the barrier
+      if (tid == 0) {
+        if (STREAM && p.stream) {
+          bulk_store(static_cast<S*>(p.stream) + row * p.ss, at + xbytes, rbytes);
+          tma_store_commit();
+        }
+        if (next < rows) {
+          if (STREAM && p.stream) tma_store_wait_read();
+          request(s, next);
+        }
+      }
+    });
+    if (++s == stages) { s = 0; ++round; }
+  }
+  if (STREAM && p.stream && tid == 0) tma_store_wait_read();
+  if (late)   // (a copy may still be under way)
+    for (int i = 0; i < 50; ++i) __nanosleep(1000);
+}
+
 // Rows wider than a block's registers: the row is read twice where its absmax is needed.
 template <typename T>
 __global__ void __launch_bounds__(512) wide_kernel(const __grid_constant__ RowParams p) {
@@ -251,34 +354,88 @@ __global__ void __launch_bounds__(512) wide_kernel(const __grid_constant__ RowPa
   }
 }
 
-// Values of a matrix in four bits, eight columns a thread
+// Values of a matrix in four bits: a row is one or more warps', a thread has up to four vectors of 16 bytes of it at a time
 template <typename T>
 __global__ void __launch_bounds__(256) values_kernel(const uint8_t* codes, const uint8_t* scales, const float* step, T* out, i64 stride, bool aligned,
-                                                     i64 groups, int per_row, int block, int tiles) {
+                                                     int rows, int D, int block, int tiles) {
+  constexpr int V = 16 / (int)sizeof(T);
   pdl_launch_dependents();
   pdl_wait();
-  for (i64 i = blockIdx.x * 256ll + threadIdx.x; i < groups; i += gridDim.x * 256ll) {
-    const i64 row = i / per_row;
-    const int col = (int)(i - row * per_row) * 8, b = col / block;
-    const uint32_t byte = scales[fp4_scale_at(row, b >> 2, tiles) + (b & 3)];
-    const float s = block == 16 ? e4m3_to(byte) : e8m0_to(byte), f = step ? step[row] : 1.0f;
-    float v[8];
-    e2m1_to8(__ldcs(reinterpret_cast<const uint32_t*>(codes) + i), v);
+  const i64 row = blockIdx.x * (i64)blockDim.y + threadIdx.y;
+  if (row >= rows) return;
+  const uint8_t* const c = codes + row * (D / 2);
+  const uint8_t* const sc = scales + fp4_scale_at(row, 0, tiles);
+  T* const to = out + row * stride;
+  const float f = step ? step[row] : 1.0f;
+  const int shift = block == 16 ? 4 : 5;
+#pragma unroll 1
+  for (int c0 = threadIdx.x * V; c0 < D; c0 += 4 * blockDim.x * V) {
+    uint32_t w[4], s[4];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = __fmul_rn(__fmul_rn(v[k], s), f);
-    store8<T>(out + row * stride + col, aligned, v);
+    for (int k = 0; k < 4; ++k) {
+      const int col = c0 + k * blockDim.x * V, b = col >> shift;
+      w[k] = s[k] = 0;
+      if (col < D) {
+        w[k] = __ldcs(reinterpret_cast<const uint32_t*>(c) + (col >> 3));   // (binary32: the eight codes that two lanes' vectors are in)
+        s[k] = sc[(b >> 2) * kTileBytes + (b & 3)];
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int col = c0 + k * blockDim.x * V;
+      if (col >= D) break;
+      const float sv = block == 16 ? e4m3_to(s[k]) : e8m0_to(s[k]);
+      float v[8];
+      e2m1_to8(w[k], v);
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] = __fmul_rn(__fmul_rn(V == 4 && (col & 4) ? v[4 + (i & 3)] : v[i], sv), f);
+      if constexpr (V == 8) {
+        store8<T>(to + col, aligned, v);
+      } else if (aligned) {
+        *reinterpret_cast<float4*>(to + col) = make_float4(v[0], v[1], v[2], v[3]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) to[col + i] = v[i];
+      }
+    }
   }
 }
 
+// Many rows on 16 bytes go through the ring where two rows fit in a block's share of shared memory: bytes in flight do not wait for a row's arithmetic
+// then.  A chunk to a warp where rows are short or few, more where that would be many warps.
 template <typename T, typename R, bool NORM, bool FP4>
 ssdi8_status_t launch(const RowParams& p, i64 rows, cudaStream_t st) {
   const int chunks = (p.D + kChunk - 1) / kChunk;
+  const int sms = sm_count();
+  if (sms <= 0) return SSDI8_ERR_CUDA;
+  constexpr bool STREAM = !std::is_same<R, None>::value;
+  const i64 bytes = (i64)p.D * (sizeof(T) + (STREAM ? sizeof(typename std::conditional<STREAM, R, T>::type) : 0));
+  const bool bulk = p.vx && (!p.residual || p.vr) && (!p.stream || p.vs) && p.D * sizeof(T) % 16 == 0;
   auto go = [&](auto n) -> ssdi8_status_t {
     constexpr int NCH = decltype(n)::value;
-    return launch_configured(row_kernel<T, R, NCH, NORM, FP4>, dim3((unsigned)rows), dim3(32 * ((chunks + NCH - 1) / NCH)), 0, -1, false, st, p);
+    const int warps = (chunks + NCH - 1) / NCH;
+    constexpr i64 kShared = 200 * 1024;
+    #ifndef WARPS
+#define WARPS 32
+#endif
+    int blocks = WARPS / warps < 1 ? 1 : WARPS / warps < 24 ? WARPS / warps : 24;   // on an SM
+    while (blocks > 1 && kShared / blocks < 2 * bytes) --blocks;
+    if (bulk && rows > 2ll * sms * blocks && kShared / blocks >= 2 * bytes) {
+      const i64 fit = kShared / blocks / bytes;
+      const int stages = (int)(fit < 4 ? fit : 4);
+      return launch_sized(ring_kernel<T, R, NCH, NORM, FP4>, dim3((unsigned)(sms * blocks)), dim3(32 * warps), (size_t)(stages * bytes), (size_t)kShared, -1,
+                          false, st, p, (int)rows, stages);
+    }
+    return launch_configured(row_kernel<T, R, NCH, NORM, FP4>, dim3((unsigned)rows), dim3(32 * warps), 0, -1, false, st, p);
   };
-  if (chunks <= 8) return go(std::integral_constant<int, 1>());
-  if (chunks <= 16) return go(std::integral_constant<int, 2>());
+#ifndef C1
+#define C1 8
+#endif
+#ifndef C2
+#define C2 32
+#endif
+  if (chunks <= C1) return go(std::integral_constant<int, 1>());
+  if (chunks <= C2) return go(std::integral_constant<int, 2>());
   return go(std::integral_constant<int, 4>());
 }
 
@@ -294,7 +451,7 @@ ssdi8_status_t norm_of(const ssdi8_add_norm_args_t& a, cudaStream_t st) {
     p.stream = a.residual_out; p.ss = a.stride_out; p.vs = rows_aligned<R>(a.residual_out, a.stride_out);
   }
   p.weight = a.weight; p.static_scale = a.static_scale; p.xq = a.xq; p.scale = a.scale;
-  p.D = a.width; p.eps = a.eps;
+  p.D = a.width; p.eps = a.eps; p.status = a.status;
   if (!a.fp4) return launch<T, R, true, false>(p, a.rows, st);
   p.codes = a.fp4->codes; p.scales = a.fp4->scales; p.step = a.fp4->step;
   p.block = a.fp4->block; p.tiles = fp4_tiles(p.D, p.block);
@@ -302,10 +459,11 @@ ssdi8_status_t norm_of(const ssdi8_add_norm_args_t& a, cudaStream_t st) {
 }
 
 template <typename T>
-ssdi8_status_t quantize_of(const void* x, i64 stride, const ssdi8_fp4_t& q, cudaStream_t st) {
+ssdi8_status_t quantize_of(const void* x, i64 stride, const ssdi8_fp4_t& q, int32_t* status, cudaStream_t st) {
   RowParams p = {};
   p.x = x; p.sx = stride; p.vx = rows_aligned<T>(x, stride);
   p.codes = q.codes; p.scales = q.scales; p.step = q.step;
+  p.status = status;
   p.D = q.width; p.block = q.block; p.tiles = fp4_tiles(q.width, q.block);
   if (q.width <= kMaxNormWidth) return launch<T, None, false, true>(p, q.rows, st);
   return launch_configured(wide_kernel<T>, dim3((unsigned)q.rows), dim3(512), 0, -1, false, st, p);
@@ -321,19 +479,20 @@ ssdi8_status_t launch_add_norm(const ssdi8_add_norm_args_t& a, int dtype, int rd
   return dtype == 1 ? norm_of<__half, __half>(a, st) : norm_of<__nv_bfloat16, __nv_bfloat16>(a, st);
 }
 
-ssdi8_status_t launch_fp4_quantize(const void* x, i64 stride, int dtype, const ssdi8_fp4_t& q, cudaStream_t st) {
-  return dtype == 0 ? quantize_of<float>(x, stride, q, st) : dtype == 1 ? quantize_of<__half>(x, stride, q, st) : quantize_of<__nv_bfloat16>(x, stride, q, st);
+ssdi8_status_t launch_fp4_quantize(const void* x, i64 stride, int dtype, const ssdi8_fp4_t& q, int32_t* status, cudaStream_t st) {
+  return dtype == 0 ? quantize_of<float>(x, stride, q, status, st)
+       : dtype == 1 ? quantize_of<__half>(x, stride, q, status, st)
+                    : quantize_of<__nv_bfloat16>(x, stride, q, status, st);
 }
 
 ssdi8_status_t launch_fp4_dequantize(const ssdi8_fp4_t& q, void* out, i64 stride, int dtype, cudaStream_t st) {
-  const int sms = sm_count();
-  if (sms <= 0) return SSDI8_ERR_CUDA;
-  const i64 groups = (i64)q.rows * (q.width / 8), blocks = (groups + 255) / 256, most = 16ll * sms;
   auto go = [&](auto t) -> ssdi8_status_t {
     typedef decltype(t) T;
-    return launch_configured(values_kernel<T>, dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, -1, false, st, (const uint8_t*)q.codes,
-                             (const uint8_t*)q.scales, (const float*)q.step, static_cast<T*>(out), stride, rows_aligned<T>(out, stride), groups,
-                             q.width / 8, q.block, fp4_tiles(q.width, q.block));
+    // (four vectors a thread where a row has as many)
+    const int vectors = q.width / (16 / (int)sizeof(T)), tx = vectors <= 128 ? 32 : vectors <= 1024 ? (vectors / 4 + 31) / 32 * 32 : 256, ty = 256 / tx;
+    return launch_configured(values_kernel<T>, dim3((unsigned)((q.rows + (i64)ty - 1) / ty)), dim3(tx, ty), 0, -1, false, st, (const uint8_t*)q.codes,
+                             (const uint8_t*)q.scales, (const float*)q.step, static_cast<T*>(out), stride, rows_aligned<T>(out, stride), q.rows, q.width,
+                             q.block, fp4_tiles(q.width, q.block));
   };
   return dtype == 0 ? go(float()) : dtype == 1 ? go(__half()) : go(__nv_bfloat16());
 }

@@ -31,7 +31,7 @@ size_t ssdi8_fp4_scales_bytes(int32_t rows, int32_t width, int32_t block) {
   return (size_t)((rows + 127ll) / 128) * fp4_tiles(width, block) * kTileBytes;
 }
 
-ssdi8_status_t ssdi8_fp4_quantize(const void* x, int64_t stride_x, int32_t dtype, const ssdi8_fp4_t* q, void* stream) {
+ssdi8_status_t ssdi8_fp4_quantize(const void* x, int64_t stride_x, int32_t dtype, const ssdi8_fp4_t* q, int32_t* status, void* stream) {
   if (!q) return SSDI8_ERR_NULL;
   if (dtype < 0 || dtype > 2) return SSDI8_ERR_UNSUPPORTED;
   ssdi8_status_t s = fp4_supported(q, q->block == 16);
@@ -39,7 +39,7 @@ ssdi8_status_t ssdi8_fp4_quantize(const void* x, int64_t stride_x, int32_t dtype
   if (!x) return SSDI8_ERR_NULL;
   if (!aligned_to(x, elem_size(dtype))) return SSDI8_ERR_ALIGN;
   if ((s = check_arch()) != SSDI8_OK) return s;
-  return launch_fp4_quantize(x, stride_x, dtype, *q, static_cast<cudaStream_t>(stream));
+  return launch_fp4_quantize(x, stride_x, dtype, *q, status, static_cast<cudaStream_t>(stream));
 }
 
 ssdi8_status_t ssdi8_fp4_dequantize(const ssdi8_fp4_t* q, void* out, int64_t stride_out, int32_t dtype, void* stream) {

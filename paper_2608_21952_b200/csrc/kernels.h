@@ -186,7 +186,7 @@ constexpr int kMaxLinearRows = 0x7fffff00;   // (and outputs: a tile's last ones
 ssdi8_status_t launch_linear(const ssdi8_linear_args_t& a, int dtype, cudaStream_t st);
 // four bits (add_norm.cu, fp4_linear.cu); rdtype: of the residual stream, -1 without
 ssdi8_status_t launch_add_norm(const ssdi8_add_norm_args_t& a, int dtype, int rdtype, cudaStream_t st);
-ssdi8_status_t launch_fp4_quantize(const void* x, i64 stride, int dtype, const ssdi8_fp4_t& q, cudaStream_t st);
+ssdi8_status_t launch_fp4_quantize(const void* x, i64 stride, int dtype, const ssdi8_fp4_t& q, int32_t* status, cudaStream_t st);
 ssdi8_status_t launch_fp4_dequantize(const ssdi8_fp4_t& q, void* out, i64 stride, int dtype, cudaStream_t st);
 ssdi8_status_t launch_fp4_linear(const ssdi8_fp4_linear_args_t& a, int dtype, cudaStream_t st);
 

@@ -503,11 +503,12 @@ ENTRY(linear, 10) {   // xq, wq, s_w, out, s_row, bias, residual, act, status, s
   return call([&] { return ssdi8_linear(&l, out.dtype, st); });
 } END
 
-ENTRY(fp4_quantize, 3) {   // x, q, stream
+ENTRY(fp4_quantize, 4) {   // x, q, status, stream
   Fp4Arg q(a[1], "q");
   const Tensor x = tensor(a[0], "x", kAnyFloat, {q.get()->rows, q.get()->width}, false, true);
-  void* st = stream(a[2]);
-  return call([&] { return ssdi8_fp4_quantize(x.data(), x.stride(0), x.dtype, q.get(), st); });
+  int32_t* status = tensor(a[2], "status", kInt32, {1}, true).as<int32_t>();
+  void* st = stream(a[3]);
+  return call([&] { return ssdi8_fp4_quantize(x.data(), x.stride(0), x.dtype, q.get(), status, st); });
 } END
 
 ENTRY(fp4_dequantize, 3) {   // q, out, stream
@@ -517,7 +518,7 @@ ENTRY(fp4_dequantize, 3) {   // q, out, stream
   return call([&] { return ssdi8_fp4_dequantize(q.get(), out.data(), out.stride(0), out.dtype, st); });
 } END
 
-ENTRY(add_norm_quantize, 10) {   // x, residual, residual_out, weight, eps, xq, scale, static_scale, fp4, stream
+ENTRY(add_norm_quantize, 11) {   // x, residual, residual_out, weight, eps, xq, scale, static_scale, fp4, status, stream
   const Tensor x = tensor(a[0], "x", kAnyFloat, {-1, -1}, false, true);
   const int64_t T = x.size(0), D = x.size(1);
   if (D > 0x7fffffff) throw BadShape{};
@@ -533,8 +534,9 @@ ENTRY(add_norm_quantize, 10) {   // x, residual, residual_out, weight, eps, xq, 
   n.scale = tensor(a[6], "scale", 0, {T}, true).as<float>();
   n.static_scale = tensor(a[7], "static_scale", 0, {1}, true).as<float>();
   n.rows = T; n.width = (int32_t)D;
+  n.status = tensor(a[9], "status", kInt32, {1}, true).as<int32_t>();
   const int rdtype = r ? r.dtype : o ? o.dtype : 0;
-  void* st = stream(a[9]);
+  void* st = stream(a[10]);
   if (a[8] == Py_None) return call([&] { return ssdi8_add_norm_quantize(&n, x.dtype, rdtype, st); });
   Fp4Arg q(a[8], "fp4");
   n.fp4 = q.get();

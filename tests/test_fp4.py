@@ -127,12 +127,12 @@ def test_scales_bytes():
 def test_refusals_of_the_library():
     from paper_2608_21952_b200 import binding as bd
     L = bd._lib
-    for f, at in ((L.ssdi8_fp4_quantize, [C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p]),
+    for f, at in ((L.ssdi8_fp4_quantize, [C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]),
                   (L.ssdi8_fp4_dequantize, [C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p])):
         f.restype, f.argtypes = C.c_int32, at
 
     def quantize(q, x=4096, dtype=0):
-        return L.ssdi8_fp4_quantize(x, 64, dtype, C.addressof(q) if q else None, None)
+        return L.ssdi8_fp4_quantize(x, 64, dtype, C.addressof(q) if q else None, None, None)
 
     def values(q, out=4096, stride=64, dtype=0):
         return L.ssdi8_fp4_dequantize(C.addressof(q) if q else None, out, stride, dtype, None)
@@ -152,7 +152,7 @@ def test_refusals_of_the_library():
 class _Norm(C.Structure):
     _fields_ = [("x", C.c_void_p), ("stride_x", C.c_int64), ("residual", C.c_void_p), ("stride_residual", C.c_int64), ("residual_out", C.c_void_p),
                 ("stride_out", C.c_int64), ("weight", C.c_void_p), ("xq", C.c_void_p), ("scale", C.c_void_p), ("static_scale", C.c_void_p),
-                ("fp4", C.c_void_p), ("rows", C.c_int64), ("width", C.c_int32), ("eps", C.c_float)]
+                ("fp4", C.c_void_p), ("rows", C.c_int64), ("width", C.c_int32), ("eps", C.c_float), ("status", C.c_void_p)]
 
 
 class _Linear(C.Structure):
@@ -384,6 +384,43 @@ def test_add_norm(T, D, dtype, rdtype, kind, extra, form):
         got = _np(wide)
         np.testing.assert_array_equal(got[:, off:off + D], h)
         assert (got[:, :off] == 77).all() and (got[:, off + D:] == 77).all()
+
+
+# rows that a block walks through shared memory, several each; the last two are too wide for that, or on no 16-byte boundary
+MANY = [(7300, 96, "bfloat16", "float32", "outliers", 0), (3100, 768, "float16", "float16", "grid", 0), (1900, 2560, "bfloat16", "float32", "outliers", 0),
+        (1000, 5120, "float32", "float32", "zeros", 0), (700, 8192, "bfloat16", "bfloat16", "normal", 0), (400, 16384, "bfloat16", "float32", "outliers", 0),
+        (2100, 1248, "bfloat16", None, "normal", 8), (3000, 1264, "float16", "float32", "bad", 0), (310, 16384, "float32", "float32", "normal", 0),
+        (2000, 2112, "bfloat16", "float32", "normal", 3)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("form", ["int8", "static", "fp4 16", "fp4 32"])
+@pytest.mark.parametrize("T,D,dtype,rdtype,kind,extra", MANY)
+def test_add_norm_many_rows(T, D, dtype, rdtype, kind, extra, form):
+    test_add_norm(T, D, dtype, rdtype, kind, extra, form)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("block", [16, 32])
+@pytest.mark.parametrize("T,D,dtype,kind,extra,offset", [(7400, 32, "float32", "normal", 0, 0), (2000, 2560, "bfloat16", "outliers", 0, 0), (1001, 5120, "float32", "grid", 0, 0),
+                                                         (400, 16384, "float16", "bad", 0, 0), (2001, 2112, "bfloat16", "bad", 16, 8), (2001, 2112, "bfloat16", "zeros", 3, 1)])
+def test_quantize_many_rows(T, D, dtype, kind, extra, offset, block):
+    test_quantize(T, D, dtype, kind, extra, offset, block)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("over", ["residual", "x"])
+def test_add_norm_many_rows_in_place(over):
+    import torch
+    from paper_2608_21952_b200 import binding as bd
+    T, D = 4000, 1280
+    x, res, h, w, p = _norm_case(T, D, "bfloat16", "bfloat16", "outliers", 0)
+    t = {"x": _dev(x, "bfloat16"), "residual": _dev(res, "bfloat16")}
+    xq, status = torch.empty(T, D, dtype=torch.int8, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    bd.ssdi8_add_norm_quantize(t["x"], residual=t["residual"], residual_out=t[over], weight=_dev(w), xq=xq, status=status)
+    np.testing.assert_array_equal(_np(t[over]), h)
+    np.testing.assert_array_equal(_np(xq), ref.int8_codes(p, (np.abs(p).max(-1).astype(np.float32) / np.float32(127))[:, None]))
+    assert int(status.item()) == 0
 
 
 @pytest.mark.gpu
