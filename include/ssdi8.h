@@ -520,8 +520,8 @@ size_t ssdi8_fp4_scales_bytes(int32_t rows, int32_t width, int32_t block);
  *   block 32: scale = the least power of two s from 2^-127 to 2^127 with absmax of the block <= 6 s (1 if that absmax is 0),
  *             code = e2m1 of p / scale, step = 1 (if given)
  * Quotients are exact ones (g has 16 bits so that their middles are binary32 numbers; for rows whose absmax lies below 2e-32, where these are
- * subnormal, g scale and the quotient are each rounded to binary32).  Beyond 6 a code is 6.  A NaN counts for nothing in an absmax and has the code
- * +6; in a row (block 16) or block (32) with an infinity other codes are 0.  q.step is needed with block 16.
+ * subnormal, g scale and the quotient are each rounded to binary32).  Beyond 6 a code is 6; a 0 of either sign has the code 0.  A NaN counts for nothing in an
+ * absmax and has the code +6; in a row (block 16) or block (32) with an infinity other codes are 0.  q.step is needed with block 16.
  * status: 1 word, or NULL: SSDI8_ERR_DEVICE_TIMEOUT if a wait ran out. */
 ssdi8_status_t ssdi8_fp4_quantize(const void* x, int64_t stride_x, int32_t dtype, const ssdi8_fp4_t* q, int32_t* status, void* stream);
 /* The values of a matrix in four bits: out[t,k] = fmul(c scale, step), rounded once more to out's type (any stride of rows, at least width). */

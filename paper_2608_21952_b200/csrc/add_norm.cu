@@ -93,37 +93,42 @@ __device__ __forceinline__ float warp_max(float v) {   // of numbers >= 0; a NaN
   return m;
 }
 __device__ __forceinline__ float absmax8(const float (&v)[8]) {
-  float m = 0.f;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(v[i]));
-  return m;
+  float a, b, c;   // (a NaN counts for nothing)
+  asm("max.abs.f32 %0, %1, %2, %3;" : "=f"(a) : "f"(v[0]), "f"(v[1]), "f"(v[2]));
+  asm("max.abs.f32 %0, %1, %2, %3;" : "=f"(b) : "f"(v[3]), "f"(v[4]), "f"(v[5]));
+  asm("max.abs.f32 %0, %1, %2, %3;" : "=f"(c) : "f"(a), "f"(v[6]), "f"(v[7]));
+  return fmaxf(fmaxf(b, c), 0.f);
 }
 
-// Codes and scales in four bits of a chunk's eight columns of this lane (`live`: inside the row); m is their absmax, g the row's step size.
-// All lanes of the warp call it.  Bytes of a tile's blocks behind the row's end are 0.
-__device__ __forceinline__ void chunk_fp4(const RowParams& p, i64 row, int chunk, bool live, const float (&v)[8], float m, float g) {
-  const int lane = threadIdx.x & 31, col = chunk * kChunk + lane * 8;
+// Codes and scales in four bits of a chunk's eight columns of this lane (`live`: inside the row) into the row's codes and the row's place in the first of
+// its tiles; m is their absmax.  All lanes of the warp call it.  Bytes of a tile's blocks behind the row's end are 0.
+template <int BLOCK, bool SAFE>
+__device__ __forceinline__ void chunk_fp4(uint8_t* codes, uint8_t* scales, int tiles, int chunk, bool live, const float (&v)[8], float m, const Fp4Row& r) {
+  const int lane = threadIdx.x & 31;
+  constexpr int lanes = BLOCK / 8, shift = BLOCK == 16 ? 3 : 4;   // of a block; of a tile's four blocks (logarithm)
   m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
-  uint32_t s, word, codes;
-  int tile;
-  if (p.block == 16) {
-    s = fp4_scale16(m, g);
-    codes = fp4_codes16(v, __fmul_rn(g, e4m3_to(s)));
-    s = live ? s : 0u;
-    word = s | __shfl_down_sync(0xffffffffu, s, 2) << 8;
-    word |= __shfl_down_sync(0xffffffffu, word, 4) << 16;
-    tile = (lane & 7) == 0 ? chunk * 4 + (lane >> 3) : p.tiles;
-  } else {
-    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
-    s = fp4_scale32(m);
-    codes = fp4_codes32(v, s);
-    s = live ? s : 0u;
-    word = s | __shfl_down_sync(0xffffffffu, s, 4) << 8;
-    word |= __shfl_down_sync(0xffffffffu, word, 8) << 16;
-    tile = (lane & 15) == 0 ? chunk * 2 + (lane >> 4) : p.tiles;
-  }
-  if (live) *reinterpret_cast<uint32_t*>(p.codes + (row * p.D + col) / 2) = codes;
-  if (tile < p.tiles) *reinterpret_cast<uint32_t*>(p.scales + fp4_scale_at(row, tile, p.tiles)) = word;
+  if (BLOCK == 32) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
+  uint32_t s = BLOCK == 16 ? fp4_scale16<SAFE>(m, r) : fp4_scale32(m);
+  const uint32_t c = BLOCK == 16 ? fp4_codes16<SAFE>(v, r, e4m3_to(s)) : fp4_codes32(v, s);
+  s = live ? s : 0u;
+  uint32_t word = s | __shfl_down_sync(0xffffffffu, s, lanes) << 8;
+  word |= __shfl_down_sync(0xffffffffu, word, 2 * lanes) << 16;
+  if (live) reinterpret_cast<uint32_t*>(codes)[chunk * 32 + lane] = c;
+  const int tile = (chunk << (5 - shift)) + (lane >> shift);
+  if ((lane & (4 * lanes - 1)) == 0 && tile < tiles) *reinterpret_cast<uint32_t*>(scales + tile * kTileBytes) = word;
+}
+template <int BLOCK, bool SAFE, int NCH>
+__device__ __forceinline__ void row_fp4(const RowParams& p, i64 row, int c0, const float (&v)[NCH][8], const float (&m)[NCH], const Fp4Row& r) {
+  uint8_t* const codes = p.codes + row * (p.D / 2);
+  uint8_t* const scales = p.scales + fp4_scale_at(row, 0, p.tiles);
+  const int col = (threadIdx.x & 31) * 8;
+#pragma unroll
+  for (int k = 0; k < NCH; ++k)
+    if ((c0 + k) * kChunk < p.D) chunk_fp4<BLOCK, SAFE>(codes, scales, p.tiles, c0 + k, (c0 + k) * kChunk + col < p.D, v[k], m[k], r);
+}
+template <int NCH>   // rows whose step size is beyond what the corrected products take
+__device__ __noinline__ void row_fp4_by_division(const RowParams& p, i64 row, int c0, const float (&v)[NCH][8], const float (&m)[NCH], const Fp4Row& r) {
+  row_fp4<16, false, NCH>(p, row, c0, v, m, r);
 }
 
 // What a row's threads say to one another; two of each, so that a row's are read while the next one's are written
@@ -134,7 +139,7 @@ struct Meeting {
 
 // A warp's chunks of a row from their h (v): p = h w, the row's sum of squares and absmax of p (the block's only barrier), step sizes and codes.
 // `behind` is called behind that barrier.
-template <int NCH, bool NORM, bool FP4, typename F>
+template <int NCH, bool NORM, bool FP4, bool RING, typename F>
 __device__ __forceinline__ void finish_row(const RowParams& p, Meeting& meet, int turn, i64 row, float (&v)[NCH][8], F behind) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nwarps = blockDim.x >> 5;
   const int c0 = warp * NCH, col0 = c0 * kChunk + lane * 8;
@@ -149,7 +154,11 @@ __device__ __forceinline__ void finish_row(const RowParams& p, Meeting& meet, in
         const float4 a = reinterpret_cast<const float4*>(p.weight + col0 + k * kChunk)[0], b = reinterpret_cast<const float4*>(p.weight + col0 + k * kChunk)[1];
         const float w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[k][i] = __fmul_rn(v[k][i], w[i]);
+        for (int i = 0; i < 8; i += 2) {
+          const float2 x = __fmul2_rn(make_float2(v[k][i], v[k][i + 1]), make_float2(w[i], w[i + 1]));
+          v[k][i] = x.x;
+          v[k][i + 1] = x.y;
+        }
       }
     }
     m[k] = absmax8(v[k]);
@@ -168,7 +177,7 @@ __device__ __forceinline__ void finish_row(const RowParams& p, Meeting& meet, in
       if (NORM) meet.sums[turn][warp] = ss;
     }
   }
-  __syncthreads();
+  if (NORM || RING || p.block == 16) __syncthreads();
   behind();
   if (NORM || p.block == 16) top = warp_max(lane < nwarps ? meet.maxima[turn][lane] : 0.f);
   // 1 / sqrt(mean + eps), by the threads that need it
@@ -178,14 +187,27 @@ __device__ __forceinline__ void finish_row(const RowParams& p, Meeting& meet, in
     return 1.0 / sqrt(s / (double)p.D + (double)p.eps);
   };
   if constexpr (FP4) {
-    const float g = p.block == 16 ? fp4_row_step(top) : 1.0f;
+    Fp4Row r = {1.0f, 6.0f, 0.f, true};
+    if (p.block == 16) r = fp4_row(top);
     if (p.step && threadIdx.x == 0) {
-      if constexpr (NORM) p.step[row] = top > 0.f ? (float)((double)g * factor()) : 1.0f;
-      else p.step[row] = g;
+      if constexpr (NORM) p.step[row] = top > 0.f ? (float)((double)r.g * factor()) : 1.0f;
+      else p.step[row] = r.g;
     }
+    if (p.block == 32) {
+      row_fp4<32, true, NCH>(p, row, c0, v, m, r);
+    } else if (r.safe) {
+      row_fp4<16, true, NCH>(p, row, c0, v, m, r);
+    } else {
+      float w[NCH][8], n[NCH];   // (copies: the call takes their addresses)
 #pragma unroll
-    for (int k = 0; k < NCH; ++k)
-      if ((c0 + k) * kChunk < p.D) chunk_fp4(p, row, c0 + k, col0 + k * kChunk < p.D, v[k], m[k], g);
+      for (int k = 0; k < NCH; ++k) {
+        n[k] = m[k];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[k][i] = v[k][i];
+      }
+      const Fp4Row q = r;
+      row_fp4_by_division<NCH>(p, row, c0, w, n, q);
+    }
   } else {
     float a;
     if (p.static_scale) {
@@ -196,7 +218,11 @@ __device__ __forceinline__ void finish_row(const RowParams& p, Meeting& meet, in
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[k][i] = __fmul_rn(v[k][i], r);
     } else {
-      a = __fdiv_rn(top, 127.0f);
+      // (the product with the rounded reciprocal and one correction: the correctly rounded quotient for all 2^23 significands)
+      constexpr float c = 1.0f / 127.0f;
+      a = __fmul_rn(top, c);
+      a = __fmaf_rn(__fmaf_rn(-a, 127.0f, top), c, a);
+      if (!(top >= 1e-25f && top <= 1e25f)) a = __fdiv_rn(top, 127.0f);
       const bool some = a > 0.f;
       a = some ? a : 1.0f;
       if (p.scale && threadIdx.x == 0) p.scale[row] = some ? (float)((double)a * factor()) : 1.0f;
@@ -245,7 +271,7 @@ __global__ void __launch_bounds__(512) row_kernel(const __grid_constant__ RowPar
         store8<R>(out ? out + row * p.ss + col0 + k * kChunk : nullptr, p.vs, v[k]);
       }
   }
-  finish_row<NCH, NORM, FP4>(p, meet, 0, row, v, [] {});
+  finish_row<NCH, NORM, FP4, false>(p, meet, 0, row, v, [] {});
 }
 
 // Many rows: a block walks rows a grid apart through a ring in shared memory, `stages` rows of x and of the residual on their way by bulk copies while one
@@ -286,9 +312,10 @@ __global__ void __launch_bounds__(512, 2) ring_kernel(const __grid_constant__ Ro
 #pragma unroll
     for (int k = 0; k < NCH; ++k) {
       const int col = col0 + k * kChunk;
+      if (col >= p.D) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[k][i] = 0.f;
-      if (col < p.D) {
+        for (int i = 0; i < 8; ++i) v[k][i] = 0.f;
+      } else {
         load8_shared<T>(reinterpret_cast<const T*>(at) + col, v[k]);
         if constexpr (STREAM) {
           S* const h = reinterpret_cast<S*>(at + xbytes) + col;
@@ -304,7 +331,7 @@ __global__ void __launch_bounds__(512, 2) ring_kernel(const __grid_constant__ Ro
     }
     if (STREAM) fence_async_smem();   // (ahead of the copies from and to the places just written)
     const i64 next = row + (i64)stages * gridDim.x;
-    finish_row<NCH, NORM, FP4>(p, meet, turn, row, v, [&] {   // behind the barrier
+    finish_row<NCH, NORM, FP4, true>(p, meet, turn, row, v, [&] {   // behind the barrier
       if (tid == 0) {
         if (STREAM && p.stream) {
           bulk_store(static_cast<S*>(p.stream) + row * p.ss, at + xbytes, rbytes);
@@ -332,7 +359,8 @@ __global__ void __launch_bounds__(512) wide_kernel(const __grid_constant__ RowPa
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const i64 row = blockIdx.x;
   const T* const x = static_cast<const T*>(p.x) + row * p.sx;
-  float v[8], g = 1.0f;
+  float v[8];
+  Fp4Row r = {1.0f, 6.0f, 0.f, true};
   if (p.block == 16) {
     float top = 0.f;
     for (int c = threadIdx.x * 8; c < p.D; c += 512 * 8) {
@@ -342,15 +370,18 @@ __global__ void __launch_bounds__(512) wide_kernel(const __grid_constant__ RowPa
     top = warp_max(top);
     if (lane == 0) maxima[warp] = top;
     __syncthreads();
-    g = fp4_row_step(warp_max(lane < 16 ? maxima[lane] : 0.f));
+    r = fp4_row(warp_max(lane < 16 ? maxima[lane] : 0.f));
   }
-  if (p.step && threadIdx.x == 0) p.step[row] = g;
+  if (p.step && threadIdx.x == 0) p.step[row] = r.g;
   for (int c = warp; c * kChunk < p.D; c += 16) {
     const int col = c * kChunk + lane * 8;
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = 0.f;
     if (col < p.D) load8<T>(x + col, p.vx, v);
-    chunk_fp4(p, row, c, col < p.D, v, absmax8(v), g);
+    const float w[1][8] = {{v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]}}, m[1] = {absmax8(v)};
+    if (p.block == 32) row_fp4<32, true, 1>(p, row, c, w, m, r);
+    else if (r.safe) row_fp4<16, true, 1>(p, row, c, w, m, r);
+    else row_fp4<16, false, 1>(p, row, c, w, m, r);
   }
 }
 

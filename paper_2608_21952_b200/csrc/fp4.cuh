@@ -58,17 +58,39 @@ __device__ __forceinline__ float e8m0_to(uint32_t b) {   // 2^(b - 127)
   return __uint_as_float(b == 0u ? 0x00400000u : b << 23);
 }
 
-// A row's step size g for blocks of 16, from the absmax m of its values: fdiv(m, 2688) (the largest code times the largest scale), the low eight
-// bits of the significand cleared; 1 if that is 0.  With 16 bits in g and 4 in a scale, what lies in the middle of two codes or of two
-// scales is a binary32 number (the middles have 3 and 5 bits of their own).  A value p that is not such a middle b d is 2^-24 of it away
-// at least, which is more than half a step of binary32 at b: the rounded quotient keeps to its side of b, so codes are those
-// of the exact quotient.  (Down to an absmax of 2e-32, below which d is subnormal.)
-__device__ __forceinline__ float fp4_row_step(float m) {
-  const float g = __uint_as_float(__float_as_uint(__fdiv_rn(m, 2688.0f)) & 0xffffff00u);
-  return g > 0.f ? g : 1.0f;
+// Blocks of 16 of a row with absmax m: the row's step size g is fdiv(m, 2688) (the largest code times the largest scale) with the low eight bits of its
+// significand cleared; 1 if that is 0.  With 16 bits in g and 4 in a scale, what lies in the middle of two codes or of two scales is a
+// binary32 number (the middles have 3 and 5 bits of their own), and a value that is not such a middle b d is 2^-24 of it away at least.
+// Quotients are formed as the product t with an approximate reciprocal y (2^-23) and one correction, t + (p - t d) y (Markstein, IBM J. Res. Dev. 34, 1990):
+// what is rounded is p / d up to 1.5 x 2^-46 of it.  That is b for p = b d, and for the p next to it 2^-44 off where it would round to b
+// (b = 1/4, the only power of two among the middles, and a significand of p up to 2 - 2^-19, as d has 20 bits; 2^-28 and more elsewhere): codes
+// and scales are those of the exact quotients.  Rows whose step size leaves [1e-25, 1e25] take divisions, which keep to the
+// side of b as well, down to an absmax of 2e-32, below which d is subnormal.
+struct Fp4Row {
+  float g, unit, y;   // step size, 6 g, its reciprocal (approximate)
+  bool safe;
+};
+__device__ __forceinline__ Fp4Row fp4_row(float m) {
+  Fp4Row r;
+  constexpr float c = 1.0f / 2688.0f;
+  // (the correctly rounded quotient: for all 2^23 significands of m)
+  const float t = __fmul_rn(m, c);
+  float g = __fmaf_rn(__fmaf_rn(-t, 2688.0f, m), c, t);
+  r.safe = g >= 1e-25f && g <= 1e25f;
+  if (!r.safe) g = __fdiv_rn(m, 2688.0f);
+  g = __uint_as_float(__float_as_uint(g) & 0xffffff00u);
+  r.g = g > 0.f ? g : 1.0f;
+  r.unit = __fmul_rn(6.0f, r.g);
+  r.y = rcp_approx(r.unit);
+  return r;
 }
 // scale byte of a block of 16 with absmax m: e4m3 of m / (6 g), at least the smallest e4m3 above 0 (inf / inf too)
-__device__ __forceinline__ uint32_t fp4_scale16(float m, float g) { return e4m3_of(fmaxf(__fdiv_rn(m, __fmul_rn(6.0f, g)), 0.001953125f)); }
+template <bool SAFE>
+__device__ __forceinline__ uint32_t fp4_scale16(float m, const Fp4Row& r) {
+  float q = __fmul_rn(m, r.y);
+  q = SAFE ? __fmaf_rn(__fmaf_rn(-q, r.unit, m), r.y, q) : __fdiv_rn(m, r.unit);
+  return e4m3_of(fmaxf(q, 0.001953125f));
+}
 // scale byte of a block of 32: the least power of two s in [2^-127, 2^127] with m <= 6 s; 1 if m is 0
 __device__ __forceinline__ uint32_t fp4_scale32(float m) {
   const uint32_t b = __float_as_uint(m), e = b >> 23;
@@ -77,34 +99,37 @@ __device__ __forceinline__ uint32_t fp4_scale32(float m) {
   const uint32_t up = (b & 0x7fffffu) > 0x400000u ? 1u : 0u;
   return e + up < 2u ? 0u : min(e + up - 2u, 254u);
 }
-// Codes of eight values of a block of 16 over d = fmul(g, scale): the product with the rounded reciprocal and one correction (Markstein, IBM J.
-// Res. Dev. 34, 1990).  What is rounded last is p / d up to 2^-46 of it.  Where p is a middle b d that rounds to b; where p is next to one it
-// is 2^-44 from where it would (b = 1/4, and a significand of p up to 2 - 2^-19, as d has 20 bits; farther elsewhere).  Step sizes out of
-// its range go by division.
-__device__ __forceinline__ uint32_t fp4_codes16(const float (&p)[8], float d) {
+// Codes of eight values: of a block of 16 over d = fmul(g, scale), of a block of 32 whose scale byte is b (exact products).  A zero of either sign has the code 0.
+template <bool SAFE>
+__device__ __forceinline__ uint32_t fp4_codes16(const float (&p)[8], const Fp4Row& r, float scale) {
+  const float d = __fmul_rn(r.g, scale);
   float q[8];
-  if (d >= 1e-30f && d <= 1e30f) {
-    const float y = -__frcp_rn(d);   // (the quotient's negative is what is formed: a zero keeps its sign so)
+  if (!SAFE) {
 #pragma unroll
-    for (int i = 0; i < 8; i += 2) {
-      const float2 v = make_float2(p[i], p[i + 1]), yy = make_float2(y, y);
-      const float2 t = __fmul2_rn(v, yy);
-      const float2 r = __ffma2_rn(__ffma2_rn(t, make_float2(d, d), v), yy, t);
-      q[i] = -r.x;
-      q[i + 1] = -r.y;
-    }
-  } else {
+    for (int i = 0; i < 8; ++i) q[i] = __fdiv_rn(p[i], d) + 0.f;
+    return e2m1_of8(q);
+  }
+  const float y = rcp_approx(d);
+  const float2 yy = make_float2(y, y), nd = make_float2(-d, -d);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) q[i] = __fdiv_rn(p[i], d);
+  for (int i = 0; i < 8; i += 2) {
+    const float2 v = make_float2(p[i], p[i + 1]), t = __fmul2_rn(v, yy);
+    const float2 x = __ffma2_rn(__ffma2_rn(t, nd, v), yy, t);
+    q[i] = x.x;
+    q[i + 1] = x.y;
   }
   return e2m1_of8(q);
 }
-// of a block of 32 whose scale byte is b (exact products)
 __device__ __forceinline__ uint32_t fp4_codes32(const float (&p)[8], uint32_t b) {
   const float y = e8m0_to(254u - b);
+  const float2 yy = make_float2(y, y), zero = make_float2(0.f, 0.f);
   float q[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) q[i] = __fmul_rn(p[i], y);
+  for (int i = 0; i < 8; i += 2) {
+    const float2 x = __ffma2_rn(make_float2(p[i], p[i + 1]), yy, zero);
+    q[i] = x.x;
+    q[i + 1] = x.y;
+  }
   return e2m1_of8(q);
 }
 

@@ -53,7 +53,7 @@ def quantize(p, block):
     if block == 16:
         c = np.where(np.isinf(d), np.where(np.isinf(a), 7, 0), c)
     c = np.where(nan, 7, c)
-    neg = np.signbit(p).reshape(a.shape) & ~nan & ~(np.isinf(d) & np.isinf(a))   # (inf / inf is a NaN, +6)
+    neg = (p < 0).reshape(a.shape) & ~nan & ~np.isinf(d)   # (-0 is 0; in a row with an infinity: inf / inf is a NaN, +6, the rest 0)
     return (c + 8 * neg).reshape(T, D).astype(np.uint8), s.astype(np.uint8), step
 
 
