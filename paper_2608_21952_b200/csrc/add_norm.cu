@@ -15,7 +15,7 @@
 namespace ssdi8 {
 namespace {
 
-constexpr int kMaxRing = 8;
+constexpr int kRing = 2;       // rows of a block's ring
 constexpr int kChunk = 256;   // columns of a chunk: a warp's lanes have eight each, so that a block of 16 is two lanes and one of 32 four
 
 struct None {};   // no residual stream
@@ -144,12 +144,13 @@ __device__ __forceinline__ void finish_row(const RowParams& p, Meeting& meet, in
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nwarps = blockDim.x >> 5;
   const int c0 = warp * NCH, col0 = c0 * kChunk + lane * 8;
   float m[NCH];
-  double ss = 0.0;
+  constexpr int SIDE = NCH == 1 ? 4 : 1;   // sums side by side: their chain is what a short row waits for (two chunks have no registers for it)
+  double part[SIDE] = {};
 #pragma unroll
   for (int k = 0; k < NCH; ++k) {
     if constexpr (NORM) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) ss = fma((double)v[k][i], (double)v[k][i], ss);
+      for (int i = 0; i < 8; ++i) part[i % SIDE] = fma((double)v[k][i], (double)v[k][i], part[i % SIDE]);
       if (p.weight && col0 + k * kChunk < p.D) {
         const float4 a = reinterpret_cast<const float4*>(p.weight + col0 + k * kChunk)[0], b = reinterpret_cast<const float4*>(p.weight + col0 + k * kChunk)[1];
         const float w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
@@ -168,6 +169,8 @@ __device__ __forceinline__ void finish_row(const RowParams& p, Meeting& meet, in
 #pragma unroll
     for (int k = 0; k < NCH; ++k) top = fmaxf(top, m[k]);
     top = warp_max(top);
+    double ss = part[0];
+    if (SIDE == 4) ss = (part[0] + part[1 % SIDE]) + (part[2 % SIDE] + part[3 % SIDE]);
     if constexpr (NORM) {
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
@@ -274,22 +277,21 @@ __global__ void __launch_bounds__(512) row_kernel(const __grid_constant__ RowPar
   finish_row<NCH, NORM, FP4, false>(p, meet, 0, row, v, [] {});
 }
 
-// Many rows: a block walks rows a grid apart through a ring in shared memory, `stages` rows of x and of the residual on their way by bulk copies while one
-// is worked on.  The row's barrier (every thread has its elements in registers then) gives its place in the ring to the row that comes
-// `stages` later; where there is a residual stream, h takes the place of the residual (of x if there is none) and leaves from
+// Many rows: a block walks rows a grid apart through a ring in shared memory, the next row's x and residual on their way by bulk copies while one
+// is worked on.  The row's barrier (every thread has its elements in registers then) gives its place in the ring to the row after the next; where there is a residual stream, h takes the place of the residual (of x if there is none) and leaves from
 // there, and the next copy waits until it has been read.
 template <typename T, typename R, int NCH, bool NORM, bool FP4>
-__global__ void __launch_bounds__(512, 2) ring_kernel(const __grid_constant__ RowParams p, int rows, int stages) {
+__global__ void __launch_bounds__(512, 2) ring_kernel(const __grid_constant__ RowParams p, int rows) {
   using namespace sm100;
   constexpr bool STREAM = !std::is_same<R, None>::value;
   extern __shared__ __align__(16) uint8_t ring[];
   __shared__ Meeting meet;
-  __shared__ uint64_t full[kMaxRing];
+  __shared__ uint64_t full[kRing];
   const int tid = threadIdx.x, col0 = (tid >> 5) * NCH * kChunk + (tid & 31) * 8;
   typedef typename std::conditional<STREAM, R, T>::type S;
   const uint32_t xbytes = p.D * (uint32_t)sizeof(T), rbytes = STREAM ? p.D * (uint32_t)sizeof(S) : 0u;
   if (tid == 0) {
-    for (int i = 0; i < stages; ++i) mbar_init(&full[i], 1);
+    for (int i = 0; i < kRing; ++i) mbar_init(&full[i], 1);
     fence_mbar_init();
   }
   __syncthreads();
@@ -302,7 +304,7 @@ __global__ void __launch_bounds__(512, 2) ring_kernel(const __grid_constant__ Ro
     if (STREAM && p.residual) bulk_load(at + xbytes, static_cast<const S*>(p.residual) + row * p.sr, rbytes, &full[s]);
   };
   if (tid == 0)
-    for (int s = 0; s < stages && blockIdx.x + (i64)s * gridDim.x < rows; ++s) request(s, blockIdx.x + (i64)s * gridDim.x);
+    for (int s = 0; s < kRing && blockIdx.x + (i64)s * gridDim.x < rows; ++s) request(s, blockIdx.x + (i64)s * gridDim.x);
   int s = 0, round = 0, turn = 0;
   bool late = false;
   for (i64 row = blockIdx.x; row < rows; row += gridDim.x, turn ^= 1) {
@@ -330,7 +332,7 @@ __global__ void __launch_bounds__(512, 2) ring_kernel(const __grid_constant__ Ro
       }
     }
     if (STREAM) fence_async_smem();   // (ahead of the copies from and to the places just written)
-    const i64 next = row + (i64)stages * gridDim.x;
+    const i64 next = row + (i64)kRing * gridDim.x;
     finish_row<NCH, NORM, FP4, true>(p, meet, turn, row, v, [&] {   // behind the barrier
       if (tid == 0) {
         if (STREAM && p.stream) {
@@ -343,7 +345,7 @@ __global__ void __launch_bounds__(512, 2) ring_kernel(const __grid_constant__ Ro
         }
       }
     });
-    if (++s == stages) { s = 0; ++round; }
+    if (++s == kRing) { s = 0; ++round; }
   }
   if (STREAM && p.stream && tid == 0) tma_store_wait_read();
   if (late)   // (a copy may still be under way)
@@ -432,41 +434,34 @@ __global__ void __launch_bounds__(256) values_kernel(const uint8_t* codes, const
   }
 }
 
-// Many rows on 16 bytes go through the ring where two rows fit in a block's share of shared memory: bytes in flight do not wait for a row's arithmetic
-// then.  A chunk to a warp where rows are short or few, more where that would be many warps.
+// Many rows on 16 bytes go through the ring, with as many blocks as have room for two rows each: what a row waits for is then on its way while the one before
+// is worked on (us, direct and ring: 16384 x 2560 bf16 with an fp32 stream to int8 81 and 79, to four bits 87 and 75, bf16 stream 72 and 56;
+// 4096 x 8192 75 and 61; quantiser 16384 x 5120 bf16 75 and 56).  Not fp32 rows without a stream, whose 32 bytes a lane meet in shared memory's banks
+// (quantiser 10576 x 2560 19 and 24).  A chunk to a warp where rows are short (or few: 300 x 2560 6.0 with two, 4.2),
+// two up to 8192 columns; four where the quantiser, which asks less of
+// a row's warps, has many rows (16384 x 5120 67 and 56; 64 x 5120 2.2 and 2.8).
 template <typename T, typename R, bool NORM, bool FP4>
 ssdi8_status_t launch(const RowParams& p, i64 rows, cudaStream_t st) {
   const int chunks = (p.D + kChunk - 1) / kChunk;
   const int sms = sm_count();
   if (sms <= 0) return SSDI8_ERR_CUDA;
   constexpr bool STREAM = !std::is_same<R, None>::value;
+  constexpr i64 kShared = 200 * 1024;
   const i64 bytes = (i64)p.D * (sizeof(T) + (STREAM ? sizeof(typename std::conditional<STREAM, R, T>::type) : 0));
-  const bool bulk = p.vx && (!p.residual || p.vr) && (!p.stream || p.vs) && p.D * sizeof(T) % 16 == 0;
+  const i64 fit = kShared / (kRing * bytes), blocks = fit < 24 ? fit : 24;   // on an SM
+  const bool ring = (STREAM || sizeof(T) == 2) && p.vx && (!p.residual || p.vr) && (!p.stream || p.vs) && blocks > 0 && rows > 2 * sms * blocks;
   auto go = [&](auto n) -> ssdi8_status_t {
     constexpr int NCH = decltype(n)::value;
     const int warps = (chunks + NCH - 1) / NCH;
-    constexpr i64 kShared = 200 * 1024;
-    #ifndef WARPS
-#define WARPS 32
-#endif
-    int blocks = WARPS / warps < 1 ? 1 : WARPS / warps < 24 ? WARPS / warps : 24;   // on an SM
-    while (blocks > 1 && kShared / blocks < 2 * bytes) --blocks;
-    if (bulk && rows > 2ll * sms * blocks && kShared / blocks >= 2 * bytes) {
-      const i64 fit = kShared / blocks / bytes;
-      const int stages = (int)(fit < 4 ? fit : 4);
-      return launch_sized(ring_kernel<T, R, NCH, NORM, FP4>, dim3((unsigned)(sms * blocks)), dim3(32 * warps), (size_t)(stages * bytes), (size_t)kShared, -1,
-                          false, st, p, (int)rows, stages);
+    if constexpr (STREAM || sizeof(T) == 2) {
+      if (ring)
+        return launch_sized(ring_kernel<T, R, NCH, NORM, FP4>, dim3((unsigned)(sms * blocks)), dim3(32 * warps), (size_t)(kRing * bytes), (size_t)kShared, -1,
+                            false, st, p, (int)rows);
     }
     return launch_configured(row_kernel<T, R, NCH, NORM, FP4>, dim3((unsigned)rows), dim3(32 * warps), 0, -1, false, st, p);
   };
-#ifndef C1
-#define C1 8
-#endif
-#ifndef C2
-#define C2 32
-#endif
-  if (chunks <= C1) return go(std::integral_constant<int, 1>());
-  if (chunks <= C2) return go(std::integral_constant<int, 2>());
+  if (chunks <= (rows <= 4 * sms ? 16 : 8)) return go(std::integral_constant<int, 1>());
+  if (chunks <= 32 && (NORM || !ring)) return go(std::integral_constant<int, 2>());
   return go(std::integral_constant<int, 4>());
 }
 
