@@ -15,8 +15,8 @@ bool sizes_supported(int32_t rows, int32_t width, int32_t block) {
 }
 ssdi8_status_t fp4_supported(const ssdi8_fp4_t* q, bool step) {
   if (!sizes_supported(q->rows, q->width, q->block)) return SSDI8_ERR_SHAPE;
-  // (rows of 128 bytes of scales are counted in 32 bits)
-  if ((i64)((q->rows + 127ll) / 128) * fp4_tiles(q->width, q->block) * 4 > 0x7fffffff) return SSDI8_ERR_SHAPE;
+  // (rows of 128 bytes of scales are counted in 32 bits, those of a tile behind the last ones too)
+  if ((i64)((q->rows + 255ll) / 128) * fp4_tiles(q->width, q->block) * 4 > 0x7fff0000) return SSDI8_ERR_SHAPE;
   if (q->rows == 0) return SSDI8_OK;
   if (!q->codes || !q->scales || (step && !q->step)) return SSDI8_ERR_NULL;
   return aligned16(q->codes) && aligned16(q->scales) && aligned_to(q->step, 4) ? SSDI8_OK : SSDI8_ERR_ALIGN;

@@ -109,7 +109,7 @@ __device__ __forceinline__ void arrive_relaxed_at(uint32_t bar) {
 
 // One epilogue warp: a quarter's 32 rows (lanes) of 128 columns of an accumulator, in units of 128 bytes of out's rows (64 columns, or 32 of
 // binary32), each through one of the warp's two slabs in shared memory.  Where out's rows (and the residual's) lie on 16-byte boundaries TMA brings the
-// residual of a unit into its slab, those of the next tile's first two while its accumulator is formed, and takes the unit from there; it leaves out
+// residual of a unit into its slab, a unit ahead, and takes the unit from there; it leaves out
 // what is beyond the last row and column.  Other rows are read back from the slabs as binary32, a row at a time by lanes that stand beside
 // one another in it, and stored in words of four bytes: in an odd row, one of 16-bit elements that starts in the middle of a word,
 // lane j has elements 2 j + 1 and 2 j + 2, and the last lane both ends.
@@ -142,25 +142,22 @@ struct Epilogue {
   }
   static __device__ __forceinline__ int odd_row(const void* q) { return (int)(reinterpret_cast<uintptr_t>(q) >> 1 & 1); }
 
-  // the residual of the unit at (t, o) on its way into a slab, whose last store has been read but for the `later` ones behind it
-  __device__ __forceinline__ void arm(int slot, int t, int o, int later) {
-    if (lane == 0) {
-      if (later) tma_store_wait_read_but_one();
-      else tma_store_wait_read();
-      if (p.residual && t < p.T && o < p.O) {
-        mbar_expect_tx(&bar[slot], 4096);
-        tma_load_2d(slab + slot * 4096, tres, &bar[slot], o, t);
-      }
+  // the first column of a tile's i-th unit
+  static __device__ __forceinline__ int column_of(int i, bool down) { return (i * U) ^ (down ? 64 : 0); }
+  // the residual of the unit at (t, o) on its way into a slab, by one lane
+  __device__ __forceinline__ void request(int slot, int t, int o) {
+    if (t < p.T && o < p.O) {
+      mbar_expect_tx(&bar[slot], 4096);
+      tma_load_2d(slab + slot * 4096, tres, &bar[slot], o, t);
     }
-    __syncwarp();
   }
-  // before the accumulator of the tile at (t, n) is there: what it needs of the residual
-  __device__ __forceinline__ void ahead(int t, int n, bool down) {
-    if (vectors) {
-      const int c0 = down ? 64 : 0;
-      arm(0, t, n + c0, 1);
-      arm(1, t, n + (sizeof(T) == 4 ? c0 + 32 : c0 ^ 64), 0);
-    } else if (p.residual && t + lane < p.T && n < p.O) {   // into L2
+  // ahead of the first tile: its first unit's
+  __device__ __forceinline__ void begin(int t, int n, bool down) {
+    if (vectors && p.residual && lane == 0) request(0, t, n + column_of(0, down));
+  }
+  // rows on other boundaries: the residual of the tile at (t, n) into L2, a tile ahead
+  __device__ __forceinline__ void ahead(int t, int n) {
+    if (!vectors && p.residual && t + lane < p.T && n < p.O) {
       const uint8_t* const at = reinterpret_cast<const uint8_t*>(static_cast<const T*>(p.residual) + (t + lane) * p.res_stride + n);
       const int bytes = min(128, p.O - n) * (int)sizeof(T);
       for (int o = 0; o < bytes; o += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(at + o));
@@ -250,18 +247,28 @@ struct Epilogue {
       for (int c = 0; c < 16; ++c) to[((sizeof(T) == 4 ? 0 : 16 * half) + c) ^ (lane & (pairs - 1))] = f[c];
     }
   }
-  // the slab is there for a unit: with the residual in it, or its last store read
+  // the slab is there for a unit: with the residual in it, or its last store, two units ago, read
   __device__ __forceinline__ void take(int slot, int c0) {
-    if (!vectors || n0 + c0 >= end || t0 >= p.T || !p.residual) return;
-    mbar_wait(&bar[slot], phase >> slot & 1u, p.status);
-    phase ^= 1u << slot;
+    if (!vectors) return;
+    if (!p.residual) {
+      if (lane == 0) tma_store_wait_read_but_one();
+      __syncwarp();
+    } else if (n0 + c0 < end && t0 < p.T) {
+      mbar_wait(&bar[slot], phase >> slot & 1u, p.status);
+      phase ^= 1u << slot;
+    }
   }
-  __device__ __forceinline__ void leave(int slot, int c0) {
+  // a unit out of its slab; (t, o): the unit that comes next, whose residual may follow as soon as the other slab's store has been read
+  __device__ __forceinline__ void leave(int slot, int c0, int t, int o) {
     const int o0 = n0 + c0;
     if (vectors) {
       fence_async_smem();
       __syncwarp();
       if (lane == 0) {
+        if (p.residual) {
+          tma_store_wait_read();
+          request(slot ^ 1, t, o);
+        }
         if (o0 < end && t0 < p.T) tma_store_2d(tout, slab + slot * 4096, o0, t0);
         tma_store_commit();
       }
@@ -328,14 +335,14 @@ struct Epilogue {
     __syncwarp();
   }
   // all 128 columns, the halves from the first or from the last on (down); `ready` waits for the accumulator, `drained` is called once the first half is
-  // in registers
+  // in registers; (t, n): the next tile, which goes the other way (t = p.T: none)
   template <typename R, typename F>
-  __device__ __forceinline__ void run(uint32_t tmem, bool down, const float* cw, const float* cb, R ready, F drained) {
-    int c0 = down ? 64 : 0;
-    fetch(n0 + c0);
+  __device__ __forceinline__ void run(uint32_t tmem, bool down, const float* cw, const float* cb, int t, int n, R ready, F drained) {
+    fetch(n0 + column_of(0, down));
     ready();
 #pragma unroll 1
-    for (int i = 0; i < 2; ++i, c0 ^= 64) {
+    for (int i = 0; i < 2; ++i) {
+      const int c0 = column_of(i * (64 / U), down);
       int v[32], u[32];
       tmem_ld32(tmem + c0, v);
       tmem_ld32(tmem + c0 + 32, u);
@@ -344,32 +351,26 @@ struct Epilogue {
         tc_fence_before();
         drained();
       }
+      const int tn = i == 0 ? t0 : t, on = i == 0 ? n0 + (c0 ^ 64) : n + column_of(0, !down);   // the first unit behind these
       float2 f[16];
       values(v, cw + c0, cb + c0, f);
       if constexpr (sizeof(T) == 4) {
         take(0, c0);
         into(f, 0, 0);
-        leave(0, c0);
+        leave(0, c0, t0, n0 + c0 + 32);
         fetch(n0 + c0 + 32);
         values(u, cw + c0 + 32, cb + c0 + 32, f);
         take(1, c0 + 32);
         into(f, 1, 0);
-        leave(1, c0 + 32);
-        if (i == 0) {
-          fetch(n0 + (c0 ^ 64));
-          if (vectors) {
-            arm(0, t0, n0 + (c0 ^ 64), 1);
-            arm(1, t0, n0 + (c0 ^ 64) + 32, 0);
-          }
-        }
+        leave(1, c0 + 32, tn, on);
       } else {
         take(i, c0);
         into(f, i, 0);
         values(u, cw + c0 + 32, cb + c0 + 32, f);
         into(f, i, 1);
-        leave(i, c0);
-        if (i == 0) fetch(n0 + (c0 ^ 64));
+        leave(i, c0, tn, on);
       }
+      if (i == 0) fetch(n0 + (c0 ^ 64));
     }
   }
 };
@@ -472,7 +473,8 @@ __global__ void __launch_bounds__(PT, 1) fp4_pair_kernel(const __grid_constant__
     int at = 0, m, n;
     tile_of<8>(pair, p.mtiles, p.ntiles, &m, &n);
     column(n);
-    ep.ahead(m * 256 + rank * 128 + quarter * 32, n * PBN + upper * 128, true);
+    ep.ahead(m * 256 + rank * 128 + quarter * 32, n * PBN + upper * 128);
+    ep.begin(m * 256 + rank * 128 + quarter * 32, n * PBN + upper * 128, true);
     for (int tile = pair; tile < ntotal; tile += npairs, ++at) {
       const int buf = at & 1;
       float* const cw = cols + (buf * 2 + upper) * 256;
@@ -482,6 +484,7 @@ __global__ void __launch_bounds__(PT, 1) fp4_pair_kernel(const __grid_constant__
       if (tile + npairs < ntotal) {
         tile_of<8>(tile + npairs, p.mtiles, p.ntiles, &m, &n);
         column(n);
+        ep.ahead(m * 256 + rank * 128 + quarter * 32, n * PBN + upper * 128);
       }
       named_bar_sync(3 + upper, 128);   // the four warps of these columns (nobody is still reading those of the tile before the last)
       // The shared columns are the last of the first accumulator and the first of the second: the upper half's or the lower's.  The warps of the other
@@ -493,11 +496,11 @@ __global__ void __launch_bounds__(PT, 1) fp4_pair_kernel(const __grid_constant__
       };
       if (!shared) free();
       ep.run(tmem + ((uint32_t)(quarter * 32) << 16) + buf * (PBN - kShared) + upper * 128, buf == 0, cw, cw + 128,
+             tile + npairs < ntotal ? m * 256 + rank * 128 + quarter * 32 : p.T, n * PBN + upper * 128,
              [&] { mbar_wait(&acc_full[buf], (at >> 1) & 1, p.status); tc_fence_after(); }, [&] {
                if (shared) free();
              });
       tc_fence_before();   // (what the next tile's arrival vouches for)
-      if (tile + npairs < ntotal) ep.ahead(m * 256 + rank * 128 + quarter * 32, n * PBN + upper * 128, buf != 0);
     }
     if (lane == 0) tma_store_wait_read();
   }

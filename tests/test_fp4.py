@@ -387,9 +387,9 @@ def test_add_norm(T, D, dtype, rdtype, kind, extra, form):
 
 
 # rows that a block walks through shared memory, several each; the last two are too wide for that, or on no 16-byte boundary
-MANY = [(7300, 96, "bfloat16", "float32", "outliers", 0), (3100, 768, "float16", "float16", "grid", 0), (1900, 2560, "bfloat16", "float32", "outliers", 0),
-        (1000, 5120, "float32", "float32", "zeros", 0), (700, 8192, "bfloat16", "bfloat16", "normal", 0), (400, 16384, "bfloat16", "float32", "outliers", 0),
-        (2100, 1248, "bfloat16", None, "normal", 8), (3000, 1264, "float16", "float32", "bad", 0), (310, 16384, "float32", "float32", "normal", 0),
+MANY = [(7300, 96, "bfloat16", "float32", "outliers", 0), (7300, 768, "float16", "float16", "grid", 0), (1900, 2560, "bfloat16", "float32", "outliers", 0),
+        (1000, 5120, "float32", "float32", "zeros", 0), (1000, 8192, "bfloat16", "bfloat16", "normal", 0), (400, 16384, "bfloat16", "float32", "outliers", 0),
+        (7300, 1248, "bfloat16", None, "normal", 0), (4000, 1264, "float16", "float32", "bad", 0), (310, 16384, "float32", "float32", "normal", 0),
         (2000, 2112, "bfloat16", "float32", "normal", 3)]
 
 
@@ -402,8 +402,8 @@ def test_add_norm_many_rows(T, D, dtype, rdtype, kind, extra, form):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("block", [16, 32])
-@pytest.mark.parametrize("T,D,dtype,kind,extra,offset", [(7400, 32, "float32", "normal", 0, 0), (2000, 2560, "bfloat16", "outliers", 0, 0), (1001, 5120, "float32", "grid", 0, 0),
-                                                         (400, 16384, "float16", "bad", 0, 0), (2001, 2112, "bfloat16", "bad", 16, 8), (2001, 2112, "bfloat16", "zeros", 3, 1)])
+@pytest.mark.parametrize("T,D,dtype,kind,extra,offset", [(7400, 32, "bfloat16", "normal", 0, 0), (6100, 2560, "bfloat16", "outliers", 0, 0), (1001, 5120, "float32", "grid", 0, 0),
+                                                         (1000, 16384, "float16", "bad", 0, 0), (7300, 2112, "bfloat16", "bad", 16, 8), (2001, 2112, "bfloat16", "zeros", 3, 1)])
 def test_quantize_many_rows(T, D, dtype, kind, extra, offset, block):
     test_quantize(T, D, dtype, kind, extra, offset, block)
 
@@ -413,7 +413,7 @@ def test_quantize_many_rows(T, D, dtype, kind, extra, offset, block):
 def test_add_norm_many_rows_in_place(over):
     import torch
     from paper_2608_21952_b200 import binding as bd
-    T, D = 4000, 1280
+    T, D = 6100, 1280
     x, res, h, w, p = _norm_case(T, D, "bfloat16", "bfloat16", "outliers", 0)
     t = {"x": _dev(x, "bfloat16"), "residual": _dev(res, "bfloat16")}
     xq, status = torch.empty(T, D, dtype=torch.int8, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
