@@ -111,8 +111,8 @@ __device__ __forceinline__ void arrive_relaxed_at(uint32_t bar) {
 // binary32), each through one of the warp's two slabs in shared memory.  Where out's rows (and the residual's) lie on 16-byte boundaries TMA brings the
 // residual of a unit into its slab, a unit ahead, and takes the unit from there; it leaves out
 // what is beyond the last row and column.  Other rows are read back from the slabs as binary32, a row at a time by lanes that stand beside
-// one another in it, and stored in words of four bytes: in an odd row, one of 16-bit elements that starts in the middle of a word,
-// lane j has elements 2 j + 1 and 2 j + 2, and the last lane both ends.
+// one another in it, and stored in words of four bytes: in an odd row, one of 16-bit elements that starts in the middle of a word, lane j has
+// elements 2 j - 1 and 2 j, and the row's own lane stores both ends.
 template <typename T>
 struct Epilogue {
   static constexpr int U = 128 / sizeof(T);   // columns of a unit
@@ -123,16 +123,15 @@ struct Epilogue {
   uint8_t* slab;
   uint64_t* bar;         // of each slab's residual
   const int lane;
-  const bool vectors, even;   // even: every row of out starts on a word of four bytes, and the residual's
+  const bool vectors;
   uint32_t phase = 0;    // of the barriers, a bit each
   int t0, n0, end;       // the tile's first row of the warp, its first column, where its columns end
   float sr;
-  uint32_t res[32];      // rows on other boundaries: the residual of a unit, this lane's word (two words' halves) of each of 32 rows
+  uint32_t res[32], ends;   // rows on other boundaries: the residual of a unit, this lane's word of each of 32 rows, and both ends of its own
+  float head, tail;         // ends of this lane's row
 
   __device__ __forceinline__ Epilogue(const Fp4Params& p_, const CUtensorMap* tout_, const CUtensorMap* tres_, uint8_t* slab_, uint64_t* bar_)
-      : p(p_), tout(tout_), tres(tres_), slab(slab_), bar(bar_), lane(threadIdx.x & 31), vectors(p_.vec_out && (!p_.residual || p_.vec_res)),
-        even(((reinterpret_cast<uintptr_t>(p_.out) >> 1 | (uintptr_t)p_.out_stride) & 1) == 0 &&
-             (!p_.residual || ((reinterpret_cast<uintptr_t>(p_.residual) >> 1 | (uintptr_t)p_.res_stride) & 1) == 0)) {}
+      : p(p_), tout(tout_), tres(tres_), slab(slab_), bar(bar_), lane(threadIdx.x & 31), vectors(p_.vec_out && (!p_.residual || p_.vec_res)) {}
 
   __device__ __forceinline__ void tile(int t_first, int n_first) {
     t0 = t_first;
@@ -164,7 +163,7 @@ struct Epilogue {
       asm volatile("prefetch.global.L2 [%0];" ::"l"(at + bytes - 1));
     }
   }
-  // rows on other boundaries: whole units are read and written without a check, a batch of rows at a time; `same`: words of the residual are where out's are
+  // rows on other boundaries: whole units are read and written without a check
   __device__ __forceinline__ bool whole(int o0) const { return t0 + 32 <= p.T && o0 + U <= end; }
   __device__ __forceinline__ void fetch(int o0) {
     if (vectors || !p.residual || !whole(o0)) return;
@@ -173,22 +172,22 @@ struct Epilogue {
 #pragma unroll
       for (int r = 0; r < 32; ++r, at += p.res_stride) res[r] = at[lane];
     } else {
-      const T* to = static_cast<const T*>(p.out) + t0 * p.out_stride + o0;
-      if (even) {   // (o0 is a multiple of 32)
+      const int odd0 = odd_row(static_cast<const T*>(p.out) + t0 * p.out_stride + o0), odd1 = odd0 ^ (int)(p.out_stride & 1);   // of every other row
+      const uint16_t* const own = at + lane * p.res_stride;
+      ends = (uint32_t)own[0] | (uint32_t)own[63] << 16;
+      const bool same = odd_row(at) == odd0 && ((p.out_stride ^ p.res_stride) & 1) == 0;
+      if (same && !(odd0 | odd1)) {
 #pragma unroll
         for (int r = 0; r < 32; ++r, at += p.res_stride) res[r] = reinterpret_cast<const uint32_t*>(at)[lane];
-      } else if (odd_row(at) == odd_row(to) && (((p.out_stride ^ p.res_stride) & 1) == 0)) {
+      } else if (same) {
+        // (the word ahead of an odd row's first whole one is the one that the row begins in)
 #pragma unroll
-        for (int r = 0; r < 32; ++r, at += p.res_stride, to += p.out_stride) {
-          const int odd = odd_row(to);
-          if (lane < 31 || !odd) res[r] = *reinterpret_cast<const uint32_t*>(at + 2 * lane + odd);
-          else res[r] = (uint32_t)at[63] | (uint32_t)at[0] << 16;
-        }
+        for (int r = 0; r < 32; ++r, at += p.res_stride) res[r] = *reinterpret_cast<const uint32_t*>(at - (r & 1 ? odd1 : odd0) + 2 * lane);
       } else {
 #pragma unroll
-        for (int r = 0; r < 32; ++r, at += p.res_stride, to += p.out_stride) {
-          const int a = 2 * lane + odd_row(to);
-          res[r] = (uint32_t)at[a] | (uint32_t)at[(a + 1) & 63] << 16;
+        for (int r = 0; r < 32; ++r, at += p.res_stride) {
+          const int first = 2 * lane - (r & 1 ? odd1 : odd0);
+          res[r] = (uint32_t)at[max(first, 0)] | (uint32_t)at[first + 1] << 16;
         }
       }
     }
@@ -242,6 +241,8 @@ struct Epilogue {
       }
     } else {   // pairs of columns, at a place that depends on the row: no two lanes of a row or of a column meet in a bank
       constexpr int pairs = U / 2;
+      if (half == 0) head = f[0].x;
+      tail = f[15].y;
       float2* const to = reinterpret_cast<float2*>(slab) + lane * pairs;
 #pragma unroll
       for (int c = 0; c < 16; ++c) to[((sizeof(T) == 4 ? 0 : 16 * half) + c) ^ (lane & (pairs - 1))] = f[c];
@@ -279,49 +280,44 @@ struct Epilogue {
     const float* const turn = reinterpret_cast<const float*>(slab);
     auto column = [&](int r, int c) { return turn[r * U + (((c >> 1) ^ (r & (pairs - 1))) << 1) + (c & 1)]; };
     T* at = static_cast<T*>(p.out) + t0 * p.out_stride + o0;
-    if (sizeof(T) == 2 && even && whole(o0)) {
+    if (whole(o0)) {
+      if constexpr (sizeof(T) == 4) {
 #pragma unroll
-      for (int r = 0; r < 32; ++r, at += p.out_stride) {
-        float2 x = reinterpret_cast<const float2*>(turn)[r * pairs + (lane ^ (r & (pairs - 1)))];
-        if (p.residual) {
-          const T* const m = reinterpret_cast<const T*>(&res[r]);
-          x = __fadd2_rn(x, make_float2(Elem<T>::get(m[0]), Elem<T>::get(m[1])));
+        for (int r = 0; r < 32; ++r, at += p.out_stride) {
+          const float x = column(r, lane);
+          at[lane] = p.residual ? x + __uint_as_float(res[r]) : x;
         }
-        if constexpr (sizeof(T) == 2) reinterpret_cast<uint32_t*>(at)[lane] = Elem<T>::pack(make_float4(x.x, x.y, 0.f, 0.f)).x;
-      }
-    } else if (whole(o0)) {
+      } else {
+        T* const own = at + lane * p.out_stride;
+        const int odd0 = odd_row(at), odd1 = odd0 ^ (int)(p.out_stride & 1);
+        if (!(odd0 | odd1)) {
 #pragma unroll
-      for (int r0 = 0; r0 < 32; r0 += 8) {
-        float2 x[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int r = r0 + i;
-          if constexpr (sizeof(T) == 4) {
-            x[i].x = column(r, lane);
-            if (p.residual) x[i].x += __uint_as_float(res[r]);
-          } else {
-            const int a = 2 * lane + odd_row(at + i * p.out_stride);
-            x[i] = make_float2(column(r, a), column(r, (a + 1) & 63));
+          for (int r = 0; r < 32; ++r, at += p.out_stride) {
+            float2 x = reinterpret_cast<const float2*>(turn)[r * pairs + (lane ^ r)];
             if (p.residual) {
               const T* const m = reinterpret_cast<const T*>(&res[r]);
-              x[i] = __fadd2_rn(x[i], make_float2(Elem<T>::get(m[0]), Elem<T>::get(m[1])));
+              x = __fadd2_rn(x, make_float2(Elem<T>::get(m[0]), Elem<T>::get(m[1])));
             }
+            reinterpret_cast<uint32_t*>(at)[lane] = Elem<T>::pack(make_float4(x.x, x.y, 0.f, 0.f)).x;
           }
+          __syncwarp();
+          return;
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i, at += p.out_stride) {
-          if constexpr (sizeof(T) == 4) {
-            at[lane] = x[i].x;
-          } else {
-            const int odd = odd_row(at);
-            const uint32_t w = Elem<T>::pack(make_float4(x[i].x, x[i].y, 0.f, 0.f)).x;
-            if (lane < 31 || !odd) {
-              *reinterpret_cast<uint32_t*>(at + 2 * lane + odd) = w;
-            } else {
-              reinterpret_cast<uint16_t*>(at)[63] = (uint16_t)w;
-              reinterpret_cast<uint16_t*>(at)[0] = (uint16_t)(w >> 16);
-            }
+        for (int r = 0; r < 32; ++r, at += p.out_stride) {
+          const int odd = r & 1 ? odd1 : odd0;
+          float2 x = reinterpret_cast<const float2*>(turn)[r * pairs + (lane ^ r)];
+          if (odd) x = make_float2(__shfl_up_sync(0xffffffffu, x.y, 1), x.x);
+          if (p.residual) {
+            const T* const m = reinterpret_cast<const T*>(&res[r]);
+            x = __fadd2_rn(x, make_float2(Elem<T>::get(m[0]), Elem<T>::get(m[1])));
           }
+          if (lane > 0 || !odd) *reinterpret_cast<uint32_t*>(at - odd + 2 * lane) = Elem<T>::pack(make_float4(x.x, x.y, 0.f, 0.f)).x;
+        }
+        if (odd_row(own)) {
+          const T* const m = reinterpret_cast<const T*>(&ends);
+          own[0] = Elem<T>::put(p.residual ? head + Elem<T>::get(m[0]) : head);
+          own[63] = Elem<T>::put(p.residual ? tail + Elem<T>::get(m[1]) : tail);
         }
       }
     } else if (o0 < end) {
@@ -592,6 +588,23 @@ __device__ __forceinline__ void few_out(const FewParams& f, const float* part, c
           y = __fadd2_rn(y, make_float2(r.z, r.w));
         }
         *reinterpret_cast<typename Elem<T>::raw4*>(dst + u * dstep) = Elem<T>::pack(make_float4(x.x, x.y, y.x, y.y));
+      } else if (sizeof(T) == 2 && no == 4) {   // words where the row's boundary allows
+        if (p.residual) {
+          const T* const r = res + u * rstep;
+          x = __fadd2_rn(x, make_float2(Elem<T>::get(r[0]), Elem<T>::get(r[1])));
+          y = __fadd2_rn(y, make_float2(Elem<T>::get(r[2]), Elem<T>::get(r[3])));
+        }
+        const typename Elem<T>::raw4 w4 = Elem<T>::pack(make_float4(x.x, x.y, y.x, y.y));
+        const uint32_t* const w = reinterpret_cast<const uint32_t*>(&w4);
+        uint16_t* const d = reinterpret_cast<uint16_t*>(dst + u * dstep);
+        if ((reinterpret_cast<uintptr_t>(d) & 2) == 0) {
+          reinterpret_cast<uint32_t*>(d)[0] = w[0];
+          reinterpret_cast<uint32_t*>(d)[1] = w[1];
+        } else {
+          d[0] = (uint16_t)w[0];
+          *reinterpret_cast<uint32_t*>(d + 1) = __byte_perm(w[0], w[1], 0x5432);
+          d[3] = (uint16_t)(w[1] >> 16);
+        }
       } else {
         const float v[4] = {x.x, x.y, y.x, y.y};
 #pragma unroll

@@ -476,7 +476,7 @@ def test_add_norm_binding_refusals():
 
 
 # ---------------------------------------------------------------------------------------------------------- product
-def _linear(T, O, K, block, dtype, bias=False, act=0, residual=False, extra=0, offset=0, seed=0, exact=False, steps=True):
+def _linear(T, O, K, block, dtype, bias=False, act=0, residual=False, extra=0, offset=0, seed=0, exact=False, steps=True, rextra=None):
     """runs a product and compares it; exact: scales and codes whose sums binary32 holds, so that only the epilogue rounds"""
     import torch
     from paper_2608_21952_b200 import binding as bd
@@ -489,7 +489,7 @@ def _linear(T, O, K, block, dtype, bias=False, act=0, residual=False, extra=0, o
     status = torch.zeros(1, dtype=torch.int32, device="cuda")
     wide = torch.full((T, O + extra), 77.0, dtype=getattr(torch, dtype), device="cuda")
     out = wide[:, offset:offset + O]
-    bd.ssdi8_fp4_linear(x, w, out, bias=None if b is None else _dev(b), residual=None if res is None else _rows(res, dtype, extra, offset), act=act, status=status)
+    bd.ssdi8_fp4_linear(x, w, out, bias=None if b is None else _dev(b), residual=None if res is None else _rows(res, dtype, *((extra, offset) if rextra is None else (rextra, rextra // 2))), act=act, status=status)
     torch.cuda.synchronize()
     assert int(status.item()) == 0
     vx, vw = ref.values(cx, sx, block), ref.values(cw, sw, block)
@@ -549,11 +549,18 @@ def test_linear_types_and_strides(T, O, K, extra, offset, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("T,O,extra,offset,rextra", [(4000, 4000, 3, 1, 0), (4000, 4000, 0, 0, 5), (4100, 4001, 0, 0, 3), (4000, 4002, 2, 1, 2), (4000, 4001, 3, 2, 1), (60, 203, 0, 0, 1),
+                                                     (60, 204, 1, 1, 0), (300, 1003, 4, 3, 2)])
+def test_linear_residual_on_other_boundaries(T, O, extra, offset, rextra):
+    _linear(T, O, 160, 16, "bfloat16", residual=True, extra=extra, offset=offset, rextra=rextra, seed=T + O)
+
+
+@pytest.mark.gpu
 def test_linear_residual_in_place_and_again():
     """out over the residual; the same call again gives the same bits, captured too, on another stream"""
     import torch
     from paper_2608_21952_b200 import binding as bd
-    for T, O, K in ((64, 2560, 5120), (4096, 2560, 512)):
+    for T, O, K in ((64, 2560, 5120), (4096, 2560, 512), (64, 2563, 512), (4096, 2563, 512)):
         x, w = _matrix(T, K, 16, 1)[0], _matrix(O, K, 16, 2)[0]
         res = torch.randn(T, O, device="cuda").bfloat16()
         a, b = torch.empty_like(res), res.clone()
@@ -599,6 +606,34 @@ def test_linear_offsets_beyond_32_bits():
         bd.ssdi8_fp4_quantize(out[:, : O // 32 * 32], again)
         assert torch.equal(q.tensors["codes"], again.tensors["codes"]) and torch.equal(q.tensors["scales"], again.tensors["scales"])
         del flat, out
+
+
+@pytest.mark.gpu
+def test_codes_and_rows_beyond_32_bits():
+    """more than 2^32 codes, and a stream of more than 2^31 elements: the last rows are as of a call on them alone"""
+    import torch
+    from paper_2608_21952_b200 import binding as bd
+    T, D, n = 34000, 131072, 130
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("not enough memory")
+    x = torch.empty(T, D, dtype=torch.bfloat16, device="cuda").fill_(1.5)
+    x[-n:] = torch.randn(n, D, device="cuda").to(torch.bfloat16)
+    big, small = bd.make_fp4(T, D), bd.make_fp4(n, D)
+    bd.ssdi8_fp4_quantize(x, big)
+    bd.ssdi8_fp4_quantize(x[-n:], small)
+    assert torch.equal(big.tensors["codes"][-n:], small.tensors["codes"]) and torch.equal(big.tensors["step"][-n:], small.tensors["step"])
+    want = torch.empty(n, D, dtype=torch.bfloat16, device="cuda")
+    bd.ssdi8_fp4_dequantize(small, want)
+    bd.ssdi8_fp4_dequantize(big, x)
+    assert torch.equal(x[-n:], want)
+    del big, small, want, x
+    T, D = 135000, 16384
+    x, res = (torch.empty(T, D, dtype=torch.bfloat16, device="cuda").fill_(0.5) for _ in range(2))
+    x[-n:] = torch.randn(n, D, device="cuda").to(torch.bfloat16)
+    last, xq, one = res[-n:].clone(), torch.empty(T, D, dtype=torch.int8, device="cuda"), torch.empty(n, D, dtype=torch.int8, device="cuda")
+    bd.ssdi8_add_norm_quantize(x, residual=res, residual_out=res, xq=xq)
+    bd.ssdi8_add_norm_quantize(x[-n:], residual=last, residual_out=last, xq=one)
+    assert torch.equal(xq[-n:], one) and torch.equal(res[-n:], last)
 
 
 @pytest.mark.gpu
