@@ -113,8 +113,10 @@ __device__ __forceinline__ void arrive_relaxed_at(uint32_t bar) {
 // what is beyond the last row and column.  Other rows are read back from the slabs as binary32, a row at a time by lanes that stand beside
 // one another in it, and stored in words of four bytes: in an odd row, one of 16-bit elements that starts in the middle of a word, lane j has
 // elements 2 j - 1 and 2 j, and the row's own lane stores both ends.
-template <typename T>
+enum { ROWS_VECTORS = 0, ROWS_WORDS = 1, ROWS_ODD = 2 };   // out's rows (and the residual's) on 16 bytes, on words (binary32: elements), on 16-bit elements
+template <typename T, int ROWS>
 struct Epilogue {
+  static constexpr bool vectors = ROWS == ROWS_VECTORS;
   static constexpr int U = 128 / sizeof(T);   // columns of a unit
   typedef typename std::conditional<sizeof(T) == 4, uint32_t, uint16_t>::type Bits;
 
@@ -123,7 +125,6 @@ struct Epilogue {
   uint8_t* slab;
   uint64_t* bar;         // of each slab's residual
   const int lane;
-  const bool vectors;
   uint32_t phase = 0;    // of the barriers, a bit each
   int t0, n0, end;       // the tile's first row of the warp, its first column, where its columns end
   float sr;
@@ -131,7 +132,7 @@ struct Epilogue {
   float head, tail;         // ends of this lane's row
 
   __device__ __forceinline__ Epilogue(const Fp4Params& p_, const CUtensorMap* tout_, const CUtensorMap* tres_, uint8_t* slab_, uint64_t* bar_)
-      : p(p_), tout(tout_), tres(tres_), slab(slab_), bar(bar_), lane(threadIdx.x & 31), vectors(p_.vec_out && (!p_.residual || p_.vec_res)) {}
+      : p(p_), tout(tout_), tres(tres_), slab(slab_), bar(bar_), lane(threadIdx.x & 31) {}
 
   __device__ __forceinline__ void tile(int t_first, int n_first) {
     t0 = t_first;
@@ -174,9 +175,9 @@ struct Epilogue {
     } else {
       const int odd0 = odd_row(static_cast<const T*>(p.out) + t0 * p.out_stride + o0), odd1 = odd0 ^ (int)(p.out_stride & 1);   // of every other row
       const uint16_t* const own = at + lane * p.res_stride;
-      ends = (uint32_t)own[0] | (uint32_t)own[63] << 16;
+      if (ROWS == ROWS_ODD) ends = (uint32_t)own[0] | (uint32_t)own[63] << 16;
       const bool same = odd_row(at) == odd0 && ((p.out_stride ^ p.res_stride) & 1) == 0;
-      if (same && !(odd0 | odd1)) {
+      if (ROWS == ROWS_WORDS) {
 #pragma unroll
         for (int r = 0; r < 32; ++r, at += p.res_stride) res[r] = reinterpret_cast<const uint32_t*>(at)[lane];
       } else if (same) {
@@ -290,7 +291,7 @@ struct Epilogue {
       } else {
         T* const own = at + lane * p.out_stride;
         const int odd0 = odd_row(at), odd1 = odd0 ^ (int)(p.out_stride & 1);
-        if (!(odd0 | odd1)) {
+        if constexpr (ROWS == ROWS_WORDS) {
 #pragma unroll
           for (int r = 0; r < 32; ++r, at += p.out_stride) {
             float2 x = reinterpret_cast<const float2*>(turn)[r * pairs + (lane ^ r)];
@@ -300,24 +301,23 @@ struct Epilogue {
             }
             reinterpret_cast<uint32_t*>(at)[lane] = Elem<T>::pack(make_float4(x.x, x.y, 0.f, 0.f)).x;
           }
-          __syncwarp();
-          return;
-        }
+        } else {
 #pragma unroll
-        for (int r = 0; r < 32; ++r, at += p.out_stride) {
-          const int odd = r & 1 ? odd1 : odd0;
-          float2 x = reinterpret_cast<const float2*>(turn)[r * pairs + (lane ^ r)];
-          if (odd) x = make_float2(__shfl_up_sync(0xffffffffu, x.y, 1), x.x);
-          if (p.residual) {
-            const T* const m = reinterpret_cast<const T*>(&res[r]);
-            x = __fadd2_rn(x, make_float2(Elem<T>::get(m[0]), Elem<T>::get(m[1])));
+          for (int r = 0; r < 32; ++r, at += p.out_stride) {
+            const int odd = r & 1 ? odd1 : odd0;
+            float2 x = reinterpret_cast<const float2*>(turn)[r * pairs + (lane ^ r)];
+            if (odd) x = make_float2(__shfl_up_sync(0xffffffffu, x.y, 1), x.x);
+            if (p.residual) {
+              const T* const m = reinterpret_cast<const T*>(&res[r]);
+              x = __fadd2_rn(x, make_float2(Elem<T>::get(m[0]), Elem<T>::get(m[1])));
+            }
+            if (lane > 0 || !odd) *reinterpret_cast<uint32_t*>(at - odd + 2 * lane) = Elem<T>::pack(make_float4(x.x, x.y, 0.f, 0.f)).x;
           }
-          if (lane > 0 || !odd) *reinterpret_cast<uint32_t*>(at - odd + 2 * lane) = Elem<T>::pack(make_float4(x.x, x.y, 0.f, 0.f)).x;
-        }
-        if (odd_row(own)) {
-          const T* const m = reinterpret_cast<const T*>(&ends);
-          own[0] = Elem<T>::put(p.residual ? head + Elem<T>::get(m[0]) : head);
-          own[63] = Elem<T>::put(p.residual ? tail + Elem<T>::get(m[1]) : tail);
+          if (odd_row(own)) {
+            const T* const m = reinterpret_cast<const T*>(&ends);
+            own[0] = Elem<T>::put(p.residual ? head + Elem<T>::get(m[0]) : head);
+            own[63] = Elem<T>::put(p.residual ? tail + Elem<T>::get(m[1]) : tail);
+          }
         }
       }
     } else if (o0 < end) {
@@ -371,7 +371,7 @@ struct Epilogue {
   }
 };
 
-template <typename T, int BLOCK>
+template <typename T, int BLOCK, int ROWS>
 __global__ void __launch_bounds__(PT, 1) fp4_pair_kernel(const __grid_constant__ CUtensorMap tx, const __grid_constant__ CUtensorMap tw,
                                                          const __grid_constant__ CUtensorMap tsx, const __grid_constant__ CUtensorMap tsw,
                                                          const __grid_constant__ CUtensorMap tout, const __grid_constant__ CUtensorMap tres,
@@ -458,7 +458,7 @@ __global__ void __launch_bounds__(PT, 1) fp4_pair_kernel(const __grid_constant__
     }
   } else if (warp >= 4) {
     const int quarter = warp & 3, upper = (warp - 4) >> 2, et = tid & 127;   // eight warps: a quarter of the rows, half of the columns
-    Epilogue<T> ep(p, &tout, &tres, smem + S::kSlabs + (warp - 4) * 2 * 4096, res_full + (warp - 4) * 2);
+    Epilogue<T, ROWS> ep(p, &tout, &tres, smem + S::kSlabs + (warp - 4) * 2 * 4096, res_full + (warp - 4) * 2);
     // a column's step size and bias, a tile ahead
     float w = 0.f, b = 0.f;
     auto column = [&](int n) {
@@ -809,8 +809,14 @@ ssdi8_status_t launch(const ssdi8_fp4_linear_args_t& a, cudaStream_t st) {
     CUtensorMap tres = tx;
     const uint64_t rstride[1] = {(uint64_t)(a.stride_residual * e)};
     if (a.residual && p.vec_res && !encode_tensor_map(&tres, a.residual, (int)e, 2, dims, rstride, box, 128)) p.vec_res = 0;
-    return launch_any(fp4_pair_kernel<T, BLOCK>, dim3((unsigned)(2 * (ptiles < pairs ? ptiles : pairs))), 2, dim3(PT), PairLayout::kAlloc, PairLayout::kAlloc,
-                      -1, true, st, tx, tw, tsx, tsw, tout, tres, p);
+    auto go = [&](auto rows) {
+      return launch_any(fp4_pair_kernel<T, BLOCK, decltype(rows)::value>, dim3((unsigned)(2 * (ptiles < pairs ? ptiles : pairs))), 2, dim3(PT), PairLayout::kAlloc,
+                        PairLayout::kAlloc, -1, true, st, tx, tw, tsx, tsw, tout, tres, p);
+    };
+    if (p.vec_out && (!a.residual || p.vec_res)) return go(std::integral_constant<int, ROWS_VECTORS>());
+    auto words = [](const void* q, i64 stride) { return reinterpret_cast<uintptr_t>(q) % 4 == 0 && stride % 2 == 0; };
+    if (sizeof(T) == 4 || (words(a.out, a.stride_out) && (!a.residual || words(a.residual, a.stride_residual)))) return go(std::integral_constant<int, ROWS_WORDS>());
+    if constexpr (sizeof(T) == 2) return go(std::integral_constant<int, ROWS_ODD>());
   }
   f.l = p;
   f.l.mtiles = (int)mt;
