@@ -4,8 +4,14 @@
 // One pass: every thread keeps eight columns of up to four chunks in registers between the row's two reductions (sum of squares in binary64,
 // absmax of p; one exchange through shared memory) and the codes.  The norm's factor r never meets a code: it is the same for the row, so it
 // goes into the row's step size (with a static step size it does, once per element).  So the sum need not be formed ahead of the codes' arithmetic, and codes
-// are functions of p alone.  In binary64 the sum cannot leave its range and costs no time that the loads do not: two instructions an element on
-// a pipe that nothing else uses.
+// are functions of p alone.  In binary64 the sum cannot leave its range (a conversion and a fused multiply-add an element, on pipes that nothing else
+// uses: 64 cycles for a warp's 256 columns).
+//
+// What bounds it (device times).  With an fp32 stream the bytes: 16384 x 2560 bf16 to int8 (461 MB, 70 us) 80 us, to four bits 75, 4096 x 8192 (56)
+// 61.  With less to move instructions, most of them on the half-rate integer pipe (unpacking, maxima, addresses; 55 % busy): bf16 stream (45) 56, without one (19)
+// 41; the quantiser 137 a warp and 256 columns, 16384 x 5120 bf16 (33) 60, 53 in blocks of 32, 10576 x 2560 fp32 (19) 19 to 21.  Divisions in
+// place of corrected products took 204 and 86.  Values: 16384 x 5120 to bf16 (33) 39, 60 with a division to find a thread's row.  2560 rows of
+// 16384 (67) 109: one block of 96 KB a row to an SM.  One row of 768: 2.0, of which the call itself takes 3.7 from Python.
 #include "fp4.cuh"
 #include "kernels.h"
 #include "sm100.cuh"
@@ -15,7 +21,7 @@
 namespace ssdi8 {
 namespace {
 
-constexpr int kRing = 2;       // rows of a block's ring
+constexpr int kRing = 2;      // rows of a block's ring
 constexpr int kChunk = 256;   // columns of a chunk: a warp's lanes have eight each, so that a block of 16 is two lanes and one of 32 four
 
 struct None {};   // no residual stream

@@ -3,7 +3,16 @@
 //
 // Operands come by TMA in rows of 128 bytes (256 columns) with the 128-byte swizzle, scales as they stand in memory: their tiles of
 // 128 rows x 4 blocks are what tcgen05.cp spreads over tensor memory (32 lanes of four words, the same for every quarter of the lanes), from where
-// the MMA takes them.  Two forms: pairs of SMs, and up to a few tiles a CTA with K shared out.
+// the MMA takes them.  Two forms: persistent tiles of 256 x 256 on pairs of SMs, and for few rows a tile of 128 x up to 256 a CTA with K shared out.
+//
+// What bounds it.  The pipe does 64 columns of a pair's tile in 148 cycles on resident operands and scales (8.2 PFLOP/s at 1965 MHz, with the scales'
+// copies between them: N 256 alone hides those, N 128 takes 76 without and 88 with).  16384 x 2560 x 5120 with bias and residual (34 us of
+// bytes, 52 of operations at that rate) takes 97 to 108 us on the device: the clock falls to 1.4 to 1.65 GHz under the power limit, at which a tile's 20 stages
+// take 13300 cycles where the pipe alone would take 11900 (89 %), and 0.9 us pass from one tile to the next: the accumulators share 48 columns.
+// 3439 x 16472 x 1248, fp16, residual (37 us of bytes) 76, 57 without the residual: five stages a tile, so that the epilogue's chain (4 us a tile for
+// accumulator, columns, slab and store) is what is waited for; 16470 columns, rows on words, 127; 16471, odd ones, 176.
+// 64 x 10576 x 2560 (2.6 us of bytes) 6.9 us from L2 and 8.8 from DRAM, one row 5.7 and 6.7: launch and first operands 1.0, ten stages' MMAs and
+// scale copies of a lone CTA 2.5 (issued without checks; 3.5 with them), the accumulator's way out and the tokens 1.5.
 #include "fp4.cuh"
 #include "kernels.h"
 #include "linear.cuh"
@@ -89,7 +98,8 @@ __device__ __forceinline__ void issue_stage(uint32_t acc, uint32_t ts, uint32_t 
 // Tiles of 256 x 256 for two SMs (cta_group::2), persistent: each CTA of a pair loads 128 rows of x, 128 of w and the scales of its rows of x and of all
 // 256 of w, the first one issues the MMAs, and each drains its 128 rows of the accumulator while the next tile's is formed.  Two accumulators
 // of 256 columns would be all of tensor memory: they share 48 columns, which the scales take at its end, and an epilogue reads
-// the shared ones first.
+// the shared ones first.  (Four stages of 38 KB and two slabs to an epilogue warp; five stages and one slab: 100 us where these take 97.  Rows
+// stored by their lanes, without slabs: 124.  Sixteen epilogue warps of 64 columns: 116, no gain where the epilogue is waited for.)
 constexpr int PBN = 256, PT = 384, kShared = 48;
 struct PairLayout {
   static constexpr int kStages = 4;
