@@ -10,7 +10,7 @@
 // bytes, 52 of operations at that rate) takes 97 to 108 us on the device: the clock falls to 1.4 to 1.65 GHz under the power limit, at which a tile's 20 stages
 // take 13300 cycles where the pipe alone would take 11900 (89 %), and 0.9 us pass from one tile to the next: the accumulators share 48 columns.
 // 3439 x 16472 x 1248, fp16, residual (37 us of bytes) 76, 57 without the residual: five stages a tile, so that the epilogue's chain (4 us a tile for
-// accumulator, columns, slab and store) is what is waited for; 16470 columns, rows on words, 127; 16471, odd ones, 176.
+// accumulator, columns, slab and store) is what is waited for; 16470 columns, rows on words, 121; 16471, odd ones, 169.
 // 64 x 10576 x 2560 (2.6 us of bytes) 6.9 us from L2 and 8.8 from DRAM, one row 5.7 and 6.7: launch and first operands 1.0, ten stages' MMAs and
 // scale copies of a lone CTA 2.5 (issued without checks; 3.5 with them), the accumulator's way out and the tokens 1.5.
 #include "fp4.cuh"
@@ -138,7 +138,9 @@ struct Epilogue {
   uint32_t phase = 0;    // of the barriers, a bit each
   int t0, n0, end;       // the tile's first row of the warp, its first column, where its columns end
   float sr;
-  uint32_t res[32], ends;   // rows on other boundaries: the residual of a unit, this lane's word of each of 32 rows, and both ends of its own
+  // rows on other boundaries: the residual of a unit, this lane's word of each of 32 rows, and both ends of its own; the next unit's on its way in the
+  // other half, so the halves are named where they are used
+  uint32_t res[2][32], ends[2];
   float head, tail;         // ends of this lane's row
 
   __device__ __forceinline__ Epilogue(const Fp4Params& p_, const CUtensorMap* tout_, const CUtensorMap* tres_, uint8_t* slab_, uint64_t* bar_)
@@ -164,6 +166,7 @@ struct Epilogue {
   // ahead of the first tile: its first unit's
   __device__ __forceinline__ void begin(int t, int n, bool down) {
     if (vectors && p.residual && lane == 0) request(0, t, n + column_of(0, down));
+    fetch<0>(t, n + column_of(0, down));
   }
   // rows on other boundaries: the residual of the tile at (t, n) into L2, a tile ahead
   __device__ __forceinline__ void ahead(int t, int n) {
@@ -175,30 +178,30 @@ struct Epilogue {
     }
   }
   // rows on other boundaries: whole units are read and written without a check
-  __device__ __forceinline__ bool whole(int o0) const { return t0 + 32 <= p.T && o0 + U <= end; }
-  __device__ __forceinline__ void fetch(int o0) {
-    if (vectors || !p.residual || !whole(o0)) return;
-    const Bits* at = static_cast<const Bits*>(p.residual) + t0 * p.res_stride + o0;
+  __device__ __forceinline__ bool whole(int t, int o) const { return t + 32 <= p.T && o + U <= p.O; }
+  template <int SLOT>
+  __device__ __forceinline__ void fetch(int t, int o) {
+    if (vectors || !p.residual || !whole(t, o)) return;
+    const Bits* at = static_cast<const Bits*>(p.residual) + t * p.res_stride + o;
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
-      for (int r = 0; r < 32; ++r, at += p.res_stride) res[r] = at[lane];
-    } else {
-      const int odd0 = odd_row(static_cast<const T*>(p.out) + t0 * p.out_stride + o0), odd1 = odd0 ^ (int)(p.out_stride & 1);   // of every other row
-      const uint16_t* const own = at + lane * p.res_stride;
-      if (ROWS == ROWS_ODD) ends = (uint32_t)own[0] | (uint32_t)own[63] << 16;
-      const bool same = odd_row(at) == odd0 && ((p.out_stride ^ p.res_stride) & 1) == 0;
-      if (ROWS == ROWS_WORDS) {
+      for (int r = 0; r < 32; ++r, at += p.res_stride) res[SLOT][r] = at[lane];
+    } else if constexpr (ROWS == ROWS_WORDS) {
 #pragma unroll
-        for (int r = 0; r < 32; ++r, at += p.res_stride) res[r] = reinterpret_cast<const uint32_t*>(at)[lane];
-      } else if (same) {
+      for (int r = 0; r < 32; ++r, at += p.res_stride) res[SLOT][r] = reinterpret_cast<const uint32_t*>(at)[lane];
+    } else {
+      const int odd0 = odd_row(static_cast<const T*>(p.out) + t * p.out_stride + o), odd1 = odd0 ^ (int)(p.out_stride & 1);   // of every other row
+      const uint16_t* const own = at + lane * p.res_stride;
+      ends[SLOT] = (uint32_t)own[0] | (uint32_t)own[63] << 16;
+      if (odd_row(at) == odd0 && ((p.out_stride ^ p.res_stride) & 1) == 0) {
         // (the word ahead of an odd row's first whole one is the one that the row begins in)
 #pragma unroll
-        for (int r = 0; r < 32; ++r, at += p.res_stride) res[r] = *reinterpret_cast<const uint32_t*>(at - (r & 1 ? odd1 : odd0) + 2 * lane);
+        for (int r = 0; r < 32; ++r, at += p.res_stride) res[SLOT][r] = *reinterpret_cast<const uint32_t*>(at - (r & 1 ? odd1 : odd0) + 2 * lane);
       } else {
 #pragma unroll
         for (int r = 0; r < 32; ++r, at += p.res_stride) {
           const int first = 2 * lane - (r & 1 ? odd1 : odd0);
-          res[r] = (uint32_t)at[max(first, 0)] | (uint32_t)at[first + 1] << 16;
+          res[SLOT][r] = (uint32_t)at[max(first, 0)] | (uint32_t)at[first + 1] << 16;
         }
       }
     }
@@ -271,7 +274,9 @@ struct Epilogue {
     }
   }
   // a unit out of its slab; (t, o): the unit that comes next, whose residual may follow as soon as the other slab's store has been read
-  __device__ __forceinline__ void leave(int slot, int c0, int t, int o) {
+  template <int SLOT>
+  __device__ __forceinline__ void leave(int c0, int t, int o) {
+    constexpr int slot = SLOT;
     const int o0 = n0 + c0;
     if (vectors) {
       fence_async_smem();
@@ -286,17 +291,18 @@ struct Epilogue {
       }
       return;
     }
+    fetch<SLOT ^ 1>(t, o);
     __syncwarp();
     constexpr int pairs = U / 2;
     const float* const turn = reinterpret_cast<const float*>(slab);
     auto column = [&](int r, int c) { return turn[r * U + (((c >> 1) ^ (r & (pairs - 1))) << 1) + (c & 1)]; };
     T* at = static_cast<T*>(p.out) + t0 * p.out_stride + o0;
-    if (whole(o0)) {
+    if (whole(t0, o0)) {
       if constexpr (sizeof(T) == 4) {
 #pragma unroll
         for (int r = 0; r < 32; ++r, at += p.out_stride) {
           const float x = column(r, lane);
-          at[lane] = p.residual ? x + __uint_as_float(res[r]) : x;
+          at[lane] = p.residual ? x + __uint_as_float(res[SLOT][r]) : x;
         }
       } else {
         T* const own = at + lane * p.out_stride;
@@ -306,7 +312,7 @@ struct Epilogue {
           for (int r = 0; r < 32; ++r, at += p.out_stride) {
             float2 x = reinterpret_cast<const float2*>(turn)[r * pairs + (lane ^ r)];
             if (p.residual) {
-              const T* const m = reinterpret_cast<const T*>(&res[r]);
+              const T* const m = reinterpret_cast<const T*>(&res[SLOT][r]);
               x = __fadd2_rn(x, make_float2(Elem<T>::get(m[0]), Elem<T>::get(m[1])));
             }
             reinterpret_cast<uint32_t*>(at)[lane] = Elem<T>::pack(make_float4(x.x, x.y, 0.f, 0.f)).x;
@@ -318,13 +324,13 @@ struct Epilogue {
             float2 x = reinterpret_cast<const float2*>(turn)[r * pairs + (lane ^ r)];
             if (odd) x = make_float2(__shfl_up_sync(0xffffffffu, x.y, 1), x.x);
             if (p.residual) {
-              const T* const m = reinterpret_cast<const T*>(&res[r]);
+              const T* const m = reinterpret_cast<const T*>(&res[SLOT][r]);
               x = __fadd2_rn(x, make_float2(Elem<T>::get(m[0]), Elem<T>::get(m[1])));
             }
             if (lane > 0 || !odd) *reinterpret_cast<uint32_t*>(at - odd + 2 * lane) = Elem<T>::pack(make_float4(x.x, x.y, 0.f, 0.f)).x;
           }
           if (odd_row(own)) {
-            const T* const m = reinterpret_cast<const T*>(&ends);
+            const T* const m = reinterpret_cast<const T*>(&ends[SLOT]);
             own[0] = Elem<T>::put(p.residual ? head + Elem<T>::get(m[0]) : head);
             own[63] = Elem<T>::put(p.residual ? tail + Elem<T>::get(m[1]) : tail);
           }
@@ -344,10 +350,9 @@ struct Epilogue {
   // in registers; (t, n): the next tile, which goes the other way (t = p.T: none)
   template <typename R, typename F>
   __device__ __forceinline__ void run(uint32_t tmem, bool down, const float* cw, const float* cb, int t, int n, R ready, F drained) {
-    fetch(n0 + column_of(0, down));
     ready();
-#pragma unroll 1
-    for (int i = 0; i < 2; ++i) {
+    auto half = [&](auto which) {
+      constexpr int i = decltype(which)::value;
       const int c0 = column_of(i * (64 / U), down);
       int v[32], u[32];
       tmem_ld32(tmem + c0, v);
@@ -363,21 +368,21 @@ struct Epilogue {
       if constexpr (sizeof(T) == 4) {
         take(0, c0);
         into(f, 0, 0);
-        leave(0, c0, t0, n0 + c0 + 32);
-        fetch(n0 + c0 + 32);
+        leave<0>(c0, t0, n0 + c0 + 32);
         values(u, cw + c0 + 32, cb + c0 + 32, f);
         take(1, c0 + 32);
         into(f, 1, 0);
-        leave(1, c0 + 32, tn, on);
+        leave<1>(c0 + 32, tn, on);
       } else {
         take(i, c0);
         into(f, i, 0);
         values(u, cw + c0 + 32, cb + c0 + 32, f);
         into(f, i, 1);
-        leave(i, c0, tn, on);
+        leave<i>(c0, tn, on);
       }
-      if (i == 0) fetch(n0 + (c0 ^ 64));
-    }
+    };
+    half(std::integral_constant<int, 0>());
+    half(std::integral_constant<int, 1>());
   }
 };
 
