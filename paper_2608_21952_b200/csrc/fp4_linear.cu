@@ -119,10 +119,10 @@ __device__ __forceinline__ void arrive_relaxed_at(uint32_t bar) {
 
 // One epilogue warp: a quarter's 32 rows (lanes) of 128 columns of an accumulator, in units of 128 bytes of out's rows (64 columns, or 32 of
 // binary32), each through one of the warp's two slabs in shared memory.  Where out's rows (and the residual's) lie on 16-byte boundaries TMA brings the
-// residual of a unit into its slab, a unit ahead, and takes the unit from there; it leaves out
-// what is beyond the last row and column.  Other rows are read back from the slabs as binary32, a row at a time by lanes that stand beside
-// one another in it, and stored in words of four bytes: in an odd row, one of 16-bit elements that starts in the middle of a word, lane j has
-// elements 2 j - 1 and 2 j, and the row's own lane stores both ends.
+// residual of a unit into its slab, a unit ahead, and takes the unit from there; it leaves out what is beyond the last row and column.  Other rows
+// are read back from the slabs as binary32, a row at a time by lanes that stand beside one another in it, and stored in words of
+// four bytes: in an odd row, one of 16-bit elements that starts in the middle of a word, lane j has elements 2 j - 1 and 2 j, and the
+// row's own lane stores both ends.
 enum { ROWS_VECTORS = 0, ROWS_WORDS = 1, ROWS_ODD = 2 };   // out's rows (and the residual's) on 16 bytes, on words (binary32: elements), on 16-bit elements
 template <typename T, int ROWS>
 struct Epilogue {
@@ -194,7 +194,8 @@ struct Epilogue {
       const uint16_t* const own = at + lane * p.res_stride;
       ends[SLOT] = (uint32_t)own[0] | (uint32_t)own[63] << 16;
       if (odd_row(at) == odd0 && ((p.out_stride ^ p.res_stride) & 1) == 0) {
-        // (the word ahead of an odd row's first whole one is the one that the row begins in)
+        // (lane 0's word of an odd row is the one that the row begins in: an element of the row before, or of the word ahead of a tensor that begins
+        // in the middle of one, comes with it and is not used)
 #pragma unroll
         for (int r = 0; r < 32; ++r, at += p.res_stride) res[SLOT][r] = *reinterpret_cast<const uint32_t*>(at - (r & 1 ? odd1 : odd0) + 2 * lane);
       } else {

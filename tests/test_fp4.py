@@ -609,6 +609,53 @@ def test_linear_offsets_beyond_32_bits():
 
 
 @pytest.mark.gpu
+def test_two_streams_at_once():
+    """quantiser, norm, values and products of every form on two streams beside one another: the results of calls alone"""
+    import torch
+    from paper_2608_21952_b200 import binding as bd
+
+    class Work:
+        def __init__(self, seed, T, O, K, block):
+            g = torch.Generator(device="cuda").manual_seed(seed)
+            self.x, self.res = (torch.randn(T, K, generator=g, device="cuda").bfloat16() for _ in range(2))
+            self.q, self.w, self.block = bd.make_fp4(T, K, block), bd.make_fp4(O, K, block), block
+            bd.ssdi8_fp4_quantize(torch.randn(O, K, generator=g, device="cuda"), self.w)
+            self.stream, self.out = torch.empty_like(self.x), torch.empty(T, O, dtype=torch.float16, device="cuda")
+            self.again, self.values = bd.make_fp4(T, O // 32 * 32, block), torch.empty(T, O // 32 * 32, device="cuda")
+
+        def run(self, stream=None):
+            bd.ssdi8_add_norm_quantize(self.x, residual=self.res, residual_out=self.stream, fp4=self.q, stream=stream)
+            bd.ssdi8_fp4_linear(self.q, self.w, self.out, act=bd.ACT_SILU, stream=stream)
+            bd.ssdi8_fp4_quantize(self.out[:, :self.values.shape[1]], self.again, stream=stream)
+            bd.ssdi8_fp4_dequantize(self.again, self.values, stream=stream)
+
+        def clear(self):
+            for t in (self.stream, self.out, self.values):
+                t.zero_()
+
+    works = [[Work(10 * s + i, *c) for i, c in enumerate(((64, 2560, 1280, 16), (2304, 2561, 512, 32), (300, 640, 2048, 16), (1, 1000, 768, 32), (4000, 1280, 256, 16)))]
+             for s in (0, 1)]
+    want = []
+    for side in works:
+        for w in side:
+            w.run()
+            want.append([t.clone() for t in (w.stream, w.out, w.values)])
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(10):
+        for side in works:
+            for w in side:
+                w.clear()
+        torch.cuda.synchronize()
+        for i in range(len(works[0])):
+            for side, st in zip(works, streams):
+                side[i].run(st)
+        torch.cuda.synchronize()
+        for w, y in zip((w for side in works for w in side), want):
+            for a, b in zip((w.stream, w.out, w.values), y):
+                assert torch.equal(a, b)
+
+
+@pytest.mark.gpu
 def test_codes_and_rows_beyond_32_bits():
     """more than 2^32 codes, and a stream of more than 2^31 elements: the last rows are as of a call on them alone"""
     import torch
