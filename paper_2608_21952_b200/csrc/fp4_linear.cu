@@ -9,8 +9,8 @@
 // copies between them: N 256 alone hides those, N 128 takes 76 without and 88 with).  16384 x 2560 x 5120 with bias and residual (34 us of
 // bytes, 52 of operations at that rate) takes 97 to 108 us on the device: the clock falls to 1.4 to 1.65 GHz under the power limit, at which a tile's 20 stages
 // take 13300 cycles where the pipe alone would take 11900 (89 %), and 0.9 us pass from one tile to the next: the accumulators share 48 columns.
-// 3439 x 16472 x 1248, fp16, residual (37 us of bytes) 76, 57 without the residual: five stages a tile, so that the epilogue's chain (4 us a tile for
-// accumulator, columns, slab and store) is what is waited for; 16470 columns, rows on words, 121; 16471, odd ones, 169.
+// 3439 x 16472 x 1248, fp16, residual (37 us of bytes) 76, 53 to 57 without the residual: five stages a tile, and operands and results
+// share the way between L2 and the SMs (459 MB, 8.7 TB/s; 36 us without the stores, whatever the epilogue does); 16470 columns, rows on words, 121; 16471, odd ones, 169.
 // 64 x 10576 x 2560 (2.6 us of bytes) 6.9 us from L2 and 8.8 from DRAM, one row 5.7 and 6.7: launch and first operands 1.0, ten stages' MMAs and
 // scale copies of a lone CTA 2.5 (issued without checks; 3.5 with them), the accumulator's way out and the tokens 1.5.
 #include "fp4.cuh"
@@ -779,9 +779,9 @@ ssdi8_status_t launch(const ssdi8_fp4_linear_args_t& a, cudaStream_t st) {
     return encode_tensor_map(tm, q.scales, 4, 2, dims, stride, box, 0);
   };
   if (!scales(&tsx, x) || !scales(&tsw, w)) return SSDI8_ERR_CUDA;
-  // What is done sooner, in cycles (the figures are measured ones).  Few rows: 7200 for a launch, the first operands and the accumulator's way out, 46
-  // bytes of operands a cycle and SM in between, or where the ring does not hold all of a CTA's stages their latency of 1400 over those
-  // that it holds; the parts' meeting, the tokens.
+  // What is done sooner, in cycles (the figures are measured ones).  Few rows: 5000 for the call, and for each wave 2200 to the first operands, 46 bytes of
+  // operands a cycle and SM, or where the ring does not hold all of a CTA's stages their latency of 1400 over those that it holds; the
+  // accumulator's way out, the parts' meeting, the tokens.  A wave behind another takes 12000 at least.
   const i64 mt = (w.rows + 127ll) / 128;
   FewParams f = {};
   double best = 0.0;
@@ -796,7 +796,8 @@ ssdi8_status_t launch(const ssdi8_fp4_linear_args_t& a, cudaStream_t st) {
         const double ctas = (double)tiles * split, waves = (double)((tiles * split + places - 1) / places), share = ctas <= sms ? 1.0 : (double)per_sm;
         const int kb = (p.kblocks + split - 1) / split;
         const double port = kb * (double)bytes * share / 46.0, latency = kb > stages ? (kb - stages) * 1400.0 / stages : 0.0;
-        const double cycles = 5000.0 + waves * (2200.0 + (port > latency ? port : latency) + n * 4.0 + (split > 1 ? 1300.0 : 0.0) + n / split * 8.0);
+        const double wave = 2200.0 + (port > latency ? port : latency) + n * 8.0 + n / split * 20.0 + (split > 1 ? 1300.0 + n * 25.0 : 0.0);
+        const double cycles = 5000.0 + (waves == 1.0 ? wave : waves * (wave > 12000.0 ? wave : 12000.0));
         if (best == 0.0 || cycles < best) {
           best = cycles;
           f.n = n;
@@ -807,12 +808,14 @@ ssdi8_status_t launch(const ssdi8_fp4_linear_args_t& a, cudaStream_t st) {
       }
     }
   }
-  // Pairs: 11400 for a launch, the first operands and the last tile's way out, 570 for 256 of K where no epilogue is beside them and 760 where one is, 1700
-  // from one tile to the next; an epilogue's 7000 hide behind the next tile's product.  (One wave of each, us: 64 x 10576 x 2560 few rows 6.9, pairs 9.7;
-  // 512 x 2560 x 5120 11.3, 11.7; 250 x 18560 x 4096 17.2, 14.8; 1024 x 2560 x 5120 15.7, 12.7.)
+  // Pairs: 10000 for the call, the first operands and the last tile's way out, 600 for 256 of K where no epilogue is beside them and 760 where one is, 1700
+  // from one tile to the next, 5000 at least.  (us, few rows and pairs: 64 x 10576 x 2560 6.9, 9.7; 64 x 10576 x 768 4.7, 6.4; 250 x 2000 x 1024 9.2, 6.1;
+  // 256 x 4096 x 8192 12.7, 16.1; 512 x 2560 x 5120 11.3, 10.9; 700 x 5000 x 256 7.4, 5.9; 3439 x 16472 x 512 80, 35.)
   const i64 ptiles = (i64)((x.rows + 255ll) / 256) * ((w.rows + PBN - 1ll) / PBN), pairs = sms / 2;
   const double each = 760.0 * p.kblocks + 1700.0;
-  const bool pair = pairs > 0 && 11400.0 + 570.0 * p.kblocks + (double)((ptiles + pairs - 1) / pairs - 1) * (each > 7000.0 ? each : 7000.0) < best;
+  // (rows on no 16-byte boundary that are shorter than a unit go out by elements: 16000 x 30 x 512 11.1, few rows 7.5)
+  const double ragged = w.rows < 64 && !p.vec_out ? 8000.0 : 0.0;
+  const bool pair = pairs > 0 && 10000.0 + ragged + 600.0 * p.kblocks + (double)((ptiles + pairs - 1) / pairs - 1) * (each > 5000.0 ? each : 5000.0) < best;
   if (pair) {
     if (ptiles > 0x3fffffff) return SSDI8_ERR_SHAPE;
     p.mtiles = (int)((x.rows + 255ll) / 256);
