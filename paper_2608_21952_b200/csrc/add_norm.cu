@@ -454,7 +454,7 @@ ssdi8_status_t launch(const RowParams& p, i64 rows, cudaStream_t st) {
   constexpr bool STREAM = !std::is_same<R, None>::value;
   constexpr i64 kShared = 200 * 1024;
   const i64 bytes = (i64)p.D * (sizeof(T) + (STREAM ? sizeof(typename std::conditional<STREAM, R, T>::type) : 0));
-  const i64 fit = kShared / (kRing * bytes), blocks = fit < 24 ? fit : 24;   // on an SM
+  const i64 fit = kShared / (kRing * bytes), blocks = fit < 32 ? fit : 32;   // on an SM
   const bool ring = (STREAM || sizeof(T) == 2) && p.vx && (!p.residual || p.vr) && (!p.stream || p.vs) && blocks > 0 && rows > 2 * sms * blocks;
   auto go = [&](auto n) -> ssdi8_status_t {
     constexpr int NCH = decltype(n)::value;
@@ -466,6 +466,10 @@ ssdi8_status_t launch(const RowParams& p, i64 rows, cudaStream_t st) {
     }
     return launch_configured(row_kernel<T, R, NCH, NORM, FP4>, dim3((unsigned)rows), dim3(32 * warps), 0, -1, false, st, p);
   };
+  // (short rows of a ring: without a second warp, or with half as many, a row's meeting is short.  16001 x 320 bf16 21 and 15, 16384 x 1024 to four bits 33 and
+  // 29, quantiser 16384 x 768 15 and 12; three chunks of a norm are better off apart: 16384 x 768 26, 28 with two warps, 32 with one)
+  if (ring && (chunks == 2 || (NORM && chunks == 4))) return go(std::integral_constant<int, 2>());
+  if (ring && !NORM && chunks > 2 && chunks <= 4) return go(std::integral_constant<int, 4>());
   if (chunks <= (rows <= 4 * sms ? 16 : 8)) return go(std::integral_constant<int, 1>());
   if (chunks <= 32 && (NORM || !ring)) return go(std::integral_constant<int, 2>());
   return go(std::integral_constant<int, 4>());

@@ -338,12 +338,27 @@ struct Epilogue {
         }
       }
     } else if (o0 < end) {
+      // the last rows and columns, by elements, sixteen rows at a time
+      constexpr int E = U / 32;
       const T* rat = static_cast<const T*>(p.residual) + t0 * p.res_stride + o0;
+      const int rows = p.T - t0;
 #pragma unroll 1
-      for (int r = 0; r < 32 && t0 + r < p.T; ++r, at += p.out_stride, rat += p.res_stride)
+      for (int r0 = 0; r0 < 32 && r0 < rows; r0 += 16) {
+        float x[16][E];
 #pragma unroll
-        for (int c = lane; c < U; c += 32)
-          if (o0 + c < end) at[c] = Elem<T>::put(p.residual ? column(r, c) + Elem<T>::get(rat[c]) : column(r, c));
+        for (int i = 0; i < 16; ++i, rat += p.res_stride)
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+            x[i][e] = p.residual && r0 + i < rows && o0 + lane + 32 * e < end ? Elem<T>::get(rat[lane + 32 * e]) : 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i, at += p.out_stride)
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+            if (r0 + i < rows && o0 + lane + 32 * e < end) {
+              const float y = column(r0 + i, lane + 32 * e);
+              at[lane + 32 * e] = Elem<T>::put(p.residual ? y + x[i][e] : y);
+            }
+      }
     }
     __syncwarp();
   }
@@ -813,8 +828,8 @@ ssdi8_status_t launch(const ssdi8_fp4_linear_args_t& a, cudaStream_t st) {
   // 256 x 4096 x 8192 12.7, 16.1; 512 x 2560 x 5120 11.3, 10.9; 700 x 5000 x 256 7.4, 5.9; 3439 x 16472 x 512 80, 35.)
   const i64 ptiles = (i64)((x.rows + 255ll) / 256) * ((w.rows + PBN - 1ll) / PBN), pairs = sms / 2;
   const double each = 760.0 * p.kblocks + 1700.0;
-  // (rows on no 16-byte boundary that are shorter than a unit go out by elements: 16000 x 30 x 512 11.1, few rows 7.5)
-  const double ragged = w.rows < 64 && !p.vec_out ? 8000.0 : 0.0;
+  // (where rows lie on no 16-byte boundary the last columns go out by elements: 134 x 115 x 256 11.3, few rows 5)
+  const double ragged = !p.vec_out && w.rows % 64 ? 6000.0 : 0.0;
   const bool pair = pairs > 0 && 10000.0 + ragged + 600.0 * p.kblocks + (double)((ptiles + pairs - 1) / pairs - 1) * (each > 5000.0 ? each : 5000.0) < best;
   if (pair) {
     if (ptiles > 0x3fffffff) return SSDI8_ERR_SHAPE;
