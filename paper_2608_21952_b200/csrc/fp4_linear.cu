@@ -587,10 +587,19 @@ __device__ __forceinline__ void few_out(const FewParams& f, const float* part, c
   for (int t0 = first; t0 < ntok; t0 += 4 * step, dst += 4 * dstep, res += 4 * rstep) {
     float4 acc[4];
     typename Elem<T>::raw4 q[4];
-    if (vector && p.residual) {
+    if (p.residual) {
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (t0 + u * step < ntok) q[u] = *reinterpret_cast<const typename Elem<T>::raw4*>(res + u * rstep);
+      for (int u = 0; u < 4; ++u) {
+        if (t0 + u * step >= ntok) break;
+        const T* const r = res + u * rstep;
+        if (vector) {
+          q[u] = *reinterpret_cast<const typename Elem<T>::raw4*>(r);
+        } else {
+          T* const e4 = reinterpret_cast<T*>(&q[u]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) e4[e] = e < no ? r[e] : Elem<T>::put(0.f);
+        }
+      }
     }
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
@@ -612,19 +621,14 @@ __device__ __forceinline__ void few_out(const FewParams& f, const float* part, c
       float2 y = __ffma2_rn(__fmul2_rn(make_float2(acc[u].z, acc[u].w), make_float2(sr, sr)), w1, b1);
       x = make_float2(activate(x.x, ACT), activate(x.y, ACT));
       y = make_float2(activate(y.x, ACT), activate(y.y, ACT));
+      if (p.residual) {
+        const float4 r = Elem<T>::cvt(q[u]);
+        x = __fadd2_rn(x, make_float2(r.x, r.y));
+        y = __fadd2_rn(y, make_float2(r.z, r.w));
+      }
       if (vector) {
-        if (p.residual) {
-          const float4 r = Elem<T>::cvt(q[u]);
-          x = __fadd2_rn(x, make_float2(r.x, r.y));
-          y = __fadd2_rn(y, make_float2(r.z, r.w));
-        }
         *reinterpret_cast<typename Elem<T>::raw4*>(dst + u * dstep) = Elem<T>::pack(make_float4(x.x, x.y, y.x, y.y));
       } else if (sizeof(T) == 2 && no == 4) {   // words where the row's boundary allows
-        if (p.residual) {
-          const T* const r = res + u * rstep;
-          x = __fadd2_rn(x, make_float2(Elem<T>::get(r[0]), Elem<T>::get(r[1])));
-          y = __fadd2_rn(y, make_float2(Elem<T>::get(r[2]), Elem<T>::get(r[3])));
-        }
         const typename Elem<T>::raw4 w4 = Elem<T>::pack(make_float4(x.x, x.y, y.x, y.y));
         const uint32_t* const w = reinterpret_cast<const uint32_t*>(&w4);
         uint16_t* const d = reinterpret_cast<uint16_t*>(dst + u * dstep);
@@ -640,7 +644,7 @@ __device__ __forceinline__ void few_out(const FewParams& f, const float* part, c
         const float v[4] = {x.x, x.y, y.x, y.y};
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (e < no) dst[u * dstep + e] = Elem<T>::put(p.residual ? v[e] + Elem<T>::get(res[u * rstep + e]) : v[e]);
+          if (e < no) dst[u * dstep + e] = Elem<T>::put(v[e]);
       }
     }
   }
