@@ -10,7 +10,7 @@
 // bytes, 52 of operations at that rate) takes 97 to 108 us on the device: the clock falls to 1.4 to 1.65 GHz under the power limit, at which a tile's 20 stages
 // take 13300 cycles where the pipe alone would take 11900 (89 %), and 0.9 us pass from one tile to the next: the accumulators share 48 columns.
 // 3439 x 16472 x 1248, fp16, residual (37 us of bytes) 76, 53 to 57 without the residual: five stages a tile, and operands and results
-// share the way between L2 and the SMs (459 MB, 8.7 TB/s; 36 us without the stores, whatever the epilogue does); 16470 columns, rows on words, 121; 16471, odd ones, 169.
+// share the way between L2 and the SMs (459 MB, 8.7 TB/s; 36 us without the stores, whatever the epilogue does); 16470 columns, rows on words, 97; 16471, odd ones, 146.
 // 64 x 10576 x 2560 (2.6 us of bytes) 6.9 us from L2 and 8.8 from DRAM, one row 5.7 and 6.7: launch and first operands 1.0, ten stages' MMAs and
 // scale copies of a lone CTA 2.5 (issued without checks; 3.5 with them), the accumulator's way out and the tokens 1.5.
 #include "fp4.cuh"
