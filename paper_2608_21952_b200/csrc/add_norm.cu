@@ -284,8 +284,8 @@ __global__ void __launch_bounds__(512) row_kernel(const __grid_constant__ RowPar
 }
 
 // Many rows: a block walks rows a grid apart through a ring in shared memory, the next row's x and residual on their way by bulk copies while one
-// is worked on.  The row's barrier (every thread has its elements in registers then) gives its place in the ring to the row after the next; where there is a residual stream, h takes the place of the residual (of x if there is none) and leaves from
-// there, and the next copy waits until it has been read.
+// is worked on.  The row's barrier (every thread has its elements in registers then) gives its place in the ring to the row after the next; where there is a
+// residual stream, h takes the place of the residual, leaves from there, and the next copy waits until it has been read.
 template <typename T, typename R, int NCH, bool NORM, bool FP4>
 __global__ void __launch_bounds__(512, 2) ring_kernel(const __grid_constant__ RowParams p, int rows) {
   using namespace sm100;
