@@ -9,9 +9,10 @@
  * Conventions for every entry point
  *  - All pointers are DEVICE pointers unless the comment says "host".  The
  *    caller owns every buffer and the library allocates no device memory.  It keeps
- *    no mutable state between calls, with four exceptions, each stated again at its
+ *    no mutable state between calls, with five exceptions, each stated again at its
  *    entry point: per device, the result of the architecture check and which kernels have had
- *    their launch attributes set (every call);
+ *    their launch attributes set (every call); the driver's function that encodes tensor maps,
+ *    looked up at the first call that needs it (every call that multiplies matrices);
  *    the address of the built-in scratch (ssdi8_chunk_scan_fwd_static); two copy
  *    streams and their events (ssdi8_layer_fwd_host, created at the first call on
  *    a device and kept for the life of the process).  All are
