@@ -566,7 +566,7 @@ __device__ __forceinline__ float4 ld_from(const float* p, int rank) {   // the s
   asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
   return v;
 }
-// (relaxed: nothing was written for the others; a release would wait for stores to out)
+// (relaxed: nothing was written for the others, and what was read of theirs has been used; a release would wait for stores to out)
 __device__ __forceinline__ void cluster_leave() {
   asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
   cluster_wait();
@@ -585,7 +585,7 @@ __device__ __forceinline__ void few_out(const FewParams& f, const float* part, c
   const float2 w0 = make_float2(sw[0], sw[1]), w1 = make_float2(sw[2], sw[3]), b0 = make_float2(bias[0], bias[1]), b1 = make_float2(bias[2], bias[3]);
 #pragma unroll 1
   for (int t0 = first; t0 < ntok; t0 += 4 * step, dst += 4 * dstep, res += 4 * rstep) {
-    float4 acc[4];
+    float4 acc[4] = {};
     typename Elem<T>::raw4 q[4];
     if (p.residual) {
 #pragma unroll
@@ -601,17 +601,28 @@ __device__ __forceinline__ void few_out(const FewParams& f, const float* part, c
         }
       }
     }
+    const auto parts = [&](auto all) {
+      // (of the others' none behind the last token: a read that nothing uses could still be on its way when the CTA that it goes to has left)
+      const auto read = [&](int u, int r) { return ld_from(part + (t0 + u * step) * 128 + 4 * lane, r); };
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const float* const at = part + min(t0 + u * step, ntok - 1) * 128 + 4 * lane;
-      acc[u] = f.split == 1 ? *reinterpret_cast<const float4*>(at) : ld_from(at, 0);
-    }
-    for (int r = 1; r < f.split; ++r) {
-      float4 v[4];
+      for (int u = 0; u < 4; ++u)
+        if (decltype(all)::value || t0 + u * step < ntok) acc[u] = read(u, 0);
+      for (int r = 1; r < f.split; ++r) {
+        float4 v[4] = {};
 #pragma unroll
-      for (int u = 0; u < 4; ++u) v[u] = ld_from(part + min(t0 + u * step, ntok - 1) * 128 + 4 * lane, r);
+        for (int u = 0; u < 4; ++u)
+          if (decltype(all)::value || t0 + u * step < ntok) v[u] = read(u, r);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) acc[u] = make_float4(acc[u].x + v[u].x, acc[u].y + v[u].y, acc[u].z + v[u].z, acc[u].w + v[u].w);
+        for (int u = 0; u < 4; ++u) acc[u] = make_float4(acc[u].x + v[u].x, acc[u].y + v[u].y, acc[u].z + v[u].z, acc[u].w + v[u].w);
+      }
+    };
+    if (f.split == 1) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) acc[u] = *reinterpret_cast<const float4*>(part + min(t0 + u * step, ntok - 1) * 128 + 4 * lane);
+    } else if (t0 + 3 * step < ntok) {
+      parts(std::true_type());
+    } else {
+      parts(std::false_type());
     }
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
