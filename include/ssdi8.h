@@ -531,10 +531,12 @@ ssdi8_status_t ssdi8_fp4_dequantize(const ssdi8_fp4_t* q, void* out, int64_t str
 /* The residual stream's addition and the RMS norm ahead of a block's projection, ending in the projection's operand:
  *   h = fadd(x, residual), rounded to the stream's type and written to residual_out (either may be NULL: h = x, nothing is written; with neither,
  *       h = x as it is);   p = fmul(h, w) (w = NULL: 1);   r = 1 / sqrt(mean over the row of h^2 + eps), in binary64
- *   int8 (xq):          a = fdiv(absmax of p, 127) (1 if that is 0), code = rne(fdiv(p, a)) saturated, scale = (float)(a r) (1 if a was 0)
+ *   int8 (xq):          a = fdiv(absmax of p, 127) (1 if that is 0), code = rne(fdiv(p, a)) saturated, scale = (float)(a r) (1 if that absmax / 127 was 0
+ *                       and r is a number)
  *   with static_scale:  code = rne(fdiv(fmul(p, (float)r), *static_scale)) saturated; scale is not written
- *   four bits (fp4):    codes and scales of p as ssdi8_fp4_quantize has them, step = (float)(its step x r) (1 for a row of zeros)
- * so the factor r, the same for a row, meets no code but the static ones.  A NaN has the code +127 (+6) and makes r one, and with it scale or step.
+ *   four bits (fp4):    codes and scales of p as ssdi8_fp4_quantize has them, step = (float)(its step x r) (1 for a row whose absmax is 0 and r a number)
+ * so the factor r, the same for a row, meets no code but the static ones.  A NaN has the code +127 (+6), counts for nothing in an absmax, and one in h makes r one, and
+ * with it scale or step, in a row without any number too.
  * x has type dtype; residual and residual_out rdtype: x's or fp32 (0); any strides of rows, an element's alignment.  residual_out may be residual, or x
  * where their types are the same.  Exactly one of xq and fp4 is given; width <= 16384, and width % 16 = 0 (xq) or fp4's own (% 32).  weight and
  * xq 16-byte aligned.  rows may be 0.  (The gated norm behind the scan is ssdi8_norm_quantize; a residual that the projection before has added

@@ -195,11 +195,16 @@ __device__ __forceinline__ void finish_row(const RowParams& p, Meeting& meet, in
     for (int i = 0; i < nwarps; ++i) s += meet.sums[turn][i];
     return 1.0 / sqrt(s / (double)p.D + (double)p.eps);
   };
+  // the step size of a row whose codes have step a: 1 where they are all 0, but for a row with a NaN in it
+  auto step_of = [&](bool some, float a) {
+    const double r = factor();
+    return some || r != r ? (float)((double)a * r) : 1.0f;
+  };
   if constexpr (FP4) {
     Fp4Row r = {1.0f, 6.0f, 0.f, true};
     if (p.block == 16) r = fp4_row(top);
     if (p.step && threadIdx.x == 0) {
-      if constexpr (NORM) p.step[row] = top > 0.f ? (float)((double)r.g * factor()) : 1.0f;
+      if constexpr (NORM) p.step[row] = step_of(top > 0.f, r.g);
       else p.step[row] = r.g;
     }
     if (p.block == 32) {
@@ -234,7 +239,7 @@ __device__ __forceinline__ void finish_row(const RowParams& p, Meeting& meet, in
       if (!(top >= 1e-25f && top <= 1e25f)) a = __fdiv_rn(top, 127.0f);
       const bool some = a > 0.f;
       a = some ? a : 1.0f;
-      if (p.scale && threadIdx.x == 0) p.scale[row] = some ? (float)((double)a * factor()) : 1.0f;
+      if (p.scale && threadIdx.x == 0) p.scale[row] = step_of(some, a);
     }
     const float4 a4 = make_float4(a, a, a, a);
     const Step4 st = step4(a4);

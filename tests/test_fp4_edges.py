@@ -29,3 +29,35 @@ def test_parts_of_few_tokens_in_a_row():
     torch.cuda.synchronize()
     for (x, w, out), y in zip(ops, want):
         assert torch.equal(out, y)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("form", ["int8", "fp4 16", "fp4 32"])
+@pytest.mark.parametrize("rdtype", [None, "float32"])
+@pytest.mark.parametrize("T,D", [(5, 96), (7300, 768), (9, 4128)])
+def test_norm_of_rows_with_nothing_beside_nan(T, D, rdtype, form):
+    """rows of NaN alone, and of NaN and zeros: no absmax, but r is a NaN, and so is the row's step size; rows of zeros keep 1"""
+    import torch
+    from paper_2608_21952_b200 import binding as bd
+    x = torch.randn(T, D, device="cuda").bfloat16()
+    x[0] = float("nan")
+    x[1], x[1, D - 1] = 0, float("nan")
+    x[2] = 0
+    x[T - 1], x[T - 1, :32] = 0, float("nan")
+    kw = {}
+    if rdtype:
+        res = torch.where(x.float() == 0, 0.0, torch.randn(T, D, device="cuda"))
+        kw = dict(residual=res, residual_out=torch.empty_like(res))
+    if form == "int8":
+        xq, scale = torch.empty(T, D, dtype=torch.int8, device="cuda"), torch.empty(T, device="cuda")
+        bd.ssdi8_add_norm_quantize(x, xq=xq, scale=scale, **kw)
+        codes, most = xq, 127
+    else:
+        q = bd.make_fp4(T, D, int(form[4:]))
+        bd.ssdi8_add_norm_quantize(x, fp4=q, **kw)
+        b = q.tensors["codes"]
+        codes, most, scale = torch.stack([b & 15, b >> 4], -1).view(T, D), 7, q.tensors["step"]
+    bad = torch.tensor([0, 1, T - 1], device="cuda")
+    assert torch.isnan(scale[bad]).all() and int(torch.isnan(scale).sum()) == 3 and float(scale[2]) == 1.0
+    assert torch.equal(codes[bad] == most, torch.isnan(x[bad])) and (codes[bad].int().abs().amax(1) == most).all() and not codes[2].any()
+    assert not codes[1, :D - 1].any()
