@@ -536,7 +536,8 @@ ssdi8_status_t ssdi8_fp4_dequantize(const ssdi8_fp4_t* q, void* out, int64_t str
  *   with static_scale:  code = rne(fdiv(fmul(p, (float)r), *static_scale)) saturated; scale is not written
  *   four bits (fp4):    codes and scales of p as ssdi8_fp4_quantize has them, step = (float)(its step x r) (1 for a row whose absmax is 0 and r a number)
  * so the factor r, the same for a row, meets no code but the static ones.  A NaN has the code +127 (+6), counts for nothing in an absmax, and one in h makes r one, and
- * with it scale or step, in a row without any number too.
+ * with it scale or step, in a row without any number too.  A row whose mean of h^2 and eps are both 0 has r = 0: without eps, too, its codes are 0 (under weights that
+ * are finite).
  * x has type dtype; residual and residual_out rdtype: x's or fp32 (0); any strides of rows, an element's alignment.  residual_out may be residual, or x
  * where their types are the same.  Exactly one of xq and fp4 is given; width <= 16384, and width % 16 = 0 (xq) or fp4's own (% 32).  weight and
  * xq 16-byte aligned.  rows may be 0.  (The gated norm behind the scan is ssdi8_norm_quantize; a residual that the projection before has added

@@ -189,11 +189,12 @@ __device__ __forceinline__ void finish_row(const RowParams& p, Meeting& meet, in
   if (NORM || RING || p.block == 16) __syncthreads();
   behind();
   if (NORM || p.block == 16) top = warp_max(lane < nwarps ? meet.maxima[turn][lane] : 0.f);
-  // 1 / sqrt(mean + eps), by the threads that need it
+  // 1 / sqrt(mean + eps), by the threads that need it; 0 for a row of zeros without an eps, whose codes are 0 under a static step too
   auto factor = [&] {
     double s = 0.0;
     for (int i = 0; i < nwarps; ++i) s += meet.sums[turn][i];
-    return 1.0 / sqrt(s / (double)p.D + (double)p.eps);
+    s = s / (double)p.D + (double)p.eps;
+    return s == 0.0 ? 0.0 : 1.0 / sqrt(s);
   };
   // the step size of a row whose codes have step a: 1 where they are all 0, but for a row with a NaN in it
   auto step_of = [&](bool some, float a) {

@@ -61,3 +61,29 @@ def test_norm_of_rows_with_nothing_beside_nan(T, D, rdtype, form):
     assert torch.isnan(scale[bad]).all() and int(torch.isnan(scale).sum()) == 3 and float(scale[2]) == 1.0
     assert torch.equal(codes[bad] == most, torch.isnan(x[bad])) and (codes[bad].int().abs().amax(1) == most).all() and not codes[2].any()
     assert not codes[1, :D - 1].any()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("form", ["static", "int8", "fp4 16", "fp4 32"])
+@pytest.mark.parametrize("T,D", [(5, 96), (7300, 768)])
+def test_norm_of_zeros_without_eps(T, D, form):
+    """a row of zeros, and one whose sum with the residual is, has the codes 0 without an eps too; rows beside it are as ever"""
+    import torch
+    from paper_2608_21952_b200 import binding as bd
+    x = torch.randn(T, D, device="cuda").bfloat16()
+    res = torch.randn(T, D, device="cuda").bfloat16()
+    x[0], res[0] = 0, -0.0
+    x[T - 1] = -res[T - 1]
+
+    def run(eps):
+        if form[:3] == "fp4":
+            q = bd.make_fp4(T, D, int(form[4:]))
+            bd.ssdi8_add_norm_quantize(x, residual=res, eps=eps, fp4=q)
+            return q.tensors["codes"], q.tensors["step"]
+        xq, scale = torch.empty(T, D, dtype=torch.int8, device="cuda"), torch.ones(T, device="cuda")
+        bd.ssdi8_add_norm_quantize(x, residual=res, eps=eps, xq=xq, scale=scale, static_scale=torch.full((1,), 0.05, device="cuda") if form == "static" else None)
+        return xq, scale
+
+    (codes, step), (near, _) = run(0.0), run(1e-30)
+    assert not codes[0].any() and not codes[T - 1].any() and float(step[0]) == float(step[T - 1]) == 1.0
+    assert torch.equal(codes, near)   # (an eps that no other row's mean of squares sees)
