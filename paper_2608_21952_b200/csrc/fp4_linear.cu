@@ -851,13 +851,15 @@ ssdi8_status_t launch(const ssdi8_fp4_linear_args_t& a, cudaStream_t st) {
     p.mtiles = (int)((x.rows + 255ll) / 256);
     p.ntiles = (int)((w.rows + PBN - 1ll) / PBN);
     if (!codes(&tx, x, 128) || !codes(&tw, w, 128)) return SSDI8_ERR_CUDA;
-    CUtensorMap tout = tx;   // (where out's rows are not on 16 bytes it is not used)
+    // (a map's rows lie behind one another: a residual whose rows overlap, one row for all among them, is read by the lanes, and a lone row of
+    // out, which may have any stride, written by them.  Where rows are not on 16 bytes the maps are not used)
+    CUtensorMap tout = tx;
     const uint64_t dims[2] = {(uint64_t)p.O, (uint64_t)p.T}, stride[1] = {(uint64_t)(a.stride_out * e)};
     const uint32_t box[2] = {(uint32_t)(128 / e), 32};
-    if (p.vec_out && !encode_tensor_map(&tout, a.out, (int)e, 2, dims, stride, box, 128)) p.vec_out = 0;
+    if (p.vec_out && (a.stride_out < w.rows || !encode_tensor_map(&tout, a.out, (int)e, 2, dims, stride, box, 128))) p.vec_out = 0;
     CUtensorMap tres = tx;
     const uint64_t rstride[1] = {(uint64_t)(a.stride_residual * e)};
-    if (a.residual && p.vec_res && !encode_tensor_map(&tres, a.residual, (int)e, 2, dims, rstride, box, 128)) p.vec_res = 0;
+    if (a.residual && p.vec_res && (a.stride_residual < w.rows || !encode_tensor_map(&tres, a.residual, (int)e, 2, dims, rstride, box, 128))) p.vec_res = 0;
     auto go = [&](auto rows) {
       return launch_any(fp4_pair_kernel<T, BLOCK, decltype(rows)::value>, dim3((unsigned)(2 * (ptiles < pairs ? ptiles : pairs))), 2, dim3(PT), PairLayout::kAlloc,
                         PairLayout::kAlloc, -1, true, st, tx, tw, tsx, tsw, tout, tres, p);

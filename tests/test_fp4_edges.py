@@ -87,3 +87,19 @@ def test_norm_of_zeros_without_eps(T, D, form):
     (codes, step), (near, _) = run(0.0), run(1e-30)
     assert not codes[0].any() and not codes[T - 1].any() and float(step[0]) == float(step[T - 1]) == 1.0
     assert torch.equal(codes, near)   # (an eps that no other row's mean of squares sees)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("T,O,stride", [(2304, 2560, 0), (2304, 2560, 64), (2304, 2561, 0), (64, 2560, 0), (64, 2560, 8)])
+def test_linear_residual_of_rows_that_overlap(T, O, stride, dtype):
+    """any stride of the residual's rows: one row for all of them, and rows that begin inside the one before"""
+    import torch
+    from paper_2608_21952_b200 import binding as bd
+    x, w = _matrix(T, 256, 16, 1)[0], _matrix(O, 256, 16, 2)[0]
+    flat = torch.randn(T * stride + O, device="cuda").to(getattr(torch, dtype))
+    res = flat.as_strided((T, O), (stride, 1))
+    out, want = (torch.empty(T, O, dtype=flat.dtype, device="cuda") for _ in range(2))
+    bd.ssdi8_fp4_linear(x, w, out, residual=res)
+    bd.ssdi8_fp4_linear(x, w, want, residual=res.contiguous())
+    assert torch.equal(out, want)
