@@ -501,7 +501,8 @@ ssdi8_status_t ssdi8_linear(const ssdi8_linear_args_t* args, int32_t dtype, void
  *
  * A matrix in four bits: the value of column k of row t is  c scale[t][k / block] step[t]  with a code c of +-{0, 0.5, 1, 1.5, 2, 3, 4, 6} (e2m1:
  * sign, two bits of exponent, one of fraction), two to a byte, the even column's in the low half.  block 16: scales in e4m3 (up to 448); block 32: powers
- * of two (e8m0, 2^(byte - 127)).  Scales stand in tiles of 128 rows and 4 blocks, 512 bytes each, the tiles of a row block beside one another: the
+ * of two (e8m0, 2^(byte - 127)).  A scale in e4m3 has no sign (its highest bit is 0); one that is a NaN (127 in e4m3, 255 in e8m0) makes its block's values NaN.
+ * Scales stand in tiles of 128 rows and 4 blocks, 512 bytes each, the tiles of a row block beside one another: the
  * byte of row t and block b is at ((t / 128) ceil(width / block / 4) + b / 4) 512 + (t % 32) 16 + (t % 128 / 32) 4 + b % 4.  Tiles are
  * whole: ssdi8_fp4_scales_bytes of them, more if the array was made for more rows.  Bytes of blocks behind a row's last one are 0 (the quantisers write
  * them so; any number would do that is not the NaN of its type); those of rows behind the last are left alone.

@@ -54,8 +54,13 @@ __device__ __forceinline__ float e4m3_to(uint32_t b) {
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)b));
   return __half2float(__ushort_as_half((unsigned short)(h & 0xffffu)));
 }
-__device__ __forceinline__ float e8m0_to(uint32_t b) {   // 2^(b - 127)
+__device__ __forceinline__ float power_of_two(uint32_t b) {   // 2^(b - 127), b < 255
   return __uint_as_float(b == 0u ? 0x00400000u : b << 23);
+}
+__device__ __forceinline__ float e8m0_to(uint32_t b) {   // the same, of 255 a NaN
+  uint32_t h;
+  asm("cvt.rn.bf16x2.ue8m0x2 %0, %1;" : "=r"(h) : "h"((uint16_t)b));
+  return __uint_as_float(h << 16);
 }
 
 // Blocks of 16 of a row with absmax m: the row's step size g is fdiv(m, 2688) (the largest code times the largest scale) with the low eight bits of its
@@ -121,7 +126,7 @@ __device__ __forceinline__ uint32_t fp4_codes16(const float (&p)[8], const Fp4Ro
   return e2m1_of8(q);
 }
 __device__ __forceinline__ uint32_t fp4_codes32(const float (&p)[8], uint32_t b) {
-  const float y = e8m0_to(254u - b);
+  const float y = power_of_two(254u - b);
   const float2 yy = make_float2(y, y), zero = make_float2(0.f, 0.f);
   float q[8];
 #pragma unroll

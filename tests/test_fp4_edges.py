@@ -103,3 +103,42 @@ def test_linear_residual_of_rows_that_overlap(T, O, stride, dtype):
     bd.ssdi8_fp4_linear(x, w, out, residual=res)
     bd.ssdi8_fp4_linear(x, w, want, residual=res.contiguous())
     assert torch.equal(out, want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("block,nan", [(16, 127), (32, 255)])
+def test_scales_that_are_nan(block, nan):
+    """the NaN of a scale's type makes its block's values NaN, and the products that they are in, those of others not"""
+    import torch
+    from paper_2608_21952_b200 import binding as bd
+    T, O, D = 5, 40, 128
+    q = _matrix(T, D, block, 3)[0]
+    w = _matrix(O, D, block, 4)[0]
+    q.tensors["scales"][0, 0, 2, 0, 1] = nan   # row 2, block 1
+    bad = torch.zeros(T, D, dtype=torch.bool, device="cuda")
+    bad[2, block:2 * block] = True
+    for dtype in (torch.float32, torch.bfloat16):
+        out = torch.zeros(T, D, dtype=dtype, device="cuda")
+        bd.ssdi8_fp4_dequantize(q, out)
+        assert torch.equal(torch.isnan(out), bad) and torch.isfinite(out[~bad]).all()
+    y = torch.zeros(T, O, device="cuda")
+    bd.ssdi8_fp4_linear(q, w, y)
+    assert torch.equal(torch.isnan(y), bad.any(1)[:, None].expand(T, O)) and torch.isfinite(y[~bad.any(1)]).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("block", [16, 32])
+def test_every_scale(block):
+    """values of every code under every scale that is a number"""
+    import numpy as np
+    import torch
+    import fp4_reference as ref
+    from paper_2608_21952_b200 import binding as bd
+    T = 127 if block == 16 else 255
+    codes = np.tile(np.arange(32, dtype=np.uint8) % 16, (T, 1))
+    scales = np.repeat(np.arange(T, dtype=np.uint8)[:, None], 32 // block, 1)
+    q = bd.fp4_of(torch.from_numpy(ref.pack(codes)).cuda(), torch.from_numpy(ref.tile(scales)).cuda(), None, block)
+    out = torch.empty(T, 32, device="cuda")
+    bd.ssdi8_fp4_dequantize(q, out)
+    with np.errstate(over="ignore"):
+        np.testing.assert_array_equal(out.cpu().numpy(), ref.values(codes, scales, block).astype(np.float32))
