@@ -522,8 +522,11 @@ size_t ssdi8_fp4_scales_bytes(int32_t rows, int32_t width, int32_t block);
  *   block 32: scale = the least power of two s from 2^-127 to 2^127 with absmax of the block <= 6 s (1 if that absmax is 0),
  *             code = e2m1 of p / scale, step = 1 (if given)
  * Quotients are exact ones (g has 16 bits so that their middles are binary32 numbers; for rows whose absmax lies below 2e-32, where these are
- * subnormal, g scale and the quotient are each rounded to binary32).  Beyond 6 a code is 6; a 0 of either sign has the code 0.  A NaN counts for nothing in an
- * absmax and has the code +6; in a row (block 16) or block (32) with an infinity other codes are 0.  q.step is needed with block 16.
+ * subnormal, g scale and the quotient are each rounded to binary32).  Beyond 6 a code is 6; a 0 of either sign has the code 0, a negative number that
+ * rounds to 0 the code 8 (-0).  A NaN counts for nothing in an absmax and has the code +6.  Infinities: in blocks of 16 the row's step size is
+ * infinite, its scales are 2^-9, an infinity of either sign has the code +6 (a quotient of two infinities is a NaN) and a number 0, so that the
+ * row's values are +infinity and NaN; in blocks of 32 the block's scale is 2^126, an infinity has the code 6 with its sign, whose value is that
+ * infinity, and a number the code of p / 2^126, 0 up to 2^124.  q.step is needed with block 16.
  * status: 1 word, or NULL: SSDI8_ERR_DEVICE_TIMEOUT if a wait ran out. */
 ssdi8_status_t ssdi8_fp4_quantize(const void* x, int64_t stride_x, int32_t dtype, const ssdi8_fp4_t* q, int32_t* status, void* stream);
 /* The values of a matrix in four bits: out[t,k] = fmul(c scale, step), rounded once more to out's type (any stride of rows, at least width). */
@@ -536,9 +539,10 @@ ssdi8_status_t ssdi8_fp4_dequantize(const ssdi8_fp4_t* q, void* out, int64_t str
  *                       and r is a number)
  *   with static_scale:  code = rne(fdiv(fmul(p, (float)r), *static_scale)) saturated; scale is not written
  *   four bits (fp4):    codes and scales of p as ssdi8_fp4_quantize has them, step = (float)(its step x r) (1 for a row whose absmax is 0 and r a number)
- * so the factor r, the same for a row, meets no code but the static ones.  A NaN has the code +127 (+6), counts for nothing in an absmax, and one in h makes r one, and
- * with it scale or step, in a row without any number too.  A row whose mean of h^2 and eps are both 0 has r = 0: without eps, too, its codes are 0 (under weights that
- * are finite).
+ * so the factor r, the same for a row, meets no code but the static ones.  A NaN has the code +127 (+6) and counts for nothing in an absmax; one in h
+ * makes r one, and with it scale or step, in a row without any number too.  An infinity in h makes r 0, and with it scale or step a NaN (blocks of
+ * 32: 0, under which the infinity's value is a NaN and those of numbers that have the code 0 are 0).  A row whose mean of h^2 and eps are both 0
+ * has r = 0: without eps, too, its codes are 0 (under weights that are finite).
  * x has type dtype; residual and residual_out rdtype: x's or fp32 (0); any strides of rows, an element's alignment.  residual_out may be residual, or x
  * where their types are the same.  Exactly one of xq and fp4 is given; width <= 16384, and width % 16 = 0 (xq) or fp4's own (% 32).  weight and
  * xq 16-byte aligned.  rows may be 0.  (The gated norm behind the scan is ssdi8_norm_quantize; a residual that the projection before has added

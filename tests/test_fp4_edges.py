@@ -142,3 +142,73 @@ def test_every_scale(block):
     bd.ssdi8_fp4_dequantize(q, out)
     with np.errstate(over="ignore"):
         np.testing.assert_array_equal(out.cpu().numpy(), ref.values(codes, scales, block).astype(np.float32))
+
+
+INFINITE = [float("inf"), 3e38, -1e38, 2.0 ** 125, 2.0 ** 124, -2.0 ** 124 * 1.01, 1.0, -float("inf"), 0.0, -0.0]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("block", [16, 32])
+@pytest.mark.parametrize("D", [64, 16416])
+def test_infinities_beside_the_largest_numbers(block, D):
+    """as the header has it.  Blocks of 16: every infinity +6, every number 0, the row's step size infinite.  Blocks of 32: the scale 2^126, an infinity
+    6 with its sign, a number what 2^126 leaves of it; other blocks as ever"""
+    import numpy as np
+    import torch
+    import fp4_reference as ref
+    from paper_2608_21952_b200 import binding as bd
+    x = torch.zeros(3, D, device="cuda")
+    x[:, 32:] = torch.randn(3, D - 32, device="cuda")
+    n = len(INFINITE)
+    x[1, :n] = torch.tensor(INFINITE, device="cuda")
+    x[2, :n] = -torch.tensor(INFINITE, device="cuda")
+    q, out = bd.make_fp4(3, D, block), torch.empty(3, D, device="cuda")
+    bd.ssdi8_fp4_quantize(x, q)
+    bd.ssdi8_fp4_dequantize(q, out)
+    codes = ref.unpack(q.tensors["codes"].cpu().numpy())
+    scales = ref.untile(q.tensors["scales"].cpu().numpy(), 3, D // block)
+    step = q.tensors["step"].cpu().numpy()
+    got = out.cpu().numpy()
+    c, s, g = ref.quantize(x.cpu().numpy(), block)
+    np.testing.assert_array_equal(codes, c)
+    np.testing.assert_array_equal(scales, s)
+    np.testing.assert_array_equal(step, g)
+    if block == 16:
+        for t in (1, 2):
+            inf = np.isinf(x[t].cpu().numpy())
+            assert (codes[t][inf] == 7).all() and not codes[t][~inf].any() and (scales[t] == 1).all() and np.isinf(step[t])
+            assert (got[t][inf] == np.inf).all() and np.isnan(got[t][~inf]).all()
+    else:
+        assert codes[1, :n].tolist() == [7, 6, 10, 1, 0, 9, 0, 15, 0, 0] and codes[2, :n].tolist() == [15, 14, 2, 9, 8, 1, 8, 7, 0, 0]
+        assert (scales[1:, 0] == 253).all() and (step == 1).all()
+        v = np.array([np.inf, np.inf, -2.0 ** 126, 2.0 ** 125, 0, -2.0 ** 125, 0, -np.inf, 0, 0], np.float32)   # (4 x 2^126 is beyond binary32)
+        np.testing.assert_array_equal(got[1, :n], v)
+        np.testing.assert_array_equal(got[2, :n], -v)
+        assert np.isfinite(got[:, 32:]).all()
+    assert np.isfinite(got[0]).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("form", ["int8", "fp4 16", "fp4 32"])
+def test_norm_of_rows_with_infinities(form):
+    """an infinity in h: r is 0, and the row's values are NaN, or 0 where a step size of 0 meets a number"""
+    import torch
+    from paper_2608_21952_b200 import binding as bd
+    T, D = 4, 128
+    x = torch.randn(T, D, device="cuda")
+    x[1, 3] = float("inf")
+    x[2, 5], x[2, 70] = -float("inf"), float("inf")
+    if form == "int8":
+        xq, scale = torch.empty(T, D, dtype=torch.int8, device="cuda"), torch.empty(T, device="cuda")
+        bd.ssdi8_add_norm_quantize(x, xq=xq, scale=scale)
+        inf = torch.isinf(x[1:3])
+        assert (xq[1:3][inf] == 127).all() and not xq[1:3][~inf].any()
+        assert torch.isnan(scale[1:3]).all() and torch.isfinite(scale[[0, 3]]).all()
+        return
+    q, out = bd.make_fp4(T, D, int(form[4:])), torch.empty(T, D, device="cuda")
+    bd.ssdi8_add_norm_quantize(x, fp4=q)
+    bd.ssdi8_fp4_dequantize(q, out)
+    assert torch.isfinite(out[[0, 3]]).all() and torch.isnan(out[1:3][torch.isinf(x[1:3])]).all()
+    step = q.tensors["step"][1:3]
+    assert torch.isnan(step).all() if form == "fp4 16" else not step.any()
+    assert torch.isnan(out[1:3]).all() if form == "fp4 16" else not out[1:3][~torch.isinf(x[1:3])].any()
