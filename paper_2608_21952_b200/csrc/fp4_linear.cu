@@ -14,6 +14,7 @@
 // 64 x 10576 x 2560 (2.6 us of bytes) 6.9 us from L2 and 8.8 from DRAM, one row 5.7 and 6.7: launch and first operands 1.0, ten stages' MMAs and
 // scale copies of a lone CTA 2.5 (issued without checks; 3.5 with them), the accumulator's way out and the tokens 1.5.
 #include "fp4.cuh"
+#include "fp4_form.h"
 #include "kernels.h"
 #include "linear.cuh"
 
@@ -545,14 +546,11 @@ __global__ void __launch_bounds__(PT, 1) fp4_pair_kernel(const __grid_constant__
 // The weight's rows are the accumulator's 128 lanes and up to 256 tokens its columns, a tile to a CTA, and K is shared out among the CTAs of a cluster
 // until the SMs are all at it.  The parts of a tile meet in shared memory, added in the order of their CTAs, each CTA finishing some tokens.
 constexpr int FT = 256;
-struct FewLayout {
-  static constexpr int kMaxStages = 10;
-  static constexpr uint32_t kW = 128 * ROW;
-  // the ring, two CTAs on an SM or one; the accumulator's image of [n][128] goes over it
-  static constexpr uint32_t kSmall = 101376, kLarge = 221184;
+struct FewLayout : Fp4Few {
   static constexpr uint32_t kRows = 256, kTail = kRows + 256 * 4 + 1024;   // barriers, step sizes of rows; the tiles start on 1024 bytes
 };
 static_assert(2 * (FewLayout::kSmall + FewLayout::kTail + 1024) <= 233472 && FewLayout::kLarge + FewLayout::kTail <= 232448, "");
+static_assert(FewLayout::kRow == ROW && FewLayout::scales(16) == Scales<16>::kBytes && FewLayout::scales(32) == Scales<32>::kBytes, "");
 struct FewParams {
   Fp4Params l;
   int n, bgroups, split, stages;   // columns of the accumulator (tokens, to 16), their 128s, CTAs of a cluster
@@ -696,7 +694,7 @@ __global__ void __launch_bounds__(FT, 2) fp4_few_kernel(const __grid_constant__ 
   const int o0 = m * 128, tok0 = n * f.n, ntok = min(f.n, p.T - tok0);
   const int kb0 = (int)((i64)p.kblocks * rank / f.split), kb1 = (int)((i64)p.kblocks * (rank + 1) / f.split);
   // (n % 16 = 0: codes and scales start on 1024 bytes)
-  const uint32_t scales = S::kW + f.n * ROW, stage = (scales + (1 + f.bgroups) * kSc + 1023) & ~1023u;
+  const uint32_t scales = S::kW + f.n * ROW, stage = (scales + (1 + f.bgroups) * kSc + 1023) & ~1023u;   // (as S::stage has it on the host)
   if (warp == 0) {
     int s = 0, round = 0;
     for (int kb = kb0; kb < kb1; ++kb) {
@@ -809,44 +807,9 @@ ssdi8_status_t launch(const ssdi8_fp4_linear_args_t& a, cudaStream_t st) {
     return encode_tensor_map(tm, q.scales, 4, 2, dims, stride, box, 0);
   };
   if (!scales(&tsx, x) || !scales(&tsw, w)) return SSDI8_ERR_CUDA;
-  // What is done sooner, in cycles (the figures are measured ones).  Few rows: 5000 for the call, and for each wave 2200 to the first operands, 46 bytes of
-  // operands a cycle and SM, or where the ring does not hold all of a CTA's stages their latency of 1400 over those that it holds; the
-  // accumulator's way out, the parts' meeting, the tokens.  A wave behind another takes 12000 at least.
-  const i64 mt = (w.rows + 127ll) / 128;
-  FewParams f = {};
-  double best = 0.0;
-  for (int n = x.rows <= 256 ? (x.rows + 15) / 16 * 16 : 128; n <= 256; n += x.rows <= 256 ? 256 : 128) {
-    const i64 tiles = mt * ((x.rows + n - 1ll) / n);
-    const uint32_t bytes = (FewLayout::kW + n * ROW + (n <= 128 ? 2 : 3) * Scales<BLOCK>::kBytes + 1023) & ~1023u;
-    for (int per_sm = n <= 128 ? 2 : 1; per_sm >= 1; --per_sm) {
-      const int ring = (int)(per_sm == 2 ? FewLayout::kSmall : FewLayout::kLarge), stages = ring / (int)bytes < FewLayout::kMaxStages ? ring / (int)bytes : FewLayout::kMaxStages;
-      // (clusters of four take 7 of 8 SMs at best, 16 of a GPC's 18; of eight fewer: 64 x 2560 x 5120 8 us with four, 19 to 22 with eight)
-      for (int split = 1; split <= 4 && split <= p.kblocks; split *= 2) {
-        const i64 places = (i64)(split == 4 ? sms - sms / 8 : sms) * per_sm;
-        const double ctas = (double)tiles * split, waves = (double)((tiles * split + places - 1) / places), share = ctas <= sms ? 1.0 : (double)per_sm;
-        const int kb = (p.kblocks + split - 1) / split;
-        const double port = kb * (double)bytes * share / 46.0, latency = kb > stages ? (kb - stages) * 1400.0 / stages : 0.0;
-        const double wave = 2200.0 + (port > latency ? port : latency) + n * 8.0 + n / split * 20.0 + (split > 1 ? 1300.0 + n * 25.0 : 0.0);
-        const double cycles = 5000.0 + (waves == 1.0 ? wave : waves * (wave > 12000.0 ? wave : 12000.0));
-        if (best == 0.0 || cycles < best) {
-          best = cycles;
-          f.n = n;
-          f.split = split;
-          f.ring = ring;
-          f.stages = stages;
-        }
-      }
-    }
-  }
-  // Pairs: 10000 for the call, the first operands and the last tile's way out, 600 for 256 of K where no epilogue is beside them and 760 where one is, 1700
-  // from one tile to the next, 5000 at least.  (us, few rows and pairs: 64 x 10576 x 2560 6.9, 9.7; 64 x 10576 x 768 4.7, 6.4; 250 x 2000 x 1024 9.2, 6.1;
-  // 256 x 4096 x 8192 12.7, 16.1; 512 x 2560 x 5120 11.3, 10.9; 700 x 5000 x 256 7.4, 5.9; 3439 x 16472 x 512 80, 35.)
-  const i64 ptiles = (i64)((x.rows + 255ll) / 256) * ((w.rows + PBN - 1ll) / PBN), pairs = sms / 2;
-  const double each = 760.0 * p.kblocks + 1700.0;
-  // (where rows lie on no 16-byte boundary the last columns go out by elements: 134 x 115 x 256 11.3, few rows 5)
-  const double ragged = !p.vec_out && w.rows % 64 ? 6000.0 : 0.0;
-  const bool pair = pairs > 0 && 10000.0 + ragged + 600.0 * p.kblocks + (double)((ptiles + pairs - 1) / pairs - 1) * (each > 5000.0 ? each : 5000.0) < best;
-  if (pair) {
+  const Fp4Form form = fp4_form(x.rows, w.rows, x.width, BLOCK, p.vec_out, sms);
+  const i64 mt = (w.rows + 127ll) / 128, ptiles = (i64)((x.rows + 255ll) / 256) * ((w.rows + PBN - 1ll) / PBN), pairs = sms / 2;
+  if (form.pair) {
     if (ptiles > 0x3fffffff) return SSDI8_ERR_SHAPE;
     p.mtiles = (int)((x.rows + 255ll) / 256);
     p.ntiles = (int)((w.rows + PBN - 1ll) / PBN);
@@ -869,6 +832,11 @@ ssdi8_status_t launch(const ssdi8_fp4_linear_args_t& a, cudaStream_t st) {
     if (sizeof(T) == 4 || (words(a.out, a.stride_out) && (!a.residual || words(a.residual, a.stride_residual)))) return go(std::integral_constant<int, ROWS_WORDS>());
     if constexpr (sizeof(T) == 2) return go(std::integral_constant<int, ROWS_ODD>());
   }
+  FewParams f = {};
+  f.n = form.n;
+  f.split = form.split;
+  f.ring = form.ring;
+  f.stages = form.stages;
   f.l = p;
   f.l.mtiles = (int)mt;
   f.l.ntiles = (int)((x.rows + f.n - 1ll) / f.n);
