@@ -7,11 +7,13 @@
 // are functions of p alone.  In binary64 the sum cannot leave its range (a conversion and a fused multiply-add an element, on pipes that nothing else
 // uses: 64 cycles for a warp's 256 columns).
 //
-// What bounds it (device times).  With an fp32 stream the bytes: 16384 x 2560 bf16 to int8 (461 MB, 70 us) 80 us, to four bits 75, 4096 x 8192 (56)
-// 61.  With less to move instructions, most of them on the half-rate integer pipe (unpacking, maxima, addresses; 55 % busy): bf16 stream (45) 56, without one (19)
-// 41; the quantiser 137 a warp and 256 columns, 16384 x 5120 bf16 (33) 60, 53 in blocks of 32, 10576 x 2560 fp32 (19) 19 to 21.  Divisions in
-// place of corrected products took 204 and 86.  Values: 16384 x 5120 to bf16 (33) 39, 60 with a division to find a thread's row.  2560 rows of
-// 16384 (67) 109: one block of 96 KB a row to an SM.  One row of 768: 2.0, of which the call itself takes 3.7 from Python.
+// What bounds it (device times; in brackets the bytes).  With an fp32 stream the bytes: 16384 x 2560 bf16 to int8 (461 MB, 70 us) 80 us, to four bits (67) 76,
+// 4096 x 8192 (56) 61.  With less to move instructions, most of them on the half-rate integer pipe (unpacking, maxima, addresses; 55 % busy): bf16
+// stream (45) 56, without one (19) 41, to four bits (41) 61 and (16) 50; the quantiser 137 a warp and 256 columns, 16384 x 5120 bf16 (33) 60, 53 in
+// blocks of 32, 10576 x 2560 fp32 (19) 19.  Divisions in place of corrected products took 204 and 86.  Values: 16384 x 5120 to bf16 (33) 39, 60 with
+// a division to find a thread's row.  2560 rows of 16384 to int8 (70) 87, to four bits (67) 110: one block of 96 KB a row to an SM.  Rows wider than
+// that are read twice in blocks of 16, 2048 x 32768 bf16 (26) 63, fp32 (47) 92, 256 x 131072 (13) 47, and once in blocks of 32, bf16 44.  One row of
+// 768: 2.0, where the call itself takes 3.7 from Python.
 #include "fp4.cuh"
 #include "kernels.h"
 #include "sm100.cuh"
@@ -446,7 +448,8 @@ __global__ void __launch_bounds__(256) values_kernel(const uint8_t* codes, const
   }
 }
 
-// Many rows on 16 bytes go through the ring, with as many blocks as have room for two rows each: what a row waits for is then on its way while the one before
+// Many rows on 16 bytes go through the ring, with as many blocks as shared memory has room for with two rows each (of narrow rows threads and registers hold fewer at
+// a time): what a row waits for is then on its way while the one before
 // is worked on (us, direct and ring: 16384 x 2560 bf16 with an fp32 stream to int8 81 and 79, to four bits 87 and 75, bf16 stream 72 and 56;
 // 4096 x 8192 75 and 61; quantiser 16384 x 5120 bf16 75 and 56).  Not fp32 rows without a stream, whose 32 bytes a lane meet in shared memory's banks
 // (quantiser 10576 x 2560 19 and 24).  A chunk to a warp where rows are short (or few: 300 x 2560 6.0 with two, 4.2),

@@ -26,8 +26,8 @@ struct Fp4Form {
 // operands a cycle and SM, or where the ring does not hold all of a CTA's stages their latency of 1400 over those that it holds; the
 // accumulator's way out, the parts' meeting, the tokens.  A wave behind another takes 12000 at least.
 // Pairs: 10000 for the call, the first operands and the last tile's way out, 600 for 256 of K where no epilogue is beside them and 760 where one is, 1700
-// from one tile to the next, 5000 at least.  (us, few rows and pairs: 64 x 10576 x 2560 6.9, 9.7; 64 x 10576 x 768 4.7, 6.4; 250 x 2000 x 1024 9.2, 6.1;
-// 256 x 4096 x 8192 12.7, 16.1; 512 x 2560 x 5120 11.3, 10.9; 700 x 5000 x 256 7.4, 5.9; 3439 x 16472 x 512 80, 35.)
+// from one tile to the next, 5000 at least.  (us, few rows and pairs: 64 x 10576 x 2560 6.9, 9.9; 64 x 10576 x 768 4.7, 6.3; 250 x 2000 x 1024 9.0, 6.0;
+// 256 x 4096 x 8192 12.8, 15.7; 512 x 2560 x 5120 12.5, 10.7; 700 x 5000 x 256 7.0, 5.9; 3439 x 16472 x 512 77, 35.)
 // vec_out: out's rows lie on 16 bytes.
 inline Fp4Form fp4_form(int rows, int outs, int width, int block, bool vec_out, int sms) {
   const int kblocks = (width + 255) / 256;
@@ -59,7 +59,7 @@ inline Fp4Form fp4_form(int rows, int outs, int width, int block, bool vec_out, 
   }
   const int64_t ptiles = (int64_t)((rows + 255ll) / 256) * ((outs + 255ll) / 256), pairs = sms / 2;
   const double each = 760.0 * kblocks + 1700.0;
-  // (where rows lie on no 16-byte boundary the last columns go out by elements: 134 x 115 x 256 11.3, few rows 5)
+  // (where rows lie on no 16-byte boundary the last columns go out by elements: 134 x 115 x 256 10.6, few rows 6.8)
   const double ragged = !vec_out && outs % 64 ? 6000.0 : 0.0;
   f.pair = pairs > 0 && 10000.0 + ragged + 600.0 * kblocks + (double)((ptiles + pairs - 1) / pairs - 1) * (each > 5000.0 ? each : 5000.0) < best;
   return f;

@@ -9,9 +9,10 @@
 // copies between them: N 256 alone hides those, N 128 takes 76 without and 88 with).  16384 x 2560 x 5120 with bias and residual (34 us of
 // bytes, 52 of operations at that rate) takes 97 to 108 us on the device: the clock falls to 1.4 to 1.65 GHz under the power limit, at which a tile's 20 stages
 // take 13300 cycles where the pipe alone would take 11900 (89 %), and 0.9 us pass from one tile to the next: the accumulators share 48 columns.
-// 3439 x 16472 x 1248, fp16, residual (37 us of bytes) 76, 53 to 57 without the residual: five stages a tile, and operands and results
-// share the way between L2 and the SMs (459 MB, 8.7 TB/s; 36 us without the stores, whatever the epilogue does); 16470 columns, rows on words, 97; 16471, odd ones, 146.
-// 64 x 10576 x 2560 (2.6 us of bytes) 6.9 us from L2 and 8.8 from DRAM, one row 5.7 and 6.7: launch and first operands 1.0, ten stages' MMAs and
+// 3439 x 16472 x 1248, fp16, residual (37 us of bytes) 72 to 76, 53 to 57 without the residual: five stages a tile, and operands and results
+// share the way between L2 and the SMs (459 MB, 8.7 TB/s; 36 us without the stores, whatever the epilogue does); 16470 columns, rows on words, 98; 16471, odd ones, 146; in
+// binary32 (72) 112, 161 and 163.
+// 64 x 10576 x 2560 (2.6 us of bytes) 6.9 us from L2 and 8.8 from DRAM, one row 5.9 and 6.8: launch and first operands 1.0, ten stages' MMAs and
 // scale copies of a lone CTA 2.5 (issued without checks; 3.5 with them), the accumulator's way out and the tokens 1.5.
 #include "fp4.cuh"
 #include "fp4_form.h"
@@ -123,7 +124,7 @@ __device__ __forceinline__ void arrive_relaxed_at(uint32_t bar) {
 // residual of a unit into its slab, a unit ahead, and takes the unit from there; it leaves out what is beyond the last row and column.  Other rows
 // are read back from the slabs as binary32, a row at a time by lanes that stand beside one another in it, and stored in words of
 // four bytes: in an odd row, one of 16-bit elements that starts in the middle of a word, lane j has elements 2 j - 1 and 2 j, and the
-// row's own lane stores both ends.
+// row's own lane stores both ends.  (The residual's words, of this unit and the next, are 64 of the 168 registers: 8 bytes spill, 112 in binary32.)
 enum { ROWS_VECTORS = 0, ROWS_WORDS = 1, ROWS_ODD = 2 };   // out's rows (and the residual's) on 16 bytes, on words (binary32: elements), on 16-bit elements
 template <typename T, int ROWS>
 struct Epilogue {
