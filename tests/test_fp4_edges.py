@@ -212,3 +212,120 @@ def test_norm_of_rows_with_infinities(form):
     step = q.tensors["step"][1:3]
     assert torch.isnan(step).all() if form == "fp4 16" else not step.any()
     assert torch.isnan(out[1:3]).all() if form == "fp4 16" else not out[1:3][~torch.isinf(x[1:3])].any()
+
+
+def _device_check(T, O, K, block, rows=None, outs=None, dtype=None):
+    """a product against binary64 on the device, some rows and outputs of it"""
+    import torch
+    from paper_2608_21952_b200 import binding as bd
+    g = torch.Generator(device="cuda").manual_seed(T + O)
+
+    def matrix(n):
+        q = bd.make_fp4(n, K, block)
+        q.tensors["codes"].copy_(torch.randint(0, 256, (n, K // 2), generator=g, device="cuda", dtype=torch.uint8))
+        lo, hi = (60, 127) if block == 16 else (120, 132)
+        s = q.tensors["scales"]
+        s.copy_(torch.randint(lo, hi, s.shape, generator=g, device="cuda", dtype=torch.uint8))
+        return q
+    x, w = matrix(T), matrix(O)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out = torch.full((T + 1, O), 77.0, dtype=dtype or torch.float32, device="cuda")
+    bd.ssdi8_fp4_linear(x, w, out[:T], status=status)
+    assert int(status.item()) == 0 and (out[T] == 77).all()
+
+    def values(q, n, at):
+        v = torch.empty(n, K, device="cuda")
+        bd.ssdi8_fp4_dequantize(q, v)
+        return v[at].double()
+    tr = torch.arange(T, device="cuda") if rows is None else torch.cat([torch.arange(rows, device="cuda"), torch.arange(T - rows, T, device="cuda")])
+    oc = torch.arange(O, device="cuda") if outs is None else torch.cat([torch.arange(outs, device="cuda"), torch.arange(O - outs, O, device="cuda")])
+    vx, vw = values(x, T, tr), values(w, O, oc)
+    want, size = vx @ vw.T, vx.abs() @ vw.abs().T
+    got = out[tr][:, oc].double()
+    # K roundings of the sum of magnitudes, the result's own (bf16: half a step of 2^-7)
+    tol = K * 2.0 ** -24 * size
+    tol = tol + (2.0 ** -24 if dtype is None else 2.0 ** -8) * (want.abs() + tol)
+    assert bool(((got - want).abs() <= tol).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("block", [16, 32])
+@pytest.mark.parametrize("T,O", [(3, 130), (300, 129), (600, 1000)])
+def test_linear_of_the_widest_rows(T, O, block):
+    _device_check(T, O, 131072, block)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,O,K", [(1, 1 << 21, 64), ((1 << 21) + 5, 9, 32), (2, (1 << 20) + 3, 96)])
+def test_linear_of_one_long_side(T, O, K):
+    """one token and millions of outputs, millions of tokens and a few outputs"""
+    import torch
+    _device_check(T, O, K, 16, rows=min(T, 700) if T > 700 else None, outs=700 if O > 700 else None, dtype=torch.bfloat16)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("block", [16, 32])
+def test_linear_of_slices(block):
+    """rows of a matrix from a multiple of 128 on are a matrix: a weight's shards, a batch's parts"""
+    import torch
+    from paper_2608_21952_b200 import binding as bd
+    T, O, K = 300, 700, 544
+    x, w = _matrix(T, K, block, 1)[0], _matrix(O, K, block, 2)[0]
+
+    def part(q, a, b):
+        t = q.tensors
+        return bd.fp4_of(t["codes"][a:b], t["scales"][a // 128:], t["step"][a:b], block)
+    whole, out = torch.empty(T, O, device="cuda"), torch.full((T, O), 77.0, device="cuda")
+    values = torch.empty(T, K, device="cuda")
+    bd.ssdi8_fp4_linear(x, w, whole)
+    for a, b in ((0, 128), (128, 300)):
+        for c, d in ((0, 384), (384, 700)):
+            bd.ssdi8_fp4_linear(part(x, a, b), part(w, c, d), out[a:b, c:d])
+    # (forms differ, and with them the order of sums)
+    vx, vw = torch.empty(T, K, device="cuda"), torch.empty(O, K, device="cuda")
+    bd.ssdi8_fp4_dequantize(x, vx)
+    bd.ssdi8_fp4_dequantize(w, vw)
+    assert bool(((whole - out).abs() <= (2 * K + 8) * 2.0 ** -24 * (vx.abs() @ vw.abs().T)).all())
+    for a, b in ((0, 128), (128, 300)):
+        bd.ssdi8_fp4_dequantize(part(x, a, b), values[a:b])
+    assert torch.equal(values, vx)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("form", ["int8", "static"])
+def test_norm_of_the_narrowest_rows(form):
+    from test_fp4 import test_add_norm
+    for T in (1, 9471, 9473, 20000):
+        test_add_norm(T, 16, "bfloat16", "float32", "normal", 0, form)
+
+
+@pytest.mark.gpu
+def test_four_and_eight_bits_on_two_streams():
+    """products of both kinds beside one another, whose tensor memory and clusters share the SMs"""
+    import torch
+    from paper_2608_21952_b200 import binding as bd
+    ops = [[], []]
+    for i, (T, O, K) in enumerate(((64, 2560, 5120), (1, 640, 8192), (134, 156, 3520), (300, 1000, 1024), (2304, 2560, 512), (100, 600, 2560))):
+        x, w, out = _matrix(T, K, 16, i)[0], _matrix(O, K, 16, i + 9)[0], torch.empty(T, O, device="cuda")
+        ops[0].append((lambda st, x=x, w=w, out=out: bd.ssdi8_fp4_linear(x, w, out, stream=st), out))
+        a, b = (torch.randint(-127, 128, s, dtype=torch.int8, device="cuda") for s in ((T, K), (O, K)))
+        s, y = torch.rand(O, device="cuda"), torch.empty(T, O, device="cuda")
+        ops[1].append((lambda st, a=a, b=b, s=s, y=y: bd.ssdi8_linear(a, b, s, y, stream=st), y))
+    want = []
+    for side in ops:
+        for f, out in side:
+            f(None)
+            torch.cuda.synchronize()
+            want.append(out.clone())
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for shift in range(12):
+        for side in ops:
+            for _, out in side:
+                out.zero_()
+        torch.cuda.synchronize()
+        for i in range(len(ops[0])):
+            ops[0][i][0](streams[0])
+            ops[1][(i + shift) % len(ops[1])][0](streams[1])
+        torch.cuda.synchronize()
+        for (_, out), y in zip(ops[0] + ops[1], want):
+            assert torch.equal(out, y)
